@@ -217,8 +217,8 @@ def _adamw_inputs(case, g):
     if case["bits"] == 32:
         s["m"], s["v"] = m, v
     else:
-        s["m"], s["m_scale"] = _encode(m)
-        s["v"], s["v_scale"] = _encode(v.sqrt())
+        s["m"], s["m_scale"] = _encode(m, 0.0)
+        s["v"], s["v_scale"] = _encode(v.sqrt(), CODE_MIN)
     if case["copy"]:
         s["copy"] = s["p"].to(torch.bfloat16)
     return s
@@ -295,7 +295,7 @@ def _run_adamw(s):
 
 def _activate(z, act):
     if act == "relu":
-        return torch.where(z > 0, z, 0)
+        return torch.where(z < 0, 0, z)
     return {"none": lambda: z, "tanh": lambda: torch.tanh(z),
             "silu": lambda: z / (1 + torch.exp(-z))}[act]()
 
@@ -364,16 +364,15 @@ def _decode(codes, scale):
     return codes.float().reshape(-1, BLOCK) * scale[:, None]
 
 
-def _encode(values):
+def _encode(values, least):
     """e4m3 numbers and a scale for each block, so that its largest magnitude is 448; a block
-    with nothing over 2^-100 is all zeros, and no other non-negative value rounds to zero."""
+    with nothing over 2^-100 is all zeros, and no positive number is rounded below `least`."""
     blocks = values.reshape(-1, BLOCK)
     top = blocks.abs().amax(1)
-    some = top >= 2.0 ** -100
-    inv = torch.where(some, CODE_MAX / top, 0)[:, None]
-    codes = blocks * inv
-    codes = torch.where((codes > 0) & (codes < CODE_MIN), CODE_MIN, codes)
-    return codes.to(torch.float8_e4m3fn).flatten(), torch.where(some, top / CODE_MAX, 0)
+    none = top < 2.0 ** -100
+    codes = blocks * torch.where(none, 0, CODE_MAX / top)[:, None]
+    codes = torch.where((codes > 0) & (codes < least), least, codes)
+    return codes.to(torch.float8_e4m3fn).flatten(), torch.where(none, 0, top / CODE_MAX)
 
 
 def _plain_adamw(s):
@@ -393,8 +392,8 @@ def _plain_adamw(s):
     if case["copy"]:
         s["copy"].copy_(p)
     if case["bits"] == 8:
-        m, s["m_scale"][:] = _encode(m)
-        v, s["v_scale"][:] = _encode(torch.sqrt(v))
+        m, s["m_scale"][:] = _encode(m, 0.0)
+        v, s["v_scale"][:] = _encode(torch.sqrt(v), CODE_MIN)
     s["m"].copy_(m.flatten())
     s["v"].copy_(v.flatten())
 
