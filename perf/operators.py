@@ -261,7 +261,8 @@ def _handle(s, case):
                                               "v_scale": views("v_scale", BLOCK)}
         s["adamw"] = train.AdamW(views("p"), state_bits=case["bits"], weight_decay=s["decay"],
                                  m=views("m"), v=views("v"),
-                                 copies=views("copy") if case["copy"] else None, **more)
+                                 copies=views("copy") if case["copy"] else None,
+                                 grad_dtypes=[g.dtype for g in s["grads"]], **more)
 
 
 # ---- one pass -----------------------------------------------------------------
