@@ -1,0 +1,404 @@
+// norm.hip -- group norm with an activation and its gradients (huge2_train.h).
+//
+// Passes over x are all that these cost.  The general form takes two: sums per
+// channel and run of pixels, a merge per group, and the pass that writes.
+#include <cmath>
+
+#include "train.hpp"
+#include "train_device.hpp"
+
+namespace huge2 {
+
+namespace {
+
+// z of a normalised value.  Rounded after the product, here and in the gradient,
+// so that both see the same sign (and the same as a framework without fused
+// multiply-adds).
+__device__ __forceinline__ float norm_z(float xh, float gamma, float beta) {
+#pragma clang fp contract(off)
+  return xh * gamma + beta;
+}
+
+// huge2_norm_activation; act is uniform over the launch.
+__device__ __forceinline__ float norm_act(float z, int act) {
+  switch (act) {
+    case 1: return z < 0.f ? 0.f : z;
+    case 2: return tanhf(z);
+    case 3: return z / (1.f + expf(-z));
+  }
+  return z;
+}
+// dy * activation'(z)
+__device__ __forceinline__ float norm_act_grad(float dy, float z, int act) {
+  switch (act) {
+    case 1: return z > 0.f ? dy : 0.f;
+    case 2: {
+      const float th = tanhf(z);
+      return dy * (1.f - th * th);
+    }
+    case 3: {
+      const float s = 1.f / (1.f + expf(-z));
+      return dy * (s * (1.f + z * (1.f - s)));
+    }
+  }
+  return dy;
+}
+
+// Sum of one value a thread over a workgroup of 256, in every thread.
+__device__ __forceinline__ float block_sum(float v, float* lds) {
+  v = lanes_sum(v, 1);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// A channel's constants: z = ((x - mean) * rstd) * gamma + beta.
+struct Channel {
+  float mean, rstd, gamma, beta;
+};
+__device__ __forceinline__ Channel channel(const NormArgs& a, const float* stats, int img, int ch) {
+  const float2 s = ((const float2*)stats)[(size_t)img * a.groups + ch / a.d];
+  return {s.x, s.y, a.gamma ? a.gamma[ch] : 1.f, a.beta ? a.beta[ch] : 0.f};
+}
+
+// Where a workgroup of 256 works in NHWC: image, run of pixels, and its threads
+// as rows of 2^lanes_log2 lanes side by side on a pixel's channels.
+struct PlaceNhwc {
+  int img, chunk, p0, p1, row, rows, ch;
+  size_t at;  // element of (img, pixel 0, ch)
+};
+template <int VW>
+__device__ __forceinline__ PlaceNhwc place_nhwc(const NormArgs& a) {
+  PlaceNhwc q;
+  const int b = blockIdx.x, cb = b % a.cblocks, t = b / a.cblocks;
+  q.chunk = t % a.chunks;
+  q.img = t / a.chunks;
+  q.p0 = q.chunk * a.chunk_len;
+  q.p1 = min(a.hw, q.p0 + a.chunk_len);
+  q.rows = 256 >> a.lanes_log2;
+  q.row = threadIdx.x >> a.lanes_log2;
+  q.ch = ((cb << a.lanes_log2) + (threadIdx.x & ((1 << a.lanes_log2) - 1))) * VW;
+  q.at = (size_t)q.img * a.hw * a.c + q.ch;
+  return q;
+}
+
+// The same in NCHW: rows of lanes side by side on the pixels of one plane's run.
+struct PlaceNchw {
+  long long plane;  // img * c + ch
+  int img, ch, chunk, p0, p1, lane, lanes;
+  bool in;
+};
+__device__ __forceinline__ PlaceNchw place_nchw(const NormArgs& a) {
+  PlaceNchw q;
+  const long long unit =
+      (long long)blockIdx.x * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+  q.in = unit < (long long)a.n * a.c * a.chunks;
+  q.plane = q.in ? unit / a.chunks : 0;
+  q.chunk = q.in ? (int)(unit % a.chunks) : 0;
+  q.img = (int)(q.plane / a.c);
+  q.ch = (int)(q.plane % a.c);
+  q.p0 = q.chunk * a.chunk_len;
+  q.p1 = q.in ? min(a.hw, q.p0 + a.chunk_len) : q.p0;
+  q.lanes = 1 << a.lanes_log2;
+  q.lane = threadIdx.x & (q.lanes - 1);
+  return q;
+}
+
+}  // namespace
+
+// Sums of a run of pixels per channel.  Forward: the run's mean and its sum of
+// squares around that, from sums around one of its own values (a pivot far from
+// the mean is then itself part of the squares it is subtracted from, which keeps
+// the loss to the run's length in units of the last place).  Gradient: the sums of
+// dz and of dz * xh.
+template <typename T, int VW, bool GRAD>
+__global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
+  const PlaceNhwc q = place_nhwc<VW>(a);
+  const bool in = q.ch < a.c;
+  const T* x = (const T*)a.x + q.at;
+  const T* dy = (const T*)a.dy + q.at;
+  float s1[VW], s2[VW], pivot[VW];
+  Channel k[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s1[e] = s2[e] = pivot[e] = 0.f;
+  if (in) {
+    if constexpr (GRAD) {
+#pragma unroll
+      for (int e = 0; e < VW; ++e) k[e] = channel(a, a.stats, q.img, q.ch + e);
+    } else {
+      unpack<T, VW>(load_pack<T, VW>(x + (size_t)q.p0 * a.c), pivot);
+    }
+#pragma unroll 4
+    for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
+      float f[VW];
+      unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
+      if constexpr (GRAD) {
+        float g[VW];
+        unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+          const float xh = (f[e] - k[e].mean) * k[e].rstd;
+          const float dz = norm_act_grad(g[e], norm_z(xh, k[e].gamma, k[e].beta), a.act);
+          s1[e] += dz;
+          s2[e] += dz * xh;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+          const float v = f[e] - pivot[e];
+          s1[e] += v;
+          s2[e] += v * v;
+        }
+      }
+    }
+  }
+  // rows of one wave, then the four waves
+  __shared__ float2 lds[4][64 * VW];
+  const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+    s1[e] = lanes_sum(s1[e], lanes);
+    s2[e] = lanes_sum(s2[e], lanes);
+    if ((threadIdx.x & 63) < lanes) lds[threadIdx.x >> 6][lane * VW + e] = make_float2(s1[e], s2[e]);
+  }
+  __syncthreads();
+  if (threadIdx.x < lanes && in) {
+    const float count = (float)(q.p1 - q.p0);
+    float2* part = a.part + ((size_t)q.img * a.chunks + q.chunk) * a.c + q.ch;
+#pragma unroll
+    for (int e = 0; e < VW; ++e) {
+      float2 s = lds[0][lane * VW + e];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        s.x += lds[w][lane * VW + e].x;
+        s.y += lds[w][lane * VW + e].y;
+      }
+      if constexpr (GRAD) {
+        part[e] = s;
+      } else {
+        const float m = s.x / count;
+        part[e] = make_float2(pivot[e] + m, fmaxf(s.y - s.x * m, 0.f));
+      }
+    }
+  }
+}
+
+template <typename T, int VW, bool GRAD>
+__global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
+  const PlaceNchw q = place_nchw(a);
+  if (!q.in) return;  // whole rows of lanes: the sums below stay in one
+  const T* x = (const T*)a.x + (size_t)q.plane * a.hw;
+  const T* dy = (const T*)a.dy + (size_t)q.plane * a.hw;
+  float s1 = 0.f, s2 = 0.f, pivot = 0.f;
+  Channel k;
+  if constexpr (GRAD)
+    k = channel(a, a.stats, q.img, q.ch);
+  else
+    pivot = to_f32<T>(x[q.p0]);
+#pragma unroll 4
+  for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
+    float f[VW];
+    unpack<T, VW>(load_pack<T, VW>(x + p), f);
+    if constexpr (GRAD) {
+      float g[VW];
+      unpack<T, VW>(load_pack<T, VW>(dy + p), g);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) {
+        const float xh = (f[e] - k.mean) * k.rstd;
+        const float dz = norm_act_grad(g[e], norm_z(xh, k.gamma, k.beta), a.act);
+        s1 += dz;
+        s2 += dz * xh;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < VW; ++e) {
+        const float v = f[e] - pivot;
+        s1 += v;
+        s2 += v * v;
+      }
+    }
+  }
+  for (int m = q.lanes >> 1; m; m >>= 1) {
+    s1 += __shfl_xor(s1, m);
+    s2 += __shfl_xor(s2, m);
+  }
+  if (q.lane == 0) {
+    float2* part = a.part + ((size_t)q.img * a.chunks + q.chunk) * a.c + q.ch;
+    if constexpr (GRAD) {
+      *part = make_float2(s1, s2);
+    } else {
+      const float m = s1 / (float)(q.p1 - q.p0);
+      *part = make_float2(pivot + m, fmaxf(s2 - s1 * m, 0.f));
+    }
+  }
+}
+
+// Joins the runs.  A workgroup to an (image, group): its statistics, or the two
+// means of its gradient; behind those, a workgroup to 16 channels: dgamma, dbeta.
+template <bool GRAD>
+__global__ __launch_bounds__(256) void norm_merge_kernel(NormArgs a) {
+  __shared__ float lds[4];
+  __shared__ float2 seg[16][16];
+  const long long ng = (long long)a.n * a.groups;
+  if ((long long)blockIdx.x < ng) {
+    const int img = (int)(blockIdx.x / a.groups), g = (int)(blockIdx.x % a.groups);
+    const float2* part = a.part + (size_t)img * a.chunks * a.c + (size_t)g * a.d;
+    const int entries = a.chunks * a.d;
+    const float m = (float)a.d * (float)a.hw;
+    if constexpr (GRAD) {
+      float s1 = 0.f, s2 = 0.f;
+      for (int e = threadIdx.x; e < entries; e += 256) {
+        const int chunk = e / a.d, j = e - chunk * a.d;
+        const float2 v = part[(size_t)chunk * a.c + j];
+        const float gamma = a.gamma ? a.gamma[g * a.d + j] : 1.f;
+        s1 += gamma * v.x;
+        s2 += gamma * v.y;
+      }
+      s1 = block_sum(s1, lds);
+      s2 = block_sum(s2, lds);
+      if (threadIdx.x == 0) a.coef[blockIdx.x] = make_float2(s1 / m, s2 / m);
+    } else {
+      float s = 0.f;
+      for (int e = threadIdx.x; e < entries; e += 256) {
+        const int chunk = e / a.d, j = e - chunk * a.d;
+        const int count = min(a.chunk_len, a.hw - chunk * a.chunk_len);
+        s += part[(size_t)chunk * a.c + j].x * (float)count;
+      }
+      const float mean = block_sum(s, lds) / m;
+      s = 0.f;
+      for (int e = threadIdx.x; e < entries; e += 256) {
+        const int chunk = e / a.d, j = e - chunk * a.d;
+        const int count = min(a.chunk_len, a.hw - chunk * a.chunk_len);
+        const float2 v = part[(size_t)chunk * a.c + j];
+        s += v.y + (float)count * (v.x - mean) * (v.x - mean);
+      }
+      const float var = block_sum(s, lds) / m;
+      if (threadIdx.x == 0)
+        ((float2*)a.stats_out)[blockIdx.x] = make_float2(mean, 1.f / sqrtf(var + a.eps));
+    }
+    return;
+  }
+  if constexpr (GRAD) {
+    const int ch = (int)(blockIdx.x - ng) * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+    float2 s = make_float2(0.f, 0.f);
+    if (ch < a.c) {
+      const long long runs = (long long)a.n * a.chunks;
+#pragma unroll 4
+      for (long long r = row; r < runs; r += 16) {
+        const float2 v = a.part[(size_t)r * a.c + ch];
+        s.x += v.x;
+        s.y += v.y;
+      }
+    }
+    seg[row][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (row == 0 && ch < a.c) {
+      for (int r = 1; r < 16; ++r) {
+        s.x += seg[r][threadIdx.x].x;
+        s.y += seg[r][threadIdx.x].y;
+      }
+      if (a.dbeta) a.dbeta[ch] = s.x;
+      if (a.dgamma) a.dgamma[ch] = s.y;
+    }
+  }
+}
+
+// y, or dx, of one value.
+template <bool GRAD>
+__device__ __forceinline__ float norm_value(float x, float dy, const Channel& k, float2 coef,
+                                            int act) {
+  const float xh = (x - k.mean) * k.rstd, z = norm_z(xh, k.gamma, k.beta);
+  if constexpr (!GRAD) return norm_act(z, act);
+  const float t = norm_act_grad(dy, z, act) * k.gamma;
+  return k.rstd * (t - coef.x - xh * coef.y);
+}
+
+template <typename T, int VW, bool GRAD>
+__global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
+  const PlaceNhwc q = place_nhwc<VW>(a);
+  if (q.ch >= a.c) return;
+  const T* x = (const T*)a.x + q.at;
+  const T* dy = (const T*)a.dy + q.at;
+  T* out = (T*)a.out + q.at;
+  Channel k[VW];
+  float2 coef[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+    k[e] = channel(a, GRAD ? a.stats : a.stats_out, q.img, q.ch + e);
+    if (GRAD) coef[e] = a.coef[(size_t)q.img * a.groups + (q.ch + e) / a.d];
+  }
+#pragma unroll 4
+  for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
+    float f[VW], g[VW];
+    unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
+    if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
+#pragma unroll
+    for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD>(f[e], g[e], k[e], coef[e], a.act);
+    *(Pack<T, VW>*)(out + (size_t)p * a.c) = pack<T, VW>(f);
+  }
+}
+
+template <typename T, int VW, bool GRAD>
+__global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a) {
+  const PlaceNchw q = place_nchw(a);
+  if (!q.in) return;
+  const T* x = (const T*)a.x + (size_t)q.plane * a.hw;
+  const T* dy = (const T*)a.dy + (size_t)q.plane * a.hw;
+  T* out = (T*)a.out + (size_t)q.plane * a.hw;
+  const Channel k = channel(a, GRAD ? a.stats : a.stats_out, q.img, q.ch);
+  float2 coef;
+  if (GRAD) coef = a.coef[(size_t)q.img * a.groups + q.ch / a.d];
+#pragma unroll 4
+  for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
+    float f[VW], g[VW];
+    unpack<T, VW>(load_pack<T, VW>(x + p), f);
+    if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + p), g);
+#pragma unroll
+    for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD>(f[e], g[e], k, coef, a.act);
+    *(Pack<T, VW>*)(out + p) = pack<T, VW>(f);
+  }
+}
+
+namespace {
+
+template <typename T, int VW, bool GRAD>
+hipError_t launch_t(const NormArgs& a, int nhwc, hipStream_t stream) {
+  const dim3 wg(256);
+  const long long units = (long long)a.n * a.chunks * (nhwc ? a.cblocks : a.c);
+  const unsigned grid =
+      (unsigned)(nhwc ? units : (units + (256 >> a.lanes_log2) - 1) / (256 >> a.lanes_log2));
+  const unsigned merge = (unsigned)((long long)a.n * a.groups +
+                                    (GRAD && (a.dgamma || a.dbeta) ? (a.c + 15) / 16 : 0));
+  if (nhwc) {
+    hipLaunchKernelGGL((norm_sums_nhwc_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
+    hipLaunchKernelGGL((norm_merge_kernel<GRAD>), dim3(merge), wg, 0, stream, a);
+    hipLaunchKernelGGL((norm_apply_nhwc_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((norm_sums_nchw_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
+    hipLaunchKernelGGL((norm_merge_kernel<GRAD>), dim3(merge), wg, 0, stream, a);
+    hipLaunchKernelGGL((norm_apply_nchw_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+template <bool GRAD>
+hipError_t launch_any(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream) {
+  if (dtype == HUGE2_BF16)
+    return vec == 8   ? launch_t<uint16_t, 8, GRAD>(a, nhwc, stream)
+           : vec == 2 ? launch_t<uint16_t, 2, GRAD>(a, nhwc, stream)
+                      : launch_t<uint16_t, 1, GRAD>(a, nhwc, stream);
+  return vec == 4 ? launch_t<uint32_t, 4, GRAD>(a, nhwc, stream)
+                  : launch_t<uint32_t, 1, GRAD>(a, nhwc, stream);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream) {
+  return launch_any<false>(a, dtype, nhwc, vec, stream);
+}
+hipError_t launch_norm_grad(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream) {
+  return launch_any<true>(a, dtype, nhwc, vec, stream);
+}
+
+}  // namespace huge2

@@ -1,0 +1,493 @@
+// train.cpp -- the C ABI of the operators around the convolutions (declared in
+// include/huge2_train.h): checks, plans, workspaces.
+#include "huge2_train.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <initializer_list>
+#include <new>
+#include <vector>
+
+#include "train.hpp"
+
+using namespace huge2;
+
+struct huge2_norm_plan {
+  huge2_norm_desc desc;
+  int vec;  // elements of a load
+  NormArgs args;
+  void* ws;
+  char kernel_name[2][96];
+};
+
+struct huge2_embedding_grad_plan {
+  huge2_embedding_desc desc;
+  int64_t max_tokens;
+  int vec, lanes_log2, passes;
+  void* ws;
+  char kernel_name[96];
+};
+
+struct huge2_adamw_plan {
+  struct Launch {
+    int tensor, tensors;
+    size_t work, works;
+  };
+  int state_bits;
+  int count;
+  std::vector<Launch> launches;
+  void* table;  // AdamTensorDev [count], then uint2 [works]
+  size_t works_at;
+};
+
+namespace {
+
+// HUGE2_FAULT=alloc, launch: as in capi.cpp (tests of the error paths).
+bool fault(const char* what) {
+  const char* f = std::getenv("HUGE2_FAULT");
+  return f && std::strcmp(f, what) == 0;
+}
+
+bool aligned(const void* p, size_t to = 16) { return ((uintptr_t)p & (to - 1)) == 0; }
+bool bad(const void* p, size_t to = 16) { return !p || !aligned(p, to); }
+bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+  return (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
+}
+bool is_dtype(int d) { return d == HUGE2_F32 || d == HUGE2_BF16; }
+int elem_size(int dtype) { return dtype == HUGE2_BF16 ? 2 : 4; }
+size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+int log2_ceil(long long v) {
+  int l = 0;
+  while ((1ll << l) < v) ++l;
+  return l;
+}
+
+// The widest load of the type that divides a run of `len` elements: 16 bytes, 4
+// or one element.
+int vector_width(int dtype, long long len) {
+  const int full = 16 / elem_size(dtype);
+  if (len % full == 0) return full;
+  return dtype == HUGE2_BF16 && len % 2 == 0 ? 2 : 1;
+}
+
+huge2_status device_alloc(void** out, size_t bytes) {
+  *out = nullptr;
+  if (bytes == 0) return HUGE2_OK;
+  if (fault("alloc")) return HUGE2_ERR_ALLOC;
+  if (hipMalloc(out, bytes) == hipSuccess) return HUGE2_OK;
+  (void)hipGetLastError();
+  (void)huge2_plan_destroy(nullptr);  // what the one-shot calls keep
+  if (hipMalloc(out, bytes) == hipSuccess) return HUGE2_OK;
+  (void)hipGetLastError();
+  *out = nullptr;
+  return HUGE2_ERR_ALLOC;
+}
+
+huge2_status device_free(void* p) {
+  if (p && hipFree(p) != hipSuccess) {
+    (void)hipGetLastError();
+    return HUGE2_ERR_HIP;
+  }
+  return HUGE2_OK;
+}
+
+huge2_status launched(hipError_t e) {
+  if (e == hipSuccess) return HUGE2_OK;
+  (void)hipGetLastError();
+  return HUGE2_ERR_HIP;
+}
+
+// ---- group norm -----------------------------------------------------------------
+
+bool valid(const huge2_norm_desc& d) {
+  return d.n >= 1 && d.c >= 1 && d.h >= 1 && d.w >= 1 && d.groups >= 1 && d.c % d.groups == 0 &&
+         (d.layout == HUGE2_NCHW || d.layout == HUGE2_NHWC) && is_dtype(d.dtype) &&
+         d.activation >= HUGE2_NORM_NONE && d.activation <= HUGE2_NORM_SILU &&
+         std::isfinite(d.eps) && d.eps > 0.f;
+}
+
+size_t norm_bytes(const huge2_norm_desc& d) {
+  return (size_t)d.n * d.c * d.h * d.w * elem_size(d.dtype);
+}
+
+huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
+  if (!out) return HUGE2_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!desc || !valid(*desc)) return HUGE2_ERR_INVALID_ARG;
+  const huge2_norm_desc& d = *desc;
+  const long long hw = (long long)d.h * d.w;
+  if (hw >= (1ll << 31) || hw * d.c >= (1ll << 31) || hw * d.c * d.n >= (1ll << 40))
+    return HUGE2_ERR_UNSUPPORTED;
+  const bool nhwc = d.layout == HUGE2_NHWC;
+  NormArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.n = d.n, a.c = d.c, a.hw = (int)hw, a.groups = d.groups, a.d = d.c / d.groups;
+  a.act = d.activation;
+  a.eps = d.eps;
+  const int vec = vector_width(d.dtype, nhwc ? d.c : hw);
+  // Runs of pixels: enough workgroups for eight a compute unit, each run long
+  // enough that its sums are few next to its pixels.
+  long long chunks;
+  if (nhwc) {
+    const int vecs = d.c / vec;
+    a.lanes_log2 = std::min(6, log2_ceil(vecs));
+    a.cblocks = (vecs + (1 << a.lanes_log2) - 1) >> a.lanes_log2;
+    const long long units = (long long)d.n * a.cblocks;
+    chunks = std::min((2048 + units - 1) / units, (hw + 63) / 64);
+  } else {
+    const long long vecs = hw / vec, units = (long long)d.n * d.c;
+    chunks = std::max(std::min((8192 + units - 1) / units, (vecs + 255) / 256), (vecs + 1023) / 1024);
+    a.lanes_log2 = std::min(6, log2_ceil((vecs + chunks - 1) / chunks));
+  }
+  a.chunk_len = (int)((hw + chunks - 1) / chunks);
+  if (!nhwc) a.chunk_len = (a.chunk_len + vec - 1) / vec * vec;
+  a.chunks = (int)((hw + a.chunk_len - 1) / a.chunk_len);
+  const long long units = (long long)d.n * a.chunks * (nhwc ? a.cblocks : d.c);
+  if (units >= (1ll << 31) || (long long)d.n * d.groups + d.c / 16 + 1 >= (1ll << 31))
+    return HUGE2_ERR_UNSUPPORTED;
+  huge2_norm_plan* p = new (std::nothrow) huge2_norm_plan();
+  if (!p) return HUGE2_ERR_ALLOC;
+  p->desc = d;
+  p->vec = vec;
+  const size_t part_b = round256((size_t)d.n * a.chunks * d.c * sizeof(float2));
+  const size_t group_b = round256((size_t)d.n * d.groups * sizeof(float2));
+  const huge2_status st = device_alloc(&p->ws, part_b + group_b);
+  if (st != HUGE2_OK) {
+    delete p;
+    return st;
+  }
+  a.part = (float2*)p->ws;
+  a.coef = (float2*)((char*)p->ws + part_b);  // the forward's statistics if it has no other place
+  a.stats_out = (float*)a.coef;
+  p->args = a;
+  for (int g = 0; g < 2; ++g)
+    std::snprintf(p->kernel_name[g], sizeof(p->kernel_name[g]), "norm_sums_%s_kernel%s v%d k%d",
+                  nhwc ? "nhwc" : "nchw", g ? " grad" : "", vec, a.chunks);
+  *out = p;
+  return HUGE2_OK;
+}
+
+huge2_status norm_run(const huge2_norm_plan* p, const void* x, const float* gamma,
+                      const float* beta, void* y, float* stats, hipStream_t stream) {
+  if (!p || bad(x) || bad(y) || !aligned(gamma) || !aligned(beta) || !aligned(stats))
+    return HUGE2_ERR_INVALID_ARG;
+  const huge2_norm_desc& d = p->desc;
+  const size_t bytes = norm_bytes(d);
+  if (overlap(x, bytes, y, bytes)) return HUGE2_ERR_INVALID_ARG;
+  if (fault("launch")) return HUGE2_ERR_HIP;
+  NormArgs a = p->args;
+  a.x = x, a.gamma = gamma, a.beta = beta, a.out = y;
+  if (stats) a.stats_out = stats;
+  return launched(launch_norm(a, d.dtype, d.layout == HUGE2_NHWC, p->vec, stream));
+}
+
+huge2_status norm_grad_run(const huge2_norm_plan* p, const void* x, const void* dy,
+                           const float* stats, const float* gamma, const float* beta, void* dx,
+                           float* dgamma, float* dbeta, hipStream_t stream) {
+  if (!p || bad(x) || bad(dy) || bad(dx) || bad(stats) || !aligned(gamma) || !aligned(beta) ||
+      !aligned(dgamma, 4) || !aligned(dbeta, 4))
+    return HUGE2_ERR_INVALID_ARG;
+  const huge2_norm_desc& d = p->desc;
+  const size_t bytes = norm_bytes(d);
+  if (overlap(dx, bytes, x, bytes) || overlap(dx, bytes, dy, bytes)) return HUGE2_ERR_INVALID_ARG;
+  if (fault("launch")) return HUGE2_ERR_HIP;
+  NormArgs a = p->args;
+  a.x = x, a.dy = dy, a.stats = stats, a.gamma = gamma, a.beta = beta, a.out = dx;
+  a.dgamma = dgamma, a.dbeta = dbeta;
+  return launched(launch_norm_grad(a, d.dtype, d.layout == HUGE2_NHWC, p->vec, stream));
+}
+
+// ---- embedding --------------------------------------------------------------------
+
+bool valid(const huge2_embedding_desc& d) {
+  return d.rows >= 1 && d.dim >= 1 && is_dtype(d.dtype) && (d.id_bits == 32 || d.id_bits == 64);
+}
+// Rows of lanes (up to a workgroup) side by side on a row of the table.
+int embed_lanes_log2(const huge2_embedding_desc& d, int vec) {
+  return std::min(8, log2_ceil(d.dim / vec));
+}
+bool embed_fits(const huge2_embedding_desc& d) {
+  return (long long)d.dim * elem_size(d.dtype) < (1ll << 31) && d.rows < INT_MAX;
+}
+
+huge2_status embed_run(const huge2_embedding_desc* desc, const void* ids, int64_t tokens,
+                       const void* table, void* y, hipStream_t stream) {
+  if (!desc || !valid(*desc) || tokens < 0) return HUGE2_ERR_INVALID_ARG;
+  const huge2_embedding_desc& d = *desc;
+  if (!embed_fits(d) || tokens >= (1ll << 31)) return HUGE2_ERR_UNSUPPORTED;
+  if (tokens == 0) return HUGE2_OK;
+  if (bad(ids, d.id_bits / 8) || bad(table) || bad(y)) return HUGE2_ERR_INVALID_ARG;
+  const size_t row_b = (size_t)d.dim * elem_size(d.dtype);
+  if (overlap(table, row_b * d.rows, y, row_b * tokens) ||
+      overlap(ids, (size_t)tokens * (d.id_bits / 8), y, row_b * tokens))
+    return HUGE2_ERR_INVALID_ARG;
+  if (fault("launch")) return HUGE2_ERR_HIP;
+  const int vec = vector_width(d.dtype, d.dim);
+  EmbedArgs a;
+  a.ids = ids, a.table = table, a.y = y, a.tokens = tokens;
+  a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64, a.scale = d.scale;
+  a.lanes_log2 = embed_lanes_log2(d, vec);
+  return launched(launch_embedding(a, d.dtype, vec, stream));
+}
+
+// Sorted tokens of a chunk: as many as leave eight waves for each compute unit,
+// at least 32, so that the parts are few next to the gradients, at most 256.
+int embed_chunk_len(const huge2_embedding_grad_plan* p, int64_t tokens) {
+  const long long vecs = p->desc.dim / p->vec;
+  const long long waves = std::max<long long>(1, tokens * vecs / 64 / 2048);
+  return (int)std::min<long long>(256, std::max<long long>(32, waves));
+}
+
+huge2_status embed_grad_create(huge2_embedding_grad_plan** out, const huge2_embedding_desc* desc,
+                               int64_t max_tokens) {
+  if (!out) return HUGE2_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!desc || !valid(*desc) || max_tokens < 0) return HUGE2_ERR_INVALID_ARG;
+  if (!embed_fits(*desc) || max_tokens >= (1ll << 30)) return HUGE2_ERR_UNSUPPORTED;
+  huge2_embedding_grad_plan* p = new (std::nothrow) huge2_embedding_grad_plan();
+  if (!p) return HUGE2_ERR_ALLOC;
+  p->desc = *desc;
+  p->max_tokens = max_tokens;
+  p->vec = vector_width(desc->dtype, desc->dim);
+  p->lanes_log2 = embed_lanes_log2(*desc, p->vec);
+  p->passes = (log2_ceil((long long)desc->rows + 1) + kDigitBits - 1) / kDigitBits;
+  const size_t tiles = (max_tokens + kSortTile - 1) / kSortTile;
+  const size_t bytes = max_tokens == 0
+                           ? 0
+                           : 4 * round256(max_tokens * 4) + round256((tiles + 1) * kDigits * 4) +
+                                 (max_tokens + 31) / 32 * 2 * (size_t)desc->dim * 4;
+  const huge2_status st = device_alloc(&p->ws, bytes);
+  if (st != HUGE2_OK) {
+    delete p;
+    return st;
+  }
+  std::snprintf(p->kernel_name, sizeof(p->kernel_name), "embedding_sum_kernel v%d s%d", p->vec,
+                p->passes);
+  *out = p;
+  return HUGE2_OK;
+}
+
+huge2_status embed_grad_run(const huge2_embedding_grad_plan* p, const void* ids, int64_t tokens,
+                            const void* dy, void* dtable, hipStream_t stream) {
+  if (!p || tokens < 0 || tokens > p->max_tokens || bad(dtable)) return HUGE2_ERR_INVALID_ARG;
+  const huge2_embedding_desc& d = p->desc;
+  const size_t row_b = (size_t)d.dim * elem_size(d.dtype);
+  if (tokens && (bad(ids, d.id_bits / 8) || bad(dy) ||
+                 overlap(dy, row_b * tokens, dtable, row_b * d.rows) ||
+                 overlap(ids, (size_t)tokens * (d.id_bits / 8), dtable, row_b * d.rows)))
+    return HUGE2_ERR_INVALID_ARG;
+  if (fault("launch")) return HUGE2_ERR_HIP;
+  EmbedGradArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.ids = ids, a.dy = dy, a.dtable = dtable;
+  a.tokens = (int)tokens, a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64;
+  a.scale = d.scale;
+  a.lanes_log2 = p->lanes_log2;
+  a.passes = p->passes;
+  a.tiles = (int)((tokens + kSortTile - 1) / kSortTile);
+  a.chunk_len = embed_chunk_len(p, tokens);
+  a.chunks = (int)((tokens + a.chunk_len - 1) / a.chunk_len);
+  char* at = (char*)p->ws;
+  const size_t list = round256(p->max_tokens * 4);
+  const size_t tiles = (p->max_tokens + kSortTile - 1) / kSortTile;
+  for (int k = 0; k < 2; ++k) {
+    a.key[k] = (int*)(at + 2 * k * list);
+    a.token[k] = (int*)(at + (2 * k + 1) * list);
+  }
+  a.hist = (int*)(at + 4 * list);
+  a.part = (float*)(at + 4 * list + round256((tiles + 1) * kDigits * 4));
+  return launched(launch_embedding_grad(a, d.dtype, p->vec, stream));
+}
+
+// ---- AdamW --------------------------------------------------------------------------
+
+bool valid(const huge2_adamw_tensor& t, int bits) {
+  if (t.count < 0 || !is_dtype(t.dtype) || !is_dtype(t.grad_dtype) ||
+      !std::isfinite(t.weight_decay) || t.weight_decay < 0.f)
+    return false;
+  if (bits == 32 ? t.m_scale || t.v_scale : !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))
+    return false;
+  if (!aligned(t.param) || !aligned(t.m) || !aligned(t.v) || !aligned(t.copy)) return false;
+  if (t.count == 0) return true;
+  return t.param && t.m && t.v && (bits == 32 || (t.m_scale && t.v_scale));
+}
+
+huge2_status adamw_create(huge2_adamw_plan** out, const huge2_adamw_tensor* tensors, int count,
+                          int state_bits, hipStream_t stream) {
+  if (!out) return HUGE2_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (count < 0 || (count && !tensors) || (state_bits != 32 && state_bits != 8))
+    return HUGE2_ERR_INVALID_ARG;
+  int64_t total = 0;
+  for (int i = 0; i < count; ++i) {
+    if (!valid(tensors[i], state_bits)) return HUGE2_ERR_INVALID_ARG;
+    if (tensors[i].count >= (1ll << 40) || (total += tensors[i].count) >= (1ll << 40))
+      return HUGE2_ERR_UNSUPPORTED;
+  }
+  std::vector<AdamTensorDev> table(count);
+  std::vector<uint2> works;
+  std::vector<huge2_adamw_plan::Launch> launches;
+  for (int i = 0; i < count; ++i) {
+    const huge2_adamw_tensor& t = tensors[i];
+    table[i] = {t.param,   t.m,     t.v, t.m_scale, t.v_scale, t.copy, t.count, t.dtype == HUGE2_BF16,
+                t.grad_dtype == HUGE2_BF16, t.weight_decay, 0};
+    if (i % kAdamTensors == 0)
+      launches.push_back({i, std::min(kAdamTensors, count - i), works.size(), 0});
+    for (int64_t k = 0; k * kAdamWork < t.count; ++k)
+      works.push_back(make_uint2(i % kAdamTensors, (unsigned)k));
+    launches.back().works = works.size() - launches.back().work;
+    if (launches.back().works >= (1u << 31)) return HUGE2_ERR_UNSUPPORTED;
+  }
+  auto* p = new huge2_adamw_plan();
+  p->state_bits = state_bits;
+  p->count = count;
+  p->launches = std::move(launches);
+  p->works_at = round256(table.size() * sizeof(AdamTensorDev));
+  std::vector<char> image(works.empty() ? 0 : p->works_at + works.size() * sizeof(uint2));
+  if (!works.empty()) {
+    std::memcpy(image.data(), table.data(), table.size() * sizeof(AdamTensorDev));
+    std::memcpy(image.data() + p->works_at, works.data(), works.size() * sizeof(uint2));
+  }
+  huge2_status st = device_alloc(&p->table, image.size());
+  if (st == HUGE2_OK && !image.empty() &&
+      (hipMemcpyAsync(p->table, image.data(), image.size(), hipMemcpyHostToDevice, stream) !=
+           hipSuccess ||
+       hipStreamSynchronize(stream) != hipSuccess)) {
+    (void)hipGetLastError();
+    st = HUGE2_ERR_HIP;
+  }
+  if (st != HUGE2_OK) {
+    (void)device_free(p->table);
+    delete p;
+    return st;
+  }
+  *out = p;
+  return HUGE2_OK;
+}
+
+huge2_status adamw_run(const huge2_adamw_plan* p, const void* const* grads,
+                       const huge2_adamw_options* o, const float* grad_scale, hipStream_t stream) {
+  if (!p || !o || (p->count && !grads) || !aligned(grad_scale, 4)) return HUGE2_ERR_INVALID_ARG;
+  const auto beta = [](double b) { return b >= 0 && b < 1 && (float)b < 1.f; };
+  if (!std::isfinite((float)o->lr) || o->lr < 0 || !beta(o->beta1) || !beta(o->beta2) ||
+      !std::isfinite((float)o->eps) || o->eps < 0x1p-126 || o->step < 1)
+    return HUGE2_ERR_INVALID_ARG;
+  for (int i = 0; i < p->count; ++i)
+    if (!aligned(grads[i])) return HUGE2_ERR_INVALID_ARG;
+  if (fault("launch")) return HUGE2_ERR_HIP;
+  AdamArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.grad_scale = grad_scale;
+  a.beta1 = (float)o->beta1, a.beta2 = (float)o->beta2;
+  a.rest1 = (float)(1 - o->beta1), a.rest2 = (float)(1 - o->beta2);
+  a.lr = (float)o->lr, a.eps = (float)o->eps;
+  a.step_size = (float)(o->lr / (1 - std::pow(o->beta1, (double)o->step)));
+  a.root = (float)(1 / std::sqrt(1 - std::pow(o->beta2, (double)o->step)));
+  for (const auto& l : p->launches) {
+    if (l.works == 0) continue;
+    std::memcpy(a.grads, grads + l.tensor, l.tensors * sizeof(void*));
+    a.tensors = (const AdamTensorDev*)p->table + l.tensor;
+    a.works = (const uint2*)((const char*)p->table + p->works_at) + l.work;
+    const huge2_status st = launched(launch_adamw(a, (unsigned)l.works, p->state_bits, stream));
+    if (st != HUGE2_OK) return st;
+  }
+  return HUGE2_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+huge2_status huge2_norm_plan_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
+  try {
+    return norm_create(out, desc);
+  } catch (...) {
+    return HUGE2_ERR_ALLOC;
+  }
+}
+
+huge2_status huge2_norm_execute(const huge2_norm_plan* plan, const void* x, const float* gamma,
+                                const float* beta, void* y, float* stats, void* hip_stream) {
+  return norm_run(plan, x, gamma, beta, y, stats, (hipStream_t)hip_stream);
+}
+
+huge2_status huge2_norm_grad_execute(const huge2_norm_plan* plan, const void* x, const void* dy,
+                                     const float* stats, const float* gamma, const float* beta,
+                                     void* dx, float* dgamma, float* dbeta, void* hip_stream) {
+  return norm_grad_run(plan, x, dy, stats, gamma, beta, dx, dgamma, dbeta,
+                       (hipStream_t)hip_stream);
+}
+
+const char* huge2_norm_plan_kernel(const huge2_norm_plan* plan, int32_t grad) {
+  return plan ? plan->kernel_name[grad != 0] : "";
+}
+
+huge2_status huge2_norm_plan_destroy(huge2_norm_plan* plan) {
+  if (!plan) return HUGE2_OK;
+  const huge2_status st = device_free(plan->ws);
+  delete plan;
+  return st;
+}
+
+huge2_status huge2_embedding(const huge2_embedding_desc* desc, const void* ids, int64_t tokens,
+                             const void* table, void* y, void* hip_stream) {
+  return embed_run(desc, ids, tokens, table, y, (hipStream_t)hip_stream);
+}
+
+huge2_status huge2_embedding_grad_plan_create(huge2_embedding_grad_plan** out,
+                                              const huge2_embedding_desc* desc,
+                                              int64_t max_tokens) {
+  try {
+    return embed_grad_create(out, desc, max_tokens);
+  } catch (...) {
+    return HUGE2_ERR_ALLOC;
+  }
+}
+
+huge2_status huge2_embedding_grad_execute(const huge2_embedding_grad_plan* plan, const void* ids,
+                                          int64_t tokens, const void* dy, void* dtable,
+                                          void* hip_stream) {
+  return embed_grad_run(plan, ids, tokens, dy, dtable, (hipStream_t)hip_stream);
+}
+
+const char* huge2_embedding_grad_plan_kernel(const huge2_embedding_grad_plan* plan, int64_t) {
+  return plan ? plan->kernel_name : "";
+}
+
+huge2_status huge2_embedding_grad_plan_destroy(huge2_embedding_grad_plan* plan) {
+  if (!plan) return HUGE2_OK;
+  const huge2_status st = device_free(plan->ws);
+  delete plan;
+  return st;
+}
+
+huge2_status huge2_adamw_plan_create(huge2_adamw_plan** out, const huge2_adamw_tensor* tensors,
+                                     int32_t count, int32_t state_bits, void* hip_stream) {
+  try {
+    return adamw_create(out, tensors, count, state_bits, (hipStream_t)hip_stream);
+  } catch (...) {
+    if (out) *out = nullptr;
+    return HUGE2_ERR_ALLOC;
+  }
+}
+
+huge2_status huge2_adamw_step(const huge2_adamw_plan* plan, const void* const* grads,
+                              const huge2_adamw_options* options, const float* grad_scale,
+                              void* hip_stream) {
+  return adamw_run(plan, grads, options, grad_scale, (hipStream_t)hip_stream);
+}
+
+huge2_status huge2_adamw_plan_destroy(huge2_adamw_plan* plan) {
+  if (!plan) return HUGE2_OK;
+  const huge2_status st = device_free(plan->table);
+  delete plan;
+  return st;
+}
+
+}  // extern "C"

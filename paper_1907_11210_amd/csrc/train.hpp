@@ -1,0 +1,108 @@
+// train.hpp -- kernel arguments and launchers of the operators around the
+// convolutions (huge2_train.h): group norm, embedding, AdamW.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstddef>
+#include <cstdint>
+
+#include "huge2.h"
+
+namespace huge2 {
+
+// ---- group norm (norm.hip) ---------------------------------------------------
+
+// Two forms share these arguments.  The maps of an image are cut into `chunks`
+// runs of `chunk_len` pixels; per (image, chunk, channel) a pair of sums goes to
+// `part`; they are merged per group, and a second pass over x writes the result.
+struct NormArgs {
+  const void* x;
+  const void* dy;
+  const float* stats;  // [n][groups][2]: mean, rstd (the gradient's input)
+  const float* gamma;  // null: ones
+  const float* beta;   // null: zeros
+  void* out;           // y or dx
+  float* stats_out;    // the forward's, the caller's or the plan's
+  float2* part;        // [n][chunks][c]
+  float2* coef;        // gradient: [n][groups], the two group means
+  float* dgamma;
+  float* dbeta;
+  int n, c, hw, groups, d;
+  int act;
+  float eps;
+  int chunks, chunk_len;
+  int lanes_log2;  // lanes of a wave side by side on one row (pixel or plane)
+  int cblocks;     // NHWC: blocks of lanes * vector width channels
+};
+
+hipError_t launch_norm(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
+hipError_t launch_norm_grad(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
+
+// ---- embedding (embedding.hip) -------------------------------------------------
+
+struct EmbedArgs {
+  const void* ids;
+  const void* table;
+  void* y;
+  long long tokens;
+  int rows, dim;
+  int id64;
+  float scale;
+  int lanes_log2;
+};
+hipError_t launch_embedding(const EmbedArgs& a, int dtype, int vec, hipStream_t stream);
+
+constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
+constexpr int kSortTile = 1024;  // tokens of a sorting workgroup, one a thread
+
+struct EmbedGradArgs {
+  const void* ids;
+  const void* dy;
+  void* dtable;
+  int tokens, rows, dim;
+  int id64;
+  float scale;
+  // tokens in the order of (id, token): keys (an id, or `rows` for one outside the
+  // table) and token numbers, twice: a sorting pass reads one and writes the other
+  int* key[2];
+  int* token[2];
+  int* hist;      // [kDigits][tiles]
+  int tiles;      // sorting workgroups
+  int passes;     // of kDigitBits each
+  float* part;    // [chunks][2][dim]: sums of rows that cross a chunk's ends
+  int chunks, chunk_len;
+  int lanes_log2;
+};
+hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, int vec, hipStream_t stream);
+
+// ---- AdamW (adamw.hip) -----------------------------------------------------------
+
+constexpr int kAdamBlock = 256;    // elements that share a scale
+constexpr int kAdamWork = 4096;    // elements of a workgroup
+constexpr int kAdamTensors = 256;  // tensors of a launch: their gradients are kernel arguments
+
+struct AdamTensorDev {
+  void* param;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  long long count;
+  int bf16, grad_bf16;
+  float weight_decay;
+  int pad;
+};
+struct AdamArgs {
+  const AdamTensorDev* tensors;  // of the launch
+  const uint2* works;            // (tensor of the launch, run of kAdamWork elements)
+  const float* grad_scale;
+  float beta1, beta2, rest1, rest2;  // rest: 1 - beta
+  float lr, eps;
+  float step_size;  // lr / (1 - beta1^step)
+  float root;       // 1 / sqrt(1 - beta2^step)
+  const void* grads[kAdamTensors];
+};
+hipError_t launch_adamw(const AdamArgs& a, unsigned works, int state_bits, hipStream_t stream);
+
+}  // namespace huge2

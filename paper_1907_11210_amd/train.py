@@ -1,0 +1,424 @@
+"""Python binding of the operators around the convolutions (the C ABI in
+include/huge2_train.h): group norm with an activation, embedding lookup and the
+AdamW step, with their gradients.
+
+Argument marshalling only, as in :mod:`paper_1907_11210_amd.huge2`: the ``huge2_*``
+functions mirror the C entry points and take raw device pointers (ints);
+:class:`GroupNorm`, :class:`Embedding` and :class:`AdamW` take torch tensors and
+enqueue on the current stream.  Objects belong to the device that was current when
+they were made; one object's calls share its workspace, so make them on one stream
+or order them.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import huge2 as h2
+
+NORM_ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "tanh": 2, "silu": 3}
+STATE_BLOCK = 256  # elements that share a scale in 8-bit states
+
+EXPORTED = (
+    "huge2_norm_plan_create", "huge2_norm_execute", "huge2_norm_grad_execute",
+    "huge2_norm_plan_kernel", "huge2_norm_plan_destroy",
+    "huge2_embedding", "huge2_embedding_grad_plan_create", "huge2_embedding_grad_execute",
+    "huge2_embedding_grad_plan_kernel", "huge2_embedding_grad_plan_destroy",
+    "huge2_adamw_plan_create", "huge2_adamw_step", "huge2_adamw_plan_destroy",
+)
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("n", "c", "h", "w", "groups", "layout", "dtype",
+                                              "activation")] + [("eps", ctypes.c_float)]
+
+
+class EmbeddingDesc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("rows", "dim", "dtype", "id_bits")] + \
+        [("scale", ctypes.c_float)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("param", "m", "v", "m_scale", "v_scale", "copy")] + \
+        [("count", ctypes.c_int64), ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+         ("weight_decay", ctypes.c_float)]
+
+
+class AdamWOptions(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_double) for f in ("lr", "beta1", "beta2", "eps")] + \
+        [("step", ctypes.c_int64)]
+
+
+_lib = None
+
+
+def lib():
+    """The loaded libhuge2.so with these entry points' types; raises if it is not built."""
+    global _lib
+    if _lib is None:
+        L = h2.lib()
+        vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+        out = ctypes.POINTER(vp)
+        types = {
+            "huge2_norm_plan_create": [out, ctypes.POINTER(NormDesc)],
+            "huge2_norm_execute": [vp] * 7,
+            "huge2_norm_grad_execute": [vp] * 10,
+            "huge2_norm_plan_kernel": [vp, i32],
+            "huge2_norm_plan_destroy": [vp],
+            "huge2_embedding": [ctypes.POINTER(EmbeddingDesc), vp, i64, vp, vp, vp],
+            "huge2_embedding_grad_plan_create": [out, ctypes.POINTER(EmbeddingDesc), i64],
+            "huge2_embedding_grad_execute": [vp, vp, i64, vp, vp, vp],
+            "huge2_embedding_grad_plan_kernel": [vp, i64],
+            "huge2_embedding_grad_plan_destroy": [vp],
+            "huge2_adamw_plan_create": [out, ctypes.POINTER(AdamWTensor), i32, i32, vp],
+            "huge2_adamw_step": [vp, out, ctypes.POINTER(AdamWOptions), vp, vp],
+            "huge2_adamw_plan_destroy": [vp],
+        }
+        for name in EXPORTED:
+            fn = getattr(L, name)
+            fn.argtypes = types[name]
+            fn.restype = ctypes.c_char_p if name.endswith("_kernel") else ctypes.c_int
+        _lib = L
+    return _lib
+
+
+# ---- the C entry points ---------------------------------------------------
+
+def huge2_norm_plan_create(desc):
+    plan = ctypes.c_void_p()
+    h2._check(lib().huge2_norm_plan_create(ctypes.byref(plan), ctypes.byref(desc)),
+              "huge2_norm_plan_create")
+    return plan
+
+
+def huge2_norm_execute(plan, x_ptr, gamma_ptr, beta_ptr, y_ptr, stats_ptr=0, stream=0):
+    h2._check(lib().huge2_norm_execute(plan, x_ptr, gamma_ptr, beta_ptr, y_ptr, stats_ptr, stream),
+              "huge2_norm_execute")
+
+
+def huge2_norm_grad_execute(plan, x_ptr, dy_ptr, stats_ptr, gamma_ptr, beta_ptr, dx_ptr,
+                            dgamma_ptr=0, dbeta_ptr=0, stream=0):
+    h2._check(lib().huge2_norm_grad_execute(plan, x_ptr, dy_ptr, stats_ptr, gamma_ptr, beta_ptr,
+                                            dx_ptr, dgamma_ptr, dbeta_ptr, stream),
+              "huge2_norm_grad_execute")
+
+
+def huge2_norm_plan_kernel(plan, grad=False):
+    return lib().huge2_norm_plan_kernel(plan, int(grad)).decode()
+
+
+def huge2_norm_plan_destroy(plan):
+    h2._check(lib().huge2_norm_plan_destroy(plan), "huge2_norm_plan_destroy")
+
+
+def huge2_embedding(desc, ids_ptr, tokens, table_ptr, y_ptr, stream=0):
+    h2._check(lib().huge2_embedding(ctypes.byref(desc), ids_ptr, tokens, table_ptr, y_ptr, stream),
+              "huge2_embedding")
+
+
+def huge2_embedding_grad_plan_create(desc, max_tokens):
+    plan = ctypes.c_void_p()
+    h2._check(lib().huge2_embedding_grad_plan_create(ctypes.byref(plan), ctypes.byref(desc),
+                                                     max_tokens),
+              "huge2_embedding_grad_plan_create")
+    return plan
+
+
+def huge2_embedding_grad_execute(plan, ids_ptr, tokens, dy_ptr, dtable_ptr, stream=0):
+    h2._check(lib().huge2_embedding_grad_execute(plan, ids_ptr, tokens, dy_ptr, dtable_ptr,
+                                                 stream), "huge2_embedding_grad_execute")
+
+
+def huge2_embedding_grad_plan_kernel(plan, tokens):
+    return lib().huge2_embedding_grad_plan_kernel(plan, tokens).decode()
+
+
+def huge2_embedding_grad_plan_destroy(plan):
+    h2._check(lib().huge2_embedding_grad_plan_destroy(plan), "huge2_embedding_grad_plan_destroy")
+
+
+def huge2_adamw_plan_create(tensors, state_bits, stream=0):
+    """tensors: a sequence of :class:`AdamWTensor`."""
+    plan = ctypes.c_void_p()
+    arr = (AdamWTensor * len(tensors))(*tensors)
+    h2._check(lib().huge2_adamw_plan_create(ctypes.byref(plan), arr, len(tensors), state_bits,
+                                            stream), "huge2_adamw_plan_create")
+    return plan
+
+
+def huge2_adamw_step(plan, grad_ptrs, options, grad_scale_ptr=0, stream=0):
+    """grad_ptrs: a ctypes array of void pointers, one a tensor."""
+    h2._check(lib().huge2_adamw_step(plan, grad_ptrs, ctypes.byref(options), grad_scale_ptr,
+                                     stream), "huge2_adamw_step")
+
+
+def huge2_adamw_plan_destroy(plan):
+    h2._check(lib().huge2_adamw_plan_destroy(plan), "huge2_adamw_plan_destroy")
+
+
+# ---- torch conveniences -----------------------------------------------------
+
+_torch = h2._torch
+
+
+def _current_device():
+    torch = _torch()
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def _stream(device):
+    return _torch().cuda.current_stream(device).cuda_stream
+
+
+def _take(t, name, device, shape, dtype):
+    """Pointer of a tensor that has to be this one's like; 0 for None."""
+    h2._check_tensor(t, name, device)
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError("%s is %s %s, expected %s %s"
+                         % (name, tuple(t.shape), t.dtype, tuple(shape), dtype))
+    return t.data_ptr()
+
+
+class _Owner:
+    """Closes its plan once."""
+    _plan = None
+    _destroy = None
+
+    def close(self):
+        plan, self._plan = self._plan, None
+        if plan is not None:
+            type(self)._destroy(plan)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GroupNorm(_Owner):
+    """y = activation(group_norm(x) * gamma + beta) for inputs of one shape
+    (``layout`` "NHWC" or "NCHW"), and its gradients.  activation: None, "relu",
+    "tanh" or "silu"."""
+    _destroy = staticmethod(huge2_norm_plan_destroy)
+
+    def __init__(self, x_shape, groups, dtype, layout="NCHW", activation=None, eps=1e-5):
+        torch = _torch()
+        lay = h2._layout_code(layout)
+        if len(x_shape) != 4:
+            raise ValueError("x must be 4-D")
+        if activation not in NORM_ACTIVATIONS:
+            raise ValueError("unknown activation %r (none, relu, tanh, silu)" % (activation,))
+        n, c, h, w = x_shape if lay == h2.HUGE2_NCHW else [x_shape[i] for i in (0, 3, 1, 2)]
+        self.x_shape, self.dtype = torch.Size(x_shape), dtype
+        self.param_shape = torch.Size((c,))
+        self.stats_shape = torch.Size((n, groups, 2))
+        self.device = _current_device()
+        self.desc = NormDesc(n, c, h, w, groups, lay, h2._dtype_code(torch.empty(0, dtype=dtype)),
+                             NORM_ACTIVATIONS[activation], eps)
+        self._plan = huge2_norm_plan_create(self.desc)
+
+    def _param(self, t, name):
+        return 0 if t is None else _take(t, name, self.device, self.param_shape,
+                                         _torch().float32)
+
+    def _out(self, out):
+        if out is None:
+            return _torch().empty(self.x_shape, dtype=self.dtype, device=self.device)
+        _take(out, "out", self.device, self.x_shape, self.dtype)
+        return out
+
+    def __call__(self, x, gamma=None, beta=None, out=None, stats=None):
+        """y; ``stats`` ([n, groups, 2] float32, :meth:`new_stats`) receives the mean and
+        reciprocal standard deviation that :meth:`grad` reads."""
+        xp = _take(x, "x", self.device, self.x_shape, self.dtype)
+        y = self._out(out)
+        sp = 0 if stats is None else _take(stats, "stats", self.device, self.stats_shape,
+                                           _torch().float32)
+        huge2_norm_execute(self._plan, xp, self._param(gamma, "gamma"), self._param(beta, "beta"),
+                           y.data_ptr(), sp, _stream(self.device))
+        return y
+
+    def new_stats(self):
+        return _torch().empty(self.stats_shape, device=self.device)
+
+    def grad(self, x, dy, stats, gamma=None, beta=None, out=None):
+        """(dx, dgamma, dbeta) for the output error dy of a call with these x, gamma and
+        beta, which filled stats."""
+        torch = _torch()
+        xp = _take(x, "x", self.device, self.x_shape, self.dtype)
+        dyp = _take(dy, "dy", self.device, self.x_shape, self.dtype)
+        sp = _take(stats, "stats", self.device, self.stats_shape, torch.float32)
+        dx = self._out(out)
+        dgamma = torch.empty(self.param_shape, device=self.device)
+        dbeta = torch.empty(self.param_shape, device=self.device)
+        huge2_norm_grad_execute(self._plan, xp, dyp, sp, self._param(gamma, "gamma"),
+                                self._param(beta, "beta"), dx.data_ptr(), dgamma.data_ptr(),
+                                dbeta.data_ptr(), _stream(self.device))
+        return dx, dgamma, dbeta
+
+    @property
+    def kernels(self):
+        """Names of the kernels that a call and a gradient launch."""
+        return huge2_norm_plan_kernel(self._plan, 0), huge2_norm_plan_kernel(self._plan, 1)
+
+
+class Embedding(_Owner):
+    """y[t] = scale * table[ids[t]] and the table's gradient.  Ids are int32 or int64
+    tensors of any shape; an id outside the table (-1 for padding) reads zeros and has no
+    gradient.  ``max_tokens``: the most that :meth:`grad` will be called with (0: none, and
+    no workspace)."""
+    _destroy = staticmethod(huge2_embedding_grad_plan_destroy)
+
+    def __init__(self, rows, dim, dtype, scale=1.0, max_tokens=0, id_dtype=None):
+        torch = _torch()
+        id_dtype = torch.int64 if id_dtype is None else id_dtype
+        if id_dtype not in (torch.int32, torch.int64):
+            raise TypeError("ids must be int32 or int64")
+        self.device = _current_device()
+        self.table_shape, self.dtype, self.id_dtype = torch.Size((rows, dim)), dtype, id_dtype
+        self.desc = EmbeddingDesc(rows, dim, h2._dtype_code(torch.empty(0, dtype=dtype)),
+                                  64 if id_dtype == torch.int64 else 32, scale)
+        self._plan = huge2_embedding_grad_plan_create(self.desc, max_tokens)
+
+    def _ids(self, ids):
+        torch = _torch()
+        if not isinstance(ids, torch.Tensor) or ids.device != self.device or \
+                not ids.is_contiguous():
+            raise ValueError("ids must be a contiguous tensor on %s" % self.device)
+        if ids.dtype != self.id_dtype:
+            raise ValueError("ids are %s, expected %s" % (ids.dtype, self.id_dtype))
+        return ids.data_ptr()
+
+    def _out(self, out, shape):
+        if out is None:
+            return _torch().empty(shape, dtype=self.dtype, device=self.device)
+        _take(out, "out", self.device, shape, self.dtype)
+        return out
+
+    def __call__(self, ids, table, out=None):
+        """y of ids' shape and the table's rows."""
+        ip = self._ids(ids)
+        tp = _take(table, "table", self.device, self.table_shape, self.dtype)
+        y = self._out(out, ids.shape + self.table_shape[1:])
+        huge2_embedding(self.desc, ip, ids.numel(), tp, y.data_ptr(), _stream(self.device))
+        return y
+
+    def grad(self, ids, dy, out=None):
+        """The table's gradient, every row of it, for the output error dy."""
+        ip = self._ids(ids)
+        dp = _take(dy, "dy", self.device, ids.shape + self.table_shape[1:], self.dtype)
+        dtable = self._out(out, self.table_shape)
+        huge2_embedding_grad_execute(self._plan, ip, ids.numel(), dp, dtable.data_ptr(),
+                                     _stream(self.device))
+        return dtable
+
+    def kernel(self, tokens):
+        """Name of the kernels that a gradient of so many tokens launches."""
+        return huge2_embedding_grad_plan_kernel(self._plan, tokens)
+
+
+class AdamW(_Owner):
+    """AdamW over a list of parameters, all in one call, in place.
+
+    params        contiguous float32 or bfloat16 tensors.
+    state_bits    32: float32 moments ``m`` and ``v``.  8: torch.float8_e4m3fn numbers of m
+                  and of sqrt(v), with float32 ``m_scale`` and ``v_scale``, one for each 256
+                  elements of a tensor.
+    weight_decay  one number, or one for each parameter.
+    copies        None, or for each parameter None or a bfloat16 tensor that receives the
+                  updated parameter (the working weights of float32 parameters).
+    grad_dtypes   None (the copies', else the parameters' own types), or one for each parameter.
+    m, v, m_scale, v_scale
+                  lists of states to go on from; made as zeros where not given.
+    """
+    _destroy = staticmethod(huge2_adamw_plan_destroy)
+
+    def __init__(self, params, state_bits=32, weight_decay=0.01, copies=None, grad_dtypes=None,
+                 m=None, v=None, m_scale=None, v_scale=None):
+        torch = _torch()
+        self.device = _current_device()
+        self.params, self.state_bits = list(params), state_bits
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits must be 32 or 8")
+        k = len(self.params)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else \
+            [weight_decay] * k
+        self.copies = list(copies) if copies is not None else [None] * k
+        state = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+
+        def states(given, sizes, dtype):
+            if given is not None:
+                return list(given)
+            return [torch.zeros(n, dtype=dtype, device=self.device) for n in sizes]
+
+        sizes = [p.numel() for p in self.params]
+        blocks = [-(-n // STATE_BLOCK) for n in sizes]
+        self.m, self.v = states(m, sizes, state), states(v, sizes, state)
+        self.m_scale = self.v_scale = None
+        if state_bits == 8:
+            self.m_scale = states(m_scale, blocks, torch.float32)
+            self.v_scale = states(v_scale, blocks, torch.float32)
+        elif m_scale is not None or v_scale is not None:
+            raise ValueError("32-bit states have no scales")
+        if grad_dtypes is None:
+            grad_dtypes = [(p if c is None else c).dtype for p, c in zip(self.params, self.copies)]
+        self.grad_dtypes = list(grad_dtypes)
+        lists = [decay, self.copies, self.m, self.v, self.grad_dtypes]
+        if state_bits == 8:
+            lists += [self.m_scale, self.v_scale]
+        if any(len(x) != k for x in lists):
+            raise ValueError("every list needs one entry for each of %d parameters" % k)
+        tensors = []
+        for i, p in enumerate(self.params):
+            def same(t, name, dtype, n=p.numel()):
+                if n == 0:
+                    return None
+                h2._check_tensor(t, name, self.device)
+                if t.dtype != dtype or t.numel() != n:
+                    raise ValueError("%s is %d x %s, expected %d x %s"
+                                     % (name, t.numel(), t.dtype, n, dtype))
+                return t.data_ptr()
+
+            t = AdamWTensor(param=same(p, "param", p.dtype), m=same(self.m[i], "m", state),
+                            v=same(self.v[i], "v", state), count=p.numel(),
+                            dtype=h2._dtype_code(p), weight_decay=decay[i],
+                            grad_dtype=h2._dtype_code(torch.empty(0, dtype=self.grad_dtypes[i])))
+            if self.copies[i] is not None:
+                t.copy = same(self.copies[i], "copy", torch.bfloat16)
+            if state_bits == 8:
+                for name in ("m_scale", "v_scale"):
+                    s = getattr(self, name)[i]
+                    if s.device != self.device or s.dtype != torch.float32 or \
+                            s.numel() != blocks[i] or not s.is_contiguous():
+                        raise ValueError("%s must be %d contiguous float32 on %s"
+                                         % (name, blocks[i], self.device))
+                    setattr(t, name, s.data_ptr() if blocks[i] else None)
+            tensors.append(t)
+        self._sizes = sizes
+        self._grads = (ctypes.c_void_p * k)()
+        self._plan = huge2_adamw_plan_create(tensors, state_bits, _stream(self.device))
+
+    def step(self, grads, lr, step, betas=(0.9, 0.999), eps=1e-8, grad_scale=None):
+        """One step (``step`` counts from 1).  grads: for each parameter its gradient, of its
+        size and gradient type, or None (the parameter stays as it is).  grad_scale: None, or
+        a float32 device tensor of one element that multiplies every gradient."""
+        if len(grads) != len(self.params):
+            raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.params)))
+        ptrs, device = self._grads, self.device
+        for i, (g, n, dtype) in enumerate(zip(grads, self._sizes, self.grad_dtypes)):
+            if g is None:
+                ptrs[i] = None
+                continue
+            if g.dtype != dtype or g.numel() != n or g.device != device or \
+                    not g.is_contiguous():
+                raise ValueError("gradient %d must be %d contiguous %s on %s"
+                                 % (i, n, dtype, device))
+            ptrs[i] = g.data_ptr()
+        sp = 0
+        if grad_scale is not None:
+            if grad_scale.device != device or grad_scale.dtype != _torch().float32 or \
+                    grad_scale.numel() != 1:
+                raise ValueError("grad_scale must be one float32 on %s" % device)
+            sp = grad_scale.data_ptr()
+        huge2_adamw_step(self._plan, ptrs, AdamWOptions(lr, betas[0], betas[1], eps, step), sp,
+                         _stream(device))

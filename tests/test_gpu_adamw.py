@@ -1,0 +1,255 @@
+"""The AdamW step over many tensors on the GPU, against its formulas in 64 bits.
+
+Tolerances: u = 2^-24.  A moment is a sum of two products with constants that are
+themselves rounded: 6u of the two terms' magnitudes.  The parameter is off by 4u of
+itself and 24u of its change (moments, root, quotient).  With 8-bit states, numbers
+are off by half a unit in e4m3's last place, 2^-4 of them or 2^-10 near zero, times
+the block's scale, which is 8u off.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_1907_11210_amd import train as tr
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+SIZES = [1, 2, 3, 4, 5, 63, 255, 256, 257, 1000, 1023, 4095, 4096, 4097, 20011, 0, 70000]
+
+
+def _within(got, ref, tol, dtype):
+    """A result of `dtype` of a value that is off by at most tol: between the roundings of
+    the interval's ends (rounding keeps order); fp32: its own rounding beside tol."""
+    if dtype == torch.bfloat16:
+        lo, hi = (v.to(dtype).double() for v in (ref - tol, ref + tol))
+        return (got >= lo) & (got <= hi)
+    return (got - ref).abs() <= tol + ref.abs() * U
+
+
+O = dict(lr=3e-3, betas=(0.9, 0.999), eps=1e-8)
+
+
+def _decode(codes, scale):
+    n = codes.numel()
+    return codes.double() * scale.double().repeat_interleave(256)[:n]
+
+
+def _encode(values, keep):
+    n = values.numel()
+    b = torch.nn.functional.pad(values, (0, -n % 256)).reshape(-1, 256)
+    top = b.abs().amax(1)
+    c = b * torch.where(top > 0, 448 / top, 0)[:, None]
+    if keep:
+        c = torch.where(c > 0, c.clamp(min=2.0 ** -9), c)
+    return c.flatten()[:n].to(torch.float8_e4m3fn), top / 448
+
+
+def _state(sizes, bits, pdtype, gdtype, seed, zero=False):
+    g = torch.Generator().manual_seed(seed)
+    s = dict(p=[(torch.randn(n, generator=g)).to(pdtype) for n in sizes],
+             g=[(torch.randn(n, generator=g) * 10.0 ** (i % 5 - 3)).to(gdtype)
+                for i, n in enumerate(sizes)])
+    m = [torch.randn(n, generator=g) * 0.1 * (not zero) for n in sizes]
+    v = [torch.rand(n, generator=g) * 0.01 * (not zero) for n in sizes]
+    if bits == 32:
+        return dict(s, m=m, v=v)
+    m, v = [_encode(x, False) for x in m], [_encode(x.sqrt(), True) for x in v]
+    return dict(s, m=[x for x, _ in m], v=[x for x, _ in v], m_scale=[x for _, x in m],
+                v_scale=[x for _, x in v])
+
+
+def _expect(s, i, bits, t, decay, gs=1.0, lr=O["lr"]):
+    (b1, b2), eps = O["betas"], O["eps"]
+    p, g = s["p"][i].double(), s["g"][i].double() * gs
+    if bits == 32:
+        m, v = s["m"][i].double(), s["v"][i].double()
+    else:
+        m = _decode(s["m"][i], s["m_scale"][i])
+        v = _decode(s["v"][i], s["v_scale"][i]) ** 2
+    m2, v2 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    mag = b1 * m.abs() + (1 - b1) * g.abs()
+    denom = v2.sqrt() / math.sqrt(1 - b2 ** t) + eps
+    size = lr / (1 - b1 ** t)
+    p2 = p * (1 - lr * decay) - size * m2 / denom
+    return p2, m2, v2, 4 * U * p.abs() + 24 * U * size * mag / denom, mag
+
+
+def _opt(s, bits, copies, decay):
+    dev = {k: [t.to(DEV) for t in s[k]] for k in s}
+    more = {k: dev[k] for k in ("m_scale", "v_scale") if k in dev}
+    copy = [torch.full((p.numel(),), 5, dtype=torch.bfloat16, device=DEV) for p in dev["p"]] \
+        if copies else None
+    opt = tr.AdamW(dev["p"], bits, decay, copy, [g.dtype for g in dev["g"]], m=dev["m"],
+                   v=dev["v"], **more)
+    return opt, dev
+
+
+@pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16], ids=["gf32", "gbf16"])
+@pytest.mark.parametrize("pdtype", [torch.float32, torch.bfloat16], ids=["pf32", "pbf16"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_step(bits, pdtype, gdtype):
+    s = _state(SIZES, bits, pdtype, gdtype, 1)
+    decay = [0.1 * (i % 3) for i in range(len(SIZES))]
+    opt, dev = _opt(s, bits, pdtype == torch.float32, decay)
+    print("adamw", bits, pdtype, gdtype, flush=True)
+    opt.step(dev["g"], step=7, **O)
+    torch.cuda.synchronize()
+    for i, n in enumerate(SIZES):
+        if n == 0:
+            continue
+        p2, m2, v2, tol, mag = _expect(s, i, bits, 7, decay[i])
+        assert _within(dev["p"][i].cpu().double(), p2, tol, pdtype).all(), (i, n)
+        if opt.copies[i] is not None:
+            assert torch.equal(opt.copies[i], dev["p"][i].bfloat16())
+        if bits == 32:
+            assert ((dev["m"][i].cpu().double() - m2).abs() <= 6 * U * mag).all()
+            assert ((dev["v"][i].cpu().double() - v2).abs() <= 6 * U * v2).all()
+            continue
+        for k, want, err in (("m", m2, 6 * U * mag), ("v", v2.sqrt(), 6 * U * v2.sqrt())):
+            scale = dev[k + "_scale"][i].cpu().double()
+            top = torch.nn.functional.pad(want, (0, -n % 256)).reshape(-1, 256).abs().amax(1)
+            assert ((scale - top / 448).abs() <= 16 * U * top / 448).all()
+            per = (top / 448).repeat_interleave(256)[:n]
+            got = _decode(dev[k][i].cpu(), dev[k + "_scale"][i].cpu())
+            # (a root that is not zero may be lifted to the smallest number)
+            tol = torch.maximum(want.abs() / 16, per * 2.0 ** -10) * (1 + 2.0 ** -10) + err + 16 * U * want.abs()
+            if k == "v":
+                tol = torch.maximum(tol, per * 2.0 ** -9)
+                assert (dev[k][i].cpu().float()[want > per * 1e-30] > 0).all()
+            assert ((got - want).abs() <= tol).all(), (k, i, n)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_from_nothing(bits):
+    """From zero states, several steps with the states that the steps leave."""
+    sizes = [300, 5000, 7]
+    s = _state(sizes, bits, torch.float32, torch.float32, 2, zero=True)
+    opt, dev = _opt(s, bits, False, 0.01)
+    for t in range(1, 6):
+        now = {k: [x.cpu() for x in dev[k]] for k in dev}
+        opt.step(dev["g"], step=t, **O)
+        for i in range(len(sizes)):
+            p2, _, _, tol, _ = _expect(now, i, bits, t, 0.01)
+            assert ((dev["p"][i].cpu().double() - p2).abs() <= tol).all(), (t, i)
+
+
+def test_more_tensors_than_a_launch_takes():
+    sizes = [1 + 37 * i % 700 for i in range(600)]
+    s = _state(sizes, 8, torch.float32, torch.bfloat16, 3)
+    opt, dev = _opt(s, 8, True, 0.0)
+    grads = list(dev["g"])
+    for i in range(0, 600, 5):
+        grads[i] = None  # no gradient: nothing of the tensor changes
+    opt.step(grads, step=2, **O)
+    for i in range(600):
+        if grads[i] is None:
+            assert torch.equal(dev["p"][i].cpu(), s["p"][i]) and bool((opt.copies[i] == 5).all())
+            assert torch.equal(dev["m"][i].cpu().view(torch.uint8), s["m"][i].view(torch.uint8))
+            assert torch.equal(dev["v_scale"][i].cpu(), s["v_scale"][i])
+        else:
+            p2, _, _, tol, _ = _expect(s, i, 8, 2, 0.0)
+            assert ((dev["p"][i].cpu().double() - p2).abs() <= tol).all(), i
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradient_scale(bits):
+    s = _state([5000], bits, torch.float32, torch.float32, 4)
+    opt, dev = _opt(s, bits, False, 0.01)
+    opt.step(dev["g"], step=3, grad_scale=torch.full((1,), 0.25, device=DEV), **O)
+    p2, _, _, tol, _ = _expect(s, 0, bits, 3, 0.01, gs=0.25)
+    assert ((dev["p"][0].cpu().double() - p2).abs() <= tol).all()
+
+
+def test_a_gradient_that_stops():
+    """8 bits: small roots next to large ones are not lost, so no parameter jumps."""
+    n = 512
+    g = torch.full((n,), 1e-7)
+    g[::256] = 1.0
+    p = torch.zeros(n, device=DEV)
+    opt = tr.AdamW([p], 8, 0.0)
+    opt.step([g.to(DEV)], step=1, **O)
+    before = p.clone()
+    for t in (2, 3, 4):
+        opt.step([torch.zeros(n, device=DEV)], step=t, **O)
+    # each step moves by less than lr * 3 (moments decay together, from at most 1 : 1)
+    assert float((p - before).abs().max()) <= 3 * 3 * O["lr"]
+    assert bool((opt.v[0].float() > 0).all())
+
+
+def test_not_finite():
+    """A NaN or infinite gradient shows: in its element, or in its block of 8-bit states."""
+    for value in (float("nan"), float("inf")):
+        for bits in (32, 8):
+            s = _state([1000], bits, torch.float32, torch.float32, 5)
+            s["g"][0][300] = value
+            opt, dev = _opt(s, bits, False, 0.0)
+            opt.step(dev["g"], step=1, **O)
+            p = dev["p"][0].cpu()
+            assert not math.isfinite(float(p[300])) and torch.isfinite(p[:300]).all() \
+                and torch.isfinite(p[301:]).all()
+            if bits == 8:
+                m = _decode(dev["m"][0].cpu(), dev["m_scale"][0].cpu())
+                v = _decode(dev["v"][0].cpu(), dev["v_scale"][0].cpu())
+                for x in (m, v):
+                    assert not torch.isfinite(x[256:512]).any()
+                    assert torch.isfinite(x[:256]).all() and torch.isfinite(x[512:]).all()
+
+
+def test_tiny_blocks_are_zeros():
+    """Moments under 2^-100 are kept as zeros with scale 0."""
+    opt = tr.AdamW([torch.ones(300, device=DEV)], 8, 0.0)
+    opt.step([torch.full((300,), 1e-33, device=DEV)], step=1, **O)
+    assert float(opt.m_scale[0].abs().max()) == 0 and float(opt.m[0].float().abs().max()) == 0
+    assert bool(torch.isfinite(opt.params[0]).all())
+
+
+def test_streams_and_graph():
+    s = _state([10000, 33], 8, torch.float32, torch.float32, 6)
+    one, dev1 = _opt(s, 8, True, 0.01)
+    two, dev2 = _opt(s, 8, True, 0.01)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            two.step(dev2["g"], step=5, **O)
+    for _ in range(3):
+        one.step(dev1["g"], step=5, **O)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in ("p", "m", "v", "m_scale", "v_scale"):
+            for a, b in zip(dev1[k], dev2[k]):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), k
+
+
+def test_refusals(monkeypatch):
+    p = torch.zeros(300, device=DEV)
+    for call in (lambda: tr.AdamW([p], 16), lambda: tr.AdamW([p.half()]), lambda: tr.AdamW([p[1:]]),
+                 lambda: tr.AdamW([p[::2]]), lambda: tr.AdamW([p.cpu()]),
+                 lambda: tr.AdamW([p], copies=[p]), lambda: tr.AdamW([p], weight_decay=[0.1, 0.1]),
+                 lambda: tr.AdamW([p], m=[p[:299]]), lambda: tr.AdamW([p], 32, m_scale=[p]),
+                 lambda: tr.AdamW([p], 8, m_scale=[p], v_scale=[p])):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    with pytest.raises(tr.h2.Huge2Error):
+        tr.AdamW([p], weight_decay=-1.0)
+    opt = tr.AdamW([p])
+    for g in (p[:299], p.bfloat16(), p.cpu(), torch.zeros(600, device=DEV)[::2]):
+        with pytest.raises(ValueError):
+            opt.step([g], step=1, **O)
+    with pytest.raises(ValueError):
+        opt.step([p, p], step=1, **O)
+    with pytest.raises(tr.h2.Huge2Error):
+        opt.step([p], step=0, **O)
+    with pytest.raises(tr.h2.Huge2Error):
+        opt.step([torch.zeros(301, device=DEV)[1:]], step=1, **O)
+    tr.AdamW([]).step([], step=1, **O)
+    monkeypatch.setenv("HUGE2_FAULT", "launch")
+    with pytest.raises(tr.h2.Huge2Error):
+        opt.step([p], step=1, **O)
+    monkeypatch.setenv("HUGE2_FAULT", "alloc")
+    with pytest.raises(tr.h2.Huge2Error):
+        tr.AdamW([p])

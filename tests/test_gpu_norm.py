@@ -1,0 +1,347 @@
+"""Group norm with an activation and its gradients on the GPU, against the
+definitions in 64 bits on the CPU.
+
+Tolerances, from the arithmetic: u = 2^-24.  A sum of values is off by less than
+DEPTH * u of the sum of their magnitudes, DEPTH the longest chain of additions (at
+most 64 in a thread, some 32 behind it).  The mean is then off by DEPTH * u * max|x|,
+a normalised value by that times rstd and by DEPTH * u of itself (half of the
+variance's share), the result by that times |gamma| (every activation's slope is at
+most 1.1), and a bf16 result by half a unit in its last place, 2^-9 of it.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_1907_11210_amd import train as tr
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U, DEPTH = 2.0 ** -24, 96
+ACTS = (None, "relu", "tanh", "silu")
+
+# n, c, h, w, groups
+SHAPES = [
+    (1, 1, 1, 1, 1),         # one value
+    (3, 8, 1, 1, 4),         # two values a group, one pixel
+    (2, 24, 5, 7, 6),        # groups of 4 in vectors of 8
+    (1, 512, 8, 8, 32),
+    (3, 200, 9, 11, 8),      # 25 channels a group
+    (2, 75, 6, 5, 5),        # odd channel count
+    (5, 30, 7, 3, 30),       # a channel a group
+    (2, 33, 16, 16, 1),      # one group, odd channels
+    (4, 128, 32, 32, 32),
+    (1, 1040, 3, 5, 2),      # wide groups, more channels than one row of lanes
+    (1, 64, 67, 131, 4),     # long odd maps: several runs
+    (70, 16, 4, 4, 4),
+    (1, 4, 256, 256, 1),     # few channels, long planes
+    (1, 2, 128, 64, 1),
+    (2, 4104, 2, 2, 3),
+]
+
+
+def _inputs(shape, dtype, seed, mean=0.5, std=1.0):
+    n, c, h, w, _ = shape
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(n, c, h, w, generator=g) * std + mean + torch.randn(c, 1, 1, generator=g)).to(dtype)
+    dy = torch.randn(n, c, h, w, generator=g).to(dtype)
+    gamma = 1 + 0.5 * torch.randn(c, generator=g)
+    beta = 0.5 * torch.randn(c, generator=g)
+    return x, dy, gamma, beta
+
+
+def _lay(t, layout):
+    return t if layout == "NCHW" else t.permute(0, 2, 3, 1).contiguous()
+
+
+def _unlay(t, layout):
+    return t if layout == "NCHW" else t.permute(0, 3, 1, 2)
+
+
+def _act(z, act):
+    if act == "relu":
+        return torch.clamp(z, min=0)
+    if act == "tanh":
+        return torch.tanh(z)
+    return z * torch.sigmoid(z) if act == "silu" else z
+
+
+def _act_slope(z, act):
+    if act == "tanh":
+        return 1 - torch.tanh(z) ** 2
+    if act == "silu":
+        s = torch.sigmoid(z)
+        return s * (1 + z * (1 - s))
+    return torch.ones_like(z)
+
+
+def _reference(x, gamma, beta, groups, act, eps):
+    n, c = x.shape[:2]
+    xg = x.double().reshape(n, groups, -1)
+    mean = xg.mean(2)
+    rstd = 1 / torch.sqrt(((xg - mean[..., None]) ** 2).mean(2) + eps)
+    z = ((xg - mean[..., None]) * rstd[..., None]).reshape(x.shape) * gamma.double()[:, None, None] \
+        + beta.double()[:, None, None]
+    return _act(z, act), mean, rstd
+
+
+def _within(got, ref, tol, dtype):
+    """A result of `dtype` of a value that is off by at most tol: between the roundings of
+    the interval's ends (rounding keeps order); fp32: its own rounding beside tol."""
+    if dtype == torch.bfloat16:
+        lo, hi = (v.to(dtype).double() for v in (ref - tol, ref + tol))
+        return (got >= lo) & (got <= hi)
+    return (got - ref).abs() <= tol + ref.abs() * U
+
+
+def _run(shape, layout, dtype, act, seed=0, **kw):
+    n, c, h, w, groups = shape
+    x, dy, gamma, beta = _inputs(shape, dtype, seed, **kw)
+    xs = _lay(x, layout).to(DEV)
+    gn = tr.GroupNorm(xs.shape, groups, dtype, layout, act)
+    stats = gn.new_stats()
+    y = gn(xs, gamma.to(DEV), beta.to(DEV), stats=stats)
+    torch.cuda.synchronize()
+    return gn, x, dy, gamma, beta, xs, y, stats
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_forward(shape, layout, dtype):
+    for act in ACTS:
+        print("norm", shape, layout, dtype, act, flush=True)
+        gn, x, _, gamma, beta, xs, y, stats = _run(shape, layout, dtype, act)
+        ref, mean, rstd = _reference(x, gamma, beta, shape[4], act, 1e-5)
+        xmax = x.double().abs().max()
+        by = rstd.repeat_interleave(shape[1] // shape[4], 1)[..., None, None]
+        xh = (x.double().abs() + xmax) * by
+        tol = U * (DEPTH * (xmax * by + xh) + 8) * gamma.double().abs()[:, None, None] * 1.1 \
+            + U * 8 * beta.double().abs()[:, None, None]
+        got = _unlay(y.cpu(), layout).double()
+        assert _within(got, ref, tol, dtype).all(), float(((got - ref).abs() / tol).max())
+        st = stats.cpu().double()
+        assert ((st[..., 0] - mean).abs() <= DEPTH * U * xmax).all()
+        assert ((st[..., 1] - rstd).abs() <= DEPTH * U * (1 + xmax * rstd) * rstd).all()
+        # without statistics, the same bits
+        assert torch.equal(gn(xs, gamma.to(DEV), beta.to(DEV)), y)
+
+
+def _grad_reference(x, dy, gamma, beta, stats, groups, act):
+    """From the statistics that the kernel is given; a ReLU's mask is that of z rounded as the
+    forward rounds it (to 24 bits after each of its four operations)."""
+    n, c = x.shape[:2]
+    per = c // groups
+    mean, rstd = (stats[..., i].repeat_interleave(per, 1)[..., None, None] for i in (0, 1))
+    z32 = ((x.float() - mean) * rstd) * gamma[:, None, None] + beta[:, None, None]
+    mean, rstd = mean.double(), rstd.double()
+    xh = (x.double() - mean) * rstd
+    ga = gamma.double()[:, None, None]
+    dz = dy.double() * _act_slope(xh * ga + beta.double()[:, None, None], act)
+    if act == "relu":
+        dz = torch.where(z32 > 0, dz, 0)
+    t = dz * ga
+
+    def group_mean(v):
+        return v.reshape(n, groups, -1).mean(2).repeat_interleave(per, 1)[..., None, None]
+
+    dx = rstd * (t - group_mean(t) - xh * group_mean(t * xh))
+    # magnitudes of what is added up, for the tolerances
+    mag = rstd * (t.abs() + group_mean(t.abs()) + xh.abs() * group_mean((t * xh).abs()))
+    near = (x.double().abs() + mean.abs()) * rstd  # what xh's own rounding is a share of
+    return dx, (dz * xh).sum((0, 2, 3)), dz.sum((0, 2, 3)), mag, dz, xh, near
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_gradients(shape, layout, dtype):
+    for act in ACTS:
+        print("norm grad", shape, layout, dtype, act, flush=True)
+        gn, x, dy, gamma, beta, xs, _, stats = _run(shape, layout, dtype, act, seed=1)
+        dx, dgamma, dbeta = gn.grad(xs, _lay(dy, layout).to(DEV), stats, gamma.to(DEV),
+                                    beta.to(DEV))
+        torch.cuda.synchronize()
+        rx, rg, rb, mag, dz, xh, near = _grad_reference(x, dy, gamma, beta, stats.cpu(), shape[4],
+                                                        act)
+        # xh is off by 2u of `near`, z by that times gamma, and the slopes' own slopes are
+        # below 1: a share of `slope` in dz
+        slope = 4 * U * (2 + (near * (1 + gamma.double().abs()[:, None, None])).max())
+        tol = mag * (DEPTH * U + slope) * 2 + dy.double().abs().max() * slope * \
+            gamma.double().abs().max() * 4 * stats.cpu().double()[..., 1].max() * (1 + xh.abs().max()) ** 2
+        if act in (None, "relu"):
+            tol = mag * (DEPTH * U + slope) * 2
+        got = _unlay(dx.cpu(), layout).double()
+        assert _within(got, rx, tol, dtype).all(), float(((got - rx).abs() / tol).max())
+        ady = dy.double().abs() if act in ("tanh", "silu") else dz.abs()
+        tol_b = (DEPTH * U * dz.abs() + slope * ady).sum((0, 2, 3))
+        tol_g = (DEPTH * U * (dz * xh).abs() + slope * ady * (1 + xh.abs())).sum((0, 2, 3))
+        assert ((dbeta.cpu().double() - rb).abs() <= tol_b).all()
+        assert ((dgamma.cpu().double() - rg).abs() <= tol_g).all()
+
+
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+@pytest.mark.parametrize("act", ["tanh", "silu", None])
+def test_gradients_against_differences(act, layout):
+    """Central differences of the 64-bit definition along random directions."""
+    shape = (2, 24, 5, 7, 6)
+    gn, x, dy, gamma, beta, xs, _, stats = _run(shape, layout, torch.float32, act, seed=2)
+    dx, dgamma, dbeta = gn.grad(xs, _lay(dy, layout).to(DEV), stats, gamma.to(DEV), beta.to(DEV))
+    g = torch.Generator().manual_seed(3)
+    x, gamma, beta = x.double(), gamma.double(), beta.double()
+    for what, grad in (("x", _unlay(dx, layout)), ("gamma", dgamma), ("beta", dbeta)):
+        base = {"x": x, "gamma": gamma, "beta": beta}
+        v = torch.randn(base[what].shape, generator=g, dtype=torch.float64)
+        h = 1e-4
+
+        def loss(s):
+            a = dict(base, **{what: base[what] + s * v})
+            return (_reference(a["x"], a["gamma"], a["beta"], shape[4], act, 1e-5)[0]
+                    * dy.double()).sum()
+
+        got = float((grad.cpu().double() * v).sum())
+        want = float((loss(h) - loss(-h)) / (2 * h))
+        # differences: h^2 times third derivatives (some 10 each); sums of some 1e3 terms of
+        # size 1 with 24 bits
+        assert abs(got - want) <= 1e-4 * (1 + abs(want)), (what, got, want)
+
+
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+def test_values_far_from_zero(layout):
+    """A mean 1000 standard deviations from zero: sums of squares around zero would lose all."""
+    for shape in SHAPES[3:5] + SHAPES[10:11]:
+        gn, x, _, gamma, beta, xs, y, stats = _run(shape, layout, torch.float32, None, mean=1e3)
+        ref, mean, rstd = _reference(x, gamma, beta, shape[4], None, 1e-5)
+        xmax = x.double().abs().max()
+        by = rstd.repeat_interleave(shape[1] // shape[4], 1)[..., None, None]
+        tol = U * DEPTH * 3 * xmax * by * (1 + gamma.double().abs()[:, None, None])
+        assert ((_unlay(y.cpu(), layout).double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+def test_an_outlier_where_sums_begin(layout):
+    """The first pixel 1e4 standard deviations out: it is what the sums are taken around."""
+    shape = (2, 32, 16, 16, 4)
+    x, _, gamma, beta = _inputs(shape, torch.float32, 4)
+    x[:, :, 0, 0] += 1e4
+    gn = tr.GroupNorm(_lay(x, layout).shape, 4, torch.float32, layout)
+    stats = gn.new_stats()
+    gn(_lay(x, layout).to(DEV), stats=stats)
+    _, mean, rstd = _reference(x, gamma, beta, 4, None, 1e-5)
+    st = stats.cpu().double()
+    # runs of up to 256 values around the pivot: 256 u of the squares
+    assert ((st[..., 1] / rstd - 1).abs() <= (256 + DEPTH) * U).all()
+    assert ((st[..., 0] - mean).abs() <= DEPTH * U * 1e4).all()
+
+
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_not_finite_stays_in_its_group(layout, value):
+    shape = (3, 24, 6, 6, 6)
+    x, dy, gamma, beta = _inputs(shape, torch.float32, 5)
+    x[1, 9, 2, 3] = value  # image 1, group 2 (channels 8 to 11)
+    xs = _lay(x, layout).to(DEV)
+    gn = tr.GroupNorm(xs.shape, 6, torch.float32, layout, "relu")
+    stats = gn.new_stats()
+    y = _unlay(gn(xs, gamma.to(DEV), beta.to(DEV), stats=stats).cpu(), layout)
+    bad = torch.zeros(3, 24, dtype=torch.bool)
+    bad[1, 8:12] = True
+    assert torch.isnan(y[bad]).all() and torch.isfinite(y[~bad]).all()
+    dx, _, _ = gn.grad(xs, _lay(dy, layout).to(DEV), stats, gamma.to(DEV), beta.to(DEV))
+    dx = _unlay(dx.cpu(), layout)
+    assert torch.isnan(dx[bad]).all() and torch.isfinite(dx[~bad]).all()
+
+
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+def test_constant_groups_and_absent_parameters(layout):
+    """No variance: y is beta's activation and dx is finite; no gamma, no beta: ones, zeros."""
+    shape = (2, 16, 4, 4, 4)
+    x = torch.full((2, 16, 4, 4), 3.25)
+    xs = _lay(x, layout).to(DEV)
+    gn = tr.GroupNorm(xs.shape, 4, torch.float32, layout)
+    stats = gn.new_stats()
+    assert float(gn(xs, stats=stats).abs().max()) == 0
+    dx, dgamma, dbeta = gn.grad(xs, xs, stats)
+    assert torch.isfinite(dx).all() and float(dgamma.abs().max()) == 0
+    assert torch.equal(dbeta.cpu(), torch.full((16,), 3.25 * 32))
+    x, dy, gamma, beta = _inputs(shape, torch.float32, 6)
+    xs, dys = _lay(x, layout).to(DEV), _lay(dy, layout).to(DEV)
+    ones, zeros = torch.ones(16, device=DEV), torch.zeros(16, device=DEV)
+    assert torch.equal(gn(xs), gn(xs, ones, zeros, stats=stats))
+    for a, b in zip(gn.grad(xs, dys, stats), gn.grad(xs, dys, stats, ones, zeros)):
+        assert torch.equal(a, b)
+
+
+def test_streams_and_repeats():
+    """On a side stream, and again: the same bits."""
+    shape = (4, 128, 32, 32, 32)
+    for layout in ("NHWC", "NCHW"):
+        gn, x, dy, gamma, beta, xs, y, stats = _run(shape, layout, torch.bfloat16, "silu")
+        dys, ga, be = _lay(dy, layout).to(DEV), gamma.to(DEV), beta.to(DEV)
+        first = gn.grad(xs, dys, stats, ga, be)
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            st2 = gn.new_stats()
+            y2 = gn(xs, ga, be, stats=st2)
+            again = gn.grad(xs, dys, st2, ga, be)
+        s.synchronize()
+        assert torch.equal(y, y2) and torch.equal(stats, st2)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_graph_replays():
+    gn, x, dy, gamma, beta, xs, y, stats = _run((4, 128, 32, 32, 32), "NHWC", torch.bfloat16, "relu")
+    dys, ga, be = _lay(dy, "NHWC").to(DEV), gamma.to(DEV), beta.to(DEV)
+    out, st = torch.empty_like(xs), gn.new_stats()
+    gn(xs, ga, be, out=out, stats=st)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gn(xs, ga, be, out=out, stats=st)
+        grads = gn.grad(xs, dys, st, ga, be)
+    for seed in (7, 8, 9):
+        x2, dy2, _, _ = _inputs((4, 128, 32, 32, 32), torch.bfloat16, seed)
+        xs.copy_(_lay(x2, "NHWC"))
+        dys.copy_(_lay(dy2, "NHWC"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, *grads)]
+        st2 = gn.new_stats()
+        want = [gn(xs, ga, be, stats=st2), *gn.grad(xs, dys, st2, ga, be)]
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_refusals():
+    x = torch.zeros(2, 4, 4, 16, device=DEV)
+    gn = tr.GroupNorm(x.shape, 4, torch.float32, "NHWC")
+    stats = gn.new_stats()
+    for call in (lambda: gn(x.cpu()), lambda: gn(x.permute(0, 3, 1, 2)), lambda: gn(x[:1]),
+                 lambda: gn(x.bfloat16()), lambda: gn(x, torch.ones(15, device=DEV)),
+                 lambda: gn(x, out=torch.empty(2, 4, 4, 8, device=DEV)),
+                 lambda: gn(x, stats=torch.empty(2, 4, device=DEV)),
+                 lambda: gn.grad(x, x.bfloat16(), stats),
+                 lambda: tr.GroupNorm((2, 4, 4), 4, torch.float32),
+                 lambda: tr.GroupNorm(x.shape, 4, torch.float32, "NHWC", "gelu")):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    with pytest.raises(TypeError):
+        tr.GroupNorm(x.shape, 4, torch.float16)
+    for call in (lambda: gn(x, out=x), lambda: gn.grad(x, x, stats, out=x),
+                 lambda: tr.GroupNorm(x.shape, 3, torch.float32, "NHWC")):
+        with pytest.raises(tr.h2.Huge2Error):
+            call()
+    assert np.isfinite(float(gn(x).sum()))
+
+
+def test_errors_of_the_device(monkeypatch):
+    x = torch.zeros(2, 4, 4, 16, device=DEV)
+    gn = tr.GroupNorm(x.shape, 4, torch.float32, "NHWC")
+    out = torch.full_like(x, 7)
+    monkeypatch.setenv("HUGE2_FAULT", "launch")
+    with pytest.raises(tr.h2.Huge2Error):
+        gn(x, out=out)
+    monkeypatch.setenv("HUGE2_FAULT", "alloc")
+    with pytest.raises(tr.h2.Huge2Error):
+        tr.GroupNorm(x.shape, 4, torch.float32, "NHWC")
+    assert bool((out == 7).all())
