@@ -62,11 +62,11 @@ template <typename T>
 __device__ __forceinline__ void store4(void* base, long long i, long long n, const float (&f)[4]) {
   T* p = (T*)base + i;
   if (i + 4 <= n) {
-    *(Pack<T, 4>*)p = pack<T, 4>(f);
+    store_pack<T, 4>(p, pack<T, 4>(f));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (i + e < n) p[e] = from_f32<T>(f[e]);
+      if (i + e < n) store_pack<T, 1>(p + e, pack<T, 1>({f[e]}));
   }
 }
 __device__ __forceinline__ uint32_t load_codes(const void* base, long long i, long long n) {

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a, int cblocks
     const float scale = id[j] < a.rows ? a.scale : 0.f;
 #pragma unroll
     for (int e = 0; e < VW; ++e) f[j][e] *= scale;
-    *(Pack<T, VW>*)((T*)a.y + (size_t)t * a.dim + col) = pack<T, VW>(f[j]);
+    store_pack<T, VW>((T*)a.y + (size_t)t * a.dim + col, pack<T, VW>(f[j]));
   }
 }
 
@@ -169,7 +169,7 @@ __device__ __forceinline__ void store_row(const EmbedGradArgs& a, int row, int c
   float f[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) f[e] = acc[e] * a.scale;
-  *(Pack<T, VW>*)((T*)a.dtable + (size_t)row * a.dim + col) = pack<T, VW>(f);
+  store_pack<T, VW>((T*)a.dtable + (size_t)row * a.dim + col, pack<T, VW>(f));
 }
 template <int VW>
 __device__ __forceinline__ void store_part(const EmbedGradArgs& a, int chunk, int which, int col,
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(256) void embedding_zero_kernel(EmbedGradArgs a) {
 #pragma unroll
   for (int e = 0; e < VW; ++e) zero[e] = 0.f;
   for (int col = (threadIdx.x & (lanes - 1)) * VW; col < a.dim; col += lanes * VW)
-    *(Pack<T, VW>*)((T*)a.dtable + (size_t)row * a.dim + col) = pack<T, VW>(zero);
+    store_pack<T, VW>((T*)a.dtable + (size_t)row * a.dim + col, pack<T, VW>(zero));
 }
 
 namespace {

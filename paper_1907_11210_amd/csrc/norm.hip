@@ -2,65 +2,11 @@
 //
 // Passes over x are all that these cost.  The general form takes two: sums per
 // channel and run of pixels, a merge per group, and the pass that writes.
-#include <cmath>
-
-#include "train.hpp"
-#include "train_device.hpp"
+#include "norm_device.hpp"
 
 namespace huge2 {
 
 namespace {
-
-// z of a normalised value.  Rounded after the product, here and in the gradient,
-// so that both see the same sign (and the same as a framework without fused
-// multiply-adds).
-__device__ __forceinline__ float norm_z(float xh, float gamma, float beta) {
-#pragma clang fp contract(off)
-  return xh * gamma + beta;
-}
-
-// huge2_norm_activation; act is uniform over the launch.
-__device__ __forceinline__ float norm_act(float z, int act) {
-  switch (act) {
-    case 1: return z < 0.f ? 0.f : z;
-    case 2: return tanhf(z);
-    case 3: return z / (1.f + expf(-z));
-  }
-  return z;
-}
-// dy * activation'(z)
-__device__ __forceinline__ float norm_act_grad(float dy, float z, int act) {
-  switch (act) {
-    case 1: return z > 0.f ? dy : 0.f;
-    case 2: {
-      const float th = tanhf(z);
-      return dy * (1.f - th * th);
-    }
-    case 3: {
-      const float s = 1.f / (1.f + expf(-z));
-      return dy * (s * (1.f + z * (1.f - s)));
-    }
-  }
-  return dy;
-}
-
-// Sum of one value a thread over a workgroup of 256, in every thread.
-__device__ __forceinline__ float block_sum(float v, float* lds) {
-  v = lanes_sum(v, 1);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
-}
-
-// A channel's constants: z = ((x - mean) * rstd) * gamma + beta.
-struct Channel {
-  float mean, rstd, gamma, beta;
-};
-__device__ __forceinline__ Channel channel(const NormArgs& a, const float* stats, int img, int ch) {
-  const float2 s = ((const float2*)stats)[(size_t)img * a.groups + ch / a.d];
-  return {s.x, s.y, a.gamma ? a.gamma[ch] : 1.f, a.beta ? a.beta[ch] : 0.f};
-}
 
 // Where a workgroup of 256 works in NHWC: image, run of pixels, and its threads
 // as rows of 2^lanes_log2 lanes side by side on a pixel's channels.
@@ -234,6 +180,31 @@ __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
   }
 }
 
+// dgamma and dbeta of 16 channels: 16 rows of threads share the runs.
+__device__ __forceinline__ void param_sums(const NormArgs& a, int block, float2 (&seg)[16][16]) {
+  const int col = threadIdx.x & 15, ch = block * 16 + col, row = threadIdx.x >> 4;
+  float2 s = make_float2(0.f, 0.f);
+  if (ch < a.c) {
+    const long long runs = (long long)a.n * a.chunks;
+#pragma unroll 4
+    for (long long r = row; r < runs; r += 16) {
+      const float2 v = a.part[(size_t)r * a.c + ch];
+      s.x += v.x;
+      s.y += v.y;
+    }
+  }
+  seg[row][col] = s;
+  __syncthreads();
+  if (row == 0 && ch < a.c) {
+    for (int r = 1; r < 16; ++r) {
+      s.x += seg[r][col].x;
+      s.y += seg[r][col].y;
+    }
+    if (a.dbeta) a.dbeta[ch] = s.x;
+    if (a.dgamma) a.dgamma[ch] = s.y;
+  }
+}
+
 // Joins the runs.  A workgroup to an (image, group): its statistics, or the two
 // means of its gradient; behind those, a workgroup to 16 channels: dgamma, dbeta.
 template <bool GRAD>
@@ -279,39 +250,12 @@ __global__ __launch_bounds__(256) void norm_merge_kernel(NormArgs a) {
     }
     return;
   }
-  if constexpr (GRAD) {
-    const int ch = (int)(blockIdx.x - ng) * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
-    float2 s = make_float2(0.f, 0.f);
-    if (ch < a.c) {
-      const long long runs = (long long)a.n * a.chunks;
-#pragma unroll 4
-      for (long long r = row; r < runs; r += 16) {
-        const float2 v = a.part[(size_t)r * a.c + ch];
-        s.x += v.x;
-        s.y += v.y;
-      }
-    }
-    seg[row][threadIdx.x & 15] = s;
-    __syncthreads();
-    if (row == 0 && ch < a.c) {
-      for (int r = 1; r < 16; ++r) {
-        s.x += seg[r][threadIdx.x].x;
-        s.y += seg[r][threadIdx.x].y;
-      }
-      if (a.dbeta) a.dbeta[ch] = s.x;
-      if (a.dgamma) a.dgamma[ch] = s.y;
-    }
-  }
+  if constexpr (GRAD) param_sums(a, (int)(blockIdx.x - ng), seg);
 }
 
-// y, or dx, of one value.
-template <bool GRAD>
-__device__ __forceinline__ float norm_value(float x, float dy, const Channel& k, float2 coef,
-                                            int act) {
-  const float xh = (x - k.mean) * k.rstd, z = norm_z(xh, k.gamma, k.beta);
-  if constexpr (!GRAD) return norm_act(z, act);
-  const float t = norm_act_grad(dy, z, act) * k.gamma;
-  return k.rstd * (t - coef.x - xh * coef.y);
+__global__ __launch_bounds__(256) void norm_params_kernel(NormArgs a) {
+  __shared__ float2 seg[16][16];
+  param_sums(a, blockIdx.x, seg);
 }
 
 template <typename T, int VW, bool GRAD>
@@ -335,7 +279,7 @@ __global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
     if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
 #pragma unroll
     for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD>(f[e], g[e], k[e], coef[e], a.act);
-    *(Pack<T, VW>*)(out + (size_t)p * a.c) = pack<T, VW>(f);
+    store_pack<T, VW>(out + (size_t)p * a.c, pack<T, VW>(f));
   }
 }
 
@@ -356,7 +300,7 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a) {
     if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + p), g);
 #pragma unroll
     for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD>(f[e], g[e], k, coef, a.act);
-    *(Pack<T, VW>*)(out + p) = pack<T, VW>(f);
+    store_pack<T, VW>(out + p, pack<T, VW>(f));
   }
 }
 
@@ -394,6 +338,10 @@ hipError_t launch_any(const NormArgs& a, int dtype, int nhwc, int vec, hipStream
 
 }  // namespace
 
+hipError_t launch_norm_params(const NormArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(norm_params_kernel, dim3((a.c + 15) / 16), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
 hipError_t launch_norm(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream) {
   return launch_any<false>(a, dtype, nhwc, vec, stream);
 }

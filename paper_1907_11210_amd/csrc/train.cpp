@@ -12,8 +12,10 @@
 #include <cstring>
 #include <initializer_list>
 #include <new>
+#include <numeric>
 #include <vector>
 
+#include "kernels.hpp"
 #include "train.hpp"
 
 using namespace huge2;
@@ -21,7 +23,8 @@ using namespace huge2;
 struct huge2_norm_plan {
   huge2_norm_desc desc;
   int vec;  // elements of a load
-  NormArgs args;
+  NormArgs args[2];  // forward, gradient
+  bool slab[2];
   void* ws;
   char kernel_name[2][96];
 };
@@ -116,6 +119,98 @@ size_t norm_bytes(const huge2_norm_desc& d) {
   return (size_t)d.n * d.c * d.h * d.w * elem_size(d.dtype);
 }
 
+// The form that holds slabs in registers, in NHWC: as few channels as make whole
+// groups, whole vectors and 64 bytes of a pixel, twice that while there are two
+// workgroups for each compute unit all the same.  False where a slab does not fit.
+bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
+  const int base = std::lcm(a->d, vec);
+  a->span = a->d % vec != 0;
+  const int most = slab_most(vec, grad, a->span != 0);
+  // workgroups whose entries of 8 bytes a channel stay under 64 KB of LDS
+  const auto most_threads = [&](int lanes) {
+    return vec == 8 && (grad ? lanes >= 64 : a->span != 0) ? 512 : 1024;
+  };
+  const auto slots = [&](int lanes, int threads) {
+    const int rows = threads / lanes;
+    return (a->hw + rows - 1) / rows;
+  };
+  const auto lanes_of = [&](int c) { return 1 << log2_ceil(c / vec); };
+  const auto fits = [&](long long c) {
+    if (c > a->c || c / vec > 1024) return false;
+    const int lanes = lanes_of((int)c);
+    return lanes <= most_threads(lanes) && slots(lanes, most_threads(lanes)) <= most;
+  };
+  if (!fits(base)) return false;
+  int c = base;
+  while (fits(2ll * c) && (c * esz < 64 || (long long)a->n * ((a->c + 2 * c - 1) / (2 * c)) >= 512))
+    c *= 2;
+  const int lanes = lanes_of(c);
+  int threads = std::max(64, lanes);
+  while (threads < most_threads(lanes) && slots(lanes, threads) > 4) threads *= 2;
+  a->slab_c = c;
+  a->lanes_log2 = log2_ceil(lanes);
+  a->cblocks = (a->c + c - 1) / c;
+  if ((long long)a->n * a->cblocks >= (1ll << 31)) return false;
+  a->threads = threads;
+  a->slots = slots(lanes, threads);
+  a->chunks = 1;
+  const int groups = c / a->d;
+  while (a->join_log2 < 6 && (2 << a->join_log2) * groups <= threads) ++a->join_log2;
+  division_magic((uint32_t)(a->span ? a->d : a->d / vec), &a->dl_mul, &a->dl_shift);
+  if (grad) {
+    const int entries = threads * vec / (lanes <= 32 ? 2 : 1);
+    a->lds_bytes = (entries + std::max(threads, lanes * vec)) * (int)sizeof(float2);
+  } else {
+    a->lds_bytes = (threads * (a->span ? vec : 1) + groups) * (int)sizeof(float2);
+  }
+  return true;
+}
+
+// In NCHW a slab is a group: planes of up to 64 lanes, as many planes side by side
+// as leave four vectors a thread.
+bool slab_nchw(NormArgs* a, int vec, bool grad) {
+  const int vecs = a->hw / vec, lanes = 1 << std::min(6, log2_ceil(vecs));
+  const int along = (vecs + lanes - 1) / lanes, most = slab_most(vec, grad, false);
+  if (along > most || (long long)a->n * a->groups >= (1ll << 31)) return false;
+  int threads = 64;
+  const auto slots = [&] {
+    const int planes = threads / lanes;
+    return (long long)along * ((a->d + planes - 1) / planes);
+  };
+  while (threads < 1024 && slots() > 4 && threads / lanes < a->d) threads *= 2;
+  if (slots() > most) return false;
+  a->lanes_log2 = log2_ceil(lanes);
+  a->along = along;
+  a->threads = threads;
+  a->slots = (int)slots();
+  a->chunks = 1;
+  return true;
+}
+
+// The general form.  Runs of pixels: enough workgroups for eight a compute unit,
+// each run long enough that its sums are few next to its pixels.  False where there
+// are too many.
+bool norm_runs(NormArgs* a, bool nhwc, int vec) {
+  long long chunks, units;
+  const long long hw = a->hw;
+  if (nhwc) {
+    const int vecs = a->c / vec;
+    a->lanes_log2 = std::min(6, log2_ceil(vecs));
+    a->cblocks = (vecs + (1 << a->lanes_log2) - 1) >> a->lanes_log2;
+    units = (long long)a->n * a->cblocks;
+    chunks = std::min((2048 + units - 1) / units, (hw + 63) / 64);
+  } else {
+    const long long vecs = hw / vec;
+    units = (long long)a->n * a->c;
+    chunks = std::max(std::min((8192 + units - 1) / units, (vecs + 255) / 256), (vecs + 1023) / 1024);
+    a->lanes_log2 = std::min(6, log2_ceil((vecs + chunks - 1) / chunks));
+  }
+  a->chunk_len = (int)((hw + chunks - 1) / chunks);
+  if (!nhwc) a->chunk_len = (a->chunk_len + vec - 1) / vec * vec;
+  a->chunks = (int)((hw + a->chunk_len - 1) / a->chunk_len);
+  return units * a->chunks < (1ll << 31);
+}
+
 huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
   if (!out) return HUGE2_ERR_INVALID_ARG;
   *out = nullptr;
@@ -131,44 +226,40 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
   a.act = d.activation;
   a.eps = d.eps;
   const int vec = vector_width(d.dtype, nhwc ? d.c : hw);
-  // Runs of pixels: enough workgroups for eight a compute unit, each run long
-  // enough that its sums are few next to its pixels.
-  long long chunks;
-  if (nhwc) {
-    const int vecs = d.c / vec;
-    a.lanes_log2 = std::min(6, log2_ceil(vecs));
-    a.cblocks = (vecs + (1 << a.lanes_log2) - 1) >> a.lanes_log2;
-    const long long units = (long long)d.n * a.cblocks;
-    chunks = std::min((2048 + units - 1) / units, (hw + 63) / 64);
-  } else {
-    const long long vecs = hw / vec, units = (long long)d.n * d.c;
-    chunks = std::max(std::min((8192 + units - 1) / units, (vecs + 255) / 256), (vecs + 1023) / 1024);
-    a.lanes_log2 = std::min(6, log2_ceil((vecs + chunks - 1) / chunks));
-  }
-  a.chunk_len = (int)((hw + chunks - 1) / chunks);
-  if (!nhwc) a.chunk_len = (a.chunk_len + vec - 1) / vec * vec;
-  a.chunks = (int)((hw + a.chunk_len - 1) / a.chunk_len);
-  const long long units = (long long)d.n * a.chunks * (nhwc ? a.cblocks : d.c);
-  if (units >= (1ll << 31) || (long long)d.n * d.groups + d.c / 16 + 1 >= (1ll << 31))
-    return HUGE2_ERR_UNSUPPORTED;
+  if ((long long)d.n * d.groups + d.c / 16 + 1 >= (1ll << 31)) return HUGE2_ERR_UNSUPPORTED;
   huge2_norm_plan* p = new (std::nothrow) huge2_norm_plan();
   if (!p) return HUGE2_ERR_ALLOC;
   p->desc = d;
   p->vec = vec;
-  const size_t part_b = round256((size_t)d.n * a.chunks * d.c * sizeof(float2));
+  size_t part_b = 0;
+  for (int g = 0; g < 2; ++g) {
+    NormArgs& b = p->args[g];
+    b = a;
+    p->slab[g] = nhwc ? slab_nhwc(&b, elem_size(d.dtype), vec, g != 0) : slab_nchw(&b, vec, g != 0);
+    if (!p->slab[g] && !norm_runs(&b, nhwc, vec)) {
+      delete p;
+      return HUGE2_ERR_UNSUPPORTED;
+    }
+    if (!p->slab[g] || g)
+      part_b = std::max(part_b, round256((size_t)d.n * b.chunks * d.c * sizeof(float2)));
+    if (p->slab[g])
+      std::snprintf(p->kernel_name[g], sizeof(p->kernel_name[g]), "norm_slab_%s%s_kernel v%d t%d r%d",
+                    g && nhwc ? "grad_" : "", nhwc ? "nhwc" : "nchw", vec, b.threads, b.slots);
+    else
+      std::snprintf(p->kernel_name[g], sizeof(p->kernel_name[g]), "norm_sums_%s_kernel v%d k%d",
+                    nhwc ? "nhwc" : "nchw", vec, b.chunks);
+  }
   const size_t group_b = round256((size_t)d.n * d.groups * sizeof(float2));
   const huge2_status st = device_alloc(&p->ws, part_b + group_b);
   if (st != HUGE2_OK) {
     delete p;
     return st;
   }
-  a.part = (float2*)p->ws;
-  a.coef = (float2*)((char*)p->ws + part_b);  // the forward's statistics if it has no other place
-  a.stats_out = (float*)a.coef;
-  p->args = a;
-  for (int g = 0; g < 2; ++g)
-    std::snprintf(p->kernel_name[g], sizeof(p->kernel_name[g]), "norm_sums_%s_kernel%s v%d k%d",
-                  nhwc ? "nhwc" : "nchw", g ? " grad" : "", vec, a.chunks);
+  for (NormArgs& b : p->args) {
+    b.part = (float2*)p->ws;
+    b.coef = (float2*)((char*)p->ws + part_b);  // the forward's statistics if it has no other place
+    b.stats_out = (float*)b.coef;
+  }
   *out = p;
   return HUGE2_OK;
 }
@@ -181,10 +272,11 @@ huge2_status norm_run(const huge2_norm_plan* p, const void* x, const float* gamm
   const size_t bytes = norm_bytes(d);
   if (overlap(x, bytes, y, bytes)) return HUGE2_ERR_INVALID_ARG;
   if (fault("launch")) return HUGE2_ERR_HIP;
-  NormArgs a = p->args;
+  NormArgs a = p->args[0];
   a.x = x, a.gamma = gamma, a.beta = beta, a.out = y;
   if (stats) a.stats_out = stats;
-  return launched(launch_norm(a, d.dtype, d.layout == HUGE2_NHWC, p->vec, stream));
+  return launched((p->slab[0] ? launch_norm_slab : launch_norm)(a, d.dtype, d.layout == HUGE2_NHWC,
+                                                                p->vec, stream));
 }
 
 huge2_status norm_grad_run(const huge2_norm_plan* p, const void* x, const void* dy,
@@ -197,10 +289,11 @@ huge2_status norm_grad_run(const huge2_norm_plan* p, const void* x, const void* 
   const size_t bytes = norm_bytes(d);
   if (overlap(dx, bytes, x, bytes) || overlap(dx, bytes, dy, bytes)) return HUGE2_ERR_INVALID_ARG;
   if (fault("launch")) return HUGE2_ERR_HIP;
-  NormArgs a = p->args;
+  NormArgs a = p->args[1];
   a.x = x, a.dy = dy, a.stats = stats, a.gamma = gamma, a.beta = beta, a.out = dx;
   a.dgamma = dgamma, a.dbeta = dbeta;
-  return launched(launch_norm_grad(a, d.dtype, d.layout == HUGE2_NHWC, p->vec, stream));
+  return launched((p->slab[1] ? launch_norm_slab_grad : launch_norm_grad)(
+      a, d.dtype, d.layout == HUGE2_NHWC, p->vec, stream));
 }
 
 // ---- embedding --------------------------------------------------------------------

@@ -32,11 +32,30 @@ struct NormArgs {
   float eps;
   int chunks, chunk_len;
   int lanes_log2;  // lanes of a wave side by side on one row (pixel or plane)
-  int cblocks;     // NHWC: blocks of lanes * vector width channels
+  int cblocks;     // NHWC: blocks of lanes * vector width channels; slabs of an image
+
+  // The form that holds a slab (norm_slab.hip); part is then [n][c], chunks 1.
+  int threads, slots;  // of a workgroup; vectors a thread holds
+  int lds_bytes;       // NHWC
+  int slab_c;          // NHWC: channels of a slab
+  int span;            // NHWC: vectors may cross groups
+  int join_log2;       // NHWC: lanes that join a group
+  uint32_t dl_mul, dl_shift;  // NHWC: division by a group's entries in a row
+  int along;           // NCHW: vectors a thread has of one plane
 };
+// The most slots: what leaves a workgroup of 1024 threads without spills (128
+// registers a thread; the gradient holds two tensors, and a vector that may cross
+// groups two more values for each of its channels).
+constexpr int slab_most(int vec, bool grad, bool span) {
+  return !grad ? 16 : vec < 8 ? 8 : span ? 4 : 7;
+}
 
 hipError_t launch_norm(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
 hipError_t launch_norm_grad(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
+hipError_t launch_norm_slab(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
+hipError_t launch_norm_slab_grad(const NormArgs& a, int dtype, int nhwc, int vec,
+                                 hipStream_t stream);
+hipError_t launch_norm_params(const NormArgs& a, hipStream_t stream);
 
 // ---- embedding (embedding.hip) -------------------------------------------------
 
