@@ -11,6 +11,7 @@ or order them.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 
 from . import huge2 as h2
@@ -70,7 +71,7 @@ def lib():
             "huge2_embedding_grad_plan_kernel": [vp, i64],
             "huge2_embedding_grad_plan_destroy": [vp],
             "huge2_adamw_plan_create": [out, ctypes.POINTER(AdamWTensor), i32, i32, vp],
-            "huge2_adamw_step": [vp, out, ctypes.POINTER(AdamWOptions), vp, vp],
+            "huge2_adamw_step": [vp, vp, ctypes.POINTER(AdamWOptions), vp, vp],
             "huge2_adamw_plan_destroy": [vp],
         }
         for name in EXPORTED:
@@ -146,7 +147,7 @@ def huge2_adamw_plan_create(tensors, state_bits, stream=0):
 
 
 def huge2_adamw_step(plan, grad_ptrs, options, grad_scale_ptr=0, stream=0):
-    """grad_ptrs: a ctypes array of void pointers, one a tensor."""
+    """grad_ptrs: the address of an array of device pointers, one a tensor."""
     h2._check(lib().huge2_adamw_step(plan, grad_ptrs, ctypes.byref(options), grad_scale_ptr,
                                      stream), "huge2_adamw_step")
 
@@ -165,17 +166,34 @@ def _current_device():
     return torch.device("cuda", torch.cuda.current_device())
 
 
-def _stream(device):
-    return _torch().cuda.current_stream(device).cuda_stream
+def _stream(index):
+    """The raw current stream of a device (a tenth of a microsecond; making a
+    torch.cuda.Stream takes one or two, as long as the smallest kernels)."""
+    return _torch()._C._cuda_getCurrentRawStream(index)
 
 
-def _take(t, name, device, shape, dtype):
-    """Pointer of a tensor that has to be this one's like; 0 for None."""
-    h2._check_tensor(t, name, device)
-    if t.shape != shape or t.dtype != dtype:
-        raise ValueError("%s is %s %s, expected %s %s"
-                         % (name, tuple(t.shape), t.dtype, tuple(shape), dtype))
-    return t.data_ptr()
+def _type_code(dtype):
+    torch = _torch()
+    if dtype == torch.float32:
+        return h2.HUGE2_F32
+    if dtype == torch.bfloat16:
+        return h2.HUGE2_BF16
+    raise TypeError("unsupported dtype %s (float32 or bfloat16)" % dtype)
+
+
+def _take(t, name, index, shape, dtype):
+    """Pointer of a contiguous, aligned tensor of this device, shape and type."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == index \
+                and t.is_contiguous():
+            p = t.data_ptr()
+            if p & 15 == 0:
+                return p
+    except AttributeError:
+        pass
+    h2._check_tensor(t, name, _torch().device("cuda", index))  # raises, or what is left is:
+    raise ValueError("%s is %s %s, expected %s %s"
+                     % (name, tuple(t.shape), t.dtype, tuple(shape), dtype))
 
 
 class _Owner:
@@ -187,6 +205,11 @@ class _Owner:
         plan, self._plan = self._plan, None
         if plan is not None:
             type(self)._destroy(plan)
+
+    def _open(self):
+        if self._plan is None:
+            raise ValueError("%s is closed" % type(self).__name__)
+        return self._plan
 
     def __del__(self):
         try:
@@ -213,29 +236,32 @@ class GroupNorm(_Owner):
         self.param_shape = torch.Size((c,))
         self.stats_shape = torch.Size((n, groups, 2))
         self.device = _current_device()
-        self.desc = NormDesc(n, c, h, w, groups, lay, h2._dtype_code(torch.empty(0, dtype=dtype)),
+        self._index, self._f32 = self.device.index, torch.float32
+        self.desc = NormDesc(n, c, h, w, groups, lay, _type_code(dtype),
                              NORM_ACTIVATIONS[activation], eps)
         self._plan = huge2_norm_plan_create(self.desc)
 
+    def _x(self, t, name):
+        return _take(t, name, self._index, self.x_shape, self.dtype)
+
     def _param(self, t, name):
-        return 0 if t is None else _take(t, name, self.device, self.param_shape,
-                                         _torch().float32)
+        return 0 if t is None else _take(t, name, self._index, self.param_shape, self._f32)
 
     def _out(self, out):
         if out is None:
-            return _torch().empty(self.x_shape, dtype=self.dtype, device=self.device)
-        _take(out, "out", self.device, self.x_shape, self.dtype)
-        return out
+            out = _torch().empty(self.x_shape, dtype=self.dtype, device=self.device)
+            return out, out.data_ptr()
+        return out, self._x(out, "out")
 
     def __call__(self, x, gamma=None, beta=None, out=None, stats=None):
         """y; ``stats`` ([n, groups, 2] float32, :meth:`new_stats`) receives the mean and
         reciprocal standard deviation that :meth:`grad` reads."""
-        xp = _take(x, "x", self.device, self.x_shape, self.dtype)
-        y = self._out(out)
-        sp = 0 if stats is None else _take(stats, "stats", self.device, self.stats_shape,
-                                           _torch().float32)
-        huge2_norm_execute(self._plan, xp, self._param(gamma, "gamma"), self._param(beta, "beta"),
-                           y.data_ptr(), sp, _stream(self.device))
+        xp = self._x(x, "x")
+        y, yp = self._out(out)
+        sp = 0 if stats is None else _take(stats, "stats", self._index, self.stats_shape,
+                                           self._f32)
+        huge2_norm_execute(self._open(), xp, self._param(gamma, "gamma"),
+                           self._param(beta, "beta"), yp, sp, _stream(self._index))
         return y
 
     def new_stats(self):
@@ -244,22 +270,23 @@ class GroupNorm(_Owner):
     def grad(self, x, dy, stats, gamma=None, beta=None, out=None):
         """(dx, dgamma, dbeta) for the output error dy of a call with these x, gamma and
         beta, which filled stats."""
-        torch = _torch()
-        xp = _take(x, "x", self.device, self.x_shape, self.dtype)
-        dyp = _take(dy, "dy", self.device, self.x_shape, self.dtype)
-        sp = _take(stats, "stats", self.device, self.stats_shape, torch.float32)
-        dx = self._out(out)
-        dgamma = torch.empty(self.param_shape, device=self.device)
-        dbeta = torch.empty(self.param_shape, device=self.device)
-        huge2_norm_grad_execute(self._plan, xp, dyp, sp, self._param(gamma, "gamma"),
-                                self._param(beta, "beta"), dx.data_ptr(), dgamma.data_ptr(),
-                                dbeta.data_ptr(), _stream(self.device))
+        xp, dyp = self._x(x, "x"), self._x(dy, "dy")
+        sp = _take(stats, "stats", self._index, self.stats_shape, self._f32)
+        dx, dxp = self._out(out)
+        # one allocation for both, the second on a 16-byte boundary
+        c = self.param_shape[0]
+        both = _torch().empty((c + 3 & ~3) + c, device=self.device)
+        dgamma, dbeta = both[:c], both[-c:]
+        gp = both.data_ptr()
+        huge2_norm_grad_execute(self._open(), xp, dyp, sp, self._param(gamma, "gamma"),
+                                self._param(beta, "beta"), dxp, gp, gp + (c + 3 & ~3) * 4,
+                                _stream(self._index))
         return dx, dgamma, dbeta
 
     @property
     def kernels(self):
         """Names of the kernels that a call and a gradient launch."""
-        return huge2_norm_plan_kernel(self._plan, 0), huge2_norm_plan_kernel(self._plan, 1)
+        return tuple(huge2_norm_plan_kernel(self._open(), g) for g in (0, 1))
 
 
 class Embedding(_Owner):
@@ -275,46 +302,46 @@ class Embedding(_Owner):
         if id_dtype not in (torch.int32, torch.int64):
             raise TypeError("ids must be int32 or int64")
         self.device = _current_device()
+        self._index = self.device.index
         self.table_shape, self.dtype, self.id_dtype = torch.Size((rows, dim)), dtype, id_dtype
-        self.desc = EmbeddingDesc(rows, dim, h2._dtype_code(torch.empty(0, dtype=dtype)),
+        self.desc = EmbeddingDesc(rows, dim, _type_code(dtype),
                                   64 if id_dtype == torch.int64 else 32, scale)
         self._plan = huge2_embedding_grad_plan_create(self.desc, max_tokens)
 
     def _ids(self, ids):
-        torch = _torch()
-        if not isinstance(ids, torch.Tensor) or ids.device != self.device or \
+        """Their pointer and the shape of their rows."""
+        if ids.dtype is not self.id_dtype or ids.get_device() != self._index or \
                 not ids.is_contiguous():
-            raise ValueError("ids must be a contiguous tensor on %s" % self.device)
-        if ids.dtype != self.id_dtype:
-            raise ValueError("ids are %s, expected %s" % (ids.dtype, self.id_dtype))
-        return ids.data_ptr()
+            raise ValueError("ids must be a contiguous %s tensor on %s"
+                             % (self.id_dtype, self.device))
+        return ids.data_ptr(), (*ids.shape, self.table_shape[1])
 
     def _out(self, out, shape):
         if out is None:
-            return _torch().empty(shape, dtype=self.dtype, device=self.device)
-        _take(out, "out", self.device, shape, self.dtype)
-        return out
+            out = _torch().empty(shape, dtype=self.dtype, device=self.device)
+            return out, out.data_ptr()
+        return out, _take(out, "out", self._index, shape, self.dtype)
 
     def __call__(self, ids, table, out=None):
         """y of ids' shape and the table's rows."""
-        ip = self._ids(ids)
-        tp = _take(table, "table", self.device, self.table_shape, self.dtype)
-        y = self._out(out, ids.shape + self.table_shape[1:])
-        huge2_embedding(self.desc, ip, ids.numel(), tp, y.data_ptr(), _stream(self.device))
+        ip, shape = self._ids(ids)
+        tp = _take(table, "table", self._index, self.table_shape, self.dtype)
+        y, yp = self._out(out, shape)
+        huge2_embedding(self.desc, ip, ids.numel(), tp, yp, _stream(self._index))
         return y
 
     def grad(self, ids, dy, out=None):
         """The table's gradient, every row of it, for the output error dy."""
-        ip = self._ids(ids)
-        dp = _take(dy, "dy", self.device, ids.shape + self.table_shape[1:], self.dtype)
-        dtable = self._out(out, self.table_shape)
-        huge2_embedding_grad_execute(self._plan, ip, ids.numel(), dp, dtable.data_ptr(),
-                                     _stream(self.device))
+        ip, shape = self._ids(ids)
+        dp = _take(dy, "dy", self._index, shape, self.dtype)
+        dtable, tp = self._out(out, self.table_shape)
+        huge2_embedding_grad_execute(self._open(), ip, ids.numel(), dp, tp,
+                                     _stream(self._index))
         return dtable
 
     def kernel(self, tokens):
         """Name of the kernels that a gradient of so many tokens launches."""
-        return huge2_embedding_grad_plan_kernel(self._plan, tokens)
+        return huge2_embedding_grad_plan_kernel(self._open(), tokens)
 
 
 class AdamW(_Owner):
@@ -337,6 +364,7 @@ class AdamW(_Owner):
                  m=None, v=None, m_scale=None, v_scale=None):
         torch = _torch()
         self.device = _current_device()
+        self._index = self.device.index
         self.params, self.state_bits = list(params), state_bits
         if state_bits not in (32, 8):
             raise ValueError("state_bits must be 32 or 8")
@@ -370,55 +398,64 @@ class AdamW(_Owner):
             raise ValueError("every list needs one entry for each of %d parameters" % k)
         tensors = []
         for i, p in enumerate(self.params):
-            def same(t, name, dtype, n=p.numel()):
+            n = sizes[i]
+
+            def same(t, name, dtype):
                 if n == 0:
                     return None
-                h2._check_tensor(t, name, self.device)
-                if t.dtype != dtype or t.numel() != n:
-                    raise ValueError("%s is %d x %s, expected %d x %s"
-                                     % (name, t.numel(), t.dtype, n, dtype))
-                return t.data_ptr()
+                if t.numel() != n:
+                    raise ValueError("%s has %d elements, expected %d" % (name, t.numel(), n))
+                return _take(t, name, self._index, t.shape, dtype)
 
             t = AdamWTensor(param=same(p, "param", p.dtype), m=same(self.m[i], "m", state),
-                            v=same(self.v[i], "v", state), count=p.numel(),
-                            dtype=h2._dtype_code(p), weight_decay=decay[i],
-                            grad_dtype=h2._dtype_code(torch.empty(0, dtype=self.grad_dtypes[i])))
+                            v=same(self.v[i], "v", state), count=n, dtype=_type_code(p.dtype),
+                            weight_decay=decay[i], grad_dtype=_type_code(self.grad_dtypes[i]))
             if self.copies[i] is not None:
                 t.copy = same(self.copies[i], "copy", torch.bfloat16)
             if state_bits == 8:
                 for name in ("m_scale", "v_scale"):
                     s = getattr(self, name)[i]
-                    if s.device != self.device or s.dtype != torch.float32 or \
+                    if s.get_device() != self._index or s.dtype != torch.float32 or \
                             s.numel() != blocks[i] or not s.is_contiguous():
                         raise ValueError("%s must be %d contiguous float32 on %s"
                                          % (name, blocks[i], self.device))
-                    setattr(t, name, s.data_ptr() if blocks[i] else None)
+                    setattr(t, name, s.data_ptr() if n else None)
             tensors.append(t)
         self._sizes = sizes
-        self._grads = (ctypes.c_void_p * k)()
-        self._plan = huge2_adamw_plan_create(tensors, state_bits, _stream(self.device))
+        self._plan = huge2_adamw_plan_create(tensors, state_bits, _stream(self._index))
 
     def step(self, grads, lr, step, betas=(0.9, 0.999), eps=1e-8, grad_scale=None):
         """One step (``step`` counts from 1).  grads: for each parameter its gradient, of its
         size and gradient type, or None (the parameter stays as it is).  grad_scale: None, or
         a float32 device tensor of one element that multiplies every gradient."""
-        if len(grads) != len(self.params):
-            raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.params)))
-        ptrs, device = self._grads, self.device
-        for i, (g, n, dtype) in enumerate(zip(grads, self._sizes, self.grad_dtypes)):
-            if g is None:
-                ptrs[i] = None
-                continue
-            if g.dtype != dtype or g.numel() != n or g.device != device or \
-                    not g.is_contiguous():
-                raise ValueError("gradient %d must be %d contiguous %s on %s"
-                                 % (i, n, dtype, device))
-            ptrs[i] = g.data_ptr()
+        k = len(self._sizes)
+        if len(grads) != k:
+            raise ValueError("%d gradients for %d parameters" % (len(grads), k))
+        try:
+            ptrs = self._pointers(grads, self._sizes, self.grad_dtypes)
+        except TypeError:  # some are None
+            kept = [i for i, g in enumerate(grads) if g is not None]
+            ptrs = [0] * k
+            for i, p in zip(kept, self._pointers(*([x[i] for i in kept] for x in (
+                    grads, self._sizes, self.grad_dtypes)))):
+                ptrs[i] = p
         sp = 0
         if grad_scale is not None:
-            if grad_scale.device != device or grad_scale.dtype != _torch().float32 or \
-                    grad_scale.numel() != 1:
-                raise ValueError("grad_scale must be one float32 on %s" % device)
+            if grad_scale.get_device() != self._index or \
+                    grad_scale.dtype != _torch().float32 or grad_scale.numel() != 1:
+                raise ValueError("grad_scale must be one float32 on %s" % self.device)
             sp = grad_scale.data_ptr()
-        huge2_adamw_step(self._plan, ptrs, AdamWOptions(lr, betas[0], betas[1], eps, step), sp,
-                         _stream(device))
+        ptrs = array.array("Q", ptrs)
+        huge2_adamw_step(self._open(), ptrs.buffer_info()[0],
+                         AdamWOptions(lr, betas[0], betas[1], eps, step), sp,
+                         _stream(self._index))
+
+    def _pointers(self, grads, sizes, dtypes):
+        # whole lists at a time: a loop over each gradient's properties takes twice as long
+        T = _torch().Tensor
+        if list(map(T.numel, grads)) != sizes or [g.dtype for g in grads] != dtypes or \
+                not all(map(T.is_contiguous, grads)) or \
+                any(map(self._index.__ne__, map(T.get_device, grads))):
+            raise ValueError("gradients must be contiguous tensors on %s of their parameters' "
+                             "sizes and of the types %s" % (self.device, dtypes))
+        return list(map(T.data_ptr, grads))
