@@ -61,6 +61,132 @@ __global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a, int cblocks
 
 // ---- the order of the tokens: a stable radix sort by id ---------------------------
 
+// One pass, up to kMostPlaced tokens: a workgroup places kPlaceTile of them, behind
+// all smaller digits, the equal ones of the tokens before its own, of its earlier
+// waves and of lower lanes.  For this it adds up the tiles' counts (COUNTED: those
+// that sort_tile_counts_kernel left), or counts all tokens itself, one launch less
+// and as much more work as there are workgroups: 42 cycles of its compute unit's LDS
+// atomics for 64 tokens, 4.7 us for 512 tokens, 11.5 for 16384 (8 in two launches).
+// Above, all workgroups reading all tiles' counts is what grows: three launches.
+__global__ __launch_bounds__(kPlaceTile) void sort_tile_counts_kernel(EmbedGradArgs a, int pass) {
+  __shared__ int count[kMostDigits];
+  const int digits = 1 << a.digit_bits;
+  for (int i = threadIdx.x; i < digits; i += kPlaceTile) count[i] = 0;
+  __syncthreads();
+  const int t = blockIdx.x * kPlaceTile + threadIdx.x;
+  if (t < a.tokens) {
+    const int key = pass == 0 ? known_id(a.ids, a.id64, t, a.rows) : a.key[pass & 1][t];
+    atomicAdd(&count[key >> (pass * a.digit_bits) & (digits - 1)], 1);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < digits; i += kPlaceTile)
+    a.hist[((size_t)blockIdx.x << a.digit_bits) + i] = count[i];
+}
+
+template <bool COUNTED>
+__global__ __launch_bounds__(1024) void sort_place_kernel(EmbedGradArgs a, int pass) {
+  __shared__ int all[kMostDigits], before[kMostDigits], lds[16];
+  const int digits = 1 << a.digit_bits, mask = digits - 1, shift = pass * a.digit_bits;
+  const int* from = a.key[pass & 1];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int first = blockIdx.x * kPlaceTile, t = first + threadIdx.x;
+  const bool in = threadIdx.x < kPlaceTile && t < a.tokens;
+  int key = 0, token = t;
+  if (in) {
+    key = pass == 0 ? known_id(a.ids, a.id64, t, a.rows) : from[t];
+    if (pass) token = a.token[pass & 1][t];
+  }
+  for (int i = threadIdx.x; i < digits; i += 1024) all[i] = before[i] = 0;
+  __syncthreads();
+  if constexpr (COUNTED) {
+    // four digits a thread, as many tiles side by side as there are threads for
+    const int quads = digits >> 2, rows = 1024 / quads, d = (threadIdx.x & (quads - 1)) * 4;
+    int4 sum = make_int4(0, 0, 0, 0), sum_before = sum;
+#pragma unroll 8
+    for (int tile = threadIdx.x / quads; tile < a.tiles; tile += rows) {
+      const int4 n = *(const int4*)(a.hist + ((size_t)tile << a.digit_bits) + d);
+      const int m = tile < (int)blockIdx.x ? -1 : 0;
+      sum.x += n.x, sum.y += n.y, sum.z += n.z, sum.w += n.w;
+      sum_before.x += n.x & m, sum_before.y += n.y & m;
+      sum_before.z += n.z & m, sum_before.w += n.w & m;
+    }
+    const int v[4] = {sum.x, sum.y, sum.z, sum.w};
+    const int u[4] = {sum_before.x, sum_before.y, sum_before.z, sum_before.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (v[e]) atomicAdd(&all[d + e], v[e]);
+      if (u[e]) atomicAdd(&before[d + e], u[e]);
+    }
+  } else {
+    const auto count = [&](int t0, int t1) {
+      for (int i = t0 + threadIdx.x; i < t1; i += 1024) {
+        const int digit =
+            (pass == 0 ? known_id(a.ids, a.id64, i, a.rows) : from[i]) >> shift & mask;
+        // one addition where many are the same: they would queue up at one address
+        const int lead = __builtin_amdgcn_readfirstlane(digit);
+        const unsigned long long same = __ballot(digit == lead);
+        if (__popcll(same) <= 16 || digit != lead)
+          atomicAdd(&all[digit], 1);
+        else if (__ffsll(same) - 1 == lane)
+          atomicAdd(&all[lead], __popcll(same));
+      }
+    };
+    count(0, first);
+    __syncthreads();
+    for (int i = threadIdx.x; i < digits; i += 1024) before[i] = all[i];
+    __syncthreads();
+    count(first, a.tokens);
+  }
+  __syncthreads();
+  // exclusive sums of the digits' counts, kMostDigits / 1024 neighbours a thread
+  constexpr int kPer = kMostDigits / 1024;
+  int v[kPer], s = 0;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const int i = threadIdx.x * kPer + e;
+    v[e] = i < digits ? all[i] : 0;
+    s += v[e];
+  }
+  int up = s;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int o = __shfl_up(up, m);
+    if (lane >= m) up += o;
+  }
+  if (lane == 63) lds[wave] = up;
+  __syncthreads();
+  int at = up - s;
+  for (int w = 0; w < wave; ++w) at += lds[w];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const int i = threadIdx.x * kPer + e;
+    if (i < digits) before[i] += at;
+    at += v[e];
+  }
+  int digit = 0, rank = 0;
+  unsigned long long same = 0;
+  if (wave < kPlaceTile / 64) {
+    digit = key >> shift & mask;
+    same = __ballot(in);
+    for (int b = 0; b < a.digit_bits; ++b) {
+      const unsigned long long one = __ballot(digit >> b & 1);
+      same &= digit >> b & 1 ? one : ~one;
+    }
+    rank = __popcll(same & ((1ull << lane) - 1));
+  }
+  for (int w = 0; w < kPlaceTile / 64; ++w) {  // the waves in order
+    __syncthreads();
+    if (w == wave && in) {
+      const int base = before[digit];
+      if (rank == 0) before[digit] = base + __popcll(same);
+      a.key[(pass + 1) & 1][base + rank] = key;
+      a.token[(pass + 1) & 1][base + rank] = token;
+    }
+  }
+}
+
+// For more tokens, three launches a pass.
+
 // Counts of each digit in a tile.
 __global__ __launch_bounds__(kSortTile) void sort_count_kernel(EmbedGradArgs a, int pass) {
   __shared__ int count[kDigits];
@@ -179,116 +305,214 @@ __device__ __forceinline__ void store_part(const EmbedGradArgs& a, int chunk, in
   for (int e = 0; e < VW; ++e) p[e] = acc[e];
 }
 
+// The first of the sorted tokens lo .. hi whose key is at least `key`; seven keys
+// are looked at together, since it is their latency that a search takes.
+__device__ __forceinline__ int lower_bound(const int* keys, int lo, int hi, int key) {
+  while (lo < hi) {
+    const int step = (hi - lo + 7) / 8;
+    int less = 0, probe[8];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) probe[i] = keys[min(lo + i * step, hi) - 1];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) less += (lo + i * step <= hi) & (probe[i] < key);
+    const int from = lo + less * step;
+    if (less < 7) hi = min(hi, from + step - 1);
+    lo = from;
+  }
+  return lo;
+}
+
+// Zeros to those of kZeroRows rows that no token has: a wave looks them all up at
+// once, a lane each.
+template <typename T, int VW>
+__device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, const int* key, long long part) {
+  const long long first = part * kZeroRows;
+  const int lane = threadIdx.x & 63;
+  const long long row = first + lane;
+  bool empty = lane < kZeroRows && row < a.rows;
+  if (empty) {
+    const int at = lower_bound(key, 0, a.tokens, (int)row);
+    empty = at >= a.tokens || key[at] != (int)row;
+  }
+  float zero[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) zero[e] = 0.f;
+  for (unsigned long long left = __ballot(empty); left; left &= left - 1) {
+    T* p = (T*)a.dtable + (size_t)(first + __ffsll(left) - 1) * a.dim;
+    for (int col = lane * VW; col < a.dim; col += 64 * VW) store_pack<T, VW>(p + col, pack<T, VW>(zero));
+  }
+}
+
 }  // namespace
 
 // A row of lanes to a chunk of sorted tokens and a block of columns: adds up the
-// gradients of equal ids in order.  A row of the table whose tokens all lie in the
-// chunk is written; what a chunk's first row has behind tokens of an earlier chunk
-// goes to part[chunk][0], what its last row has before a later chunk to
-// part[chunk][1].
-template <typename T, int VW>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, int cblocks) {
+// gradients of equal ids in order, 8 or 16 rows in flight.  A row of the table whose
+// tokens all lie in the chunk is written; what a chunk's first row has behind tokens
+// of an earlier chunk goes to part[chunk][0], what its last row has before a later
+// chunk to part[chunk][1].  Behind the chunks' workgroups, those of the rows without
+// tokens.
+//
+// Bound by the reads of dy, rows anywhere in memory.  A chunk is short (16 tokens)
+// so that a few thousand tokens already make a few thousand waves; the parts then
+// are an eighth of the reads at most.
+template <typename T, int VW, bool WAVE>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, int cblocks,
+                                                            unsigned sum_blocks) {
+  const int* __restrict__ key = a.key[a.passes & 1];
+  const int* __restrict__ token = a.token[a.passes & 1];
+  if (blockIdx.x >= sum_blocks) {
+    zero_rows<T, VW>(a, key, (long long)(blockIdx.x - sum_blocks) * 4 + (threadIdx.x >> 6));
+    return;
+  }
   const int lanes = 1 << a.lanes_log2;
-  const int* key = a.key[a.passes & 1];
-  const int* token = a.token[a.passes & 1];
-  const int chunk = (blockIdx.x / cblocks) * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
-  const int col = (blockIdx.x % cblocks * lanes + (threadIdx.x & (lanes - 1))) * VW;
-  if (chunk >= a.chunks || col >= a.dim) return;
+  int chunk = (blockIdx.x / cblocks) * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+  if (WAVE) chunk = __builtin_amdgcn_readfirstlane(chunk);
+  int col = (blockIdx.x % cblocks * lanes + (threadIdx.x & (lanes - 1))) * VW;
+  if (chunk >= a.chunks) return;
+  // lanes behind the last column stay (the others read keys out of theirs), on column
+  // 0, and store nothing
+  const bool in = col < a.dim;
+  if (!in) col = 0;
   const int c0 = chunk * a.chunk_len, c1 = min(a.tokens, c0 + a.chunk_len);
-  int cur = key[c0];
-  bool head = c0 > 0 && key[c0 - 1] == cur;
+  // (everything that can be is loaded before the first wait)
+  const int last = a.tokens - 1;
+  int before = key[max(c0 - 1, 0)], next = key[min(c1, last)], cur = key[c0];
+  if (WAVE) {
+    before = __builtin_amdgcn_readfirstlane(before);
+    next = __builtin_amdgcn_readfirstlane(next);
+    cur = __builtin_amdgcn_readfirstlane(cur);
+  }
+  bool head = c0 > 0 && before == cur;
   float acc[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) acc[e] = 0.f;
-  constexpr int kDeep = 8;
+  // WAVE: a whole wave to a chunk, whose keys and tokens are scalars, out of one load
+  constexpr int kDeep = WAVE ? kChunk : kChunk / 2;
   for (int i = c0; i < c1 && cur < a.rows; i += kDeep) {
-    int k[kDeep];
+    int k[kDeep], t[kDeep];
     Pack<T, VW> g[kDeep];
+    if constexpr (WAVE) {
+      const int at = min(i + (int)(threadIdx.x & (kDeep - 1)), last);
+      const int mine = key[at], token_mine = token[at];
 #pragma unroll
-    for (int j = 0; j < kDeep; ++j) k[j] = i + j < c1 ? key[i + j] : a.rows;
+      for (int j = 0; j < kDeep; ++j) {
+        k[j] = __builtin_amdgcn_readlane(mine, j);
+        t[j] = __builtin_amdgcn_readlane(token_mine, j);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        const int at = min(i + j, last);
+        k[j] = key[at];
+        t[j] = token[at];
+      }
+    }
 #pragma unroll
     for (int j = 0; j < kDeep; ++j)
-      if (k[j] < a.rows)
-        g[j] = load_pack<T, VW>((const T*)a.dy + (size_t)token[i + j] * a.dim + col);
+      if (i + j < c1 && k[j] < a.rows)
+        g[j] = load_pack<T, VW>((const T*)a.dy + (size_t)t[j] * a.dim + col);
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) {
-      if (i + j >= c1) break;
-      if (k[j] != cur) {
-        if (head)
-          store_part<VW>(a, chunk, 0, col, acc);
-        else
-          store_row<T, VW>(a, cur, col, acc);
-        head = false;
-        cur = k[j];
+      if (i + j < c1 && cur < a.rows) {
+        if (k[j] != cur) {
+          if (!in)
+            ;
+          else if (head)
+            store_part<VW>(a, chunk, 0, col, acc);
+          else
+            store_row<T, VW>(a, cur, col, acc);
+          head = false;
+          cur = k[j];
 #pragma unroll
-        for (int e = 0; e < VW; ++e) acc[e] = 0.f;
-        if (cur >= a.rows) break;
+          for (int e = 0; e < VW; ++e) acc[e] = 0.f;
+        }
+        if (cur < a.rows) {
+          float f[VW];
+          unpack<T, VW>(g[j], f);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) acc[e] += f[e];
+        }
       }
-      float f[VW];
-      unpack<T, VW>(g[j], f);
-#pragma unroll
-      for (int e = 0; e < VW; ++e) acc[e] += f[e];
     }
   }
-  if (cur >= a.rows) return;
-  const bool open = c1 < a.tokens && key[c1] == cur;
+  if (cur >= a.rows || !in) return;
   if (head)
     store_part<VW>(a, chunk, 0, col, acc);
-  else if (open)
+  else if (c1 <= last && next == cur)
     store_part<VW>(a, chunk, 1, col, acc);
   else
     store_row<T, VW>(a, cur, col, acc);
 }
 
-// The rows that cross chunks: a row of lanes to the chunk in which such a row
-// begins adds the chunks' parts in order.
+// The rows that cross chunks: a wave to the chunk in which such a row begins adds
+// the chunks' parts in order; a row of more than kFewParts parts is shared by the
+// workgroup's 16 waves, whose sums are added in wave order.
 template <typename T, int VW>
-__global__ __launch_bounds__(256) void embedding_join_kernel(EmbedGradArgs a, int cblocks) {
-  const int lanes = 1 << a.lanes_log2;
-  const int* key = a.key[a.passes & 1];
-  int chunk = (blockIdx.x / cblocks) * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
-  const int col = (blockIdx.x % cblocks * lanes + (threadIdx.x & (lanes - 1))) * VW;
-  if (chunk + 1 >= a.chunks || col >= a.dim) return;
-  const int c0 = chunk * a.chunk_len, c1 = c0 + a.chunk_len;
-  const int row = key[c1 - 1];
-  if (row >= a.rows || key[c1] != row) return;
-  if (key[c0] == row && c0 > 0 && key[c0 - 1] == row) return;  // begins earlier
+__global__ __launch_bounds__(1024) void embedding_join_kernel(EmbedGradArgs a, int cblocks) {
+  __shared__ int2 many[16];  // first part, parts
+  __shared__ float sums[16][64 * VW];
+  const int* __restrict__ key = a.key[a.passes & 1];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int chunk = blockIdx.x / cblocks * 16 + wave;
+  const int col = (blockIdx.x % cblocks * 64 + lane) * VW;
+  const bool in = col < a.dim;
+  const auto add = [&](float (&acc)[VW], int part) {
+    const float* p = a.part + (size_t)part * a.dim + col;
+    float f[VW];
+#pragma unroll
+    for (int e = 0; e < VW; ++e) f[e] = p[e];
+#pragma unroll
+    for (int e = 0; e < VW; ++e) acc[e] += f[e];
+  };
+  // the keys at the chunk's ends and where the next chunks begin, all together
+  const int c0 = chunk * a.chunk_len, c1 = c0 + a.chunk_len, last = a.tokens - 1;
+  const int before = key[min(max(c0 - 1, 0), last)], first = key[min(c0, last)];
+  const int row = key[min(c1 - 1, last)];
+  int begin[kFewParts + 1], parts = 0;
+#pragma unroll
+  for (int j = 0; j <= kFewParts; ++j) begin[j] = key[min(c1 + j * a.chunk_len, last)];
+  if (c1 <= last && row < a.rows && begin[0] == row && !(first == row && c0 > 0 && before == row)) {
+#pragma unroll
+    for (int j = 0; j <= kFewParts; ++j)  // sorted: those that it reaches come first
+      parts += (c1 + j * a.chunk_len <= last) & (begin[j] == row);
+    if (parts > kFewParts)
+      parts = (lower_bound(key, c1, a.tokens, row + 1) - 1) / a.chunk_len - chunk;
+  }
   float acc[VW];
-  const float* p = a.part + ((size_t)chunk * 2 + 1) * a.dim + col;
 #pragma unroll
-  for (int e = 0; e < VW; ++e) acc[e] = p[e];
-  for (;;) {
-    ++chunk;
-    p = a.part + (size_t)chunk * 2 * a.dim + col;
+  for (int e = 0; e < VW; ++e) acc[e] = 0.f;
+  if (lane == 0) many[wave] = make_int2(chunk, parts > kFewParts ? parts : 0);
+  if (parts && parts <= kFewParts && in) {
+    add(acc, chunk * 2 + 1);
 #pragma unroll
-    for (int e = 0; e < VW; ++e) acc[e] += p[e];
-    const int end = (chunk + 1) * a.chunk_len;
-    if (end >= a.tokens || key[end] != row) break;
+    for (int j = 0; j < kFewParts; ++j)
+      if (j < parts) add(acc, (chunk + 1 + j) * 2);
+    store_row<T, VW>(a, row, col, acc);
   }
-  store_row<T, VW>(a, row, col, acc);
-}
-
-// Zeros to the rows that no token has.
-template <typename T, int VW>
-__global__ __launch_bounds__(256) void embedding_zero_kernel(EmbedGradArgs a) {
-  const int* key = a.key[a.passes & 1];
-  const int lanes = 1 << a.lanes_log2;
-  const int row = blockIdx.x * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
-  if (row >= a.rows) return;
-  int lo = 0, hi = a.tokens;  // the first token of this row or a later one
-  while (lo < hi) {
-    const int mid = lo + (hi - lo) / 2;
-    if (key[mid] < row)
-      lo = mid + 1;
-    else
-      hi = mid;
-  }
-  if (lo < a.tokens && key[lo] == row) return;
-  float zero[VW];
+  __syncthreads();
+  for (int w = 0; w < 16; ++w) {
+    const int2 m = many[w];
+    if (m.y == 0) continue;
 #pragma unroll
-  for (int e = 0; e < VW; ++e) zero[e] = 0.f;
-  for (int col = (threadIdx.x & (lanes - 1)) * VW; col < a.dim; col += lanes * VW)
-    store_pack<T, VW>((T*)a.dtable + (size_t)row * a.dim + col, pack<T, VW>(zero));
+    for (int e = 0; e < VW; ++e) acc[e] = 0.f;
+    if (in) {
+#pragma unroll 8
+      for (int j = wave; j < m.y; j += 16) add(acc, (m.x + 1 + j) * 2);
+    }
+#pragma unroll
+    for (int e = 0; e < VW; ++e) sums[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    if (wave == w && in) {
+      for (int q = 0; q < 16; ++q)
+        if (q != wave) {
+#pragma unroll
+          for (int e = 0; e < VW; ++e) acc[e] += sums[q][e * 64 + lane];
+        }
+      add(acc, m.x * 2 + 1);
+      store_row<T, VW>(a, row, col, acc);
+    }
+    __syncthreads();
+  }
 }
 
 namespace {
@@ -309,19 +533,34 @@ hipError_t launch_grad(const EmbedGradArgs& a, hipStream_t stream) {
   const int per = 256 >> a.lanes_log2;
   const int cblocks = (a.dim / VW + (1 << a.lanes_log2) - 1) >> a.lanes_log2;
   for (int pass = 0; pass < a.passes && a.tokens; ++pass) {
+    if (a.digit_bits) {
+      if (a.tokens <= kMostRecounted) {
+        hipLaunchKernelGGL(sort_place_kernel<false>, dim3(a.tiles), dim3(1024), 0, stream, a, pass);
+      } else {
+        hipLaunchKernelGGL(sort_tile_counts_kernel, dim3(a.tiles), dim3(kPlaceTile), 0, stream, a,
+                           pass);
+        hipLaunchKernelGGL(sort_place_kernel<true>, dim3(a.tiles), dim3(1024), 0, stream, a, pass);
+      }
+      continue;
+    }
     hipLaunchKernelGGL(sort_count_kernel, dim3(a.tiles), dim3(kSortTile), 0, stream, a, pass);
     hipLaunchKernelGGL(sort_scan_kernel, dim3(kDigits), wg, 0, stream, a);
     hipLaunchKernelGGL(sort_scatter_kernel, dim3(a.tiles), dim3(kSortTile), 0, stream, a, pass);
   }
-  hipLaunchKernelGGL((embedding_zero_kernel<T, VW>), dim3((unsigned)(((long long)a.rows + per - 1) / per)),
-                     wg, 0, stream, a);
-  if (a.tokens) {
-    const long long grid = (long long)((a.chunks + per - 1) / per) * cblocks;
-    hipLaunchKernelGGL((embedding_sum_kernel<T, VW>), dim3((unsigned)grid), wg, 0, stream, a,
-                       cblocks);
-    if (a.chunks > 1)
-      hipLaunchKernelGGL((embedding_join_kernel<T, VW>), dim3((unsigned)grid), wg, 0, stream, a,
-                         cblocks);
+  const unsigned sums = (unsigned)((a.chunks + per - 1) / per * cblocks);
+  const unsigned zeros = (unsigned)(((long long)a.rows + 4 * kZeroRows - 1) / (4 * kZeroRows));
+  if (a.lanes_log2 == 6)
+    hipLaunchKernelGGL((embedding_sum_kernel<T, VW, true>), dim3(sums + zeros), wg, 0, stream, a,
+                       cblocks, sums);
+  else
+    hipLaunchKernelGGL((embedding_sum_kernel<T, VW, false>), dim3(sums + zeros), wg, 0, stream, a,
+                       cblocks, sums);
+  if (a.chunks > 1) {
+    // four columns a lane: a row with most of the tokens has more workgroups then
+    constexpr int kJoin = VW < 4 ? VW : 4;
+    const int blocks = (a.dim / kJoin + 63) / 64;
+    hipLaunchKernelGGL((embedding_join_kernel<T, kJoin>), dim3((a.chunks + 15) / 16 * blocks),
+                       dim3(1024), 0, stream, a, blocks);
   }
   return hipGetLastError();
 }

@@ -32,7 +32,7 @@ struct huge2_norm_plan {
 struct huge2_embedding_grad_plan {
   huge2_embedding_desc desc;
   int64_t max_tokens;
-  int vec, lanes_log2, passes;
+  int vec, lanes_log2;
   void* ws;
   char kernel_name[96];
 };
@@ -329,12 +329,15 @@ huge2_status embed_run(const huge2_embedding_desc* desc, const void* ids, int64_
   return launched(launch_embedding(a, d.dtype, vec, stream));
 }
 
-// Sorted tokens of a chunk: as many as leave eight waves for each compute unit,
-// at least 32, so that the parts are few next to the gradients, at most 256.
-int embed_chunk_len(const huge2_embedding_grad_plan* p, int64_t tokens) {
-  const long long vecs = p->desc.dim / p->vec;
-  const long long waves = std::max<long long>(1, tokens * vecs / 64 / 2048);
-  return (int)std::min<long long>(256, std::max<long long>(32, waves));
+// Sorted tokens of a chunk: 16, or where tokens abound and the parts would take
+// much memory 64.
+int embed_chunk_len(int64_t max_tokens) { return max_tokens > (1 << 17) ? 4 * kChunk : kChunk; }
+
+// Counts of digits: those of the placed sorts' tiles, or of the long sorts'.
+size_t embed_hist_bytes(int64_t max_tokens) {
+  const size_t placed = (std::min<int64_t>(max_tokens, kMostPlaced) + kPlaceTile - 1) / kPlaceTile;
+  const size_t tiles = max_tokens > kMostPlaced ? (max_tokens + kSortTile - 1) / kSortTile : 0;
+  return std::max(placed * kMostDigits, (tiles + 1) * kDigits) * 4;
 }
 
 huge2_status embed_grad_create(huge2_embedding_grad_plan** out, const huge2_embedding_desc* desc,
@@ -348,20 +351,18 @@ huge2_status embed_grad_create(huge2_embedding_grad_plan** out, const huge2_embe
   p->desc = *desc;
   p->max_tokens = max_tokens;
   p->vec = vector_width(desc->dtype, desc->dim);
-  p->lanes_log2 = embed_lanes_log2(*desc, p->vec);
-  p->passes = (log2_ceil((long long)desc->rows + 1) + kDigitBits - 1) / kDigitBits;
-  const size_t tiles = (max_tokens + kSortTile - 1) / kSortTile;
+  p->lanes_log2 = std::min(6, log2_ceil(desc->dim / p->vec));
+  const int chunk = embed_chunk_len(max_tokens);
   const size_t bytes = max_tokens == 0
                            ? 0
-                           : 4 * round256(max_tokens * 4) + round256((tiles + 1) * kDigits * 4) +
-                                 (max_tokens + 31) / 32 * 2 * (size_t)desc->dim * 4;
+                           : 4 * round256(max_tokens * 4) + round256(embed_hist_bytes(max_tokens)) +
+                                 (max_tokens + chunk - 1) / chunk * 2 * (size_t)desc->dim * 4;
   const huge2_status st = device_alloc(&p->ws, bytes);
   if (st != HUGE2_OK) {
     delete p;
     return st;
   }
-  std::snprintf(p->kernel_name, sizeof(p->kernel_name), "embedding_sum_kernel v%d s%d", p->vec,
-                p->passes);
+  std::snprintf(p->kernel_name, sizeof(p->kernel_name), "embedding_sum_kernel v%d", p->vec);
   *out = p;
   return HUGE2_OK;
 }
@@ -382,19 +383,25 @@ huge2_status embed_grad_run(const huge2_embedding_grad_plan* p, const void* ids,
   a.tokens = (int)tokens, a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64;
   a.scale = d.scale;
   a.lanes_log2 = p->lanes_log2;
-  a.passes = p->passes;
-  a.tiles = (int)((tokens + kSortTile - 1) / kSortTile);
-  a.chunk_len = embed_chunk_len(p, tokens);
+  const int bits = std::max(2, log2_ceil((long long)d.rows + 1));  // keys are ids, and `rows`
+  const int tile = tokens <= kMostPlaced ? kPlaceTile : kSortTile;
+  a.tiles = (int)((tokens + tile - 1) / tile);
+  if (tokens <= kMostPlaced) {
+    a.passes = (bits + kMostDigitBits - 1) / kMostDigitBits;
+    a.digit_bits = (bits + a.passes - 1) / a.passes;
+  } else {
+    a.passes = (bits + kDigitBits - 1) / kDigitBits;
+  }
+  a.chunk_len = embed_chunk_len(p->max_tokens);
   a.chunks = (int)((tokens + a.chunk_len - 1) / a.chunk_len);
   char* at = (char*)p->ws;
   const size_t list = round256(p->max_tokens * 4);
-  const size_t tiles = (p->max_tokens + kSortTile - 1) / kSortTile;
   for (int k = 0; k < 2; ++k) {
     a.key[k] = (int*)(at + 2 * k * list);
     a.token[k] = (int*)(at + (2 * k + 1) * list);
   }
   a.hist = (int*)(at + 4 * list);
-  a.part = (float*)(at + 4 * list + round256((tiles + 1) * kDigits * 4));
+  a.part = (float*)(at + 4 * list + round256(embed_hist_bytes(p->max_tokens)));
   return launched(launch_embedding_grad(a, d.dtype, p->vec, stream));
 }
 

@@ -73,6 +73,13 @@ hipError_t launch_embedding(const EmbedArgs& a, int dtype, int vec, hipStream_t 
 
 constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
 constexpr int kSortTile = 1024;  // tokens of a sorting workgroup, one a thread
+// Up to kMostPlaced tokens a pass takes one launch or (over kMostRecounted) two:
+// workgroups place kPlaceTile each, by digits of up to kMostDigits values.
+constexpr int kMostRecounted = 4096, kMostPlaced = 1 << 17, kPlaceTile = 512;
+constexpr int kMostDigitBits = 12, kMostDigits = 1 << kMostDigitBits;
+constexpr int kChunk = 16;     // sorted tokens of a chunk, or a multiple
+constexpr int kZeroRows = 16;  // rows of the table that a wave looks up
+constexpr int kFewParts = 8;   // parts that a wave adds alone
 
 struct EmbedGradArgs {
   const void* ids;
@@ -85,9 +92,10 @@ struct EmbedGradArgs {
   // table) and token numbers, twice: a sorting pass reads one and writes the other
   int* key[2];
   int* token[2];
-  int* hist;      // [kDigits][tiles]
+  int* hist;      // [kDigits][tiles], or [tiles][digits]
   int tiles;      // sorting workgroups
-  int passes;     // of kDigitBits each
+  int passes;     // of digit_bits each, or with digit_bits 0 of kDigitBits
+  int digit_bits;
   float* part;    // [chunks][2][dim]: sums of rows that cross a chunk's ends
   int chunks, chunk_len;
   int lanes_log2;
