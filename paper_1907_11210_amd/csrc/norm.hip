@@ -180,37 +180,11 @@ __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
   }
 }
 
-// dgamma and dbeta of 16 channels: 16 rows of threads share the runs.
-__device__ __forceinline__ void param_sums(const NormArgs& a, int block, float2 (&seg)[16][16]) {
-  const int col = threadIdx.x & 15, ch = block * 16 + col, row = threadIdx.x >> 4;
-  float2 s = make_float2(0.f, 0.f);
-  if (ch < a.c) {
-    const long long runs = (long long)a.n * a.chunks;
-#pragma unroll 4
-    for (long long r = row; r < runs; r += 16) {
-      const float2 v = a.part[(size_t)r * a.c + ch];
-      s.x += v.x;
-      s.y += v.y;
-    }
-  }
-  seg[row][col] = s;
-  __syncthreads();
-  if (row == 0 && ch < a.c) {
-    for (int r = 1; r < 16; ++r) {
-      s.x += seg[r][col].x;
-      s.y += seg[r][col].y;
-    }
-    if (a.dbeta) a.dbeta[ch] = s.x;
-    if (a.dgamma) a.dgamma[ch] = s.y;
-  }
-}
-
 // Joins the runs.  A workgroup to an (image, group): its statistics, or the two
 // means of its gradient; behind those, a workgroup to 16 channels: dgamma, dbeta.
 template <bool GRAD>
 __global__ __launch_bounds__(256) void norm_merge_kernel(NormArgs a) {
   __shared__ float lds[4];
-  __shared__ float2 seg[16][16];
   const long long ng = (long long)a.n * a.groups;
   if ((long long)blockIdx.x < ng) {
     const int img = (int)(blockIdx.x / a.groups), g = (int)(blockIdx.x % a.groups);
@@ -250,12 +224,15 @@ __global__ __launch_bounds__(256) void norm_merge_kernel(NormArgs a) {
     }
     return;
   }
-  if constexpr (GRAD) param_sums(a, (int)(blockIdx.x - ng), seg);
+  if constexpr (GRAD) {
+    __shared__ ParamSums sums;
+    param_sums(a, (int)(blockIdx.x - ng), sums);
+  }
 }
 
 __global__ __launch_bounds__(256) void norm_params_kernel(NormArgs a) {
-  __shared__ float2 seg[16][16];
-  param_sums(a, blockIdx.x, seg);
+  __shared__ ParamSums sums;
+  param_sums(a, blockIdx.x, sums);
 }
 
 template <typename T, int VW, bool GRAD>

@@ -74,4 +74,33 @@ __device__ __forceinline__ float norm_value(float x, float dy, const Channel& k,
   return k.rstd * (t - coef.x - xh * coef.y);
 }
 
+// dgamma and dbeta of 16 channels: rows of 16 threads share the runs.
+struct ParamSums {
+  float2 of[64][16];
+};
+__device__ __forceinline__ void param_sums(const NormArgs& a, int block, ParamSums& sums) {
+  const int col = threadIdx.x & 15, ch = block * 16 + col, row = threadIdx.x >> 4;
+  const int rows = blockDim.x >> 4;
+  float2 s = make_float2(0.f, 0.f);
+  if (ch < a.c) {
+    const long long runs = (long long)a.n * a.chunks;
+#pragma unroll 4
+    for (long long r = row; r < runs; r += rows) {
+      const float2 v = a.part[(size_t)r * a.c + ch];
+      s.x += v.x;
+      s.y += v.y;
+    }
+  }
+  sums.of[row][col] = s;
+  __syncthreads();
+  if (row == 0 && ch < a.c) {
+    for (int r = 1; r < rows; ++r) {
+      s.x += sums.of[r][col].x;
+      s.y += sums.of[r][col].y;
+    }
+    if (a.dbeta) a.dbeta[ch] = s.x;
+    if (a.dgamma) a.dgamma[ch] = s.y;
+  }
+}
+
 }  // namespace huge2

@@ -1,0 +1,562 @@
+// norm_nhwc.hip -- group norm in NHWC by slabs: some whole groups of channels of an
+// image, all of its pixels or a run of them, to a workgroup.
+//
+// Where a slab of all pixels fits the registers of a workgroup, x (and dy for the
+// gradient) are read once.  Else a first pass leaves each run's sums and a second one
+// joins them and reads x again: 1.5 times the bytes for the forward, 5/3 for the
+// gradient, of which what the Infinity Cache still holds costs less.
+#include "norm_device.hpp"
+
+namespace huge2 {
+
+namespace {
+
+// Rows of 2^lanes_log2 lanes lie side by side on a pixel's channels; a thread has one
+// vector of channels at every `rows`-th pixel of the run.
+struct Slab {
+  int img, chunk, p0, len;    // the run of pixels
+  int c0, channels, groups;   // of the slab
+  int lane, row, rows, ch;    // ch: the thread's first channel in the slab
+  bool in;
+  size_t at;                  // element of (img, p0, c0 + ch)
+};
+template <int VW>
+__device__ __forceinline__ Slab slab_of(const NormArgs& a) {
+  Slab q;
+  int s = xcd_remap(blockIdx.x, a.slabs);
+  q.c0 = s % a.cblocks * a.slab_c;
+  s /= a.cblocks;
+  q.chunk = s % a.chunks;
+  q.img = s / a.chunks;
+  q.p0 = q.chunk * a.chunk_len;
+  q.len = min(a.chunk_len, a.hw - q.p0);
+  q.channels = min(a.slab_c, a.c - q.c0);
+  q.groups = q.channels / a.d;
+  q.rows = 1 << a.rows_log2;
+  q.lane = threadIdx.x & ((1 << a.lanes_log2) - 1);
+  q.row = threadIdx.x >> a.lanes_log2;
+  q.ch = q.lane * VW;
+  q.in = q.ch < q.channels;
+  q.at = ((size_t)q.img * a.hw + q.p0) * a.c + q.c0 + q.ch;
+  return q;
+}
+// Pixels of row r.
+__device__ __forceinline__ int pixels_of(const NormArgs& a, const Slab& q, int r) {
+  return (q.len - r + q.rows - 1) >> a.rows_log2;
+}
+
+// A thread's vectors: their mean and the squares around it, per channel where a
+// vector may span groups, else over all in s[0], m2[0].
+template <typename T, int VW, int R, bool SPAN>
+__device__ __forceinline__ void own_stats(Pack<T, VW> (&f)[R], int mine, float (&s)[VW],
+                                          float (&m2)[VW]) {
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s[e] = m2[e] = 0.f;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (k < mine) {
+      float v[VW];
+      unpack<T, VW>(f[k], v);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) s[e] += v[e];
+      forget(f[k]);
+    }
+  }
+  if constexpr (!SPAN) {
+#pragma unroll
+    for (int e = 1; e < VW; ++e) s[0] += s[e];
+#pragma unroll
+    for (int e = 1; e < VW; ++e) s[e] = s[0];
+  }
+  const float own = 1.f / (float)max(1, mine * (SPAN ? 1 : VW));
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s[e] *= own;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (k < mine) {
+      float v[VW];
+      unpack<T, VW>(f[k], v);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) m2[e] += (v[e] - s[e]) * (v[e] - s[e]);
+      forget(f[k]);
+    }
+  }
+  if constexpr (!SPAN) {
+#pragma unroll
+    for (int e = 1; e < VW; ++e) m2[0] += m2[e];
+  }
+}
+
+// Joins the threads' entries: f(group of the slab, mean, squares around it) by one
+// lane of those that join the group.
+template <int VW, bool SPAN, typename F>
+__device__ __forceinline__ void join_stats(const NormArgs& a, const Slab& q, float2* lds,
+                                           const float (&s)[VW], const float (&m2)[VW], F&& f) {
+  constexpr int kPer = SPAN ? VW : 1;  // entries a thread
+  const int width = kPer << a.lanes_log2, dl = SPAN ? a.d : a.d / VW;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) lds[q.row * width + q.lane * kPer + e] = make_float2(s[e], m2[e]);
+  __syncthreads();
+  const int gl = 1 << a.join_log2, l = threadIdx.x & (gl - 1);
+  const int terms = min(q.rows, q.len) * dl;
+  constexpr float kEach = (float)(VW / kPer);
+  for (int g = threadIdx.x >> a.join_log2; g < q.groups; g += blockDim.x >> a.join_log2) {
+    const float2* e = lds + g * dl;
+    float sum = 0.f, sq = 0.f;
+    for (int t = l; t < terms; t += gl) {
+      const int r = (int)fast_div(t, a.dl_mul, a.dl_shift), j = t - r * dl;
+      sum += (float)pixels_of(a, q, r) * e[r * width + j].x;
+    }
+    for (int m = gl >> 1; m; m >>= 1) sum += __shfl_xor(sum, m);
+    const float mean = sum * kEach / ((float)a.d * (float)q.len);
+    for (int t = l; t < terms; t += gl) {
+      const int r = (int)fast_div(t, a.dl_mul, a.dl_shift), j = t - r * dl;
+      const float2 v = e[r * width + j];
+      sq += v.y + (float)pixels_of(a, q, r) * kEach * (v.x - mean) * (v.x - mean);
+    }
+    for (int m = gl >> 1; m; m >>= 1) sq += __shfl_xor(sq, m);
+    if (l == 0) f(g, mean, sq);
+  }
+}
+
+// The channels' constants of a thread whose groups' (mean, rstd) are in LDS.
+template <int VW, bool SPAN>
+__device__ __forceinline__ void channels_of(const NormArgs& a, const Slab& q, const float2* result,
+                                            Channel (&k)[VW]) {
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+    const float2 st = result[(q.ch + (SPAN ? e : 0)) / a.d];
+    k[e] = {st.x, st.y, a.gamma ? a.gamma[q.c0 + q.ch + e] : 1.f,
+            a.beta ? a.beta[q.c0 + q.ch + e] : 0.f};
+  }
+}
+
+template <typename T, int VW, int R>
+__device__ __forceinline__ void load_rows(const NormArgs& a, const Slab& q, const T* x, int first,
+                                          int mine, Pack<T, VW> (&f)[R]) {
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+    if (first + k < mine) f[k] = load_pack<T, VW>(x + (size_t)(q.row + (first + k) * q.rows) * a.c);
+}
+
+template <typename T, int VW, int R>
+__device__ __forceinline__ void write_rows(const NormArgs& a, const Slab& q, T* out, int first,
+                                           int mine, const Pack<T, VW> (&f)[R],
+                                           const Channel (&k)[VW]) {
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (first + i < mine) {
+      float v[VW];
+      unpack<T, VW>(f[i], v);
+#pragma unroll
+      for (int e = 0; e < VW; ++e)
+        v[e] = norm_value<false>(v[e], 0.f, k[e], make_float2(0.f, 0.f), a.act);
+      store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v));
+    }
+  }
+}
+
+// A thread's sums of dz and dz * xh over some of its vectors.
+template <typename T, int VW, int R>
+__device__ __forceinline__ void add_grad_sums(const NormArgs& a, int first, int mine,
+                                              Pack<T, VW> (&f)[R], Pack<T, VW> (&g)[R],
+                                              const Channel (&k)[VW], float (&s1)[VW],
+                                              float (&s2)[VW]) {
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (first + i < mine) {
+      float v[VW], w[VW];
+      unpack<T, VW>(f[i], v);
+      unpack<T, VW>(g[i], w);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) {
+        const float xh = (v[e] - k[e].mean) * k[e].rstd;
+        const float dz = norm_act_grad(w[e], norm_z(xh, k[e].gamma, k[e].beta), a.act);
+        s1[e] += dz;
+        s2[e] += dz * xh;
+      }
+      forget(f[i]);
+      forget(g[i]);
+    }
+  }
+}
+
+template <int VW, bool SPAN>
+__device__ __forceinline__ void grad_channels(const NormArgs& a, const Slab& q, Channel (&k)[VW]) {
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+    k[e] = channel(a, a.stats, q.img, min(q.c0 + q.ch + e, a.c - 1));
+    if (!SPAN && e) k[e].mean = k[0].mean, k[e].rstd = k[0].rstd;
+  }
+}
+
+// The slab's sums per channel, to part; then f(group, sum of gamma * dz, sum of
+// gamma * dz * xh) by one lane of those that join the group.  Rows first, through LDS
+// with consecutive lanes on consecutive channels.
+template <int VW, typename F>
+__device__ __forceinline__ void join_grad_sums(const NormArgs& a, const Slab& q, float2* lds,
+                                               float (&s1)[VW], float (&s2)[VW], F&& f) {
+  const int lanes = 1 << a.lanes_log2, width = lanes * VW;
+  const int width_log2 = a.lanes_log2 + (VW == 8 ? 3 : VW == 4 ? 2 : VW == 2 ? 1 : 0);
+  // a wave's two halves first where both have the same channels
+  int held = q.rows, slot = q.row;
+  if (lanes <= 32) {
+#pragma unroll
+    for (int e = 0; e < VW; ++e) {
+      s1[e] += __shfl_xor(s1[e], 32);
+      s2[e] += __shfl_xor(s2[e], 32);
+    }
+    const int half = 32 >> a.lanes_log2;  // rows of half a wave
+    held = q.rows >> 1;
+    slot = (threadIdx.x >> 6) * half + (q.row & (half - 1));
+  }
+  if (lanes > 32 || (threadIdx.x & 32) == 0) {
+#pragma unroll
+    for (int e = 0; e < VW; ++e) lds[slot * width + q.ch + e] = make_float2(s1[e], s2[e]);
+  }
+  __syncthreads();
+  float2* const sums = lds + held * width;  // [segments][width]
+  int segments;
+  if (width >= (int)blockDim.x) {
+    segments = 1;
+    for (int ch = threadIdx.x; ch < width; ch += blockDim.x) {
+      float2 t = lds[ch];
+      for (int r = 1; r < held; ++r) {
+        t.x += lds[r * width + ch].x;
+        t.y += lds[r * width + ch].y;
+      }
+      sums[ch] = t;
+    }
+  } else {
+    const int ch = threadIdx.x & (width - 1), parts = blockDim.x >> width_log2;
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int r = threadIdx.x >> width_log2; r < held; r += parts) {
+      t.x += lds[r * width + ch].x;
+      t.y += lds[r * width + ch].y;
+    }
+    for (int m = 32; m >= width; m >>= 1) {
+      t.x += __shfl_xor(t.x, m);
+      t.y += __shfl_xor(t.y, m);
+    }
+    segments = width >= 64 ? parts : (int)(blockDim.x >> 6);
+    const int seg = width >= 64 ? (int)(threadIdx.x >> width_log2) : (int)(threadIdx.x >> 6);
+    if (width >= 64 || (int)(threadIdx.x & 63) < width) sums[seg * width + ch] = t;
+  }
+  __syncthreads();
+  float2* part = a.part + ((size_t)q.img * a.chunks + q.chunk) * a.c + q.c0;
+  for (int ch = threadIdx.x; ch < q.channels; ch += blockDim.x) {
+    float2 t = sums[ch];
+    for (int p = 1; p < segments; ++p) {
+      t.x += sums[p * width + ch].x;
+      t.y += sums[p * width + ch].y;
+    }
+    part[ch] = t;
+    const float gamma = a.gamma ? a.gamma[q.c0 + ch] : 1.f;
+    sums[ch] = make_float2(gamma * t.x, gamma * t.y);  // read by this thread alone so far
+  }
+  __syncthreads();
+  const int gl = 1 << a.join_log2, l = threadIdx.x & (gl - 1);
+  for (int g = threadIdx.x >> a.join_log2; g < q.groups; g += blockDim.x >> a.join_log2) {
+    float2 t = make_float2(0.f, 0.f);
+    for (int j = l; j < a.d; j += gl) {
+      t.x += sums[g * a.d + j].x;
+      t.y += sums[g * a.d + j].y;
+    }
+    for (int m = gl >> 1; m; m >>= 1) {
+      t.x += __shfl_xor(t.x, m);
+      t.y += __shfl_xor(t.y, m);
+    }
+    if (l == 0) f(g, t.x, t.y);
+  }
+}
+
+template <typename T, int VW, int R, bool SPAN>
+__device__ __forceinline__ void write_grad_rows(const NormArgs& a, const Slab& q, T* out,
+                                                int first, int mine, const Pack<T, VW> (&f)[R],
+                                                const Pack<T, VW> (&g)[R], const Channel (&k)[VW],
+                                                const float2 (&coef)[VW]) {
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (first + i < mine) {
+      float v[VW], w[VW];
+      unpack<T, VW>(f[i], v);
+      unpack<T, VW>(g[i], w);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) v[e] = norm_value<true>(v[e], w[e], k[e], coef[e], a.act);
+      store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v));
+    }
+  }
+}
+
+}  // namespace
+
+// ---- all pixels in registers ----------------------------------------------------
+
+template <typename T, int VW, int R, bool SPAN>
+__global__ __launch_bounds__(1024) void norm_slab_nhwc_kernel(NormArgs a) {
+  extern __shared__ float2 lds[];
+  const Slab q = slab_of<VW>(a);
+  const int mine = q.in ? pixels_of(a, q, q.row) : 0;
+  Pack<T, VW> f[R];
+  load_rows<T, VW, R>(a, q, (const T*)a.x + q.at, 0, mine, f);
+  float s[VW], m2[VW];
+  own_stats<T, VW, R, SPAN>(f, mine, s, m2);
+  float2* const result = lds + ((SPAN ? VW : 1) << a.lanes_log2) * q.rows;
+  join_stats<VW, SPAN>(a, q, lds, s, m2, [&](int g, float mean, float sq) {
+    const float2 st = make_float2(mean, 1.f / sqrtf(sq / ((float)a.d * (float)a.hw) + a.eps));
+    result[g] = st;
+    ((float2*)a.stats_out)[(size_t)q.img * a.groups + q.c0 / a.d + g] = st;
+  });
+  __syncthreads();
+  if (!q.in) return;
+  Channel k[VW];
+  channels_of<VW, SPAN>(a, q, result, k);
+  write_rows<T, VW, R>(a, q, (T*)a.out + q.at, 0, mine, f, k);
+}
+
+template <typename T, int VW, int R, bool SPAN>
+__global__ __launch_bounds__(1024) void norm_slab_grad_nhwc_kernel(NormArgs a) {
+  extern __shared__ float2 lds[];
+  const Slab q = slab_of<VW>(a);
+  const int mine = q.in ? pixels_of(a, q, q.row) : 0;
+  Pack<T, VW> f[R], g[R];
+  load_rows<T, VW, R>(a, q, (const T*)a.x + q.at, 0, mine, f);
+  load_rows<T, VW, R>(a, q, (const T*)a.dy + q.at, 0, mine, g);
+  Channel k[VW];
+  grad_channels<VW, SPAN>(a, q, k);
+  float s1[VW], s2[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s1[e] = s2[e] = 0.f;
+  add_grad_sums<T, VW, R>(a, 0, mine, f, g, k, s1, s2);
+  const float total = (float)a.d * (float)a.hw;
+  float2* const result = lds;  // the rows are done with by then
+  join_grad_sums<VW>(a, q, lds, s1, s2, [&](int grp, float t1, float t2) {
+    result[grp] = make_float2(t1 / total, t2 / total);
+  });
+  __syncthreads();
+  if (!q.in) return;
+  float2 coef[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) coef[e] = result[(q.ch + (SPAN ? e : 0)) / a.d];
+  write_grad_rows<T, VW, R, SPAN>(a, q, (T*)a.out + q.at, 0, mine, f, g, k, coef);
+}
+
+// ---- runs of pixels, two passes ---------------------------------------------------
+
+constexpr int kRun = 4;  // vectors of a thread in flight
+
+// First pass: a run's (mean, squares around it) per group.
+template <typename T, int VW, bool SPAN>
+__global__ __launch_bounds__(1024) void norm_run_nhwc_kernel(NormArgs a) {
+  extern __shared__ float2 lds[];
+  const Slab q = slab_of<VW>(a);
+  const int mine = q.in ? pixels_of(a, q, q.row) : 0;
+  float s[VW], m2[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s[e] = m2[e] = 0.f;
+  for (int i = 0; i < mine; i += kRun) {
+    Pack<T, VW> f[kRun];
+    load_rows<T, VW, kRun>(a, q, (const T*)a.x + q.at, i, mine, f);
+    float bs[VW], bm2[VW];
+    own_stats<T, VW, kRun, SPAN>(f, min(kRun, mine - i), bs, bm2);
+    // join with what came before: i pixels and these
+    const float now = (float)min(kRun, mine - i), share = now / ((float)i + now);
+    const float cross = (float)i * share * (SPAN ? 1 : VW);
+#pragma unroll
+    for (int e = 0; e < (SPAN ? VW : 1); ++e) {
+      const float d = bs[e] - s[e];
+      s[e] += d * share;
+      m2[e] += bm2[e] + d * d * cross;
+    }
+  }
+  join_stats<VW, SPAN>(a, q, lds, s, m2, [&](int g, float mean, float sq) {
+    a.gpart[((size_t)q.img * a.chunks + q.chunk) * a.groups + q.c0 / a.d + g] =
+        make_float2(mean, sq);
+  });
+}
+
+// Second pass: the runs' sums joined by every workgroup for its own groups, and y.
+template <typename T, int VW, bool SPAN>
+__global__ __launch_bounds__(1024) void norm_run_apply_nhwc_kernel(NormArgs a) {
+  extern __shared__ float2 lds[];
+  const Slab q = slab_of<VW>(a);
+  const int mine = q.in ? pixels_of(a, q, q.row) : 0;
+  const T* x = (const T*)a.x + q.at;
+  Pack<T, VW> f[kRun];
+  load_rows<T, VW, kRun>(a, q, x, 0, mine, f);  // in flight meanwhile
+  const int gl = 1 << a.join_log2, l = threadIdx.x & (gl - 1);
+  for (int g = threadIdx.x >> a.join_log2; g < q.groups; g += blockDim.x >> a.join_log2) {
+    const float2* part = a.gpart + (size_t)q.img * a.chunks * a.groups + q.c0 / a.d + g;
+    const float total = (float)a.d * (float)a.hw;
+    float sum = 0.f, sq = 0.f;
+    for (int c = l; c < a.chunks; c += gl)
+      sum += (float)min(a.chunk_len, a.hw - c * a.chunk_len) * part[(size_t)c * a.groups].x;
+    for (int m = gl >> 1; m; m >>= 1) sum += __shfl_xor(sum, m);
+    const float mean = sum / (float)a.hw;
+    for (int c = l; c < a.chunks; c += gl) {
+      const float2 v = part[(size_t)c * a.groups];
+      const float count = (float)min(a.chunk_len, a.hw - c * a.chunk_len) * (float)a.d;
+      sq += v.y + count * (v.x - mean) * (v.x - mean);
+    }
+    for (int m = gl >> 1; m; m >>= 1) sq += __shfl_xor(sq, m);
+    if (l == 0) {
+      const float2 st = make_float2(mean, 1.f / sqrtf(sq / total + a.eps));
+      lds[g] = st;
+      if (q.chunk == 0) ((float2*)a.stats_out)[(size_t)q.img * a.groups + q.c0 / a.d + g] = st;
+    }
+  }
+  __syncthreads();
+  if (!q.in) return;
+  Channel k[VW];
+  channels_of<VW, SPAN>(a, q, lds, k);
+  T* out = (T*)a.out + q.at;
+  write_rows<T, VW, kRun>(a, q, out, 0, mine, f, k);
+  for (int i = kRun; i < mine; i += kRun) {
+    load_rows<T, VW, kRun>(a, q, x, i, mine, f);
+    write_rows<T, VW, kRun>(a, q, out, i, mine, f, k);
+  }
+}
+
+template <typename T, int VW, bool SPAN>
+__global__ __launch_bounds__(1024) void norm_run_grad_nhwc_kernel(NormArgs a) {
+  extern __shared__ float2 lds[];
+  const Slab q = slab_of<VW>(a);
+  const int mine = q.in ? pixels_of(a, q, q.row) : 0;
+  Channel k[VW];
+  grad_channels<VW, SPAN>(a, q, k);
+  float s1[VW], s2[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s1[e] = s2[e] = 0.f;
+  for (int i = 0; i < mine; i += kRun) {
+    Pack<T, VW> f[kRun], g[kRun];
+    load_rows<T, VW, kRun>(a, q, (const T*)a.x + q.at, i, mine, f);
+    load_rows<T, VW, kRun>(a, q, (const T*)a.dy + q.at, i, mine, g);
+    add_grad_sums<T, VW, kRun>(a, i, mine, f, g, k, s1, s2);
+  }
+  join_grad_sums<VW>(a, q, lds, s1, s2, [&](int grp, float t1, float t2) {
+    a.gpart[((size_t)q.img * a.chunks + q.chunk) * a.groups + q.c0 / a.d + grp] =
+        make_float2(t1, t2);
+  });
+}
+
+// ... and dx; workgroups behind the slabs': dgamma and dbeta.
+template <typename T, int VW, bool SPAN>
+__global__ __launch_bounds__(1024) void norm_run_grad_apply_nhwc_kernel(NormArgs a) {
+  extern __shared__ float2 lds[];
+  if ((int)blockIdx.x >= a.slabs) {
+    __shared__ ParamSums sums;
+    param_sums(a, blockIdx.x - a.slabs, sums);
+    return;
+  }
+  const Slab q = slab_of<VW>(a);
+  const int mine = q.in ? pixels_of(a, q, q.row) : 0;
+  const T* x = (const T*)a.x + q.at;
+  const T* dy = (const T*)a.dy + q.at;
+  Pack<T, VW> f[kRun], w[kRun];
+  load_rows<T, VW, kRun>(a, q, x, 0, mine, f);
+  load_rows<T, VW, kRun>(a, q, dy, 0, mine, w);
+  const int gl = 1 << a.join_log2, l = threadIdx.x & (gl - 1);
+  for (int g = threadIdx.x >> a.join_log2; g < q.groups; g += blockDim.x >> a.join_log2) {
+    const float2* part = a.gpart + (size_t)q.img * a.chunks * a.groups + q.c0 / a.d + g;
+    float2 t = make_float2(0.f, 0.f);
+    for (int c = l; c < a.chunks; c += gl) {
+      const float2 v = part[(size_t)c * a.groups];
+      t.x += v.x;
+      t.y += v.y;
+    }
+    for (int m = gl >> 1; m; m >>= 1) {
+      t.x += __shfl_xor(t.x, m);
+      t.y += __shfl_xor(t.y, m);
+    }
+    const float total = (float)a.d * (float)a.hw;
+    if (l == 0) lds[g] = make_float2(t.x / total, t.y / total);
+  }
+  __syncthreads();
+  if (!q.in) return;
+  Channel k[VW];
+  grad_channels<VW, SPAN>(a, q, k);
+  float2 coef[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) coef[e] = lds[(q.ch + (SPAN ? e : 0)) / a.d];
+  T* out = (T*)a.out + q.at;
+  write_grad_rows<T, VW, kRun, SPAN>(a, q, out, 0, mine, f, w, k, coef);
+  for (int i = kRun; i < mine; i += kRun) {
+    load_rows<T, VW, kRun>(a, q, x, i, mine, f);
+    load_rows<T, VW, kRun>(a, q, dy, i, mine, w);
+    write_grad_rows<T, VW, kRun, SPAN>(a, q, out, i, mine, f, w, k, coef);
+  }
+}
+
+namespace {
+
+template <typename T, int VW, int R, bool GRAD, bool SPAN>
+void launch_slab(const NormArgs& a, hipStream_t stream) {
+  if constexpr (GRAD)
+    hipLaunchKernelGGL((norm_slab_grad_nhwc_kernel<T, VW, R, SPAN>), dim3(a.slabs),
+                       dim3(a.threads), a.lds_bytes, stream, a);
+  else
+    hipLaunchKernelGGL((norm_slab_nhwc_kernel<T, VW, R, SPAN>), dim3(a.slabs), dim3(a.threads),
+                       a.lds_bytes, stream, a);
+}
+
+template <typename T, int VW, bool GRAD, bool SPAN>
+void launch_t(const NormArgs& a, hipStream_t stream) {
+  if (a.slots == 0) {
+    const dim3 grid(a.slabs), wg(a.threads);
+    const int group_bytes = a.slab_c / a.d * (int)sizeof(float2);
+    if constexpr (GRAD) {
+      const unsigned params = a.dgamma || a.dbeta ? (a.c + 15) / 16 : 0;
+      hipLaunchKernelGGL((norm_run_grad_nhwc_kernel<T, VW, SPAN>), grid, wg, a.lds_bytes, stream, a);
+      hipLaunchKernelGGL((norm_run_grad_apply_nhwc_kernel<T, VW, SPAN>), dim3(a.slabs + params), wg,
+                         group_bytes, stream, a);
+    } else {
+      hipLaunchKernelGGL((norm_run_nhwc_kernel<T, VW, SPAN>), grid, wg, a.lds_bytes, stream, a);
+      hipLaunchKernelGGL((norm_run_apply_nhwc_kernel<T, VW, SPAN>), grid, wg, group_bytes, stream,
+                         a);
+    }
+    return;
+  }
+  if (a.slots == 1)
+    launch_slab<T, VW, 1, GRAD, SPAN>(a, stream);
+  else if (a.slots <= 4)
+    launch_slab<T, VW, 4, GRAD, SPAN>(a, stream);
+  else if constexpr (slab_most(VW, GRAD, SPAN) > 4)
+    launch_slab<T, VW, slab_most(VW, GRAD, SPAN), GRAD, SPAN>(a, stream);
+  if (GRAD && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);  // its error is the last one, read below
+}
+
+template <typename T, int VW, bool GRAD>
+void launch_v(const NormArgs& a, hipStream_t stream) {
+  if constexpr (VW > 1)
+    if (a.span) return launch_t<T, VW, GRAD, true>(a, stream);
+  launch_t<T, VW, GRAD, false>(a, stream);
+}
+
+template <bool GRAD>
+hipError_t launch_any(const NormArgs& a, int dtype, int vec, hipStream_t stream) {
+  if (dtype == HUGE2_BF16) {
+    if (vec == 8)
+      launch_v<uint16_t, 8, GRAD>(a, stream);
+    else if (vec == 2)
+      launch_v<uint16_t, 2, GRAD>(a, stream);
+    else
+      launch_v<uint16_t, 1, GRAD>(a, stream);
+  } else if (vec == 4) {
+    launch_v<uint32_t, 4, GRAD>(a, stream);
+  } else {
+    launch_v<uint32_t, 1, GRAD>(a, stream);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm_nhwc(const NormArgs& a, int dtype, int vec, hipStream_t stream) {
+  return launch_any<false>(a, dtype, vec, stream);
+}
+hipError_t launch_norm_grad_nhwc(const NormArgs& a, int dtype, int vec, hipStream_t stream) {
+  return launch_any<true>(a, dtype, vec, stream);
+}
+
+}  // namespace huge2

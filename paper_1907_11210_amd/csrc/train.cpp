@@ -20,11 +20,13 @@
 
 using namespace huge2;
 
+enum class NormForm { kSlab, kRun, kGeneral };
+
 struct huge2_norm_plan {
   huge2_norm_desc desc;
   int vec;  // elements of a load
   NormArgs args[2];  // forward, gradient
-  bool slab[2];
+  NormForm form[2];
   void* ws;
   char kernel_name[2][96];
 };
@@ -119,17 +121,34 @@ size_t norm_bytes(const huge2_norm_desc& d) {
   return (size_t)d.n * d.c * d.h * d.w * elem_size(d.dtype);
 }
 
-// The form that holds slabs in registers, in NHWC: as few channels as make whole
-// groups, whole vectors and 64 bytes of a pixel, twice that while there are two
-// workgroups for each compute unit all the same.  False where a slab does not fit.
+// NHWC slabs are whole groups and whole vectors of channels; the workgroup's most
+// threads, and what follows from channels and threads.  (The slab_ and run_ functions
+// return false where their form does not fit.)
+int slab_threads(const NormArgs& a, int vec, bool grad, int lanes) {
+  // entries of 8 bytes a channel stay under 64 KB of LDS
+  return vec == 8 && (grad ? lanes >= 64 : a.span != 0) ? 512 : 1024;
+}
+void slab_set(NormArgs* a, int vec, bool grad, int c, int threads) {
+  const int lanes = 1 << log2_ceil(c / vec), groups = c / a->d;
+  a->slab_c = c;
+  a->lanes_log2 = log2_ceil(lanes);
+  a->cblocks = (a->c + c - 1) / c;
+  a->threads = threads;
+  a->rows_log2 = log2_ceil(threads / lanes);
+  a->join_log2 = 0;
+  while (a->join_log2 < 6 && (2 << a->join_log2) * groups <= threads) ++a->join_log2;
+  division_magic((uint32_t)(a->span ? a->d : a->d / vec), &a->dl_mul, &a->dl_shift);
+  const int entries = grad ? threads * vec / (lanes <= 32 ? 2 : 1) + std::max(threads, lanes * vec)
+                           : threads * (a->span ? vec : 1) + groups;
+  a->lds_bytes = entries * (int)sizeof(float2);
+}
+
+// Slabs of all pixels, held in registers: 64 bytes of a pixel, twice that while there
+// are two workgroups for each compute unit all the same.
 bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const int base = std::lcm(a->d, vec);
   a->span = a->d % vec != 0;
   const int most = slab_most(vec, grad, a->span != 0);
-  // workgroups whose entries of 8 bytes a channel stay under 64 KB of LDS
-  const auto most_threads = [&](int lanes) {
-    return vec == 8 && (grad ? lanes >= 64 : a->span != 0) ? 512 : 1024;
-  };
   const auto slots = [&](int lanes, int threads) {
     const int rows = threads / lanes;
     return (a->hw + rows - 1) / rows;
@@ -137,32 +156,46 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const auto lanes_of = [&](int c) { return 1 << log2_ceil(c / vec); };
   const auto fits = [&](long long c) {
     if (c > a->c || c / vec > 1024) return false;
-    const int lanes = lanes_of((int)c);
-    return lanes <= most_threads(lanes) && slots(lanes, most_threads(lanes)) <= most;
+    const int lanes = lanes_of((int)c), most_threads = slab_threads(*a, vec, grad, lanes);
+    return lanes <= most_threads && slots(lanes, most_threads) <= most;
   };
   if (!fits(base)) return false;
   int c = base;
   while (fits(2ll * c) && (c * esz < 64 || (long long)a->n * ((a->c + 2 * c - 1) / (2 * c)) >= 512))
     c *= 2;
-  const int lanes = lanes_of(c);
+  const int lanes = lanes_of(c), most_threads = slab_threads(*a, vec, grad, lanes);
   int threads = std::max(64, lanes);
-  while (threads < most_threads(lanes) && slots(lanes, threads) > 4) threads *= 2;
-  a->slab_c = c;
-  a->lanes_log2 = log2_ceil(lanes);
-  a->cblocks = (a->c + c - 1) / c;
-  if ((long long)a->n * a->cblocks >= (1ll << 31)) return false;
-  a->threads = threads;
+  while (threads < most_threads && slots(lanes, threads) > 4) threads *= 2;
+  slab_set(a, vec, grad, c, threads);
+  const long long slabs = (long long)a->n * a->cblocks;
+  if (slabs >= (1ll << 31)) return false;
+  a->slabs = (int)slabs;
   a->slots = slots(lanes, threads);
   a->chunks = 1;
-  const int groups = c / a->d;
-  while (a->join_log2 < 6 && (2 << a->join_log2) * groups <= threads) ++a->join_log2;
-  division_magic((uint32_t)(a->span ? a->d : a->d / vec), &a->dl_mul, &a->dl_shift);
-  if (grad) {
-    const int entries = threads * vec / (lanes <= 32 ? 2 : 1);
-    a->lds_bytes = (entries + std::max(threads, lanes * vec)) * (int)sizeof(float2);
-  } else {
-    a->lds_bytes = (threads * (a->span ? vec : 1) + groups) * (int)sizeof(float2);
-  }
+  a->chunk_len = a->hw;
+  return true;
+}
+
+// Slabs cut into runs of pixels: 512 bytes of a pixel, workgroups of 256 threads
+// (more where a group is wider), eight workgroups for each compute unit but at least
+// four pixels a thread; at most 256 runs, since every workgroup of the second pass
+// joins them all.
+bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
+  const int base = std::lcm(a->d, vec);
+  a->span = a->d % vec != 0;
+  if (base > a->c || base / vec > 1024) return false;
+  int c = base;
+  while (2ll * c <= a->c && c * esz < 512 && 2 * c / vec <= 64) c *= 2;
+  const int lanes = 1 << log2_ceil(c / vec);
+  if (lanes > slab_threads(*a, vec, grad, lanes)) return false;
+  slab_set(a, vec, grad, c, std::max(256, lanes));
+  const long long units = (long long)a->n * a->cblocks, rows = 1ll << a->rows_log2;
+  long long chunks = std::min<long long>({256, (2048 + units - 1) / units, (a->hw + 4 * rows - 1) / (4 * rows)});
+  a->chunk_len = (int)((a->hw + chunks - 1) / chunks);
+  a->chunks = (a->hw + a->chunk_len - 1) / a->chunk_len;
+  if (units * a->chunks >= (1ll << 31) - a->c) return false;
+  a->slabs = (int)(units * a->chunks);
+  a->slots = 0;
   return true;
 }
 
@@ -183,6 +216,7 @@ bool slab_nchw(NormArgs* a, int vec, bool grad) {
   a->along = along;
   a->threads = threads;
   a->slots = (int)slots();
+  a->slabs = a->n * a->groups;
   a->chunks = 1;
   return true;
 }
@@ -231,33 +265,52 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
   if (!p) return HUGE2_ERR_ALLOC;
   p->desc = d;
   p->vec = vec;
-  size_t part_b = 0;
+  size_t part_b = 0, gpart_b = 0;
   for (int g = 0; g < 2; ++g) {
     NormArgs& b = p->args[g];
+    const int esz = elem_size(d.dtype);
     b = a;
-    p->slab[g] = nhwc ? slab_nhwc(&b, elem_size(d.dtype), vec, g != 0) : slab_nchw(&b, vec, g != 0);
-    if (!p->slab[g] && !norm_runs(&b, nhwc, vec)) {
+    const auto fit = [&](auto&& form) {
+      b = a;
+      return form();
+    };
+    if (nhwc ? fit([&] { return slab_nhwc(&b, esz, vec, g != 0); })
+             : fit([&] { return slab_nchw(&b, vec, g != 0); }))
+      p->form[g] = NormForm::kSlab;
+    else if (nhwc && fit([&] { return run_nhwc(&b, esz, vec, g != 0); }))
+      p->form[g] = NormForm::kRun;
+    else if (fit([&] { return norm_runs(&b, nhwc, vec); }))
+      p->form[g] = NormForm::kGeneral;
+    else {
       delete p;
       return HUGE2_ERR_UNSUPPORTED;
     }
-    if (!p->slab[g] || g)
+    if (g || p->form[g] == NormForm::kGeneral)
       part_b = std::max(part_b, round256((size_t)d.n * b.chunks * d.c * sizeof(float2)));
-    if (p->slab[g])
-      std::snprintf(p->kernel_name[g], sizeof(p->kernel_name[g]), "norm_slab_%s%s_kernel v%d t%d r%d",
-                    g && nhwc ? "grad_" : "", nhwc ? "nhwc" : "nchw", vec, b.threads, b.slots);
+    if (p->form[g] == NormForm::kRun)
+      gpart_b = std::max(gpart_b, round256((size_t)d.n * b.chunks * d.groups * sizeof(float2)));
+    const char* const layout = nhwc ? "nhwc" : "nchw";
+    char* const name = p->kernel_name[g];
+    const size_t room = sizeof(p->kernel_name[g]);
+    if (p->form[g] == NormForm::kSlab)
+      std::snprintf(name, room, "norm_slab_%s%s_kernel v%d t%d r%d", g && nhwc ? "grad_" : "",
+                    layout, vec, b.threads, b.slots);
+    else if (p->form[g] == NormForm::kRun)
+      std::snprintf(name, room, "norm_run_%snhwc_kernel v%d t%d k%d", g ? "grad_" : "", vec,
+                    b.threads, b.chunks);
     else
-      std::snprintf(p->kernel_name[g], sizeof(p->kernel_name[g]), "norm_sums_%s_kernel v%d k%d",
-                    nhwc ? "nhwc" : "nchw", vec, b.chunks);
+      std::snprintf(name, room, "norm_sums_%s_kernel v%d k%d", layout, vec, b.chunks);
   }
   const size_t group_b = round256((size_t)d.n * d.groups * sizeof(float2));
-  const huge2_status st = device_alloc(&p->ws, part_b + group_b);
+  const huge2_status st = device_alloc(&p->ws, part_b + gpart_b + group_b);
   if (st != HUGE2_OK) {
     delete p;
     return st;
   }
   for (NormArgs& b : p->args) {
     b.part = (float2*)p->ws;
-    b.coef = (float2*)((char*)p->ws + part_b);  // the forward's statistics if it has no other place
+    b.gpart = (float2*)((char*)p->ws + part_b);
+    b.coef = (float2*)((char*)p->ws + part_b + gpart_b);  // the forward's statistics if it has no other place
     b.stats_out = (float*)b.coef;
   }
   *out = p;
@@ -275,8 +328,9 @@ huge2_status norm_run(const huge2_norm_plan* p, const void* x, const float* gamm
   NormArgs a = p->args[0];
   a.x = x, a.gamma = gamma, a.beta = beta, a.out = y;
   if (stats) a.stats_out = stats;
-  return launched((p->slab[0] ? launch_norm_slab : launch_norm)(a, d.dtype, d.layout == HUGE2_NHWC,
-                                                                p->vec, stream));
+  const int nhwc = d.layout == HUGE2_NHWC;
+  if (p->form[0] == NormForm::kGeneral) return launched(launch_norm(a, d.dtype, nhwc, p->vec, stream));
+  return launched((nhwc ? launch_norm_nhwc : launch_norm_nchw)(a, d.dtype, p->vec, stream));
 }
 
 huge2_status norm_grad_run(const huge2_norm_plan* p, const void* x, const void* dy,
@@ -292,8 +346,10 @@ huge2_status norm_grad_run(const huge2_norm_plan* p, const void* x, const void* 
   NormArgs a = p->args[1];
   a.x = x, a.dy = dy, a.stats = stats, a.gamma = gamma, a.beta = beta, a.out = dx;
   a.dgamma = dgamma, a.dbeta = dbeta;
-  return launched((p->slab[1] ? launch_norm_slab_grad : launch_norm_grad)(
-      a, d.dtype, d.layout == HUGE2_NHWC, p->vec, stream));
+  const int nhwc = d.layout == HUGE2_NHWC;
+  if (p->form[1] == NormForm::kGeneral)
+    return launched(launch_norm_grad(a, d.dtype, nhwc, p->vec, stream));
+  return launched((nhwc ? launch_norm_grad_nhwc : launch_norm_grad_nchw)(a, d.dtype, p->vec, stream));
 }
 
 // ---- embedding --------------------------------------------------------------------

@@ -12,9 +12,9 @@ namespace huge2 {
 
 // ---- group norm (norm.hip) ---------------------------------------------------
 
-// Two forms share these arguments.  The maps of an image are cut into `chunks`
-// runs of `chunk_len` pixels; per (image, chunk, channel) a pair of sums goes to
-// `part`; they are merged per group, and a second pass over x writes the result.
+// Three forms share these arguments: slabs held in registers (one pass over x), slabs
+// cut into runs of pixels (two), and the general form (two, and a merge between).
+// Runs: the maps of an image are cut into `chunks` of `chunk_len` pixels.
 struct NormArgs {
   const void* x;
   const void* dy;
@@ -23,7 +23,8 @@ struct NormArgs {
   const float* beta;   // null: zeros
   void* out;           // y or dx
   float* stats_out;    // the forward's, the caller's or the plan's
-  float2* part;        // [n][chunks][c]
+  float2* part;        // [n][chunks][c]: sums per channel
+  float2* gpart;       // [n][chunks][groups]: sums per group
   float2* coef;        // gradient: [n][groups], the two group means
   float* dgamma;
   float* dbeta;
@@ -34,8 +35,10 @@ struct NormArgs {
   int lanes_log2;  // lanes of a wave side by side on one row (pixel or plane)
   int cblocks;     // NHWC: blocks of lanes * vector width channels; slabs of an image
 
-  // The form that holds a slab (norm_slab.hip); part is then [n][c], chunks 1.
-  int threads, slots;  // of a workgroup; vectors a thread holds
+  // Slabs: a workgroup's channels and pixels.
+  int slabs;           // workgroups
+  int threads, slots;  // of a workgroup; vectors a thread holds, 0: runs
+  int rows_log2;       // NHWC: pixels side by side in a workgroup
   int lds_bytes;       // NHWC
   int slab_c;          // NHWC: channels of a slab
   int span;            // NHWC: vectors may cross groups
@@ -52,9 +55,10 @@ constexpr int slab_most(int vec, bool grad, bool span) {
 
 hipError_t launch_norm(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
 hipError_t launch_norm_grad(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
-hipError_t launch_norm_slab(const NormArgs& a, int dtype, int nhwc, int vec, hipStream_t stream);
-hipError_t launch_norm_slab_grad(const NormArgs& a, int dtype, int nhwc, int vec,
-                                 hipStream_t stream);
+hipError_t launch_norm_nhwc(const NormArgs& a, int dtype, int vec, hipStream_t stream);
+hipError_t launch_norm_grad_nhwc(const NormArgs& a, int dtype, int vec, hipStream_t stream);
+hipError_t launch_norm_nchw(const NormArgs& a, int dtype, int vec, hipStream_t stream);
+hipError_t launch_norm_grad_nchw(const NormArgs& a, int dtype, int vec, hipStream_t stream);
 hipError_t launch_norm_params(const NormArgs& a, hipStream_t stream);
 
 // ---- embedding (embedding.hip) -------------------------------------------------
