@@ -28,7 +28,8 @@ template <typename T, int VW>
 __global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a, int cblocks) {
   const int lanes = 1 << a.lanes_log2, per = 256 >> a.lanes_log2;
   const int cb = blockIdx.x % cblocks;
-  const long long t0 = (long long)(blockIdx.x / cblocks) * per * kLookups + (threadIdx.x >> a.lanes_log2);
+  const long long t0 =
+      (long long)(blockIdx.x / cblocks) * per * kLookups + (threadIdx.x >> a.lanes_log2);
   const int col = (cb * lanes + (threadIdx.x & (lanes - 1))) * VW;
   if (col >= a.dim) return;
   int id[kLookups];
@@ -339,7 +340,8 @@ __device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, const int* key
   for (int e = 0; e < VW; ++e) zero[e] = 0.f;
   for (unsigned long long left = __ballot(empty); left; left &= left - 1) {
     T* p = (T*)a.dtable + (size_t)(first + __ffsll(left) - 1) * a.dim;
-    for (int col = lane * VW; col < a.dim; col += 64 * VW) store_pack<T, VW>(p + col, pack<T, VW>(zero));
+    for (int col = lane * VW; col < a.dim; col += 64 * VW)
+      store_pack<T, VW>(p + col, pack<T, VW>(zero));
   }
 }
 

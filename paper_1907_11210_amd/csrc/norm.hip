@@ -75,6 +75,7 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
     } else {
       unpack<T, VW>(load_pack<T, VW>(x + (size_t)q.p0 * a.c), pivot);
     }
+  by_act(GRAD ? a.act : 0, [&](auto act) {
 #pragma unroll 4
     for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
       float f[VW];
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < VW; ++e) {
           const float xh = (f[e] - k[e].mean) * k[e].rstd;
-          const float dz = norm_act_grad(g[e], norm_z(xh, k[e].gamma, k[e].beta), a.act);
+          const float dz = norm_act_grad<act.value>(g[e], norm_z(xh, k[e].gamma, k[e].beta));
           s1[e] += dz;
           s2[e] += dz * xh;
         }
@@ -98,6 +99,7 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
         }
       }
     }
+  });
   }
   // rows of one wave, then the four waves
   __shared__ float2 lds[4][64 * VW];
@@ -106,7 +108,8 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
   for (int e = 0; e < VW; ++e) {
     s1[e] = lanes_sum(s1[e], lanes);
     s2[e] = lanes_sum(s2[e], lanes);
-    if ((threadIdx.x & 63) < lanes) lds[threadIdx.x >> 6][lane * VW + e] = make_float2(s1[e], s2[e]);
+    if ((threadIdx.x & 63) < lanes)
+      lds[threadIdx.x >> 6][lane * VW + e] = make_float2(s1[e], s2[e]);
   }
   __syncthreads();
   if (threadIdx.x < lanes && in) {
@@ -142,29 +145,31 @@ __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
     k = channel(a, a.stats, q.img, q.ch);
   else
     pivot = to_f32<T>(x[q.p0]);
+  by_act(GRAD ? a.act : 0, [&](auto act) {
 #pragma unroll 4
-  for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
-    float f[VW];
-    unpack<T, VW>(load_pack<T, VW>(x + p), f);
-    if constexpr (GRAD) {
-      float g[VW];
-      unpack<T, VW>(load_pack<T, VW>(dy + p), g);
+    for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
+      float f[VW];
+      unpack<T, VW>(load_pack<T, VW>(x + p), f);
+      if constexpr (GRAD) {
+        float g[VW];
+        unpack<T, VW>(load_pack<T, VW>(dy + p), g);
 #pragma unroll
-      for (int e = 0; e < VW; ++e) {
-        const float xh = (f[e] - k.mean) * k.rstd;
-        const float dz = norm_act_grad(g[e], norm_z(xh, k.gamma, k.beta), a.act);
-        s1 += dz;
-        s2 += dz * xh;
-      }
-    } else {
+        for (int e = 0; e < VW; ++e) {
+          const float xh = (f[e] - k.mean) * k.rstd;
+          const float dz = norm_act_grad<act.value>(g[e], norm_z(xh, k.gamma, k.beta));
+          s1 += dz;
+          s2 += dz * xh;
+        }
+      } else {
 #pragma unroll
-      for (int e = 0; e < VW; ++e) {
-        const float v = f[e] - pivot;
-        s1 += v;
-        s2 += v * v;
+        for (int e = 0; e < VW; ++e) {
+          const float v = f[e] - pivot;
+          s1 += v;
+          s2 += v * v;
+        }
       }
     }
-  }
+  });
   for (int m = q.lanes >> 1; m; m >>= 1) {
     s1 += __shfl_xor(s1, m);
     s2 += __shfl_xor(s2, m);
@@ -249,15 +254,17 @@ __global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
     k[e] = channel(a, GRAD ? a.stats : a.stats_out, q.img, q.ch + e);
     if (GRAD) coef[e] = a.coef[(size_t)q.img * a.groups + (q.ch + e) / a.d];
   }
+  by_act(a.act, [&](auto act) {
 #pragma unroll 4
-  for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
-    float f[VW], g[VW];
-    unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
-    if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
+    for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
+      float f[VW], g[VW];
+      unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
+      if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
 #pragma unroll
-    for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD>(f[e], g[e], k[e], coef[e], a.act);
-    store_pack<T, VW>(out + (size_t)p * a.c, pack<T, VW>(f));
-  }
+      for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD, act.value>(f[e], g[e], k[e], coef[e]);
+      store_pack<T, VW>(out + (size_t)p * a.c, pack<T, VW>(f));
+    }
+  });
 }
 
 template <typename T, int VW, bool GRAD>
@@ -270,15 +277,17 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a) {
   const Channel k = channel(a, GRAD ? a.stats : a.stats_out, q.img, q.ch);
   float2 coef;
   if (GRAD) coef = a.coef[(size_t)q.img * a.groups + q.ch / a.d];
+  by_act(a.act, [&](auto act) {
 #pragma unroll 4
-  for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
-    float f[VW], g[VW];
-    unpack<T, VW>(load_pack<T, VW>(x + p), f);
-    if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + p), g);
+    for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
+      float f[VW], g[VW];
+      unpack<T, VW>(load_pack<T, VW>(x + p), f);
+      if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + p), g);
 #pragma unroll
-    for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD>(f[e], g[e], k, coef, a.act);
-    store_pack<T, VW>(out + p, pack<T, VW>(f));
-  }
+      for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD, act.value>(f[e], g[e], k, coef);
+      store_pack<T, VW>(out + p, pack<T, VW>(f));
+    }
+  });
 }
 
 namespace {

@@ -64,60 +64,70 @@ __global__ __launch_bounds__(1024) void norm_slab_nchw_kernel(NormArgs a) {
   } else {
     stats = ((const float2*)a.stats)[(size_t)img * a.groups + c0 / a.d];
     float g1 = 0.f, g2 = 0.f, s1 = 0.f, s2 = 0.f;
-    int pl = plane, j = 0;
+    by_act(a.act, [&](auto act) {
+      int pl = plane, j = 0;
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const int ch = c0 + min(pl, a.d - 1);
+        const float gamma = a.gamma ? a.gamma[ch] : 1.f;
+        if (place[k] >= 0) {
+          const float beta = a.beta ? a.beta[ch] : 0.f;
+          float v[VW], w[VW];
+          unpack<T, VW>(f[k], v);
+          unpack<T, VW>(g[k], w);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            const float xh = (v[e] - stats.x) * stats.y;
+            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, gamma, beta));
+            s1 += dz;
+            s2 += dz * xh;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // vector by vector: all at once would spill
+        if (++j == a.along) {  // the plane is done: its sums over the row of lanes
+          for (int m = lanes >> 1; m; m >>= 1) {
+            s1 += __shfl_xor(s1, m);
+            s2 += __shfl_xor(s2, m);
+          }
+          if (lane == 0 && pl < a.d) {
+            a.part[(size_t)img * a.c + ch] = make_float2(s1, s2);
+            g1 += gamma * s1;
+            g2 += gamma * s2;
+          }
+          s1 = s2 = 0.f;
+          j = 0;
+          pl += planes;
+        }
+      }
+    });
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      const int ch = c0 + min(pl, a.d - 1);
-      const float gamma = a.gamma ? a.gamma[ch] : 1.f;
-      if (place[k] >= 0) {
-        const float beta = a.beta ? a.beta[ch] : 0.f;
-        float v[VW], w[VW];
-        unpack<T, VW>(f[k], v);
-        unpack<T, VW>(g[k], w);
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const float xh = (v[e] - stats.x) * stats.y;
-          const float dz = norm_act_grad(w[e], norm_z(xh, gamma, beta), a.act);
-          s1 += dz;
-          s2 += dz * xh;
-        }
-        forget(f[k]);
-        forget(g[k]);
-      }
-      if (++j == a.along) {  // the plane is done: its sums over the row of lanes
-        for (int m = lanes >> 1; m; m >>= 1) {
-          s1 += __shfl_xor(s1, m);
-          s2 += __shfl_xor(s2, m);
-        }
-        if (lane == 0 && pl < a.d) {
-          a.part[(size_t)img * a.c + ch] = make_float2(s1, s2);
-          g1 += gamma * s1;
-          g2 += gamma * s2;
-        }
-        s1 = s2 = 0.f;
-        j = 0;
-        pl += planes;
-      }
+      forget(f[k]);
+      forget(g[k]);
     }
     coef.x = block_sum(g1, lds) / total;
     coef.y = block_sum(g2, lds) / total;
   }
   T* out = (T*)a.out + at;
-  int pl = plane, j = 0;
+  by_act(a.act, [&](auto act) {
+    int pl = plane, j = 0;
 #pragma unroll
-  for (int k = 0; k < R; ++k) {
-    if (place[k] >= 0) {
-      const int ch = c0 + pl;
-      const Channel c = {stats.x, stats.y, a.gamma ? a.gamma[ch] : 1.f, a.beta ? a.beta[ch] : 0.f};
-      float v[VW], w[VW];
-      unpack<T, VW>(f[k], v);
-      if constexpr (GRAD) unpack<T, VW>(g[k], w);
+    for (int k = 0; k < R; ++k) {
+      if (place[k] >= 0) {
+        const int ch = c0 + pl;
+        const Channel c = {stats.x, stats.y, a.gamma ? a.gamma[ch] : 1.f,
+                           a.beta ? a.beta[ch] : 0.f};
+        float v[VW], w[VW];
+        unpack<T, VW>(f[k], v);
+        if constexpr (GRAD) unpack<T, VW>(g[k], w);
 #pragma unroll
-      for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD>(v[e], w[e], c, coef, a.act);
-      store_pack<T, VW>(out + place[k], pack<T, VW>(v));
+        for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD, act.value>(v[e], w[e], c, coef);
+        store_pack<T, VW>(out + place[k], pack<T, VW>(v));
+      }
+      if (GRAD) __builtin_amdgcn_sched_barrier(0);
+      if (++j == a.along) j = 0, pl += planes;
     }
-    if (++j == a.along) j = 0, pl += planes;
-  }
+  });
 }
 
 namespace {
@@ -132,7 +142,8 @@ void launch_t(const NormArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((norm_slab_nchw_kernel<T, VW, 4, GRAD>), grid, wg, 0, stream, a);
   else
     hipLaunchKernelGGL((norm_slab_nchw_kernel<T, VW, kMost, GRAD>), grid, wg, 0, stream, a);
-  if (GRAD && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);  // its error is the last one, read below
+  // (its error is the last one, read by the caller)
+  if (GRAD && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
 }
 
 template <bool GRAD>

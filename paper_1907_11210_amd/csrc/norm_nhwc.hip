@@ -139,7 +139,7 @@ __device__ __forceinline__ void load_rows(const NormArgs& a, const Slab& q, cons
     if (first + k < mine) f[k] = load_pack<T, VW>(x + (size_t)(q.row + (first + k) * q.rows) * a.c);
 }
 
-template <typename T, int VW, int R>
+template <int ACT, typename T, int VW, int R>
 __device__ __forceinline__ void write_rows(const NormArgs& a, const Slab& q, T* out, int first,
                                            int mine, const Pack<T, VW> (&f)[R],
                                            const Channel (&k)[VW]) {
@@ -150,16 +150,17 @@ __device__ __forceinline__ void write_rows(const NormArgs& a, const Slab& q, T* 
       unpack<T, VW>(f[i], v);
 #pragma unroll
       for (int e = 0; e < VW; ++e)
-        v[e] = norm_value<false>(v[e], 0.f, k[e], make_float2(0.f, 0.f), a.act);
+        v[e] = norm_value<false, ACT>(v[e], 0.f, k[e], make_float2(0.f, 0.f));
       store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v));
     }
   }
 }
 
 // A thread's sums of dz and dz * xh over some of its vectors.
-template <typename T, int VW, int R>
+template <int ACT, typename T, int VW, int R>
 __device__ __forceinline__ void add_grad_sums(const NormArgs& a, int first, int mine,
-                                              Pack<T, VW> (&f)[R], Pack<T, VW> (&g)[R],
+                                              const Pack<T, VW> (&f)[R],
+                                              const Pack<T, VW> (&g)[R],
                                               const Channel (&k)[VW], float (&s1)[VW],
                                               float (&s2)[VW]) {
 #pragma unroll
@@ -171,13 +172,12 @@ __device__ __forceinline__ void add_grad_sums(const NormArgs& a, int first, int 
 #pragma unroll
       for (int e = 0; e < VW; ++e) {
         const float xh = (v[e] - k[e].mean) * k[e].rstd;
-        const float dz = norm_act_grad(w[e], norm_z(xh, k[e].gamma, k[e].beta), a.act);
+        const float dz = norm_act_grad<ACT>(w[e], norm_z(xh, k[e].gamma, k[e].beta));
         s1[e] += dz;
         s2[e] += dz * xh;
       }
-      forget(f[i]);
-      forget(g[i]);
     }
+    __builtin_amdgcn_sched_barrier(0);  // row by row: all at once would spill
   }
 }
 
@@ -271,7 +271,7 @@ __device__ __forceinline__ void join_grad_sums(const NormArgs& a, const Slab& q,
   }
 }
 
-template <typename T, int VW, int R, bool SPAN>
+template <int ACT, typename T, int VW, int R>
 __device__ __forceinline__ void write_grad_rows(const NormArgs& a, const Slab& q, T* out,
                                                 int first, int mine, const Pack<T, VW> (&f)[R],
                                                 const Pack<T, VW> (&g)[R], const Channel (&k)[VW],
@@ -283,9 +283,10 @@ __device__ __forceinline__ void write_grad_rows(const NormArgs& a, const Slab& q
       unpack<T, VW>(f[i], v);
       unpack<T, VW>(g[i], w);
 #pragma unroll
-      for (int e = 0; e < VW; ++e) v[e] = norm_value<true>(v[e], w[e], k[e], coef[e], a.act);
+      for (int e = 0; e < VW; ++e) v[e] = norm_value<true, ACT>(v[e], w[e], k[e], coef[e]);
       store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v));
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -312,7 +313,9 @@ __global__ __launch_bounds__(1024) void norm_slab_nhwc_kernel(NormArgs a) {
   if (!q.in) return;
   Channel k[VW];
   channels_of<VW, SPAN>(a, q, result, k);
-  write_rows<T, VW, R>(a, q, (T*)a.out + q.at, 0, mine, f, k);
+  by_act(a.act, [&](auto act) {
+    write_rows<act.value, T, VW, R>(a, q, (T*)a.out + q.at, 0, mine, f, k);
+  });
 }
 
 template <typename T, int VW, int R, bool SPAN>
@@ -328,7 +331,14 @@ __global__ __launch_bounds__(1024) void norm_slab_grad_nhwc_kernel(NormArgs a) {
   float s1[VW], s2[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) s1[e] = s2[e] = 0.f;
-  add_grad_sums<T, VW, R>(a, 0, mine, f, g, k, s1, s2);
+  by_act(a.act, [&](auto act) {
+    add_grad_sums<act.value, T, VW, R>(a, 0, mine, f, g, k, s1, s2);
+  });
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    forget(f[i]);
+    forget(g[i]);
+  }
   const float total = (float)a.d * (float)a.hw;
   float2* const result = lds;  // the rows are done with by then
   join_grad_sums<VW>(a, q, lds, s1, s2, [&](int grp, float t1, float t2) {
@@ -339,7 +349,9 @@ __global__ __launch_bounds__(1024) void norm_slab_grad_nhwc_kernel(NormArgs a) {
   float2 coef[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) coef[e] = result[(q.ch + (SPAN ? e : 0)) / a.d];
-  write_grad_rows<T, VW, R, SPAN>(a, q, (T*)a.out + q.at, 0, mine, f, g, k, coef);
+  by_act(a.act, [&](auto act) {
+    write_grad_rows<act.value, T, VW, R>(a, q, (T*)a.out + q.at, 0, mine, f, g, k, coef);
+  });
 }
 
 // ---- runs of pixels, two passes ---------------------------------------------------
@@ -389,17 +401,22 @@ __global__ __launch_bounds__(1024) void norm_run_apply_nhwc_kernel(NormArgs a) {
   for (int g = threadIdx.x >> a.join_log2; g < q.groups; g += blockDim.x >> a.join_log2) {
     const float2* part = a.gpart + (size_t)q.img * a.chunks * a.groups + q.c0 / a.d + g;
     const float total = (float)a.d * (float)a.hw;
+    // around the first run's mean, in one go: the loads' latency is what this takes
+    const float pivot = part[0].x;
     float sum = 0.f, sq = 0.f;
-    for (int c = l; c < a.chunks; c += gl)
-      sum += (float)min(a.chunk_len, a.hw - c * a.chunk_len) * part[(size_t)c * a.groups].x;
-    for (int m = gl >> 1; m; m >>= 1) sum += __shfl_xor(sum, m);
-    const float mean = sum / (float)a.hw;
+#pragma unroll 8
     for (int c = l; c < a.chunks; c += gl) {
       const float2 v = part[(size_t)c * a.groups];
       const float count = (float)min(a.chunk_len, a.hw - c * a.chunk_len) * (float)a.d;
-      sq += v.y + count * (v.x - mean) * (v.x - mean);
+      sum += count * (v.x - pivot);
+      sq += v.y + count * (v.x - pivot) * (v.x - pivot);
     }
-    for (int m = gl >> 1; m; m >>= 1) sq += __shfl_xor(sq, m);
+    for (int m = gl >> 1; m; m >>= 1) {
+      sum += __shfl_xor(sum, m);
+      sq += __shfl_xor(sq, m);
+    }
+    const float mean = pivot + sum / total;
+    sq = fmaxf(sq - sum * (sum / total), 0.f);
     if (l == 0) {
       const float2 st = make_float2(mean, 1.f / sqrtf(sq / total + a.eps));
       lds[g] = st;
@@ -411,11 +428,13 @@ __global__ __launch_bounds__(1024) void norm_run_apply_nhwc_kernel(NormArgs a) {
   Channel k[VW];
   channels_of<VW, SPAN>(a, q, lds, k);
   T* out = (T*)a.out + q.at;
-  write_rows<T, VW, kRun>(a, q, out, 0, mine, f, k);
-  for (int i = kRun; i < mine; i += kRun) {
-    load_rows<T, VW, kRun>(a, q, x, i, mine, f);
-    write_rows<T, VW, kRun>(a, q, out, i, mine, f, k);
-  }
+  by_act(a.act, [&](auto act) {
+    write_rows<act.value, T, VW, kRun>(a, q, out, 0, mine, f, k);
+    for (int i = kRun; i < mine; i += kRun) {
+      load_rows<T, VW, kRun>(a, q, x, i, mine, f);
+      write_rows<act.value, T, VW, kRun>(a, q, out, i, mine, f, k);
+    }
+  });
 }
 
 template <typename T, int VW, bool SPAN>
@@ -428,12 +447,14 @@ __global__ __launch_bounds__(1024) void norm_run_grad_nhwc_kernel(NormArgs a) {
   float s1[VW], s2[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) s1[e] = s2[e] = 0.f;
-  for (int i = 0; i < mine; i += kRun) {
-    Pack<T, VW> f[kRun], g[kRun];
-    load_rows<T, VW, kRun>(a, q, (const T*)a.x + q.at, i, mine, f);
-    load_rows<T, VW, kRun>(a, q, (const T*)a.dy + q.at, i, mine, g);
-    add_grad_sums<T, VW, kRun>(a, i, mine, f, g, k, s1, s2);
-  }
+  by_act(a.act, [&](auto act) {
+    for (int i = 0; i < mine; i += kRun) {
+      Pack<T, VW> f[kRun], g[kRun];
+      load_rows<T, VW, kRun>(a, q, (const T*)a.x + q.at, i, mine, f);
+      load_rows<T, VW, kRun>(a, q, (const T*)a.dy + q.at, i, mine, g);
+      add_grad_sums<act.value, T, VW, kRun>(a, i, mine, f, g, k, s1, s2);
+    }
+  });
   join_grad_sums<VW>(a, q, lds, s1, s2, [&](int grp, float t1, float t2) {
     a.gpart[((size_t)q.img * a.chunks + q.chunk) * a.groups + q.c0 / a.d + grp] =
         make_float2(t1, t2);
@@ -444,6 +465,7 @@ __global__ __launch_bounds__(1024) void norm_run_grad_nhwc_kernel(NormArgs a) {
 template <typename T, int VW, bool SPAN>
 __global__ __launch_bounds__(1024) void norm_run_grad_apply_nhwc_kernel(NormArgs a) {
   extern __shared__ float2 lds[];
+  constexpr int kDeep = SPAN && VW == 8 ? kRun / 2 : kRun;  // 128 registers
   if ((int)blockIdx.x >= a.slabs) {
     __shared__ ParamSums sums;
     param_sums(a, blockIdx.x - a.slabs, sums);
@@ -453,13 +475,14 @@ __global__ __launch_bounds__(1024) void norm_run_grad_apply_nhwc_kernel(NormArgs
   const int mine = q.in ? pixels_of(a, q, q.row) : 0;
   const T* x = (const T*)a.x + q.at;
   const T* dy = (const T*)a.dy + q.at;
-  Pack<T, VW> f[kRun], w[kRun];
-  load_rows<T, VW, kRun>(a, q, x, 0, mine, f);
-  load_rows<T, VW, kRun>(a, q, dy, 0, mine, w);
+  Pack<T, VW> f[kDeep], w[kDeep];
+  load_rows<T, VW, kDeep>(a, q, x, 0, mine, f);
+  load_rows<T, VW, kDeep>(a, q, dy, 0, mine, w);
   const int gl = 1 << a.join_log2, l = threadIdx.x & (gl - 1);
   for (int g = threadIdx.x >> a.join_log2; g < q.groups; g += blockDim.x >> a.join_log2) {
     const float2* part = a.gpart + (size_t)q.img * a.chunks * a.groups + q.c0 / a.d + g;
     float2 t = make_float2(0.f, 0.f);
+#pragma unroll 8
     for (int c = l; c < a.chunks; c += gl) {
       const float2 v = part[(size_t)c * a.groups];
       t.x += v.x;
@@ -480,12 +503,14 @@ __global__ __launch_bounds__(1024) void norm_run_grad_apply_nhwc_kernel(NormArgs
 #pragma unroll
   for (int e = 0; e < VW; ++e) coef[e] = lds[(q.ch + (SPAN ? e : 0)) / a.d];
   T* out = (T*)a.out + q.at;
-  write_grad_rows<T, VW, kRun, SPAN>(a, q, out, 0, mine, f, w, k, coef);
-  for (int i = kRun; i < mine; i += kRun) {
-    load_rows<T, VW, kRun>(a, q, x, i, mine, f);
-    load_rows<T, VW, kRun>(a, q, dy, i, mine, w);
-    write_grad_rows<T, VW, kRun, SPAN>(a, q, out, i, mine, f, w, k, coef);
-  }
+  by_act(a.act, [&](auto act) {
+    write_grad_rows<act.value, T, VW, kDeep>(a, q, out, 0, mine, f, w, k, coef);
+    for (int i = kDeep; i < mine; i += kDeep) {
+      load_rows<T, VW, kDeep>(a, q, x, i, mine, f);
+      load_rows<T, VW, kDeep>(a, q, dy, i, mine, w);
+      write_grad_rows<act.value, T, VW, kDeep>(a, q, out, i, mine, f, w, k, coef);
+    }
+  });
 }
 
 namespace {
@@ -507,7 +532,8 @@ void launch_t(const NormArgs& a, hipStream_t stream) {
     const int group_bytes = a.slab_c / a.d * (int)sizeof(float2);
     if constexpr (GRAD) {
       const unsigned params = a.dgamma || a.dbeta ? (a.c + 15) / 16 : 0;
-      hipLaunchKernelGGL((norm_run_grad_nhwc_kernel<T, VW, SPAN>), grid, wg, a.lds_bytes, stream, a);
+      hipLaunchKernelGGL((norm_run_grad_nhwc_kernel<T, VW, SPAN>), grid, wg, a.lds_bytes, stream,
+                         a);
       hipLaunchKernelGGL((norm_run_grad_apply_nhwc_kernel<T, VW, SPAN>), dim3(a.slabs + params), wg,
                          group_bytes, stream, a);
     } else {
@@ -523,7 +549,8 @@ void launch_t(const NormArgs& a, hipStream_t stream) {
     launch_slab<T, VW, 4, GRAD, SPAN>(a, stream);
   else if constexpr (slab_most(VW, GRAD, SPAN) > 4)
     launch_slab<T, VW, slab_most(VW, GRAD, SPAN), GRAD, SPAN>(a, stream);
-  if (GRAD && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);  // its error is the last one, read below
+  // (its error is the last one, read by the caller)
+  if (GRAD && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
 }
 
 template <typename T, int VW, bool GRAD>

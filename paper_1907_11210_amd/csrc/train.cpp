@@ -176,21 +176,30 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   return true;
 }
 
-// Slabs cut into runs of pixels: 512 bytes of a pixel, workgroups of 256 threads
-// (more where a group is wider), eight workgroups for each compute unit but at least
-// four pixels a thread; at most 256 runs, since every workgroup of the second pass
-// joins them all.
+// Slabs cut into runs of pixels: 64 bytes of a pixel, up to 512 while there are two
+// workgroups for each compute unit all the same (every workgroup of the second pass
+// joins all runs of its groups: few groups, few runs); workgroups of 256 threads, more
+// where a group is wider; at least four pixels a thread.
 bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const int base = std::lcm(a->d, vec);
   a->span = a->d % vec != 0;
   if (base > a->c || base / vec > 1024) return false;
+  const auto lanes_of = [&](int c) { return 1 << log2_ceil(c / vec); };
+  const auto threads_of = [&](int c) { return std::max(256, lanes_of(c)); };
+  const auto units_of = [&](int c) { return (long long)a->n * ((a->c + c - 1) / c); };
+  const auto most_chunks = [&](int c) {
+    const long long rows = threads_of(c) / lanes_of(c);
+    return std::min(std::max(64ll, (512 + units_of(c) - 1) / units_of(c)),
+                    (a->hw + 4 * rows - 1) / (4 * rows));
+  };
   int c = base;
-  while (2ll * c <= a->c && c * esz < 512 && 2 * c / vec <= 64) c *= 2;
-  const int lanes = 1 << log2_ceil(c / vec);
-  if (lanes > slab_threads(*a, vec, grad, lanes)) return false;
-  slab_set(a, vec, grad, c, std::max(256, lanes));
-  const long long units = (long long)a->n * a->cblocks, rows = 1ll << a->rows_log2;
-  long long chunks = std::min<long long>({256, (2048 + units - 1) / units, (a->hw + 4 * rows - 1) / (4 * rows)});
+  while (2ll * c <= a->c && 2 * c / vec <= 64 && c * esz < 512 &&
+         (c * esz < 64 || units_of(2 * c) * std::min(64ll, most_chunks(2 * c)) >= 512))
+    c *= 2;
+  if (lanes_of(c) > slab_threads(*a, vec, grad, lanes_of(c))) return false;
+  slab_set(a, vec, grad, c, threads_of(c));
+  const long long units = units_of(c);
+  const long long chunks = std::min((2048 + units - 1) / units, most_chunks(c));
   a->chunk_len = (int)((a->hw + chunks - 1) / chunks);
   a->chunks = (a->hw + a->chunk_len - 1) / a->chunk_len;
   if (units * a->chunks >= (1ll << 31) - a->c) return false;
@@ -236,7 +245,8 @@ bool norm_runs(NormArgs* a, bool nhwc, int vec) {
   } else {
     const long long vecs = hw / vec;
     units = (long long)a->n * a->c;
-    chunks = std::max(std::min((8192 + units - 1) / units, (vecs + 255) / 256), (vecs + 1023) / 1024);
+    chunks = std::max(std::min((8192 + units - 1) / units, (vecs + 255) / 256),
+                      (vecs + 1023) / 1024);
     a->lanes_log2 = std::min(6, log2_ceil((vecs + chunks - 1) / chunks));
   }
   a->chunk_len = (int)((hw + chunks - 1) / chunks);
@@ -310,8 +320,8 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
   for (NormArgs& b : p->args) {
     b.part = (float2*)p->ws;
     b.gpart = (float2*)((char*)p->ws + part_b);
-    b.coef = (float2*)((char*)p->ws + part_b + gpart_b);  // the forward's statistics if it has no other place
-    b.stats_out = (float*)b.coef;
+    b.coef = (float2*)((char*)p->ws + part_b + gpart_b);
+    b.stats_out = (float*)b.coef;  // where the caller has no place for them
   }
   *out = p;
   return HUGE2_OK;
