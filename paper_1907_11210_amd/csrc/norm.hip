@@ -255,14 +255,13 @@ __global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
     if (GRAD) coef[e] = a.coef[(size_t)q.img * a.groups + (q.ch + e) / a.d];
   }
   by_act(a.act, [&](auto act) {
-#pragma unroll 4
     for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
       float f[VW], g[VW];
       unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
       if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
 #pragma unroll
       for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD, act.value>(f[e], g[e], k[e], coef[e]);
-      store_pack<T, VW>(out + (size_t)p * a.c, pack<T, VW>(f));
+      store_pack<T, VW>(out + (size_t)p * a.c, pack<T, VW>(f), a.stream);
     }
   });
 }
@@ -278,14 +277,13 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a) {
   float2 coef;
   if (GRAD) coef = a.coef[(size_t)q.img * a.groups + q.ch / a.d];
   by_act(a.act, [&](auto act) {
-#pragma unroll 4
     for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
       float f[VW], g[VW];
       unpack<T, VW>(load_pack<T, VW>(x + p), f);
       if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + p), g);
 #pragma unroll
       for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD, act.value>(f[e], g[e], k, coef);
-      store_pack<T, VW>(out + p, pack<T, VW>(f));
+      store_pack<T, VW>(out + p, pack<T, VW>(f), a.stream);
     }
   });
 }

@@ -122,7 +122,7 @@ __global__ __launch_bounds__(1024) void norm_slab_nchw_kernel(NormArgs a) {
         if constexpr (GRAD) unpack<T, VW>(g[k], w);
 #pragma unroll
         for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD, act.value>(v[e], w[e], c, coef);
-        store_pack<T, VW>(out + place[k], pack<T, VW>(v));
+        store_pack<T, VW>(out + place[k], pack<T, VW>(v), a.stream);
       }
       if (GRAD) __builtin_amdgcn_sched_barrier(0);
       if (++j == a.along) j = 0, pl += planes;

@@ -295,6 +295,12 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
       delete p;
       return HUGE2_ERR_UNSUPPORTED;
     }
+    // A result that fills the Infinity Cache is stored past it (64x64x2048 batch 8: 72
+    // against 82 us, since the first pass then need not write the last call's result
+    // back); a smaller one stays for the layer that reads it.  Not in pieces of less than
+    // 64 bytes: 176 against 66 us with 16 bytes of a pixel to a workgroup.
+    b.stream = norm_bytes(d) >= (64u << 20) &&
+               (!nhwc || p->form[g] == NormForm::kGeneral || b.slab_c * esz >= 64);
     if (g || p->form[g] == NormForm::kGeneral)
       part_b = std::max(part_b, round256((size_t)d.n * b.chunks * d.c * sizeof(float2)));
     if (p->form[g] == NormForm::kRun)

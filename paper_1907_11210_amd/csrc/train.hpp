@@ -31,6 +31,7 @@ struct NormArgs {
   int n, c, hw, groups, d;
   int act;
   float eps;
+  int stream;  // the result is stored past the caches
   int chunks, chunk_len;
   int lanes_log2;  // lanes of a wave side by side on one row (pixel or plane)
   int cblocks;     // NHWC: blocks of lanes * vector width channels; slabs of an image

@@ -43,6 +43,21 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, VW>& r) {
   else
     *(uint16_t*)p = (uint16_t)r.w[0];
 }
+// The same past the caches (uniform; 16 bytes only).
+template <typename T, int VW>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, VW>& r, int stream) {
+  if constexpr (sizeof(T) * VW == 16) {
+    if (stream) {
+      // (between two empty statements: the compiler would else make the two stores one
+      // ahead of or behind the branch, and that an ordinary one)
+      asm volatile("");
+      __builtin_nontemporal_store(u32x4{r.w[0], r.w[1], r.w[2], r.w[3]}, (u32x4*)p);
+      asm volatile("");
+      return;
+    }
+  }
+  store_pack<T, VW>(p, r);
+}
 template <typename T, int VW>
 __device__ __forceinline__ void unpack(const Pack<T, VW>& p, float (&f)[VW]) {
 #pragma unroll
