@@ -517,6 +517,113 @@ __global__ __launch_bounds__(1024) void embedding_join_kernel(EmbedGradArgs a, i
   }
 }
 
+// Up to kMostFew tokens: all in one launch, no order and no workspace.  A workgroup
+// to a token looks for the tokens of the same id among all; if its own is the first of
+// them, it adds up their gradients in order, the waves sharing the columns or, where
+// the tokens are many, the tokens.  Behind those, workgroups of kFewRows rows
+// clear the ones that no token has.
+//
+// Bound by latency, three loads one behind the other (5.5 us where the sort, the sums
+// and the join took 15); every workgroup reading all ids is what limits the tokens.
+template <typename T, int VW>
+__global__ __launch_bounds__(kFewThreads) void embedding_few_kernel(EmbedGradArgs a) {
+  __shared__ int list[kMostFew];
+  __shared__ int counts[kMostFew / 64];
+  constexpr int kWaves = kFewThreads / 64, kSteps = kMostFew / kFewThreads;
+  __shared__ float sums[kWaves][64 * VW];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if ((int)blockIdx.x >= a.tokens) {
+    const int first = (blockIdx.x - a.tokens) * kFewRows;
+    for (int i = threadIdx.x; i < kFewRows; i += kFewThreads) list[i] = 0;
+    __syncthreads();
+    for (int t = threadIdx.x; t < a.tokens; t += kFewThreads) {
+      const int row = known_id(a.ids, a.id64, t, a.rows) - first;
+      if (row >= 0 && row < kFewRows) list[row] = 1;  // (`rows` itself may mark a row beyond)
+    }
+    __syncthreads();
+    float zero[VW];
+#pragma unroll
+    for (int e = 0; e < VW; ++e) zero[e] = 0.f;
+    for (int r = wave; r < kFewRows && first + r < a.rows; r += kWaves) {
+      if (list[r]) continue;
+      T* p = (T*)a.dtable + (size_t)(first + r) * a.dim;
+      for (int col = lane * VW; col < a.dim; col += 64 * VW)
+        store_pack<T, VW>(p + col, pack<T, VW>(zero));
+    }
+    return;
+  }
+  const int mine = known_id(a.ids, a.id64, blockIdx.x, a.rows);
+  // a bit for each token, kFewThreads tokens a step
+  unsigned long long same[kSteps];
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    const int t = k * kFewThreads + threadIdx.x;
+    same[k] = __ballot(t < a.tokens && known_id(a.ids, a.id64, min(t, a.tokens - 1), a.rows) == mine);
+    if (lane == 0) counts[k * kWaves + wave] = __popcll(same[k]);
+  }
+  if (mine >= a.rows) return;
+  __syncthreads();
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    int at = n;
+    for (int w = 0; w < kWaves; ++w) {
+      at += w < wave ? counts[k * kWaves + w] : 0;
+      n += counts[k * kWaves + w];
+    }
+    if (same[k] >> lane & 1)
+      list[at + __popcll(same[k] & ((1ull << lane) - 1))] = k * kFewThreads + threadIdx.x;
+  }
+  __syncthreads();
+  if (list[0] != (int)blockIdx.x) return;
+  constexpr int kAhead = 16;
+  const auto add = [&](int from, int to, int col, float (&acc)[VW]) {
+    for (int i = from; i < to; i += kAhead) {
+      Pack<T, VW> g[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < to) g[j] = load_pack<T, VW>((const T*)a.dy + (size_t)list[i + j] * a.dim + col);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (i + j < to) {
+          float f[VW];
+          unpack<T, VW>(g[j], f);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) acc[e] += f[e];
+        }
+      }
+    }
+  };
+  const bool share = n > kAhead;  // the tokens
+  for (int c0 = share ? 0 : wave * 64 * VW; c0 < a.dim; c0 += share ? 64 * VW : kFewThreads * VW) {
+    const int col = c0 + lane * VW;
+    const bool in = col < a.dim;
+    float acc[VW];
+#pragma unroll
+    for (int e = 0; e < VW; ++e) acc[e] = 0.f;
+    if (!share) {
+      if (in) {
+        add(0, n, col, acc);
+        store_row<T, VW>(a, mine, col, acc);
+      }
+      continue;
+    }
+    const int each = (n + kWaves - 1) / kWaves;
+    if (in) add(min(n, wave * each), min(n, (wave + 1) * each), col, acc);
+#pragma unroll
+    for (int e = 0; e < VW; ++e) sums[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    if (wave == 0 && in) {
+      for (int w = 1; w < kWaves; ++w) {
+#pragma unroll
+        for (int e = 0; e < VW; ++e) acc[e] += sums[w][e * 64 + lane];
+      }
+      store_row<T, VW>(a, mine, col, acc);
+    }
+    __syncthreads();
+  }
+}
+
 namespace {
 
 template <typename T, int VW>
@@ -532,6 +639,12 @@ hipError_t launch_lookup(const EmbedArgs& a, hipStream_t stream) {
 template <typename T, int VW>
 hipError_t launch_grad(const EmbedGradArgs& a, hipStream_t stream) {
   const dim3 wg(256);
+  if (a.tokens <= kMostFew) {
+    const unsigned rows = (unsigned)(((long long)a.rows + kFewRows - 1) / kFewRows);
+    hipLaunchKernelGGL((embedding_few_kernel<T, VW>), dim3(a.tokens + rows),
+                       dim3(kFewThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   const int per = 256 >> a.lanes_log2;
   const int cblocks = (a.dim / VW + (1 << a.lanes_log2) - 1) >> a.lanes_log2;
   for (int pass = 0; pass < a.passes && a.tokens; ++pass) {

@@ -83,6 +83,8 @@ constexpr int kSortTile = 1024;  // tokens of a sorting workgroup, one a thread
 constexpr int kMostRecounted = 4096, kMostPlaced = 1 << 17, kPlaceTile = 512;
 constexpr int kMostDigitBits = 12, kMostDigits = 1 << kMostDigitBits;
 constexpr int kChunk = 16;     // sorted tokens of a chunk, or a multiple
+// The form without a sort: its most tokens, rows that a workgroup clears, its threads.
+constexpr int kMostFew = 1024, kFewRows = 64, kFewThreads = 512;
 constexpr int kZeroRows = 16;  // rows of the table that a wave looks up
 constexpr int kFewParts = 8;   // parts that a wave adds alone
 
