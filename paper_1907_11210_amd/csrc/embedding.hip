@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a, int cblocks
     const float scale = id[j] < a.rows ? a.scale : 0.f;
 #pragma unroll
     for (int e = 0; e < VW; ++e) f[j][e] *= scale;
-    store_pack<T, VW>((T*)a.y + (size_t)t * a.dim + col, pack<T, VW>(f[j]));
+    store_pack<T, VW>((T*)a.y + (size_t)t * a.dim + col, pack<T, VW>(f[j]), a.stream);
   }
 }
 

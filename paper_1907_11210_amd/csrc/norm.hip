@@ -1,7 +1,8 @@
 // norm.hip -- group norm with an activation and its gradients (huge2_train.h).
 //
-// Passes over x are all that these cost.  The general form takes two: sums per
-// channel and run of pixels, a merge per group, and the pass that writes.
+// The general form, two passes over x: sums per channel and run of pixels, a merge per
+// group, and the pass that writes.  In NHWC it takes groups wider than a workgroup; in
+// NCHW all that do not fit one, with the merge in the second pass.
 #include "norm_device.hpp"
 
 namespace huge2 {
@@ -266,24 +267,92 @@ __global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
   });
 }
 
-template <typename T, int VW, bool GRAD>
-__global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a) {
-  const PlaceNchw q = place_nchw(a);
-  if (!q.in) return;
-  const T* x = (const T*)a.x + (size_t)q.plane * a.hw;
-  const T* dy = (const T*)a.dy + (size_t)q.plane * a.hw;
-  T* out = (T*)a.out + (size_t)q.plane * a.hw;
-  const Channel k = channel(a, GRAD ? a.stats : a.stats_out, q.img, q.ch);
-  float2 coef;
-  if (GRAD) coef = a.coef[(size_t)q.img * a.groups + q.ch / a.d];
-  by_act(a.act, [&](auto act) {
-    for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
-      float f[VW], g[VW];
-      unpack<T, VW>(load_pack<T, VW>(x + p), f);
-      if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + p), g);
+// A workgroup to some runs of a group's planes (a row of lanes each).  Where the
+// group has few runs (JOIN) it joins them itself: no launch between the two passes,
+// and dgamma and dbeta come from workgroups behind the others.
+template <typename T, int VW, bool GRAD, bool JOIN>
+__global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a, int parts) {
+  __shared__ float lds[4];
+  constexpr int kAhead = 4;
+  const long long ng = (long long)a.n * a.groups;
+  if (GRAD && JOIN && (long long)blockIdx.x >= ng * parts) {
+    __shared__ ParamSums sums;
+    param_sums(a, (int)(blockIdx.x - ng * parts), sums);
+    return;
+  }
+  const long long ig = blockIdx.x / parts;
+  const int img = (int)(ig / a.groups), c0 = (int)(ig % a.groups) * a.d;
+  const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+  const int unit = blockIdx.x % parts * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+  const bool in = unit < a.d * a.chunks;
+  const int ch = c0 + (in ? unit / a.chunks : 0), first = in ? unit % a.chunks * a.chunk_len : 0;
+  const int end = in ? min(a.hw, first + a.chunk_len) : 0, step = lanes * VW;
+  const size_t at = ((size_t)img * a.c + ch) * a.hw;
+  const T* x = (const T*)a.x + at;
+  const T* dy = (const T*)a.dy + at;
+  T* out = (T*)a.out + at;
+  Pack<T, VW> f[kAhead], g[kAhead];
+  const auto load = [&](int p) {
 #pragma unroll
-      for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD, act.value>(f[e], g[e], k, coef);
-      store_pack<T, VW>(out + p, pack<T, VW>(f), a.stream);
+    for (int j = 0; j < kAhead; ++j) {
+      if (p + j * step < end) {
+        f[j] = load_pack<T, VW>(x + p + j * step);
+        if constexpr (GRAD) g[j] = load_pack<T, VW>(dy + p + j * step);
+      }
+    }
+  };
+  int p = first + lane * VW;
+  load(p);  // in flight meanwhile
+  float2 stats, coef = make_float2(0.f, 0.f);
+  if constexpr (JOIN) {
+    const float2* part = a.part + (size_t)img * a.chunks * a.c + c0;
+    const int entries = a.chunks * a.d;
+    const float total = (float)a.d * (float)a.hw, pivot = GRAD ? 0.f : part[0].x;
+    float s1 = 0.f, s2 = 0.f;
+    for (int e = threadIdx.x; e < entries; e += 256) {
+      const int chunk = e / a.d, j = e - chunk * a.d;
+      const float2 v = part[(size_t)chunk * a.c + j];
+      if constexpr (GRAD) {
+        const float gamma = a.gamma ? a.gamma[c0 + j] : 1.f;
+        s1 += gamma * v.x;
+        s2 += gamma * v.y;
+      } else {
+        const float count = (float)min(a.chunk_len, a.hw - chunk * a.chunk_len);
+        s1 += count * (v.x - pivot);
+        s2 += v.y + count * (v.x - pivot) * (v.x - pivot);
+      }
+    }
+    s1 = block_sum(s1, lds);
+    s2 = block_sum(s2, lds);
+    if constexpr (GRAD) {
+      coef = make_float2(s1 / total, s2 / total);
+      stats = ((const float2*)a.stats)[ig];
+    } else {
+      const float var = fmaxf(s2 - s1 * (s1 / total), 0.f) / total;
+      stats = make_float2(pivot + s1 / total, 1.f / sqrtf(var + a.eps));
+      if (threadIdx.x == 0 && blockIdx.x % parts == 0) ((float2*)a.stats_out)[ig] = stats;
+    }
+  } else {
+    stats = ((const float2*)(GRAD ? a.stats : a.stats_out))[ig];
+    if (GRAD) coef = a.coef[ig];
+  }
+  const Channel k = {stats.x, stats.y, a.gamma ? a.gamma[ch] : 1.f, a.beta ? a.beta[ch] : 0.f};
+  by_act(a.act, [&](auto act) {
+    for (;;) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (p + j * step < end) {
+          float v[VW], w[VW];
+          unpack<T, VW>(f[j], v);
+          if constexpr (GRAD) unpack<T, VW>(g[j], w);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD, act.value>(v[e], w[e], k, coef);
+          store_pack<T, VW>(out + p + j * step, pack<T, VW>(v), a.stream);
+        }
+      }
+      p += kAhead * step;
+      if (p >= end) break;
+      load(p);
     }
   });
 }
@@ -302,10 +371,18 @@ hipError_t launch_t(const NormArgs& a, int nhwc, hipStream_t stream) {
     hipLaunchKernelGGL((norm_sums_nhwc_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
     hipLaunchKernelGGL((norm_merge_kernel<GRAD>), dim3(merge), wg, 0, stream, a);
     hipLaunchKernelGGL((norm_apply_nhwc_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
+    return hipGetLastError();
+  }
+  const int rows = 256 >> a.lanes_log2, parts = (a.d * a.chunks + rows - 1) / rows;
+  const unsigned apply = (unsigned)a.n * a.groups * parts;
+  hipLaunchKernelGGL((norm_sums_nchw_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
+  if (a.d * a.chunks <= 1024) {  // four entries a thread
+    hipLaunchKernelGGL((norm_apply_nchw_kernel<T, VW, GRAD, true>),
+                       dim3(apply + merge - a.n * a.groups), wg, 0, stream, a, parts);
   } else {
-    hipLaunchKernelGGL((norm_sums_nchw_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
     hipLaunchKernelGGL((norm_merge_kernel<GRAD>), dim3(merge), wg, 0, stream, a);
-    hipLaunchKernelGGL((norm_apply_nchw_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
+    hipLaunchKernelGGL((norm_apply_nchw_kernel<T, VW, GRAD, false>), dim3(apply), wg, 0, stream, a,
+                       parts);
   }
   return hipGetLastError();
 }

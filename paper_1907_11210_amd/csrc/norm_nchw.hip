@@ -90,7 +90,12 @@ __global__ __launch_bounds__(1024) void norm_slab_nchw_kernel(NormArgs a) {
             s2 += __shfl_xor(s2, m);
           }
           if (lane == 0 && pl < a.d) {
-            a.part[(size_t)img * a.c + ch] = make_float2(s1, s2);
+            if (a.n > 1) {
+              a.part[(size_t)img * a.c + ch] = make_float2(s1, s2);
+            } else {  // nothing to add up
+              if (a.dbeta) a.dbeta[ch] = s1;
+              if (a.dgamma) a.dgamma[ch] = s2;
+            }
             g1 += gamma * s1;
             g2 += gamma * s2;
           }
@@ -143,7 +148,7 @@ void launch_t(const NormArgs& a, hipStream_t stream) {
   else
     hipLaunchKernelGGL((norm_slab_nchw_kernel<T, VW, kMost, GRAD>), grid, wg, 0, stream, a);
   // (its error is the last one, read by the caller)
-  if (GRAD && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
+  if (GRAD && a.n > 1 && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
 }
 
 template <bool GRAD>

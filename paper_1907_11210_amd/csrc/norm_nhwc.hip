@@ -251,7 +251,12 @@ __device__ __forceinline__ void join_grad_sums(const NormArgs& a, const Slab& q,
       t.x += sums[p * width + ch].x;
       t.y += sums[p * width + ch].y;
     }
-    part[ch] = t;
+    if (a.n * a.chunks == 1) {  // nothing to add up
+      if (a.dbeta) a.dbeta[q.c0 + ch] = t.x;
+      if (a.dgamma) a.dgamma[q.c0 + ch] = t.y;
+    } else {
+      part[ch] = t;
+    }
     const float gamma = a.gamma ? a.gamma[q.c0 + ch] : 1.f;
     sums[ch] = make_float2(gamma * t.x, gamma * t.y);  // read by this thread alone so far
   }
@@ -531,7 +536,7 @@ void launch_t(const NormArgs& a, hipStream_t stream) {
     const dim3 grid(a.slabs), wg(a.threads);
     const int group_bytes = a.slab_c / a.d * (int)sizeof(float2);
     if constexpr (GRAD) {
-      const unsigned params = a.dgamma || a.dbeta ? (a.c + 15) / 16 : 0;
+      const unsigned params = (a.dgamma || a.dbeta) && a.n * a.chunks > 1 ? (a.c + 15) / 16 : 0;
       hipLaunchKernelGGL((norm_run_grad_nhwc_kernel<T, VW, SPAN>), grid, wg, a.lds_bytes, stream,
                          a);
       hipLaunchKernelGGL((norm_run_grad_apply_nhwc_kernel<T, VW, SPAN>), dim3(a.slabs + params), wg,
@@ -550,7 +555,7 @@ void launch_t(const NormArgs& a, hipStream_t stream) {
   else if constexpr (slab_most(VW, GRAD, SPAN) > 4)
     launch_slab<T, VW, slab_most(VW, GRAD, SPAN), GRAD, SPAN>(a, stream);
   // (its error is the last one, read by the caller)
-  if (GRAD && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
+  if (GRAD && a.n > 1 && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
 }
 
 template <typename T, int VW, bool GRAD>

@@ -81,6 +81,10 @@ int vector_width(int dtype, long long len) {
   return dtype == HUGE2_BF16 && len % 2 == 0 ? 2 : 1;
 }
 
+// A result that fills much of the 256 MB Infinity Cache is stored past it; a smaller
+// one stays there for the layer that reads it.
+bool streams(size_t bytes) { return bytes >= (size_t)64 << 20; }
+
 huge2_status device_alloc(void** out, size_t bytes) {
   *out = nullptr;
   if (bytes == 0) return HUGE2_OK;
@@ -252,7 +256,8 @@ bool norm_runs(NormArgs* a, bool nhwc, int vec) {
   a->chunk_len = (int)((hw + chunks - 1) / chunks);
   if (!nhwc) a->chunk_len = (a->chunk_len + vec - 1) / vec * vec;
   a->chunks = (int)((hw + a->chunk_len - 1) / a->chunk_len);
-  return units * a->chunks < (1ll << 31);
+  const long long parts = ((long long)a->d * a->chunks << a->lanes_log2) / 256 + 1;
+  return units * a->chunks < (1ll << 31) && a->n * a->groups * parts < (1ll << 31) - a->c;
 }
 
 huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
@@ -295,11 +300,10 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
       delete p;
       return HUGE2_ERR_UNSUPPORTED;
     }
-    // A result that fills the Infinity Cache is stored past it (64x64x2048 batch 8: 72
-    // against 82 us, since the first pass then need not write the last call's result
-    // back); a smaller one stays for the layer that reads it.  Not in pieces of less than
-    // 64 bytes: 176 against 66 us with 16 bytes of a pixel to a workgroup.
-    b.stream = norm_bytes(d) >= (64u << 20) &&
+    // 64x64x2048 batch 8: 72 against 82 us, since the first pass then need not write the
+    // last call's result back.  Not in pieces of less than 64 bytes: 176 against 66 us
+    // with 16 bytes of a pixel to a workgroup.
+    b.stream = streams(norm_bytes(d)) &&
                (!nhwc || p->form[g] == NormForm::kGeneral || b.slab_c * esz >= 64);
     if (g || p->form[g] == NormForm::kGeneral)
       part_b = std::max(part_b, round256((size_t)d.n * b.chunks * d.c * sizeof(float2)));
@@ -398,6 +402,7 @@ huge2_status embed_run(const huge2_embedding_desc* desc, const void* ids, int64_
   a.ids = ids, a.table = table, a.y = y, a.tokens = tokens;
   a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64, a.scale = d.scale;
   a.lanes_log2 = embed_lanes_log2(d, vec);
+  a.stream = streams(row_b * tokens);  // 65536 rows of 512 bf16: 21 -> 17 us
   return launched(launch_embedding(a, d.dtype, vec, stream));
 }
 

@@ -73,6 +73,7 @@ struct EmbedArgs {
   int id64;
   float scale;
   int lanes_log2;
+  int stream;  // y is stored past the caches
 };
 hipError_t launch_embedding(const EmbedArgs& a, int dtype, int vec, hipStream_t stream);
 

@@ -273,14 +273,12 @@ class GroupNorm(_Owner):
         xp, dyp = self._x(x, "x"), self._x(dy, "dy")
         sp = _take(stats, "stats", self._index, self.stats_shape, self._f32)
         dx, dxp = self._out(out)
-        # one allocation for both, the second on a 16-byte boundary
-        c = self.param_shape[0]
-        both = _torch().empty((c + 3 & ~3) + c, device=self.device)
-        dgamma, dbeta = both[:c], both[-c:]
+        both = _torch().empty((2, self.param_shape[0]), device=self.device)
         gp = both.data_ptr()
         huge2_norm_grad_execute(self._open(), xp, dyp, sp, self._param(gamma, "gamma"),
-                                self._param(beta, "beta"), dxp, gp, gp + (c + 3 & ~3) * 4,
-                                _stream(self._index))
+                                self._param(beta, "beta"), dxp, gp,
+                                gp + 4 * self.param_shape[0], _stream(self._index))
+        dgamma, dbeta = both.unbind(0)
         return dx, dgamma, dbeta
 
     @property

@@ -37,6 +37,10 @@ SHAPES = [
     (1, 4, 256, 256, 1),     # few channels, long planes
     (1, 2, 128, 64, 1),
     (2, 4104, 2, 2, 3),
+    (1, 24, 150, 160, 6),    # several runs whose vectors cross groups
+    (1, 30, 150, 160, 3),
+    (1, 1100, 8, 8, 1),      # a group of more planes than one workgroup joins
+    (1, 16400, 1, 3, 1),     # a group wider than a workgroup
 ]
 
 
