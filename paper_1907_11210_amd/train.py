@@ -166,10 +166,11 @@ def _current_device():
     return torch.device("cuda", torch.cuda.current_device())
 
 
-def _stream(index):
-    """The raw current stream of a device (a tenth of a microsecond; making a
-    torch.cuda.Stream takes one or two, as long as the smallest kernels)."""
-    return _torch()._C._cuda_getCurrentRawStream(index)
+def _raw_stream():
+    """The function that gives a device's current stream as a pointer (a tenth of a
+    microsecond; making a torch.cuda.Stream takes one or two, as long as the smallest
+    kernels)."""
+    return _torch()._C._cuda_getCurrentRawStream
 
 
 def _type_code(dtype):
@@ -182,12 +183,13 @@ def _type_code(dtype):
 
 
 def _take(t, name, index, shape, dtype):
-    """Pointer of a contiguous, aligned tensor of this device, shape and type."""
+    """Pointer of a contiguous, aligned tensor of this device, shape and type.  (The checks
+    of a call's tensors take as long as half a launch: they ask each thing once.)"""
     try:
         if t.dtype is dtype and t.shape == shape and t.get_device() == index \
                 and t.is_contiguous():
             p = t.data_ptr()
-            if p & 15 == 0:
+            if not p & 15:
                 return p
     except AttributeError:
         pass
@@ -236,7 +238,9 @@ class GroupNorm(_Owner):
         self.param_shape = torch.Size((c,))
         self.stats_shape = torch.Size((n, groups, 2))
         self.device = _current_device()
-        self._index, self._f32 = self.device.index, torch.float32
+        self._index, self._f32, self._stream = self.device.index, torch.float32, _raw_stream()
+        self._execute, self._grad_execute = (lib().huge2_norm_execute,
+                                             lib().huge2_norm_grad_execute)
         self.desc = NormDesc(n, c, h, w, groups, lay, _type_code(dtype),
                              NORM_ACTIVATIONS[activation], eps)
         self._plan = huge2_norm_plan_create(self.desc)
@@ -260,8 +264,10 @@ class GroupNorm(_Owner):
         y, yp = self._out(out)
         sp = 0 if stats is None else _take(stats, "stats", self._index, self.stats_shape,
                                            self._f32)
-        huge2_norm_execute(self._open(), xp, self._param(gamma, "gamma"),
-                           self._param(beta, "beta"), yp, sp, _stream(self._index))
+        status = self._execute(self._open(), xp, self._param(gamma, "gamma"),
+                               self._param(beta, "beta"), yp, sp, self._stream(self._index))
+        if status:
+            h2._check(status, "huge2_norm_execute")
         return y
 
     def new_stats(self):
@@ -275,9 +281,11 @@ class GroupNorm(_Owner):
         dx, dxp = self._out(out)
         both = _torch().empty((2, self.param_shape[0]), device=self.device)
         gp = both.data_ptr()
-        huge2_norm_grad_execute(self._open(), xp, dyp, sp, self._param(gamma, "gamma"),
-                                self._param(beta, "beta"), dxp, gp,
-                                gp + 4 * self.param_shape[0], _stream(self._index))
+        status = self._grad_execute(self._open(), xp, dyp, sp, self._param(gamma, "gamma"),
+                                    self._param(beta, "beta"), dxp, gp,
+                                    gp + 4 * self.param_shape[0], self._stream(self._index))
+        if status:
+            h2._check(status, "huge2_norm_grad_execute")
         dgamma, dbeta = both.unbind(0)
         return dx, dgamma, dbeta
 
@@ -300,10 +308,12 @@ class Embedding(_Owner):
         if id_dtype not in (torch.int32, torch.int64):
             raise TypeError("ids must be int32 or int64")
         self.device = _current_device()
-        self._index = self.device.index
+        self._index, self._stream = self.device.index, _raw_stream()
+        self._lookup = lib().huge2_embedding
         self.table_shape, self.dtype, self.id_dtype = torch.Size((rows, dim)), dtype, id_dtype
         self.desc = EmbeddingDesc(rows, dim, _type_code(dtype),
                                   64 if id_dtype == torch.int64 else 32, scale)
+        self._desc_ref = ctypes.byref(self.desc)
         self._plan = huge2_embedding_grad_plan_create(self.desc, max_tokens)
 
     def _ids(self, ids):
@@ -325,7 +335,9 @@ class Embedding(_Owner):
         ip, shape = self._ids(ids)
         tp = _take(table, "table", self._index, self.table_shape, self.dtype)
         y, yp = self._out(out, shape)
-        huge2_embedding(self.desc, ip, ids.numel(), tp, yp, _stream(self._index))
+        status = self._lookup(self._desc_ref, ip, ids.numel(), tp, yp, self._stream(self._index))
+        if status:
+            h2._check(status, "huge2_embedding")
         return y
 
     def grad(self, ids, dy, out=None):
@@ -334,7 +346,7 @@ class Embedding(_Owner):
         dp = _take(dy, "dy", self._index, shape, self.dtype)
         dtable, tp = self._out(out, self.table_shape)
         huge2_embedding_grad_execute(self._open(), ip, ids.numel(), dp, tp,
-                                     _stream(self._index))
+                                     self._stream(self._index))
         return dtable
 
     def kernel(self, tokens):
@@ -362,7 +374,7 @@ class AdamW(_Owner):
                  m=None, v=None, m_scale=None, v_scale=None):
         torch = _torch()
         self.device = _current_device()
-        self._index = self.device.index
+        self._index, self._stream = self.device.index, _raw_stream()
         self.params, self.state_bits = list(params), state_bits
         if state_bits not in (32, 8):
             raise ValueError("state_bits must be 32 or 8")
@@ -420,7 +432,7 @@ class AdamW(_Owner):
                     setattr(t, name, s.data_ptr() if n else None)
             tensors.append(t)
         self._sizes = sizes
-        self._plan = huge2_adamw_plan_create(tensors, state_bits, _stream(self._index))
+        self._plan = huge2_adamw_plan_create(tensors, state_bits, self._stream(self._index))
 
     def step(self, grads, lr, step, betas=(0.9, 0.999), eps=1e-8, grad_scale=None):
         """One step (``step`` counts from 1).  grads: for each parameter its gradient, of its
@@ -446,7 +458,7 @@ class AdamW(_Owner):
         ptrs = array.array("Q", ptrs)
         huge2_adamw_step(self._open(), ptrs.buffer_info()[0],
                          AdamWOptions(lr, betas[0], betas[1], eps, step), sp,
-                         _stream(self._index))
+                         self._stream(self._index))
 
     def _pointers(self, grads, sizes, dtypes):
         # whole lists at a time: a loop over each gradient's properties takes twice as long
