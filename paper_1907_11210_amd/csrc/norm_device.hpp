@@ -90,9 +90,36 @@ __device__ __forceinline__ float block_sum(float v, float* lds) {
 struct Channel {
   float mean, rstd, gamma, beta;
 };
+__device__ __forceinline__ int group_of(const NormArgs& a, int ch) {
+  return (int)fast_div((uint32_t)ch, a.d_mul, a.d_shift);
+}
 __device__ __forceinline__ Channel channel(const NormArgs& a, const float* stats, int img, int ch) {
-  const float2 s = ((const float2*)stats)[(size_t)img * a.groups + ch / a.d];
+  const float2 s = ((const float2*)stats)[(size_t)img * a.groups + group_of(a, ch)];
   return {s.x, s.y, a.gamma ? a.gamma[ch] : 1.f, a.beta ? a.beta[ch] : 0.f};
+}
+// gamma and beta of VW channels from ch, a multiple of VW.
+template <int VW>
+__device__ __forceinline__ void channel_params(const NormArgs& a, int ch, Channel (&k)[VW]) {
+  float g[VW], b[VW];
+  const auto load = [&](const float* p, float none, float (&f)[VW]) {
+    if (!p) {
+#pragma unroll
+      for (int e = 0; e < VW; ++e) f[e] = none;
+    } else if constexpr (VW % 4 == 0) {
+#pragma unroll
+      for (int e = 0; e < VW; e += 4) {
+        const float4 v = *(const float4*)(p + ch + e);
+        f[e] = v.x, f[e + 1] = v.y, f[e + 2] = v.z, f[e + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < VW; ++e) f[e] = p[ch + e];
+    }
+  };
+  load(a.gamma, 1.f, g);
+  load(a.beta, 0.f, b);
+#pragma unroll
+  for (int e = 0; e < VW; ++e) k[e].gamma = g[e], k[e].beta = b[e];
 }
 
 // y, or dx, of one value.

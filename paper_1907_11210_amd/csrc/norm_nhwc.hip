@@ -123,11 +123,11 @@ __device__ __forceinline__ void join_stats(const NormArgs& a, const Slab& q, flo
 template <int VW, bool SPAN>
 __device__ __forceinline__ void channels_of(const NormArgs& a, const Slab& q, const float2* result,
                                             Channel (&k)[VW]) {
+  channel_params<VW>(a, q.c0 + q.ch, k);
 #pragma unroll
   for (int e = 0; e < VW; ++e) {
-    const float2 st = result[(q.ch + (SPAN ? e : 0)) / a.d];
-    k[e] = {st.x, st.y, a.gamma ? a.gamma[q.c0 + q.ch + e] : 1.f,
-            a.beta ? a.beta[q.c0 + q.ch + e] : 0.f};
+    const float2 st = result[group_of(a, q.ch + (SPAN ? e : 0))];
+    k[e].mean = st.x, k[e].rstd = st.y;
   }
 }
 
@@ -181,12 +181,16 @@ __device__ __forceinline__ void add_grad_sums(const NormArgs& a, int first, int 
   }
 }
 
+// The same from the caller's statistics (lanes behind the last channel: of that).
 template <int VW, bool SPAN>
 __device__ __forceinline__ void grad_channels(const NormArgs& a, const Slab& q, Channel (&k)[VW]) {
+  const int ch = min(q.c0 + q.ch, a.c - VW);
+  channel_params<VW>(a, ch, k);
+  const float2* stats = (const float2*)a.stats + (size_t)q.img * a.groups;
 #pragma unroll
   for (int e = 0; e < VW; ++e) {
-    k[e] = channel(a, a.stats, q.img, min(q.c0 + q.ch + e, a.c - 1));
-    if (!SPAN && e) k[e].mean = k[0].mean, k[e].rstd = k[0].rstd;
+    const float2 st = stats[group_of(a, ch + (SPAN ? e : 0))];
+    k[e].mean = st.x, k[e].rstd = st.y;
   }
 }
 
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(1024) void norm_slab_grad_nhwc_kernel(NormArgs a) {
   if (!q.in) return;
   float2 coef[VW];
 #pragma unroll
-  for (int e = 0; e < VW; ++e) coef[e] = result[(q.ch + (SPAN ? e : 0)) / a.d];
+  for (int e = 0; e < VW; ++e) coef[e] = result[group_of(a, q.ch + (SPAN ? e : 0))];
   by_act(a.act, [&](auto act) {
     write_grad_rows<act.value, T, VW, R>(a, q, (T*)a.out + q.at, 0, mine, f, g, k, coef);
   });
@@ -506,7 +510,7 @@ __global__ __launch_bounds__(1024) void norm_run_grad_apply_nhwc_kernel(NormArgs
   grad_channels<VW, SPAN>(a, q, k);
   float2 coef[VW];
 #pragma unroll
-  for (int e = 0; e < VW; ++e) coef[e] = lds[(q.ch + (SPAN ? e : 0)) / a.d];
+  for (int e = 0; e < VW; ++e) coef[e] = lds[group_of(a, q.ch + (SPAN ? e : 0))];
   T* out = (T*)a.out + q.at;
   by_act(a.act, [&](auto act) {
     write_grad_rows<act.value, T, VW, kDeep>(a, q, out, 0, mine, f, w, k, coef);

@@ -169,9 +169,11 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
     c *= 2;
   const int lanes = lanes_of(c), most_threads = slab_threads(*a, vec, grad, lanes);
   int threads = std::max(64, lanes);
-  while (threads < most_threads && slots(lanes, threads) > 4) threads *= 2;
+  const long long slabs = (long long)a->n * ((a->c + c - 1) / c);
+  while (threads < most_threads &&
+         (slots(lanes, threads) > most || (slots(lanes, threads) > 4 && slabs * (threads / 32) <= 8192)))
+    threads *= 2;
   slab_set(a, vec, grad, c, threads);
-  const long long slabs = (long long)a->n * a->cblocks;
   if (slabs >= (1ll << 31)) return false;
   a->slabs = (int)slabs;
   a->slots = slots(lanes, threads);
@@ -182,19 +184,27 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
 
 // Slabs cut into runs of pixels: 64 bytes of a pixel, up to 512 while there are two
 // workgroups for each compute unit all the same (every workgroup of the second pass
-// joins all runs of its groups: few groups, few runs); workgroups of 256 threads, more
-// where a group is wider; at least four pixels a thread.
+// joins all runs of its groups: few groups, few runs).  Of runs as many as fill the
+// compute units with the waves that their registers allow, at least four pixels a
+// thread.  The gradient's sums are 8 bytes for each channel of a run: there wide groups
+// have four pixels side by side, and a run 32 pixels where that leaves a workgroup for
+// each compute unit (39 x 3x59x1344 with 4 pixels a run 53 us, so 40; the forward is
+// slower with the larger workgroups, 32 against 28 us for 13 x 41x29x1216).
 bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const int base = std::lcm(a->d, vec);
   a->span = a->d % vec != 0;
   if (base > a->c || base / vec > 1024) return false;
   const auto lanes_of = [&](int c) { return 1 << log2_ceil(c / vec); };
-  const auto threads_of = [&](int c) { return std::max(256, lanes_of(c)); };
+  const auto threads_of = [&](int c) {
+    const int lanes = lanes_of(c), most = slab_threads(*a, vec, grad, lanes);
+    return std::max(lanes, std::min(std::max(256, (grad ? 4 : 1) * lanes), most));
+  };
   const auto units_of = [&](int c) { return (long long)a->n * ((a->c + c - 1) / c); };
   const auto most_chunks = [&](int c) {
-    const long long rows = threads_of(c) / lanes_of(c);
-    return std::min(std::max(64ll, (512 + units_of(c) - 1) / units_of(c)),
-                    (a->hw + 4 * rows - 1) / (4 * rows));
+    const long long rows = threads_of(c) / lanes_of(c), units = units_of(c);
+    const long long most = grad ? std::max((a->hw + 31) / 32ll, 256 / units) : 1 << 20;
+    return std::min({std::max(64ll, (512 + units - 1) / units), most,
+                     (a->hw + 4 * rows - 1) / (4 * rows)});
   };
   int c = base;
   while (2ll * c <= a->c && 2 * c / vec <= 64 && c * esz < 512 &&
@@ -202,8 +212,8 @@ bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
     c *= 2;
   if (lanes_of(c) > slab_threads(*a, vec, grad, lanes_of(c))) return false;
   slab_set(a, vec, grad, c, threads_of(c));
-  const long long units = units_of(c);
-  const long long chunks = std::min((2048 + units - 1) / units, most_chunks(c));
+  const long long units = units_of(c), waves = units * (a->threads / 64);
+  const long long chunks = std::min(((grad ? 4096 : 8192) + waves - 1) / waves, most_chunks(c));
   a->chunk_len = (int)((a->hw + chunks - 1) / chunks);
   a->chunks = (a->hw + a->chunk_len - 1) / a->chunk_len;
   if (units * a->chunks >= (1ll << 31) - a->c) return false;
@@ -213,7 +223,8 @@ bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
 }
 
 // In NCHW a slab is a group: planes of up to 64 lanes, as many planes side by side
-// as leave four vectors a thread.
+// as leave four vectors a thread, or more where the waves then run at once (8192 of
+// them: 57x2 pixels, 50 channels a group, 640 groups, gradient: 21.5 -> 19 us).
 bool slab_nchw(NormArgs* a, int vec, bool grad) {
   const int vecs = a->hw / vec, lanes = 1 << std::min(6, log2_ceil(vecs));
   const int along = (vecs + lanes - 1) / lanes, most = slab_most(vec, grad, false);
@@ -223,7 +234,9 @@ bool slab_nchw(NormArgs* a, int vec, bool grad) {
     const int planes = threads / lanes;
     return (long long)along * ((a->d + planes - 1) / planes);
   };
-  while (threads < 1024 && slots() > 4 && threads / lanes < a->d) threads *= 2;
+  while (threads < 1024 && threads / lanes < a->d &&
+         (slots() > most || (slots() > 4 && (long long)a->n * a->groups * (threads / 32) <= 8192)))
+    threads *= 2;
   if (slots() > most) return false;
   a->lanes_log2 = log2_ceil(lanes);
   a->along = along;
@@ -275,6 +288,7 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
   a.act = d.activation;
   a.eps = d.eps;
   const int vec = vector_width(d.dtype, nhwc ? d.c : hw);
+  division_magic((uint32_t)a.d, &a.d_mul, &a.d_shift);
   if ((long long)d.n * d.groups + d.c / 16 + 1 >= (1ll << 31)) return HUGE2_ERR_UNSUPPORTED;
   huge2_norm_plan* p = new (std::nothrow) huge2_norm_plan();
   if (!p) return HUGE2_ERR_ALLOC;

@@ -29,6 +29,7 @@ struct NormArgs {
   float* dgamma;
   float* dbeta;
   int n, c, hw, groups, d;
+  uint32_t d_mul, d_shift;  // floor(channel / d) = (channel * d_mul) >> d_shift
   int act;
   float eps;
   int stream;  // the result is stored past the caches
