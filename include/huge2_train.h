@@ -57,10 +57,12 @@ typedef struct {
 
 typedef struct huge2_norm_plan huge2_norm_plan;
 
-/* Chooses the kernels for desc and allocates their workspace (8 bytes for
- * each channel of each run of 64 pixels or more of each image, and for each
- * group of each image).  No work is enqueued.  Errors: INVALID_ARG,
- * UNSUPPORTED (c*h*w of 2^31 or more, or 2^40 elements in all), ALLOC. */
+/* Chooses the kernels for desc and allocates their workspace: 8 bytes for each
+ * group of each image, and for each channel (and group) of each run of pixels that
+ * an image is cut into: one run where the slabs of an image fit the registers of
+ * compute units, else runs of 4 pixels or more.  No work is enqueued.  Errors:
+ * INVALID_ARG, UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or 2^31
+ * workgroups), ALLOC. */
 huge2_status huge2_norm_plan_create(huge2_norm_plan** out, const huge2_norm_desc* desc);
 
 /* Enqueues y from x.  gamma and beta are [c] float; NULL gamma is all ones,
@@ -109,8 +111,9 @@ huge2_status huge2_embedding(const huge2_embedding_desc* desc, const void* ids, 
 typedef struct huge2_embedding_grad_plan huge2_embedding_grad_plan;
 
 /* A plan for the gradients of up to max_tokens (>= 0) tokens.  Allocates the
- * buffers of the tokens' order and of partial sums: about 24 bytes a token, and
- * a 32nd of dy's values in fp32, twice.  No work is enqueued.  Errors: INVALID_ARG,
+ * buffers of the tokens' order and of partial sums: 16 bytes a token, 16 KB for each
+ * 512 tokens up to 131072, and an 8th of dy's values (a 32nd above 131072 tokens) in
+ * fp32.  No work is enqueued.  Errors: INVALID_ARG,
  * UNSUPPORTED (2^30 tokens or more, or rows of 2^31 bytes), ALLOC. */
 huge2_status huge2_embedding_grad_plan_create(huge2_embedding_grad_plan** out,
                                               const huge2_embedding_desc* desc,
@@ -123,7 +126,8 @@ huge2_status huge2_embedding_grad_execute(const huge2_embedding_grad_plan* plan,
                                           int64_t tokens, const void* dy, void* dtable,
                                           void* hip_stream);
 
-/* Name of the kernels that the plan launches for so many tokens. */
+/* Name of the kernel that adds up so many tokens' gradients.  Storage of the plan's;
+ * "" for a NULL plan. */
 const char* huge2_embedding_grad_plan_kernel(const huge2_embedding_grad_plan* plan,
                                              int64_t tokens);
 

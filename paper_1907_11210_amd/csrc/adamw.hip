@@ -93,7 +93,12 @@ __device__ __forceinline__ void store_codes(void* base, long long i, long long n
 
 // A workgroup updates kAdamWork consecutive elements of one tensor: each of its
 // four waves four blocks of 256, four elements a lane, so that a block of 8-bit
-// moments is one wave's own and its largest magnitude needs no LDS.
+// moments is one wave's own and its largest magnitude needs no LDS.  All loads come
+// before the first store.
+//
+// Bound by bytes: 134 M fp32 parameters, 28 bytes each, 691 us (5.45 TB/s); with 8-bit
+// moments and bf16 gradients and copies 67 M, 212 us (5.1 TB/s).  Results stored past
+// the caches: 705 against 691 us, 80 against 83 for 14 M with bf16 copies: not done.
 template <int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   const uint2 work = a.works[blockIdx.x];

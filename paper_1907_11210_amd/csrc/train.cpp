@@ -36,7 +36,7 @@ struct huge2_embedding_grad_plan {
   int64_t max_tokens;
   int vec, lanes_log2;
   void* ws;
-  char kernel_name[96];
+  char kernel_name[2][48];  // few tokens, many
 };
 
 struct huge2_adamw_plan {
@@ -453,7 +453,9 @@ huge2_status embed_grad_create(huge2_embedding_grad_plan** out, const huge2_embe
     delete p;
     return st;
   }
-  std::snprintf(p->kernel_name, sizeof(p->kernel_name), "embedding_sum_kernel v%d", p->vec);
+  for (int many = 0; many < 2; ++many)
+    std::snprintf(p->kernel_name[many], sizeof(p->kernel_name[many]), "embedding_%s_kernel v%d",
+                  many ? "sum" : "few", p->vec);
   *out = p;
   return HUGE2_OK;
 }
@@ -647,8 +649,9 @@ huge2_status huge2_embedding_grad_execute(const huge2_embedding_grad_plan* plan,
   return embed_grad_run(plan, ids, tokens, dy, dtable, (hipStream_t)hip_stream);
 }
 
-const char* huge2_embedding_grad_plan_kernel(const huge2_embedding_grad_plan* plan, int64_t) {
-  return plan ? plan->kernel_name : "";
+const char* huge2_embedding_grad_plan_kernel(const huge2_embedding_grad_plan* plan,
+                                             int64_t tokens) {
+  return plan ? plan->kernel_name[tokens > kMostFew] : "";
 }
 
 huge2_status huge2_embedding_grad_plan_destroy(huge2_embedding_grad_plan* plan) {
