@@ -48,21 +48,24 @@ __device__ __forceinline__ uint32_t encode4(const float (&f)[4], float top, floa
 
 // Four elements from element i of an array of n (i a multiple of 4, the array
 // 16-byte aligned); zeros behind its end.
-template <typename T>
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ void load4(const void* base, long long i, long long n, float (&f)[4]) {
   const T* p = (const T*)base + i;
   if (i + 4 <= n) {
-    unpack<T, 4>(load_pack<T, 4>(p), f);
+    if constexpr (STREAM)
+      unpack<T, 4>(load_stream<T, 4>(p), f);
+    else
+      unpack<T, 4>(load_pack<T, 4>(p), f);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) f[e] = i + e < n ? to_f32<T>(p[e]) : 0.f;
   }
 }
-template <typename T>
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ void store4(void* base, long long i, long long n, const float (&f)[4]) {
   T* p = (T*)base + i;
   if (i + 4 <= n) {
-    store_pack<T, 4>(p, pack<T, 4>(f));
+    store_pack<T, 4>(p, pack<T, 4>(f), STREAM);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -91,15 +94,17 @@ __device__ __forceinline__ void store_codes(void* base, long long i, long long n
 
 }  // namespace
 
-// A workgroup updates kAdamWork consecutive elements of one tensor: each of its
-// four waves four blocks of 256, four elements a lane, so that a block of 8-bit
-// moments is one wave's own and its largest magnitude needs no LDS.  All loads come
-// before the first store.
+// A workgroup updates adam_work consecutive elements of one tensor, each of its
+// four waves blocks of 256, four elements a lane, so that a block of 8-bit moments is
+// one wave's own and its largest magnitude needs no LDS.  All loads come before the
+// first store.
 //
-// Bound by bytes: 134 M fp32 parameters, 28 bytes each, 691 us (5.45 TB/s); with 8-bit
-// moments and bf16 gradients and copies 67 M, 212 us (5.1 TB/s).  Results stored past
-// the caches: 705 against 691 us, 80 against 83 for 14 M with bf16 copies: not done.
-template <int BITS>
+// STREAM: fp32 parameters and moments, which nothing reads before the next step, pass
+// the caches both ways, and gradients and copies find room there.
+//
+// Bound by bytes: 134 M fp32 parameters, 28 bytes each, 645 us (5.8 TB/s); with 8-bit
+// moments and bf16 gradients and copies 67 M, 197 us (5.4 TB/s).
+template <int BITS, bool STREAM>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   const uint2 work = a.works[blockIdx.x];
   const void* grad = a.grads[work.x];
@@ -107,8 +112,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   const AdamTensorDev t = a.tensors[work.x];
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const float keep = 1.f - a.lr * t.weight_decay;
-  const long long first = (long long)work.y * kAdamWork + threadIdx.x * 4;
-  constexpr int kIter = kAdamWork / 1024;
+  const long long first = (long long)work.y * adam_work(BITS) + threadIdx.x * 4;
+  constexpr int kIter = adam_work(BITS) / 1024;
   float p[kIter][4], g[kIter][4], m[kIter][4], v[kIter][4];
 #pragma unroll
   for (int j = 0; j < kIter; ++j) {
@@ -116,14 +121,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
     if (t.bf16)
       load4<uint16_t>(t.param, i, t.count, p[j]);
     else
-      load4<uint32_t>(t.param, i, t.count, p[j]);
+      load4<uint32_t, STREAM>(t.param, i, t.count, p[j]);
     if (t.grad_bf16)
       load4<uint16_t>(grad, i, t.count, g[j]);
     else
       load4<uint32_t>(grad, i, t.count, g[j]);
     if constexpr (BITS == 32) {
-      load4<uint32_t>(t.m, i, t.count, m[j]);
-      load4<uint32_t>(t.v, i, t.count, v[j]);
+      load4<uint32_t, STREAM>(t.m, i, t.count, m[j]);
+      load4<uint32_t, STREAM>(t.v, i, t.count, v[j]);
     } else {
       const bool in = i < t.count;  // a whole wave's block, or none of it, up to the last
       const long long block = i / kAdamBlock;
@@ -148,11 +153,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
     if (t.bf16)
       store4<uint16_t>(t.param, i, t.count, p[j]);
     else
-      store4<uint32_t>(t.param, i, t.count, p[j]);
+      store4<uint32_t, STREAM>(t.param, i, t.count, p[j]);
     if (t.copy) store4<uint16_t>(t.copy, i, t.count, p[j]);
     if constexpr (BITS == 32) {
-      store4<uint32_t>(t.m, i, t.count, m[j]);
-      store4<uint32_t>(t.v, i, t.count, v[j]);
+      store4<uint32_t, STREAM>(t.m, i, t.count, m[j]);
+      store4<uint32_t, STREAM>(t.v, i, t.count, v[j]);
     } else {
       float ms, vs;
       const uint32_t mc = encode4<false>(m[j], wave_top(m[j]), &ms);
@@ -167,11 +172,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   }
 }
 
-hipError_t launch_adamw(const AdamArgs& a, unsigned works, int state_bits, hipStream_t stream) {
-  if (state_bits == 8)
-    hipLaunchKernelGGL(adamw_kernel<8>, dim3(works), dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL(adamw_kernel<32>, dim3(works), dim3(256), 0, stream, a);
+hipError_t launch_adamw(const AdamArgs& a, unsigned works, int state_bits, bool past_caches,
+                        hipStream_t stream) {
+  const auto kernel = state_bits == 8 ? past_caches ? adamw_kernel<8, true> : adamw_kernel<8, false>
+                      : past_caches   ? adamw_kernel<32, true>
+                                      : adamw_kernel<32, false>;
+  hipLaunchKernelGGL(kernel, dim3(works), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

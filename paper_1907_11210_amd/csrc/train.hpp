@@ -114,7 +114,12 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, int vec, hip
 // ---- AdamW (adamw.hip) -----------------------------------------------------------
 
 constexpr int kAdamBlock = 256;    // elements that share a scale
-constexpr int kAdamWork = 4096;    // elements of a workgroup
+// Elements of a workgroup of 256.  Four a thread with moments in 32 bits: 134 M
+// parameters 675 us, 14 M with bf16 gradients and copies 74, 0.3 M in 20 tensors 5.0; eight
+// a thread 700, 77 and 5.7; sixteen 690, 83 and 8.2.  Eight with moments in 8 bits, where
+// a thread's loads are short: 67 M 201 us, 2 M in 160 tensors 13.0; four a thread 215 and
+// 12.2, sixteen 215 and 16.1.
+constexpr int adam_work(int state_bits) { return state_bits == 8 ? 2048 : 1024; }
 constexpr int kAdamTensors = 256;  // tensors of a launch: their gradients are kernel arguments
 
 struct AdamTensorDev {
@@ -131,7 +136,7 @@ struct AdamTensorDev {
 };
 struct AdamArgs {
   const AdamTensorDev* tensors;  // of the launch
-  const uint2* works;            // (tensor of the launch, run of kAdamWork elements)
+  const uint2* works;            // (tensor of the launch, run of adam_work elements)
   const float* grad_scale;
   float beta1, beta2, rest1, rest2;  // rest: 1 - beta
   float lr, eps;
@@ -139,6 +144,7 @@ struct AdamArgs {
   float root;       // 1 / sqrt(1 - beta2^step)
   const void* grads[kAdamTensors];
 };
-hipError_t launch_adamw(const AdamArgs& a, unsigned works, int state_bits, hipStream_t stream);
+hipError_t launch_adamw(const AdamArgs& a, unsigned works, int state_bits, bool past_caches,
+                        hipStream_t stream);
 
 }  // namespace huge2

@@ -32,6 +32,15 @@ __device__ __forceinline__ Pack<T, VW> load_pack(const T* p) {
   }
   return r;
 }
+// The same past the caches (16 bytes only).
+template <typename T, int VW>
+__device__ __forceinline__ Pack<T, VW> load_stream(const T* p) {
+  Pack<T, VW> r;
+  const u32x4 v = __builtin_nontemporal_load((const u32x4*)p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.w[i] = v[i];
+  return r;
+}
 template <typename T, int VW>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, VW>& r) {
   if constexpr (sizeof(T) * VW == 16)

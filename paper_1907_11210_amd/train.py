@@ -465,7 +465,7 @@ class AdamW(_Owner):
         T = _torch().Tensor
         if list(map(T.numel, grads)) != sizes or [g.dtype for g in grads] != dtypes or \
                 not all(map(T.is_contiguous, grads)) or \
-                any(map(self._index.__ne__, map(T.get_device, grads))):
+                list(map(T.get_device, grads)) != [self._index] * len(sizes):
             raise ValueError("gradients must be contiguous tensors on %s of their parameters' "
                              "sizes and of the types %s" % (self.device, dtypes))
         return list(map(T.data_ptr, grads))
