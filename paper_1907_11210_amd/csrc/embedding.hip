@@ -357,7 +357,7 @@ __device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, const int* key
 // Bound by the reads of dy, rows anywhere in memory.  A chunk is short (16 tokens)
 // so that a few thousand tokens already make a few thousand waves; the parts then
 // are an eighth of the reads at most.
-template <typename T, int VW, bool WAVE>
+template <typename T, int VW, bool WAVE, bool PAST>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, int cblocks,
                                                             unsigned sum_blocks) {
   const int* __restrict__ key = a.key[a.passes & 1];
@@ -411,8 +411,13 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, int
     }
 #pragma unroll
     for (int j = 0; j < kDeep; ++j)
-      if (i + j < c1 && k[j] < a.rows)
-        g[j] = load_pack<T, VW>((const T*)a.dy + (size_t)t[j] * a.dim + col);
+      if (i + j < c1 && k[j] < a.rows) {
+        const T* p = (const T*)a.dy + (size_t)t[j] * a.dim + col;
+        if constexpr (PAST)
+          g[j] = load_stream<T, VW>(p);
+        else
+          g[j] = load_pack<T, VW>(p);
+      }
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) {
       if (i + j < c1 && cur < a.rows) {
@@ -676,12 +681,11 @@ hipError_t launch_grad(const EmbedGradArgs& a, hipStream_t stream) {
   }
   const unsigned sums = (unsigned)((a.chunks + per - 1) / per * cblocks);
   const unsigned zeros = (unsigned)(((long long)a.rows + 4 * kZeroRows - 1) / (4 * kZeroRows));
-  if (a.lanes_log2 == 6)
-    hipLaunchKernelGGL((embedding_sum_kernel<T, VW, true>), dim3(sums + zeros), wg, 0, stream, a,
-                       cblocks, sums);
-  else
-    hipLaunchKernelGGL((embedding_sum_kernel<T, VW, false>), dim3(sums + zeros), wg, 0, stream, a,
-                       cblocks, sums);
+  constexpr bool kWide = sizeof(T) * VW == 16;
+  const auto sum = a.lanes_log2 < 6         ? embedding_sum_kernel<T, VW, false, false>
+                   : kWide && a.past_caches ? embedding_sum_kernel<T, VW, true, kWide>
+                                            : embedding_sum_kernel<T, VW, true, false>;
+  hipLaunchKernelGGL(sum, dim3(sums + zeros), wg, 0, stream, a, cblocks, sums);
   if (a.chunks > 1) {
     // four columns a lane: a row with most of the tokens has more workgroups then
     constexpr int kJoin = VW < 4 ? VW : 4;

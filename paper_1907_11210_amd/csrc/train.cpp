@@ -417,7 +417,10 @@ huge2_status embed_run(const huge2_embedding_desc* desc, const void* ids, int64_
   a.ids = ids, a.table = table, a.y = y, a.tokens = tokens;
   a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64, a.scale = d.scale;
   a.lanes_log2 = embed_lanes_log2(d, vec);
-  a.stream = streams(row_b * tokens);  // 65536 rows of 512 bf16: 21 -> 17 us
+  // Results of 16 MiB and more are stored past the caches.  65536 rows of bf16: of 128
+  // (16 MiB) 6.2 -> 5.0 us, of 256 10.5 -> 8.3, of 512 19.3 -> 16.6, and together with a
+  // kernel that reads them 18.9 -> 18.6, 25.5 -> 25.5, 40.6 -> 40.0; of 64 no difference.
+  a.stream = row_b * tokens >= (size_t)16 << 20;
   return launched(launch_embedding(a, d.dtype, vec, stream));
 }
 
@@ -477,6 +480,12 @@ huge2_status embed_grad_run(const huge2_embedding_grad_plan* p, const void* ids,
   a.tokens = (int)tokens, a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64;
   a.scale = d.scale;
   a.lanes_log2 = p->lanes_log2;
+  // dy is read once, and the table's gradient finds more room in the caches.  bf16, inputs
+  // out of the caches, and with dy written before and an AdamW step behind: 65536 tokens of
+  // 512 (64 MiB), 30000 ids 51.8 -> 47.1 and 136 -> 134 us; 32768 of 1024, 40000 ids
+  // 60 -> 50.4 and 250 -> 245; 131072 of 1024, 30000 ids 120 -> 110 and 334 -> 322; 32 MiB
+  // and 16 MiB no difference.
+  a.past_caches = streams(row_b * tokens);
   const int bits = std::max(2, log2_ceil((long long)d.rows + 1));  // keys are ids, and `rows`
   const int tile = tokens <= kMostPlaced ? kPlaceTile : kSortTile;
   a.tiles = (int)((tokens + tile - 1) / tile);

@@ -108,6 +108,7 @@ struct EmbedGradArgs {
   float* part;    // [chunks][2][dim]: sums of rows that cross a chunk's ends
   int chunks, chunk_len;
   int lanes_log2;
+  int past_caches;  // dy is read past the caches
 };
 hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, int vec, hipStream_t stream);
 
