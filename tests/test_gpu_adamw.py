@@ -122,6 +122,24 @@ def test_step(bits, pdtype, gdtype):
             assert ((got - want).abs() <= tol).all(), (k, i, n)
 
 
+@pytest.mark.parametrize("bits,sizes", [(32, [6000003, 70001, 5]), (8, [17000001, 1025, 2047])],
+                         ids=["32", "8"])
+def test_step_of_many(bits, sizes):
+    """More fp32 parameters and moments than are kept in the caches."""
+    s = _state(sizes, bits, torch.float32, torch.bfloat16, 9)
+    opt, dev = _opt(s, bits, True, 0.1)
+    print("adamw", bits, sizes, flush=True)
+    opt.step(dev["g"], step=3, **O)
+    torch.cuda.synchronize()
+    for i in range(len(sizes)):
+        p2, m2, v2, tol, mag = _expect(s, i, bits, 3, 0.1)
+        assert _within(dev["p"][i].cpu().double(), p2, tol, torch.float32).all(), i
+        assert torch.equal(opt.copies[i], dev["p"][i].bfloat16())
+        if bits == 32:
+            assert ((dev["m"][i].cpu().double() - m2).abs() <= 6 * U * mag).all()
+            assert ((dev["v"][i].cpu().double() - v2).abs() <= 6 * U * v2).all()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_steps_from_nothing(bits):
     """From zero states, several steps with the states that the steps leave."""
