@@ -22,7 +22,10 @@ __device__ __forceinline__ int digit_of(int key, int pass) {
 }  // namespace
 
 // A row of 2^lanes_log2 lanes to a token, kLookups tokens each, whose ids and then
-// whose rows are all in flight together.
+// whose rows are all in flight together (1, 2 and 8 were no faster).
+//
+// Bound by the result's bytes: 65536 tokens of 256 bf16 out of 8192: 9.8 us for 34 MB,
+// and 22 MB of the table's 4 read by the XCDs together; 64 tokens of 100: 2.8 us.
 constexpr int kLookups = 4;
 template <typename T, int VW>
 __global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a, int cblocks) {
@@ -67,7 +70,8 @@ __global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a, int cblocks
 // waves and of lower lanes.  For this it adds up the tiles' counts (COUNTED: those
 // that sort_tile_counts_kernel left), or counts all tokens itself, one launch less
 // and as much more work as there are workgroups: 42 cycles of its compute unit's LDS
-// atomics for 64 tokens, 4.7 us for 512 tokens, 11.5 for 16384 (8 in two launches).
+// atomics for 64 tokens, 4.7 us for 512 tokens, 6.3 for 4096, 11.5 for 16384, 15.8 for
+// 32768 (in two launches 11.2 for 16384 with 2048 digits, 10.1 for 32768 with 256).
 // Above, all workgroups reading all tiles' counts is what grows: three launches.
 __global__ __launch_bounds__(kPlaceTile) void sort_tile_counts_kernel(EmbedGradArgs a, int pass) {
   __shared__ int count[kMostDigits];
@@ -354,9 +358,10 @@ __device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, const int* key
 // chunk to part[chunk][1].  Behind the chunks' workgroups, those of the rows without
 // tokens.
 //
-// Bound by the reads of dy, rows anywhere in memory.  A chunk is short (16 tokens)
-// so that a few thousand tokens already make a few thousand waves; the parts then
-// are an eighth of the reads at most.
+// Bound by the reads of dy, rows anywhere in memory, and the table's bytes.  A chunk is
+// short (16 tokens) so that a few thousand tokens already make a few thousand waves; the
+// parts then are an eighth of the reads at most.  PAST: dy is read past the caches.
+// 32768 tokens of 1024 bf16, 40000 ids: 25 us for 150 MB; 16384 of 256 fp32, 1024 ids: 6.9.
 template <typename T, int VW, bool WAVE, bool PAST>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, int cblocks,
                                                             unsigned sum_blocks) {
