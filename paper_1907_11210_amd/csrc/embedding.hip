@@ -580,7 +580,8 @@ __global__ __launch_bounds__(kFewThreads) void embedding_few_kernel(EmbedGradArg
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
     const int t = k * kFewThreads + threadIdx.x;
-    same[k] = __ballot(t < a.tokens && known_id(a.ids, a.id64, min(t, a.tokens - 1), a.rows) == mine);
+    same[k] =
+        __ballot(t < a.tokens && known_id(a.ids, a.id64, min(t, a.tokens - 1), a.rows) == mine);
     if (lane == 0) counts[k * kWaves + wave] = __popcll(same[k]);
   }
   if (mine >= a.rows) return;

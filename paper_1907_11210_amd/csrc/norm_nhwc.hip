@@ -156,7 +156,8 @@ __device__ __forceinline__ void write_rows(const NormArgs& a, const Slab& q, T* 
 #pragma unroll
       for (int e = 0; e < VW; ++e)
         v[e] = norm_value<false, ACT>(v[e], 0.f, k[e], make_float2(0.f, 0.f));
-      store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v), a.stream);
+      store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v),
+                        a.stream);
     }
   }
 }
@@ -298,7 +299,8 @@ __device__ __forceinline__ void write_grad_rows(const NormArgs& a, const Slab& q
       unpack<T, VW>(g[i], w);
 #pragma unroll
       for (int e = 0; e < VW; ++e) v[e] = norm_value<true, ACT>(v[e], w[e], k[e], coef[e]);
-      store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v), a.stream);
+      store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v),
+                        a.stream);
     }
     __builtin_amdgcn_sched_barrier(0);
   }

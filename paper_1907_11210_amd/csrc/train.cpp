@@ -172,7 +172,8 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   int threads = std::max(64, lanes);
   const long long slabs = (long long)a->n * ((a->c + c - 1) / c);
   while (threads < most_threads &&
-         (slots(lanes, threads) > most || (slots(lanes, threads) > 4 && slabs * (threads / 32) <= 8192)))
+         (slots(lanes, threads) > most ||
+          (slots(lanes, threads) > 4 && slabs * (threads / 32) <= 8192)))
     threads *= 2;
   slab_set(a, vec, grad, c, threads);
   if (slabs >= (1ll << 31)) return false;
@@ -364,7 +365,8 @@ huge2_status norm_run(const huge2_norm_plan* p, const void* x, const float* gamm
   a.x = x, a.gamma = gamma, a.beta = beta, a.out = y;
   if (stats) a.stats_out = stats;
   const int nhwc = d.layout == HUGE2_NHWC;
-  if (p->form[0] == NormForm::kGeneral) return launched(launch_norm(a, d.dtype, nhwc, p->vec, stream));
+  if (p->form[0] == NormForm::kGeneral)
+    return launched(launch_norm(a, d.dtype, nhwc, p->vec, stream));
   return launched((nhwc ? launch_norm_nhwc : launch_norm_nchw)(a, d.dtype, p->vec, stream));
 }
 
@@ -384,7 +386,8 @@ huge2_status norm_grad_run(const huge2_norm_plan* p, const void* x, const void* 
   const int nhwc = d.layout == HUGE2_NHWC;
   if (p->form[1] == NormForm::kGeneral)
     return launched(launch_norm_grad(a, d.dtype, nhwc, p->vec, stream));
-  return launched((nhwc ? launch_norm_grad_nhwc : launch_norm_grad_nchw)(a, d.dtype, p->vec, stream));
+  return launched(
+      (nhwc ? launch_norm_grad_nhwc : launch_norm_grad_nchw)(a, d.dtype, p->vec, stream));
 }
 
 // ---- embedding --------------------------------------------------------------------

@@ -86,8 +86,8 @@ constexpr int kMostRecounted = 4096, kMostPlaced = 1 << 17, kPlaceTile = 512;
 constexpr int kMostDigitBits = 12, kMostDigits = 1 << kMostDigitBits;
 constexpr int kChunk = 16;     // sorted tokens of a chunk, or a multiple
 // The form without a sort: its most tokens, rows that a workgroup clears, its threads.
-// (1024 tokens 5.5 to 10.6 us as few or all have one id, the others 15 to 19; 2048 tokens
-// 15 and 34 against 25 and 19.)
+// (512 tokens 5.5 to 10.6 us as few or all have one id, 15 and more with a sort; 2048
+// tokens 15 to 34 against 25 to 19.)
 constexpr int kMostFew = 1024, kFewRows = 64, kFewThreads = 512;
 constexpr int kZeroRows = 16;  // rows of the table that a wave looks up
 constexpr int kFewParts = 8;   // parts that a wave adds alone
