@@ -61,8 +61,8 @@ typedef struct huge2_norm_plan huge2_norm_plan;
  * group of each image, and for each channel (and group) of each run of pixels that
  * an image is cut into: one run where the slabs of an image fit the registers of
  * compute units, else runs of 4 pixels or more.  No work is enqueued.  Errors:
- * INVALID_ARG, UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or 2^31
- * workgroups), ALLOC. */
+ * INVALID_ARG, UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or more
+ * groups and images than the 2^32 threads of a launch can take), ALLOC. */
 huge2_status huge2_norm_plan_create(huge2_norm_plan** out, const huge2_norm_desc* desc);
 
 /* Enqueues y from x.  gamma and beta are [c] float; NULL gamma is all ones,
@@ -114,7 +114,8 @@ typedef struct huge2_embedding_grad_plan huge2_embedding_grad_plan;
  * buffers of the tokens' order and of partial sums: 16 bytes a token, 16 KB for each
  * 512 tokens up to 131072, and an 8th of dy's values (a 32nd above 131072 tokens) in
  * fp32.  No work is enqueued.  Errors: INVALID_ARG,
- * UNSUPPORTED (2^30 tokens or more, or rows of 2^31 bytes), ALLOC. */
+ * UNSUPPORTED (2^30 tokens or more, rows of 2^31 bytes, or more rows or tokens than
+ * the 2^32 threads of a launch can take: 2^28 rows always fit), ALLOC. */
 huge2_status huge2_embedding_grad_plan_create(huge2_embedding_grad_plan** out,
                                               const huge2_embedding_desc* desc,
                                               int64_t max_tokens);

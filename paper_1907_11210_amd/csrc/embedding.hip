@@ -653,10 +653,19 @@ template <typename T, int VW>
 hipError_t launch_lookup(const EmbedArgs& a, hipStream_t stream) {
   const long long per = (256 >> a.lanes_log2) * kLookups;
   const int cblocks = (a.dim / VW + (1 << a.lanes_log2) - 1) >> a.lanes_log2;
-  const long long grid = (a.tokens + per - 1) / per * cblocks;
-  hipLaunchKernelGGL((embedding_kernel<T, VW>), dim3((unsigned)grid), dim3(256), 0, stream, a,
-                     cblocks);
-  return hipGetLastError();
+  const long long most = ((1 << 24) - 1) / cblocks * per;  // tokens that a launch can have
+  for (long long t = 0; t < a.tokens; t += most) {
+    EmbedArgs b = a;
+    b.ids = (const char*)a.ids + t * (a.id64 ? 8 : 4);
+    b.y = (T*)a.y + t * a.dim;
+    b.tokens = a.tokens - t < most ? a.tokens - t : most;
+    const long long grid = (b.tokens + per - 1) / per * cblocks;
+    hipLaunchKernelGGL((embedding_kernel<T, VW>), dim3((unsigned)grid), dim3(256), 0, stream, b,
+                       cblocks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T, int VW>

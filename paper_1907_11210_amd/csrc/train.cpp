@@ -176,7 +176,7 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
           (slots(lanes, threads) > 4 && slabs * (threads / 32) <= 8192)))
     threads *= 2;
   slab_set(a, vec, grad, c, threads);
-  if (slabs >= (1ll << 31)) return false;
+  if (!launchable(slabs, threads)) return false;
   a->slabs = (int)slabs;
   a->slots = slots(lanes, threads);
   a->chunks = 1;
@@ -218,7 +218,7 @@ bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const long long chunks = std::min(((grad ? 4096 : 8192) + waves - 1) / waves, most_chunks(c));
   a->chunk_len = (int)((a->hw + chunks - 1) / chunks);
   a->chunks = (a->hw + a->chunk_len - 1) / a->chunk_len;
-  if (units * a->chunks >= (1ll << 31) - a->c) return false;
+  if (!launchable(units * a->chunks + a->c, a->threads)) return false;
   a->slabs = (int)(units * a->chunks);
   a->slots = 0;
   return true;
@@ -230,7 +230,7 @@ bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
 bool slab_nchw(NormArgs* a, int vec, bool grad) {
   const int vecs = a->hw / vec, lanes = 1 << std::min(6, log2_ceil(vecs));
   const int along = (vecs + lanes - 1) / lanes, most = slab_most(vec, grad, false);
-  if (along > most || (long long)a->n * a->groups >= (1ll << 31)) return false;
+  if (along > most) return false;
   int threads = 64;
   const auto slots = [&] {
     const int planes = threads / lanes;
@@ -239,7 +239,7 @@ bool slab_nchw(NormArgs* a, int vec, bool grad) {
   while (threads < 1024 && threads / lanes < a->d &&
          (slots() > most || (slots() > 4 && (long long)a->n * a->groups * (threads / 32) <= 8192)))
     threads *= 2;
-  if (slots() > most) return false;
+  if (slots() > most || !launchable((long long)a->n * a->groups, threads)) return false;
   a->lanes_log2 = log2_ceil(lanes);
   a->along = along;
   a->threads = threads;
@@ -272,7 +272,8 @@ bool norm_runs(NormArgs* a, bool nhwc, int vec) {
   if (!nhwc) a->chunk_len = (a->chunk_len + vec - 1) / vec * vec;
   a->chunks = (int)((hw + a->chunk_len - 1) / a->chunk_len);
   const long long parts = ((long long)a->d * a->chunks << a->lanes_log2) / 256 + 1;
-  return units * a->chunks < (1ll << 31) && a->n * a->groups * parts < (1ll << 31) - a->c;
+  return launchable(units * a->chunks, 256) &&
+         launchable((long long)a->n * a->groups * parts + a->c, 256);
 }
 
 huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
@@ -291,7 +292,7 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
   a.eps = d.eps;
   const int vec = vector_width(d.dtype, nhwc ? d.c : hw);
   division_magic((uint32_t)a.d, &a.d_mul, &a.d_shift);
-  if ((long long)d.n * d.groups + d.c / 16 + 1 >= (1ll << 31)) return HUGE2_ERR_UNSUPPORTED;
+  if (!launchable(d.c / 16 + 1, 256)) return HUGE2_ERR_UNSUPPORTED;
   huge2_norm_plan* p = new (std::nothrow) huge2_norm_plan();
   if (!p) return HUGE2_ERR_ALLOC;
   p->desc = d;
@@ -451,6 +452,14 @@ huge2_status embed_grad_create(huge2_embedding_grad_plan** out, const huge2_embe
   p->vec = vector_width(desc->dtype, desc->dim);
   p->lanes_log2 = std::min(6, log2_ceil(desc->dim / p->vec));
   const int chunk = embed_chunk_len(max_tokens);
+  const long long chunks = (max_tokens + chunk - 1) / chunk, vecs = desc->dim / p->vec;
+  const int per = 256 >> p->lanes_log2;
+  if (!launchable((chunks + per - 1) / per * ((vecs + 63) / 64) + desc->rows / 64 + 1, 256) ||
+      !launchable((chunks + 15) / 16 * ((desc->dim / std::min(p->vec, 4) + 63) / 64), 1024) ||
+      !launchable(desc->rows / kFewRows + 1 + kMostFew, kFewThreads)) {
+    delete p;
+    return HUGE2_ERR_UNSUPPORTED;
+  }
   const size_t bytes = max_tokens == 0
                            ? 0
                            : 4 * round256(max_tokens * 4) + round256(embed_hist_bytes(max_tokens)) +
@@ -543,14 +552,15 @@ huge2_status adamw_create(huge2_adamw_plan** out, const huge2_adamw_tensor* tens
   std::vector<huge2_adamw_plan::Launch> launches;
   for (int i = 0; i < count; ++i) {
     const huge2_adamw_tensor& t = tensors[i];
-    table[i] = {t.param,   t.m,     t.v, t.m_scale, t.v_scale, t.copy, t.count, t.dtype == HUGE2_BF16,
-                t.grad_dtype == HUGE2_BF16, t.weight_decay, 0};
+    table[i] = {t.param,    t.m,       t.v,
+                t.m_scale,  t.v_scale, t.copy,
+                t.count,    t.dtype == HUGE2_BF16, t.grad_dtype == HUGE2_BF16,
+                t.weight_decay, 0};
     if (i % kAdamTensors == 0)
       launches.push_back({i, std::min(kAdamTensors, count - i), works.size(), 0});
     for (int64_t k = 0; k * adam_work(state_bits) < t.count; ++k)
       works.push_back(make_uint2(i % kAdamTensors, (unsigned)k));
     launches.back().works = works.size() - launches.back().work;
-    if (launches.back().works >= (1u << 31)) return HUGE2_ERR_UNSUPPORTED;
   }
   auto* p = new huge2_adamw_plan();
   p->state_bits = state_bits;
@@ -604,10 +614,14 @@ huge2_status adamw_run(const huge2_adamw_plan* p, const void* const* grads,
     if (l.works == 0) continue;
     std::memcpy(a.grads, grads + l.tensor, l.tensors * sizeof(void*));
     a.tensors = (const AdamTensorDev*)p->table + l.tensor;
-    a.works = (const uint2*)((const char*)p->table + p->works_at) + l.work;
-    const huge2_status st = launched(
-        launch_adamw(a, (unsigned)l.works, p->state_bits, p->past_caches, stream));
-    if (st != HUGE2_OK) return st;
+    const size_t most = (1u << 24) - 1;  // of 256 threads: what a launch can have
+    for (size_t w = 0; w < l.works; w += most) {
+      a.works = (const uint2*)((const char*)p->table + p->works_at) + l.work + w;
+      const huge2_status st =
+          launched(launch_adamw(a, (unsigned)std::min(most, l.works - w), p->state_bits,
+                                p->past_caches, stream));
+      if (st != HUGE2_OK) return st;
+    }
   }
   return HUGE2_OK;
 }

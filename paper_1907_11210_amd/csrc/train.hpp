@@ -10,6 +10,11 @@
 
 namespace huge2 {
 
+// A launch's threads along an axis are counted in 32 bits.
+constexpr bool launchable(long long blocks, long long threads) {
+  return blocks < (1ll << 32) / threads;
+}
+
 // ---- group norm (norm.hip) ---------------------------------------------------
 
 // Three forms share these arguments: slabs held in registers (one pass over x), slabs

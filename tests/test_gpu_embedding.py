@@ -186,3 +186,16 @@ def test_refusals(monkeypatch):
     monkeypatch.setenv("HUGE2_FAULT", "launch")
     with pytest.raises(tr.h2.Huge2Error):
         emb(ids, table)
+
+
+def test_lookup_of_more_than_a_launch_takes():
+    """2^26 tokens of 129 channels are 2^24 workgroups of 256: two launches."""
+    tokens, rows, dim = (1 << 26) + 5, 7, 129
+    ids = torch.arange(tokens, device=DEV) % (rows + 1)  # the last is outside the table
+    table = torch.randn(rows, dim, generator=torch.Generator().manual_seed(6)).bfloat16()
+    y = tr.Embedding(rows, dim, torch.bfloat16)(ids, table.to(DEV))
+    torch.cuda.synchronize()
+    padded = torch.cat((table, torch.zeros(1, dim, dtype=torch.bfloat16))).to(DEV)
+    for first in range(0, tokens, 1 << 22):
+        part = slice(first, min(tokens, first + (1 << 22)))
+        assert torch.equal(y[part], padded[ids[part]]), first

@@ -59,6 +59,19 @@ def test_norm_refuses_what_is_too_large(L, kw):
     assert plan.value is None
 
 
+def test_refuses_more_than_a_launch_takes(L):
+    """2^32 threads: 64 and more for a group in NCHW, 8 for a row of a gradient's table."""
+    plan = ctypes.c_void_p(77)
+    d = _norm(n=1 << 21, c=64, groups=64, h=1, w=1, layout=h2.HUGE2_NCHW)
+    assert L.huge2_norm_plan_create(ctypes.byref(plan), ctypes.byref(d)) == h2.HUGE2_ERR_UNSUPPORTED
+    assert plan.value is None
+    plan.value = 77
+    d = tr.EmbeddingDesc((1 << 31) - 2, 1, h2.HUGE2_BF16, 64, 1.0)
+    assert L.huge2_embedding_grad_plan_create(ctypes.byref(plan), ctypes.byref(d), 4) == \
+        h2.HUGE2_ERR_UNSUPPORTED
+    assert plan.value is None
+
+
 def test_null_plans_and_pointers(L):
     d = _norm()
     inv = h2.HUGE2_ERR_INVALID_ARG
