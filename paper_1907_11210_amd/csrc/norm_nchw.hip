@@ -7,13 +7,76 @@
 
 namespace huge2 {
 
+namespace {
+
+// dgamma and dbeta of a channel for each row of 2^direct_log2 lanes, from all images' x
+// and dy.
+template <typename T, int VW>
+__device__ __forceinline__ void direct_params(const NormArgs& a, int block) {
+  constexpr int kDeep = 4;
+  const int lanes = 1 << a.direct_log2, lane = threadIdx.x & (lanes - 1);
+  const int mine = block * (blockDim.x >> a.direct_log2) + (threadIdx.x >> a.direct_log2);
+  const int ch = min(mine, a.c - 1);  // (rows behind the last: of that, and not written)
+  const int vecs = a.hw / VW, all = a.n * vecs;
+  const float gamma = a.gamma ? a.gamma[ch] : 1.f, beta = a.beta ? a.beta[ch] : 0.f;
+  const float2* stats = (const float2*)a.stats + group_of(a, ch);
+  float s1 = 0.f, s2 = 0.f;
+  by_act(a.act, [&](auto act) {
+    for (int i = lane; i < all; i += lanes * kDeep) {
+      Pack<T, VW> f[kDeep], g[kDeep];
+      float2 st[kDeep];
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        const int p = min(i + j * lanes, all - 1);
+        const int img = (int)fast_div((uint32_t)p, a.px_mul, a.px_shift);
+        const size_t at = ((size_t)img * a.c + ch) * a.hw + (size_t)(p - img * vecs) * VW;
+        f[j] = load_pack<T, VW>((const T*)a.x + at);
+        g[j] = load_pack<T, VW>((const T*)a.dy + at);
+        st[j] = stats[(size_t)img * a.groups];
+      }
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        if (i + j * lanes < all) {
+          float v[VW], w[VW];
+          unpack<T, VW>(f[j], v);
+          unpack<T, VW>(g[j], w);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            const float xh = (v[e] - st[j].x) * st[j].y;
+            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, gamma, beta));
+            s1 += dz;
+            s2 += dz * xh;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  });
+  for (int m = lanes >> 1; m; m >>= 1) {
+    s1 += __shfl_xor(s1, m);
+    s2 += __shfl_xor(s2, m);
+  }
+  if (lane == 0 && mine < a.c) {
+    if (a.dbeta) a.dbeta[ch] = s1;
+    if (a.dgamma) a.dgamma[ch] = s2;
+  }
+}
+
+}  // namespace
+
 // NCHW: a slab is a group of an image, d planes one behind the other.  Rows of
 // lanes lie side by side on a plane; a thread has every `lanes`-th vector of every
 // `planes`-th plane, `along` vectors of a plane, R in all.
-template <typename T, int VW, int R, bool GRAD>
+template <typename T, int VW, int R, bool GRAD, bool DIRECT>
 __global__ __launch_bounds__(1024) void norm_slab_nchw_kernel(NormArgs a) {
   __shared__ float lds[16];
-  const int slab = xcd_remap(blockIdx.x, gridDim.x);
+  if constexpr (DIRECT) {  // (a kernel of its own: these take more registers)
+    if ((int)blockIdx.x >= a.slabs) {
+      direct_params<T, VW>(a, blockIdx.x - a.slabs);
+      return;
+    }
+  }
+  const int slab = xcd_remap(blockIdx.x, a.slabs);
   const int img = slab / a.groups, c0 = slab % a.groups * a.d;
   const int lanes = 1 << a.lanes_log2, planes = blockDim.x >> a.lanes_log2;
   const int lane = threadIdx.x & (lanes - 1), plane = threadIdx.x >> a.lanes_log2;
@@ -94,7 +157,7 @@ __global__ __launch_bounds__(1024) void norm_slab_nchw_kernel(NormArgs a) {
           }
           if (lane == 0 && pl < a.d) {
             if (a.n > 1) {
-              a.part[(size_t)img * a.c + ch] = make_float2(s1, s2);
+              if (!a.direct) a.part[(size_t)img * a.c + ch] = make_float2(s1, s2);
             } else {  // nothing to add up
               if (a.dbeta) a.dbeta[ch] = s1;
               if (a.dgamma) a.dgamma[ch] = s2;
@@ -143,15 +206,21 @@ namespace {
 template <typename T, int VW, bool GRAD>
 void launch_t(const NormArgs& a, hipStream_t stream) {
   constexpr int kMost = slab_most(VW, GRAD, false);
-  const dim3 grid(a.slabs), wg(a.threads);
+  const int direct = GRAD && (a.dgamma || a.dbeta) ? a.direct : 0;
+  const auto launch = [&](auto slots) {
+    constexpr int R = slots.value;
+    const auto kernel = direct ? norm_slab_nchw_kernel<T, VW, R, GRAD, GRAD>
+                               : norm_slab_nchw_kernel<T, VW, R, GRAD, false>;
+    hipLaunchKernelGGL(kernel, dim3(a.slabs + direct), dim3(a.threads), 0, stream, a);
+  };
   if (a.slots == 1)
-    hipLaunchKernelGGL((norm_slab_nchw_kernel<T, VW, 1, GRAD>), grid, wg, 0, stream, a);
+    launch(std::integral_constant<int, 1>());
   else if (a.slots <= 4)
-    hipLaunchKernelGGL((norm_slab_nchw_kernel<T, VW, 4, GRAD>), grid, wg, 0, stream, a);
+    launch(std::integral_constant<int, 4>());
   else
-    hipLaunchKernelGGL((norm_slab_nchw_kernel<T, VW, kMost, GRAD>), grid, wg, 0, stream, a);
+    launch(std::integral_constant<int, kMost>());
   // (its error is the last one, read by the caller)
-  if (GRAD && a.n > 1 && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
+  if (GRAD && a.n > 1 && !a.direct && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
 }
 
 template <bool GRAD>

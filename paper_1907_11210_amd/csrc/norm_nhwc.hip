@@ -200,12 +200,11 @@ __device__ __forceinline__ void grad_channels(const NormArgs& a, const Slab& q, 
   }
 }
 
-// The slab's sums per channel, to part; then f(group, sum of gamma * dz, sum of
-// gamma * dz * xh) by one lane of those that join the group.  Rows first, through LDS
-// with consecutive lanes on consecutive channels.
-template <int VW, typename F>
-__device__ __forceinline__ void join_grad_sums(const NormArgs& a, const Slab& q, float2* lds,
-                                               float (&s1)[VW], float (&s2)[VW], F&& f) {
+// The rows' sums added up through LDS with consecutive lanes on consecutive channels:
+// behind a barrier, [segments][width] of them at `sums`.  Returns the segments.
+template <int VW>
+__device__ __forceinline__ int add_rows(const NormArgs& a, const Slab& q, float2* lds,
+                                        float (&s1)[VW], float (&s2)[VW], float2*& sums) {
   const int lanes = 1 << a.lanes_log2, width = lanes * VW;
   const int width_log2 = a.lanes_log2 + (VW == 8 ? 3 : VW == 4 ? 2 : VW == 2 ? 1 : 0);
   // a wave's two halves first where both have the same channels
@@ -225,7 +224,7 @@ __device__ __forceinline__ void join_grad_sums(const NormArgs& a, const Slab& q,
     for (int e = 0; e < VW; ++e) lds[slot * width + q.ch + e] = make_float2(s1[e], s2[e]);
   }
   __syncthreads();
-  float2* const sums = lds + held * width;  // [segments][width]
+  sums = lds + held * width;
   int segments;
   if (width >= (int)blockDim.x) {
     segments = 1;
@@ -254,17 +253,32 @@ __device__ __forceinline__ void join_grad_sums(const NormArgs& a, const Slab& q,
     if (width >= 64 || (int)(threadIdx.x & 63) < width) sums[seg * width + ch] = t;
   }
   __syncthreads();
+  return segments;
+}
+__device__ __forceinline__ float2 add_segments(const float2* sums, int segments, int width,
+                                               int ch) {
+  float2 t = sums[ch];
+  for (int p = 1; p < segments; ++p) {
+    t.x += sums[p * width + ch].x;
+    t.y += sums[p * width + ch].y;
+  }
+  return t;
+}
+
+// The slab's sums per channel, to part; then f(group, sum of gamma * dz, sum of
+// gamma * dz * xh) by one lane of those that join the group.
+template <int VW, typename F>
+__device__ __forceinline__ void join_grad_sums(const NormArgs& a, const Slab& q, float2* lds,
+                                               float (&s1)[VW], float (&s2)[VW], F&& f) {
+  float2* sums;
+  const int segments = add_rows<VW>(a, q, lds, s1, s2, sums), width = VW << a.lanes_log2;
   float2* part = a.part + ((size_t)q.img * a.chunks + q.chunk) * a.c + q.c0;
   for (int ch = threadIdx.x; ch < q.channels; ch += blockDim.x) {
-    float2 t = sums[ch];
-    for (int p = 1; p < segments; ++p) {
-      t.x += sums[p * width + ch].x;
-      t.y += sums[p * width + ch].y;
-    }
+    const float2 t = add_segments(sums, segments, width, ch);
     if (a.n * a.chunks == 1) {  // nothing to add up
       if (a.dbeta) a.dbeta[q.c0 + ch] = t.x;
       if (a.dgamma) a.dgamma[q.c0 + ch] = t.y;
-    } else {
+    } else if (!a.direct) {
       part[ch] = t;
     }
     const float gamma = a.gamma ? a.gamma[q.c0 + ch] : 1.f;
@@ -308,6 +322,69 @@ __device__ __forceinline__ void write_grad_rows(const NormArgs& a, const Slab& q
 
 }  // namespace
 
+namespace {
+
+// dgamma and dbeta of a slab's channels from all images' x and dy.
+template <typename T, int VW, bool SPAN>
+__device__ __forceinline__ void direct_params(const NormArgs& a, int block, float2* lds) {
+  constexpr int kDeep = SPAN && VW == 8 ? 2 : 4;
+  Slab q;
+  q.c0 = block * a.slab_c;
+  q.channels = min(a.slab_c, a.c - q.c0);
+  q.rows = 1 << a.rows_log2;
+  q.row = threadIdx.x >> a.lanes_log2;
+  q.ch = (threadIdx.x & ((1 << a.lanes_log2) - 1)) * VW;
+  const int ch = min(q.c0 + q.ch, a.c - VW), pixels = a.n * a.hw;
+  const float2* stats = (const float2*)a.stats;
+  Channel k[VW];
+  channel_params<VW>(a, ch, k);
+  float s1[VW], s2[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s1[e] = s2[e] = 0.f;
+  by_act(a.act, [&](auto act) {
+    for (int i = q.row; i < pixels; i += q.rows * kDeep) {
+      Pack<T, VW> f[kDeep], g[kDeep];
+      float2 st[kDeep][SPAN ? VW : 1];
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        const int p = min(i + j * q.rows, pixels - 1);
+        const int img = (int)fast_div((uint32_t)p, a.px_mul, a.px_shift);
+        f[j] = load_pack<T, VW>((const T*)a.x + (size_t)p * a.c + ch);
+        g[j] = load_pack<T, VW>((const T*)a.dy + (size_t)p * a.c + ch);
+#pragma unroll
+        for (int e = 0; e < (SPAN ? VW : 1); ++e)
+          st[j][e] = stats[(size_t)img * a.groups + group_of(a, ch + e)];
+      }
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        if (i + j * q.rows < pixels) {
+          float v[VW], w[VW];
+          unpack<T, VW>(f[j], v);
+          unpack<T, VW>(g[j], w);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            const float2 s = st[j][SPAN ? e : 0];
+            const float xh = (v[e] - s.x) * s.y;
+            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, k[e].gamma, k[e].beta));
+            s1[e] += dz;
+            s2[e] += dz * xh;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  });
+  float2* sums;
+  const int segments = add_rows<VW>(a, q, lds, s1, s2, sums), width = VW << a.lanes_log2;
+  for (int i = threadIdx.x; i < q.channels; i += blockDim.x) {
+    const float2 t = add_segments(sums, segments, width, i);
+    if (a.dbeta) a.dbeta[q.c0 + i] = t.x;
+    if (a.dgamma) a.dgamma[q.c0 + i] = t.y;
+  }
+}
+
+}  // namespace
+
 // ---- all pixels in registers ----------------------------------------------------
 
 // Mean, then the squares around it: two passes, but over registers.  Between loads
@@ -338,9 +415,15 @@ __global__ __launch_bounds__(1024) void norm_slab_nhwc_kernel(NormArgs a) {
   });
 }
 
-template <typename T, int VW, int R, bool SPAN>
+template <typename T, int VW, int R, bool SPAN, bool DIRECT>
 __global__ __launch_bounds__(1024) void norm_slab_grad_nhwc_kernel(NormArgs a) {
   extern __shared__ float2 lds[];
+  if constexpr (DIRECT) {  // (a kernel of its own: these take more registers)
+    if ((int)blockIdx.x >= a.slabs) {
+      direct_params<T, VW, SPAN>(a, blockIdx.x - a.slabs, lds);
+      return;
+    }
+  }
   const Slab q = slab_of<VW>(a);
   const int mine = q.in ? pixels_of(a, q, q.row) : 0;
   Pack<T, VW> f[R], g[R];
@@ -537,10 +620,12 @@ namespace {
 
 template <typename T, int VW, int R, bool GRAD, bool SPAN>
 void launch_slab(const NormArgs& a, hipStream_t stream) {
-  if constexpr (GRAD)
-    hipLaunchKernelGGL((norm_slab_grad_nhwc_kernel<T, VW, R, SPAN>), dim3(a.slabs),
-                       dim3(a.threads), a.lds_bytes, stream, a);
-  else
+  if constexpr (GRAD) {
+    const int direct = a.dgamma || a.dbeta ? a.direct : 0;
+    const auto kernel = direct ? norm_slab_grad_nhwc_kernel<T, VW, R, SPAN, true>
+                               : norm_slab_grad_nhwc_kernel<T, VW, R, SPAN, false>;
+    hipLaunchKernelGGL(kernel, dim3(a.slabs + direct), dim3(a.threads), a.lds_bytes, stream, a);
+  } else
     hipLaunchKernelGGL((norm_slab_nhwc_kernel<T, VW, R, SPAN>), dim3(a.slabs), dim3(a.threads),
                        a.lds_bytes, stream, a);
 }
@@ -570,7 +655,7 @@ void launch_t(const NormArgs& a, hipStream_t stream) {
   else if constexpr (slab_most(VW, GRAD, SPAN) > 4)
     launch_slab<T, VW, slab_most(VW, GRAD, SPAN), GRAD, SPAN>(a, stream);
   // (its error is the last one, read by the caller)
-  if (GRAD && a.n > 1 && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
+  if (GRAD && a.n > 1 && !a.direct && (a.dgamma || a.dbeta)) (void)launch_norm_params(a, stream);
 }
 
 template <typename T, int VW, bool GRAD>

@@ -52,6 +52,11 @@ struct NormArgs {
   int join_log2;       // NHWC: lanes that join a group
   uint32_t dl_mul, dl_shift;  // NHWC: division by a group's entries in a row
   int along;           // NCHW: vectors a thread has of one plane
+  // Gradient: workgroups behind the slabs' that add up dgamma and dbeta from x and dy
+  // themselves, 0: from the slabs' sums in a launch of its own.
+  int direct;
+  int direct_log2;            // NCHW: lanes side by side on one channel
+  uint32_t px_mul, px_shift;  // division by the pixels (NCHW: vectors) of a map
 };
 // The most slots: what leaves a workgroup of 1024 threads without spills (128
 // registers a thread; the gradient holds two tensors, and a vector that may cross

@@ -244,6 +244,9 @@ class GroupNorm(_Owner):
         self.desc = NormDesc(n, c, h, w, groups, lay, _type_code(dtype),
                              NORM_ACTIVATIONS[activation], eps)
         self._plan = huge2_norm_plan_create(self.desc)
+        # (the quickest way to a new tensor)
+        self._param_like = torch.empty(c, dtype=torch.float32, device=self.device)
+        self._like = torch.empty_like
 
     def _x(self, t, name):
         return _take(t, name, self._index, self.x_shape, self.dtype)
@@ -271,7 +274,7 @@ class GroupNorm(_Owner):
         return y
 
     def new_stats(self):
-        return _torch().empty(self.stats_shape, device=self.device)
+        return _torch().empty(self.stats_shape, dtype=self._f32, device=self.device)
 
     def grad(self, x, dy, stats, gamma=None, beta=None, out=None):
         """(dx, dgamma, dbeta) for the output error dy of a call with these x, gamma and
@@ -279,14 +282,12 @@ class GroupNorm(_Owner):
         xp, dyp = self._x(x, "x"), self._x(dy, "dy")
         sp = _take(stats, "stats", self._index, self.stats_shape, self._f32)
         dx, dxp = self._out(out)
-        both = _torch().empty((2, self.param_shape[0]), device=self.device)
-        gp = both.data_ptr()
+        dgamma, dbeta = self._like(self._param_like), self._like(self._param_like)
         status = self._grad_execute(self._open(), xp, dyp, sp, self._param(gamma, "gamma"),
-                                    self._param(beta, "beta"), dxp, gp,
-                                    gp + 4 * self.param_shape[0], self._stream(self._index))
+                                    self._param(beta, "beta"), dxp, dgamma.data_ptr(),
+                                    dbeta.data_ptr(), self._stream(self._index))
         if status:
             h2._check(status, "huge2_norm_grad_execute")
-        dgamma, dbeta = both.unbind(0)
         return dx, dgamma, dbeta
 
     @property

@@ -184,6 +184,17 @@ def test_gradients(shape, layout, dtype):
         assert ((dgamma.cpu().double() - rg).abs() <= tol_g).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+@pytest.mark.parametrize("shape", [
+    (40, 16, 24, 24, 4),     # parameters' gradients from the slabs' sums
+    (64, 64, 4, 4, 8),       # ... and from x and dy: many images, the last channels alone
+    (16, 200, 8, 8, 25), (9, 72, 11, 9, 12), (33, 136, 5, 5, 17)],
+    ids=lambda s: "x".join(map(str, s)))
+def test_gradients_of_many_images(shape, layout, dtype):
+    test_gradients(shape, layout, dtype)
+
+
 @pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
 @pytest.mark.parametrize("act", ["tanh", "silu", None])
 def test_gradients_against_differences(act, layout):
@@ -292,6 +303,22 @@ def test_streams_and_repeats():
         s.synchronize()
         assert torch.equal(y, y2) and torch.equal(stats, st2)
         assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_other_default_type():
+    """Statistics and parameters' gradients are fp32 whatever the default type is."""
+    x = torch.randn(4, 16, 6, 6, device=DEV)
+    torch.set_default_dtype(torch.float64)
+    try:
+        norm = tr.GroupNorm(x.shape, 4, torch.float32)
+        stats = norm.new_stats()
+        norm(x, stats=stats)
+        _, dgamma, dbeta = norm.grad(x, x, stats)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert stats.dtype == dgamma.dtype == dbeta.dtype == torch.float32
+    total, mag = x.double().sum((0, 2, 3)), x.double().abs().sum((0, 2, 3))
+    assert ((dbeta.double() - total).abs() <= DEPTH * U * mag).all()
 
 
 def test_graph_replays():
