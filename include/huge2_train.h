@@ -77,7 +77,7 @@ huge2_status huge2_norm_execute(const huge2_norm_plan* plan, const void* x, cons
  *   dz = dy * activation'(z),  dbeta = sum over n, pixels of dz,
  *   dgamma = sum over n, pixels of dz * xh,  t = dz * gamma,
  *   dx = rstd * (t - mean over the group of t - xh * mean over the group of t*xh).
- * z is formed with the forward's own roundings, so that a ReLU masks the same
+ * A ReLU's z is formed with the forward's own roundings, so that it masks the same
  * values both ways (its slope at 0 is 0).  dgamma and dbeta are [c] float and
  * may be NULL.  dx must not alias x or dy.  Errors: INVALID_ARG, HIP. */
 huge2_status huge2_norm_grad_execute(const huge2_norm_plan* plan, const void* x, const void* dy,

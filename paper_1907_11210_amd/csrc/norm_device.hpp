@@ -10,9 +10,9 @@
 
 namespace huge2 {
 
-// z of a normalised value.  Rounded after the product, here and in the gradient,
-// so that both see the same sign (and the same as a framework without fused
-// multiply-adds).
+// z of a normalised value where its sign counts.  Rounded after the product, here and
+// in the gradient, so that both see the same sign (and the same as a framework without
+// fused multiply-adds).
 __device__ __forceinline__ float norm_z(float xh, float gamma, float beta) {
 #pragma clang fp contract(off)
   return xh * gamma + beta;
@@ -44,7 +44,8 @@ __device__ __forceinline__ float sigmoid(float z) {
 // 1 - 2 / (exp(2z) + 1), and its series near 0, where that cancels: the term left out
 // is 62/2835 z^8 of the value, 6e-8 at 0.2.
 __device__ __forceinline__ float fast_tanh(float z) {
-  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(fast_exp(2.f * z) + 1.f);
+  const float far =
+      1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * 2.88539008177792681f) + 1.f);
   const float q = z * z;
   const float near = z + z * q * (-1.f / 3 + q * (2.f / 15 - q * (17.f / 315)));
   return fabsf(z) < 0.2f ? near : far;
@@ -125,7 +126,13 @@ __device__ __forceinline__ void channel_params(const NormArgs& a, int ch, Channe
 // y, or dx, of one value.
 template <bool GRAD, int ACT>
 __device__ __forceinline__ float norm_value(float x, float dy, const Channel& k, float2 coef) {
-  const float xh = (x - k.mean) * k.rstd, z = norm_z(xh, k.gamma, k.beta);
+  // (A smooth activation is bound by its operations and has no mask to keep: fewer of them.
+  // 4002x5 pixels of 1280 bf16: tanh 31.8 -> 28.6 us, SiLU 23.0 -> 21.5.)
+  constexpr bool kSmooth = ACT == HUGE2_NORM_TANH || ACT == HUGE2_NORM_SILU;
+  if constexpr (!GRAD && kSmooth)
+    return norm_act<ACT>(fmaf(x - k.mean, k.rstd * k.gamma, k.beta));
+  const float xh = (x - k.mean) * k.rstd;
+  const float z = kSmooth ? fmaf(xh, k.gamma, k.beta) : norm_z(xh, k.gamma, k.beta);
   if constexpr (!GRAD) return norm_act<ACT>(z);
   const float t = norm_act_grad<ACT>(dy, z) * k.gamma;
   return k.rstd * (t - coef.x - xh * coef.y);
