@@ -716,17 +716,23 @@ hipError_t launch_grad(const EmbedGradArgs& a, hipStream_t stream) {
 hipError_t launch_embedding(const EmbedArgs& a, int dtype, int vec, hipStream_t stream) {
   if (dtype == HUGE2_BF16)
     return vec == 8   ? launch_lookup<uint16_t, 8>(a, stream)
+           : vec == 4 ? launch_lookup<uint16_t, 4>(a, stream)
            : vec == 2 ? launch_lookup<uint16_t, 2>(a, stream)
                       : launch_lookup<uint16_t, 1>(a, stream);
-  return vec == 4 ? launch_lookup<uint32_t, 4>(a, stream) : launch_lookup<uint32_t, 1>(a, stream);
+  return vec == 4   ? launch_lookup<uint32_t, 4>(a, stream)
+         : vec == 2 ? launch_lookup<uint32_t, 2>(a, stream)
+                    : launch_lookup<uint32_t, 1>(a, stream);
 }
 
 hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, int vec, hipStream_t stream) {
   if (dtype == HUGE2_BF16)
     return vec == 8   ? launch_grad<uint16_t, 8>(a, stream)
+           : vec == 4 ? launch_grad<uint16_t, 4>(a, stream)
            : vec == 2 ? launch_grad<uint16_t, 2>(a, stream)
                       : launch_grad<uint16_t, 1>(a, stream);
-  return vec == 4 ? launch_grad<uint32_t, 4>(a, stream) : launch_grad<uint32_t, 1>(a, stream);
+  return vec == 4   ? launch_grad<uint32_t, 4>(a, stream)
+         : vec == 2 ? launch_grad<uint32_t, 2>(a, stream)
+                    : launch_grad<uint32_t, 1>(a, stream);
 }
 
 }  // namespace huge2

@@ -92,6 +92,15 @@ def test_gradient(shape, dtype):
         assert (got[count == 0] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3000, 50, 100), (1500, 700, 6), (3000, 50, 50), (500, 90, 12)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_rows_of_half_vectors(shape, dtype):
+    """Rows that 8 bytes divide and 16 do not (and 4, in the other type)."""
+    test_lookup(shape, dtype)
+    test_gradient(shape, dtype)
+
+
 @pytest.mark.parametrize("id_dtype", [torch.int32, torch.int64])
 def test_gradient_of_whole_numbers(id_dtype):
     """Exact, over every number of tokens around the sizes at which work is cut."""
