@@ -356,9 +356,12 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
       nhwc ? direct_nhwc(&b, vec) : direct_nchw(&b, vec);
     // 64x64x2048 batch 8: 72 against 82 us, since the first pass then need not write the
     // last call's result back.  Not in pieces of less than 64 bytes: 176 against 66 us
-    // with 16 bytes of a pixel to a workgroup.
+    // with 16 bytes of a pixel to a workgroup; and in NCHW not by less than 16 bytes: 104
+    // against 100 us for 32 images of 300x31x123 fp32 (NHWC, 250 and 251 channels: 53 against
+    // 57 by 4 bytes, bf16, and 78 against 82, fp32).
     b.stream = streams(norm_bytes(d)) &&
-               (!nhwc || p->form[g] == NormForm::kGeneral || b.slab_c * esz >= 64);
+               (!nhwc ? vec * esz == 16
+                      : p->form[g] == NormForm::kGeneral || b.slab_c * esz >= 64);
     if (g || p->form[g] == NormForm::kGeneral)
       part_b = std::max(part_b, round256((size_t)d.n * b.chunks * d.c * sizeof(float2)));
     if (p->form[g] == NormForm::kRun)
@@ -465,7 +468,8 @@ huge2_status embed_run(const huge2_embedding_desc* desc, const void* ids, int64_
   a.ids = ids, a.table = table, a.y = y, a.tokens = tokens;
   a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64, a.scale = d.scale;
   a.lanes_log2 = embed_lanes_log2(d, vec);
-  // Results of 16 MiB and more are stored past the caches.  65536 rows of bf16: of 128
+  // Results of 16 MiB and more are stored past the caches, by 4 bytes and more a lane (26813
+  // rows of 1217 fp32 70 -> 48 us).  65536 rows of bf16: of 128
   // (16 MiB) 6.2 -> 5.0 us, of 256 10.5 -> 8.3, of 512 19.3 -> 16.6, and together with a
   // kernel that reads them 18.9 -> 18.6, 25.5 -> 25.5, 40.6 -> 40.0; of 64 no difference.
   a.stream = row_b * tokens >= (size_t)16 << 20;

@@ -52,15 +52,20 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, VW>& r) {
   else
     *(uint16_t*)p = (uint16_t)r.w[0];
 }
-// The same past the caches (uniform; 16 bytes only).
+// The same past the caches (uniform; 4 bytes and more).
 template <typename T, int VW>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, VW>& r, int stream) {
-  if constexpr (sizeof(T) * VW == 16) {
+  if constexpr (sizeof(T) * VW >= 4) {
     if (stream) {
       // (between two empty statements: the compiler would else make the two stores one
       // ahead of or behind the branch, and that an ordinary one)
       asm volatile("");
-      __builtin_nontemporal_store(u32x4{r.w[0], r.w[1], r.w[2], r.w[3]}, (u32x4*)p);
+      if constexpr (sizeof(T) * VW == 16)
+        __builtin_nontemporal_store(u32x4{r.w[0], r.w[1], r.w[2], r.w[3]}, (u32x4*)p);
+      else if constexpr (sizeof(T) * VW == 8)
+        __builtin_nontemporal_store((uint64_t)r.w[1] << 32 | r.w[0], (uint64_t*)p);
+      else
+        __builtin_nontemporal_store(r.w[0], (uint32_t*)p);
       asm volatile("");
       return;
     }
