@@ -284,6 +284,23 @@ void direct_nchw(NormArgs* a, int vec) {
   division_magic((uint32_t)(a->hw / vec), &a->px_mul, &a->px_shift);
 }
 
+// Slabs too few to fill the compute units, whose two launches another form fills: the
+// forward where a thread has many vectors, so that a launch more costs less (NHWC: 2 images
+// of 38x53x768 bf16 16.2 -> 9.8 us, 8 of 42x28x384 12.1 -> 10.3; with less than 10 vectors
+// 7 to 9 either way; NCHW: 2 of 60x46x60, 4 groups, 11.5 -> 7.6), the gradient where it has
+// a launch for dgamma and dbeta anyway (NHWC: 6 images of 27x87x128 15.6 -> 10.8; NCHW: 8
+// of 64x40x40 12.9 -> 9.2, 4 of 816x26x14 fp32 15.4 -> 10.5).  With a slab for each compute
+// unit the slabs win: 64 of 32x32x128 17.3 and 24; but not with half a memory line of each
+// pixel: 54 of 29x79x64 fp32 by 32 bytes 37.7 and 32.4, 64 of 64x64x64 bf16 56.3 and 38.3.
+bool weak_slabs(const NormArgs& a, bool nhwc, int esz, int vec, bool grad) {
+  if (grad && nhwc && a.slab_c * esz < 64 && a.slab_c < a.c) return !a.direct;
+  if (a.slabs >= 256) return false;
+  if (!grad)
+    return vec * esz == 16 && (nhwc ? a.slots >= 10 : a.slots * vec >= 48 && a.slabs < 64);
+  if (a.direct || (nhwc && a.threads < 1024)) return false;
+  return a.n > 1 || (a.slots > 4 && a.slabs < 64);
+}
+
 // The general form.  Runs of pixels: enough workgroups for eight a compute unit,
 // each run long enough that its sums are few next to its pixels.  False where there
 // are too many.
@@ -354,6 +371,13 @@ huge2_status norm_create(huge2_norm_plan** out, const huge2_norm_desc* desc) {
     }
     if (g && p->form[g] == NormForm::kSlab && d.n > 1 && norm_bytes(d) <= kDirectBytes)
       nhwc ? direct_nhwc(&b, vec) : direct_nchw(&b, vec);
+    if (p->form[g] == NormForm::kSlab && weak_slabs(b, nhwc, esz, vec, g != 0)) {
+      const NormArgs slabs = b;
+      if (fit([&] { return nhwc ? run_nhwc(&b, esz, vec, g != 0) : norm_runs(&b, false, vec); }))
+        p->form[g] = nhwc ? NormForm::kRun : NormForm::kGeneral;
+      else
+        b = slabs;
+    }
     // 64x64x2048 batch 8: 72 against 82 us, since the first pass then need not write the
     // last call's result back.  Not in pieces of less than 64 bytes: 176 against 66 us
     // with 16 bytes of a pixel to a workgroup; and in NCHW not by less than 16 bytes: 104

@@ -187,7 +187,8 @@ def test_gradients(shape, layout, dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
 @pytest.mark.parametrize("shape", [
-    (40, 16, 24, 24, 4),     # parameters' gradients from the slabs' sums
+    (40, 16, 24, 24, 4),     # parameters' gradients from the slabs' sums, or the runs'
+    (260, 16, 24, 24, 4), (280, 24, 30, 27, 2), (2, 64, 46, 60, 2), (1, 64, 46, 60, 2),
     (64, 64, 4, 4, 8),       # ... and from x and dy: many images, the last channels alone
     (16, 200, 8, 8, 25), (9, 72, 11, 9, 12), (33, 136, 5, 5, 17)],
     ids=lambda s: "x".join(map(str, s)))
