@@ -2,8 +2,9 @@
 //
 // The general form, two passes over x: sums per channel and run of pixels, a merge per
 // group, and the pass that writes.  In NHWC it takes groups wider than a workgroup; in
-// NCHW all that do not fit one, with the merge in the second pass.  Bound by the
-// bytes of the two passes.
+// NCHW all that do not fit one or would occupy too few compute units, with the merge in
+// the second pass.  Bound by the bytes of the two passes: 32 images of 300x42x123 bf16,
+// forward, by 4 bytes 30 and 38 us; 8 of 64x40x40, gradient, 9 us for both.
 #include "norm_device.hpp"
 
 namespace huge2 {

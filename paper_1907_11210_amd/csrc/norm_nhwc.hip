@@ -1,8 +1,8 @@
 // norm_nhwc.hip -- group norm in NHWC by slabs: some whole groups of channels of an
 // image, all of its pixels or a run of them, to a workgroup.
 //
-// Where a slab of all pixels fits the registers of a workgroup, x (and dy for the
-// gradient) are read once.  Else a first pass leaves each run's sums and a second one
+// Where a slab of all pixels fits the registers of a workgroup, and the slabs are enough,
+// x (and dy for the gradient) are read once.  Else a first pass leaves each run's sums and a second one
 // joins them and reads x again: 1.5 times the bytes for the forward, 5/3 for the
 // gradient, of which what the Infinity Cache still holds costs less.
 //
