@@ -129,8 +129,7 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
       if constexpr (GRAD) {
         part[e] = s;
       } else {
-        const float m = s.x / count;
-        part[e] = make_float2(pivot[e] + m, fmaxf(s.y - s.x * m, 0.f));
+        part[e] = make_float2(pivot[e] + s.x / count, squares_around_mean(s.x, s.y, count));
       }
     }
   }
@@ -182,8 +181,8 @@ __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
     if constexpr (GRAD) {
       *part = make_float2(s1, s2);
     } else {
-      const float m = s1 / (float)(q.p1 - q.p0);
-      *part = make_float2(pivot + m, fmaxf(s2 - s1 * m, 0.f));
+      const float count = (float)(q.p1 - q.p0);
+      *part = make_float2(pivot + s1 / count, squares_around_mean(s1, s2, count));
     }
   }
 }
@@ -330,7 +329,7 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a, int pa
       coef = make_float2(s1 / total, s2 / total);
       stats = ((const float2*)a.stats)[ig];
     } else {
-      const float var = fmaxf(s2 - s1 * (s1 / total), 0.f) / total;
+      const float var = squares_around_mean(s1, s2, total) / total;
       stats = make_float2(pivot + s1 / total, 1.f / sqrtf(var + a.eps));
       if (threadIdx.x == 0 && blockIdx.x % parts == 0) ((float2*)a.stats_out)[ig] = stats;
     }

@@ -482,7 +482,7 @@ __global__ __launch_bounds__(1024) void norm_run_nhwc_kernel(NormArgs a) {
     for (int e = 0; e < (SPAN ? VW : 1); ++e) {
       const float d = bs[e] - s[e];
       s[e] += d * share;
-      m2[e] += bm2[e] + d * d * cross;
+      m2[e] += bm2[e] + d * (d * cross);  // (with nothing before, 0 however large d is)
     }
   }
   join_stats<VW, SPAN>(a, q, lds, s, m2, [&](int g, float mean, float sq) {
@@ -519,9 +519,9 @@ __global__ __launch_bounds__(1024) void norm_run_apply_nhwc_kernel(NormArgs a) {
       sq += __shfl_xor(sq, m);
     }
     const float mean = pivot + sum / total;
-    sq = fmaxf(sq - sum * (sum / total), 0.f);
+    const float var = squares_around_mean(sum, sq, total) / total;
     if (l == 0) {
-      const float2 st = make_float2(mean, 1.f / sqrtf(sq / total + a.eps));
+      const float2 st = make_float2(mean, 1.f / sqrtf(var + a.eps));
       lds[g] = st;
       if (q.chunk == 0) ((float2*)a.stats_out)[(size_t)q.img * a.groups + q.c0 / a.d + g] = st;
     }

@@ -1,0 +1,97 @@
+"""Group norm by each of its forms: what a form has to keep that no other shows.  The
+forms are named, so that a case does not move to another one unnoticed.
+"""
+import pytest
+import torch
+
+from paper_1907_11210_amd import train as tr
+from test_gpu_norm import DEV, _inputs, _lay, _unlay
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+# layout, type, (n, c, h, w, groups), what the names of the forward's and gradient's kernels
+# begin with
+FORMS = [
+    ("NHWC", F32, (3, 24, 6, 6, 6), "norm_slab_nhwc", "norm_slab_grad_nhwc"),
+    ("NCHW", F32, (3, 24, 6, 6, 6), "norm_slab_nchw", "norm_slab_nchw"),
+    ("NHWC", BF16, (3, 24, 6, 6, 6), "norm_slab_nhwc", "norm_slab_grad_nhwc"),  # groups share vectors
+    ("NHWC", F32, (2, 64, 96, 96, 4), "norm_run_nhwc", "norm_run_grad_nhwc"),   # 36 runs
+    ("NHWC", BF16, (2, 24, 75, 80, 6), "norm_run_nhwc", "norm_run_grad_nhwc"),  # groups share vectors
+    ("NHWC", F32, (2, 16400, 12, 12, 1), "norm_sums_nhwc", "norm_sums_nhwc"),   # 3 runs
+    ("NCHW", F32, (2, 64, 96, 96, 4), "norm_sums_nchw", "norm_sums_nchw"),      # 144 entries to join
+    ("NCHW", BF16, (2, 64, 96, 96, 4), "norm_sums_nchw", "norm_sums_nchw"),
+    ("NCHW", F32, (2, 1100, 64, 64, 1), "norm_sums_nchw", "norm_sums_nchw"),    # too many: a merge
+]
+
+
+def _ids(form):
+    layout, dtype, shape = form[:3]
+    return "%s-%s-%s" % (layout, "f32" if dtype == F32 else "bf16", "x".join(map(str, shape)))
+
+
+def _norm(form, act=None):
+    """The form's object, whose kernels are what the form says."""
+    layout, dtype, (n, c, h, w, groups), forward, grad = form
+    gn = tr.GroupNorm((n, h, w, c) if layout == "NHWC" else (n, c, h, w), groups, dtype, layout, act)
+    assert [k.startswith(name) for k, name in zip(gn.kernels, (forward, grad))] == [True, True], \
+        gn.kernels
+    print("norm", _ids(form), act, gn.kernels, flush=True)
+    return gn
+
+
+def _group(shape, group):
+    n, c, _, _, groups = shape
+    of = torch.zeros(n, c, dtype=torch.bool)
+    per = c // groups
+    of[n - 1, group * per:(group + 1) * per] = True
+    return of
+
+
+@pytest.mark.parametrize("form", FORMS, ids=_ids)
+def test_not_finite_stays_in_its_group(form):
+    """A NaN or an infinity anywhere makes its group NaN, and nothing else: a variance that is
+    not a number must not become none."""
+    layout, dtype, shape = form[:3]
+    n, c, h, w, groups = shape
+    gn = _norm(form, "relu")
+    group = groups // 2
+    bad = _group(shape, group)
+    x, dy, gamma, beta = _inputs(shape, dtype, 5)
+    ga, be, dys = gamma.to(DEV), beta.to(DEV), _lay(dy, layout).to(DEV)
+    last = (group + 1) * c // groups - 1
+    for value in (float("nan"), float("inf"), -float("inf")):
+        for ch, row, col in ((group * c // groups, 0, 0), (last, h // 2, w // 3), (last, h - 1, w - 1)):
+            xb = x.clone()
+            xb[n - 1, ch, row, col] = value
+            xs = _lay(xb, layout).to(DEV)
+            stats = gn.new_stats()
+            y = _unlay(gn(xs, ga, be, stats=stats).cpu(), layout)
+            case = (value, ch, row, col)
+            assert torch.isnan(y[bad]).all() and torch.isfinite(y[~bad]).all(), case
+            st = stats.cpu()
+            assert torch.isnan(st[n - 1, group, 1]) and not torch.isfinite(st[n - 1, group, 0]), case
+            st[n - 1, group] = 0
+            assert torch.isfinite(st).all(), case
+            dx = _unlay(gn.grad(xs, dys, stats, ga, be)[0].cpu(), layout)
+            assert torch.isnan(dx[bad]).all() and torch.isfinite(dx[~bad]).all(), case
+
+
+@pytest.mark.parametrize("form", FORMS, ids=_ids)
+def test_squares_that_overflow(form):
+    """Values of 1e20, whose squares 32 bits do not hold: the variance is infinite, its root's
+    reciprocal 0, and z is beta, in every form."""
+    layout, dtype, shape = form[:3]
+    n, c, h, w, groups = shape
+    gn = _norm(form, "relu")
+    bad = _group(shape, 0)
+    x, _, gamma, beta = _inputs(shape, dtype, 6)
+    for row, col in ((0, 0), (h - 1, w - 1)):
+        xb = x.clone()
+        xb[n - 1, 0, row, col] = 1e20
+        stats = gn.new_stats()
+        y = _unlay(gn(_lay(xb, layout).to(DEV), gamma.to(DEV), beta.to(DEV), stats=stats).cpu(), layout)
+        assert float(stats[n - 1, 0, 1]) == 0 and torch.isfinite(stats).all()
+        want = torch.relu(beta).to(dtype).expand(n, c)[bad][:, None, None]
+        assert torch.equal(y[bad], want.expand_as(y[bad]))
