@@ -54,83 +54,108 @@ __device__ __forceinline__ PlaceNchw place_nchw(const NormArgs& a) {
   return q;
 }
 
+// Vectors of a batch: their loads are in flight together.
+template <int VW>
+constexpr int kBatch = VW >= 4 ? 4 : 8;
+
+// Joins what the lanes hold (a mean of `own` values and the squares around it), `count`
+// values in all, in each of them; sum: over those lanes.
+template <typename F>
+__device__ __forceinline__ void join_lanes(float own, float count, float& mean, float& m2, F&& sum) {
+  const float all = sum(own * mean) / fmaxf(count, 1.f);
+  m2 = sum(m2 + own * ((mean - all) * (mean - all)));
+  mean = all;
+}
+
 }  // namespace
 
-// Sums of a run of pixels per channel.  Forward: the run's mean and its sum of
-// squares around that, from sums around one of its own values (a pivot far from
-// the mean is then itself part of the squares it is subtracted from, which keeps
-// the loss to the run's length in units of the last place).  Gradient: the sums of
-// dz and of dz * xh.
+// Sums of a run of pixels per channel.  Forward: the run's mean and its squares around
+// that, from the means of a few vectors at a time, so that no value is measured from
+// another one that may lie far from it.  Gradient: the sums of dz and of dz * xh.
 template <typename T, int VW, bool GRAD>
 __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
   const PlaceNhwc q = place_nhwc<VW>(a);
   const bool in = q.ch < a.c;
   const T* x = (const T*)a.x + q.at;
   const T* dy = (const T*)a.dy + q.at;
-  float s1[VW], s2[VW], pivot[VW];
-  Channel k[VW];
+  float s1[VW], s2[VW];
 #pragma unroll
-  for (int e = 0; e < VW; ++e) s1[e] = s2[e] = pivot[e] = 0.f;
-  if (in) {
-    if constexpr (GRAD) {
-#pragma unroll
-      for (int e = 0; e < VW; ++e) k[e] = channel(a, a.stats, q.img, q.ch + e);
-    } else {
-      unpack<T, VW>(load_pack<T, VW>(x + (size_t)q.p0 * a.c), pivot);
-    }
-  by_act(GRAD ? a.act : 0, [&](auto act) {
-#pragma unroll 4
-    for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
-      float f[VW];
-      unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
-      if constexpr (GRAD) {
-        float g[VW];
-        unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const float xh = (f[e] - k[e].mean) * k[e].rstd;
-          const float dz = norm_act_grad<act.value>(g[e], norm_z(xh, k[e].gamma, k[e].beta));
-          s1[e] += dz;
-          s2[e] += dz * xh;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const float v = f[e] - pivot[e];
-          s1[e] += v;
-          s2[e] += v * v;
-        }
-      }
-    }
-  });
-  }
+  for (int e = 0; e < VW; ++e) s1[e] = s2[e] = 0.f;
   // rows of one wave, then the four waves
   __shared__ float2 lds[4][64 * VW];
-  const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+  __shared__ float pixels[4];
+  const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), wave = threadIdx.x >> 6;
+  if constexpr (GRAD) {
+    if (in) {
+      Channel k[VW];
 #pragma unroll
-  for (int e = 0; e < VW; ++e) {
-    s1[e] = lanes_sum(s1[e], lanes);
-    s2[e] = lanes_sum(s2[e], lanes);
-    if ((threadIdx.x & 63) < lanes)
-      lds[threadIdx.x >> 6][lane * VW + e] = make_float2(s1[e], s2[e]);
+      for (int e = 0; e < VW; ++e) k[e] = channel(a, a.stats, q.img, q.ch + e);
+      by_act(a.act, [&](auto act) {
+#pragma unroll 4
+        for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
+          float f[VW], g[VW];
+          unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
+          unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            const float xh = (f[e] - k[e].mean) * k[e].rstd;
+            const float dz = norm_act_grad<act.value>(g[e], norm_z(xh, k[e].gamma, k[e].beta));
+            s1[e] += dz;
+            s2[e] += dz * xh;
+          }
+        }
+      });
+    }
+#pragma unroll
+    for (int e = 0; e < VW; ++e) {
+      s1[e] = lanes_sum(s1[e], lanes);
+      s2[e] = lanes_sum(s2[e], lanes);
+    }
+  } else {
+    const int mine = (q.p1 - q.p0 - q.row + q.rows - 1) >> (8 - a.lanes_log2);
+    for (int i = 0; in && i < mine; i += kBatch<VW>) {
+      Pack<T, VW> f[kBatch<VW>];
+#pragma unroll
+      for (int k = 0; k < kBatch<VW>; ++k)
+        if (i + k < mine)
+          f[k] = load_pack<T, VW>(x + (size_t)(q.p0 + q.row + (i + k) * q.rows) * a.c);
+      float mean[VW], m2[VW];
+      own_stats<T, VW, kBatch<VW>, true>(f, min(kBatch<VW>, mine - i), mean, m2);
+      join_batch<VW, true>(i, min(kBatch<VW>, mine - i), mean, m2, s1, s2);
+    }
+    const float count = lanes_sum((float)mine, lanes);
+#pragma unroll
+    for (int e = 0; e < VW; ++e)
+      join_lanes((float)mine, count, s1[e], s2[e], [&](float v) { return lanes_sum(v, lanes); });
+    if ((threadIdx.x & 63) == 0) pixels[wave] = count;
+  }
+  if ((threadIdx.x & 63) < lanes) {
+#pragma unroll
+    for (int e = 0; e < VW; ++e) lds[wave][lane * VW + e] = make_float2(s1[e], s2[e]);
   }
   __syncthreads();
   if (threadIdx.x < lanes && in) {
-    const float count = (float)(q.p1 - q.p0);
     float2* part = a.part + ((size_t)q.img * a.chunks + q.chunk) * a.c + q.ch;
 #pragma unroll
     for (int e = 0; e < VW; ++e) {
-      float2 s = lds[0][lane * VW + e];
-#pragma unroll
-      for (int w = 1; w < 4; ++w) {
-        s.x += lds[w][lane * VW + e].x;
-        s.y += lds[w][lane * VW + e].y;
-      }
+      float2 s = make_float2(0.f, 0.f);
       if constexpr (GRAD) {
-        part[e] = s;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          s.x += lds[w][lane * VW + e].x;
+          s.y += lds[w][lane * VW + e].y;
+        }
       } else {
-        part[e] = make_float2(pivot[e] + s.x / count, squares_around_mean(s.x, s.y, count));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) s.x += pixels[w] * lds[w][lane * VW + e].x;
+        s.x /= (float)(q.p1 - q.p0);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float2 v = lds[w][lane * VW + e];
+          s.y += v.y + pixels[w] * ((v.x - s.x) * (v.x - s.x));
+        }
       }
+      part[e] = s;
     }
   }
 }
@@ -141,19 +166,19 @@ __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
   if (!q.in) return;  // whole rows of lanes: the sums below stay in one
   const T* x = (const T*)a.x + (size_t)q.plane * a.hw;
   const T* dy = (const T*)a.dy + (size_t)q.plane * a.hw;
-  float s1 = 0.f, s2 = 0.f, pivot = 0.f;
-  Channel k;
-  if constexpr (GRAD)
-    k = channel(a, a.stats, q.img, q.ch);
-  else
-    pivot = to_f32<T>(x[q.p0]);
-  by_act(GRAD ? a.act : 0, [&](auto act) {
+  const auto row_sum = [&](float v) {
+    for (int m = q.lanes >> 1; m; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+  };
+  float2 part;
+  if constexpr (GRAD) {
+    const Channel k = channel(a, a.stats, q.img, q.ch);
+    float s1 = 0.f, s2 = 0.f;
+    by_act(a.act, [&](auto act) {
 #pragma unroll 4
-    for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
-      float f[VW];
-      unpack<T, VW>(load_pack<T, VW>(x + p), f);
-      if constexpr (GRAD) {
-        float g[VW];
+      for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
+        float f[VW], g[VW];
+        unpack<T, VW>(load_pack<T, VW>(x + p), f);
         unpack<T, VW>(load_pack<T, VW>(dy + p), g);
 #pragma unroll
         for (int e = 0; e < VW; ++e) {
@@ -162,29 +187,26 @@ __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
           s1 += dz;
           s2 += dz * xh;
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const float v = f[e] - pivot;
-          s1 += v;
-          s2 += v * v;
-        }
       }
+    });
+    part = make_float2(row_sum(s1), row_sum(s2));
+  } else {
+    const int vecs = (q.p1 - q.p0) / VW, mine = (vecs - q.lane + q.lanes - 1) >> a.lanes_log2;
+    float s[VW], m2[VW];  // (the first of each)
+    s[0] = m2[0] = 0.f;
+    for (int i = 0; i < mine; i += kBatch<VW>) {
+      Pack<T, VW> f[kBatch<VW>];
+#pragma unroll
+      for (int k = 0; k < kBatch<VW>; ++k)
+        if (i + k < mine) f[k] = load_pack<T, VW>(x + q.p0 + (q.lane + (i + k) * q.lanes) * VW);
+      float mean[VW], batch_m2[VW];
+      own_stats<T, VW, kBatch<VW>, false>(f, min(kBatch<VW>, mine - i), mean, batch_m2);
+      join_batch<VW, false>(i, min(kBatch<VW>, mine - i), mean, batch_m2, s, m2);
     }
-  });
-  for (int m = q.lanes >> 1; m; m >>= 1) {
-    s1 += __shfl_xor(s1, m);
-    s2 += __shfl_xor(s2, m);
+    join_lanes((float)(mine * VW), (float)(q.p1 - q.p0), s[0], m2[0], row_sum);
+    part = make_float2(s[0], m2[0]);
   }
-  if (q.lane == 0) {
-    float2* part = a.part + ((size_t)q.img * a.chunks + q.chunk) * a.c + q.ch;
-    if constexpr (GRAD) {
-      *part = make_float2(s1, s2);
-    } else {
-      const float count = (float)(q.p1 - q.p0);
-      *part = make_float2(pivot + s1 / count, squares_around_mean(s1, s2, count));
-    }
-  }
+  if (q.lane == 0) a.part[((size_t)q.img * a.chunks + q.chunk) * a.c + q.ch] = part;
 }
 
 // Joins the runs.  A workgroup to an (image, group): its statistics, or the two

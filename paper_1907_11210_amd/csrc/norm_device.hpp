@@ -87,6 +87,63 @@ __device__ __forceinline__ float block_sum(float v, float* lds) {
   return s;
 }
 
+// A thread's vectors: their mean and the squares around it, per channel where a
+// vector may span groups, else over all in s[0], m2[0].
+template <typename T, int VW, int R, bool SPAN>
+__device__ __forceinline__ void own_stats(Pack<T, VW> (&f)[R], int mine, float (&s)[VW],
+                                          float (&m2)[VW]) {
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s[e] = m2[e] = 0.f;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (k < mine) {
+      float v[VW];
+      unpack<T, VW>(f[k], v);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) s[e] += v[e];
+      forget(f[k]);
+    }
+  }
+  if constexpr (!SPAN) {
+#pragma unroll
+    for (int e = 1; e < VW; ++e) s[0] += s[e];
+#pragma unroll
+    for (int e = 1; e < VW; ++e) s[e] = s[0];
+  }
+  const float own = 1.f / (float)max(1, mine * (SPAN ? 1 : VW));
+#pragma unroll
+  for (int e = 0; e < VW; ++e) s[e] *= own;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (k < mine) {
+      float v[VW];
+      unpack<T, VW>(f[k], v);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) m2[e] += (v[e] - s[e]) * (v[e] - s[e]);
+      forget(f[k]);
+    }
+  }
+  if constexpr (!SPAN) {
+#pragma unroll
+    for (int e = 1; e < VW; ++e) m2[0] += m2[e];
+  }
+}
+
+// Joins a batch of `now` vectors with the `before` vectors that came before it.
+template <int VW, bool SPAN>
+__device__ __forceinline__ void join_batch(int before, int now, const float (&batch)[VW],
+                                           const float (&batch_m2)[VW], float (&s)[VW],
+                                           float (&m2)[VW]) {
+  const float share = (float)now / ((float)before + (float)now);
+  const float cross = (float)before * share * (SPAN ? 1 : VW);
+#pragma unroll
+  for (int e = 0; e < (SPAN ? VW : 1); ++e) {
+    const float d = batch[e] - s[e];
+    s[e] += d * share;
+    m2[e] += batch_m2[e] + d * (d * cross);  // (with nothing before, 0 however large d is)
+  }
+}
+
 // Squares of `count` values around their mean, from the sum of the values less another one
 // and the squares of that.  Rounding may leave less than nothing; what is no number stays
 // none (a maximum with 0 would drop it), and squares that 32 bits do not hold stay infinite.

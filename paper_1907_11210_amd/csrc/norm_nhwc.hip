@@ -50,48 +50,6 @@ __device__ __forceinline__ int pixels_of(const NormArgs& a, const Slab& q, int r
   return (q.len - r + q.rows - 1) >> a.rows_log2;
 }
 
-// A thread's vectors: their mean and the squares around it, per channel where a
-// vector may span groups, else over all in s[0], m2[0].
-template <typename T, int VW, int R, bool SPAN>
-__device__ __forceinline__ void own_stats(Pack<T, VW> (&f)[R], int mine, float (&s)[VW],
-                                          float (&m2)[VW]) {
-#pragma unroll
-  for (int e = 0; e < VW; ++e) s[e] = m2[e] = 0.f;
-#pragma unroll
-  for (int k = 0; k < R; ++k) {
-    if (k < mine) {
-      float v[VW];
-      unpack<T, VW>(f[k], v);
-#pragma unroll
-      for (int e = 0; e < VW; ++e) s[e] += v[e];
-      forget(f[k]);
-    }
-  }
-  if constexpr (!SPAN) {
-#pragma unroll
-    for (int e = 1; e < VW; ++e) s[0] += s[e];
-#pragma unroll
-    for (int e = 1; e < VW; ++e) s[e] = s[0];
-  }
-  const float own = 1.f / (float)max(1, mine * (SPAN ? 1 : VW));
-#pragma unroll
-  for (int e = 0; e < VW; ++e) s[e] *= own;
-#pragma unroll
-  for (int k = 0; k < R; ++k) {
-    if (k < mine) {
-      float v[VW];
-      unpack<T, VW>(f[k], v);
-#pragma unroll
-      for (int e = 0; e < VW; ++e) m2[e] += (v[e] - s[e]) * (v[e] - s[e]);
-      forget(f[k]);
-    }
-  }
-  if constexpr (!SPAN) {
-#pragma unroll
-    for (int e = 1; e < VW; ++e) m2[0] += m2[e];
-  }
-}
-
 // Joins the threads' entries: f(group of the slab, mean, squares around it) by one
 // lane of those that join the group.
 template <int VW, bool SPAN, typename F>
@@ -475,15 +433,7 @@ __global__ __launch_bounds__(1024) void norm_run_nhwc_kernel(NormArgs a) {
     load_rows<T, VW, kRun>(a, q, (const T*)a.x + q.at, i, mine, f);
     float bs[VW], bm2[VW];
     own_stats<T, VW, kRun, SPAN>(f, min(kRun, mine - i), bs, bm2);
-    // join with what came before: i pixels and these
-    const float now = (float)min(kRun, mine - i), share = now / ((float)i + now);
-    const float cross = (float)i * share * (SPAN ? 1 : VW);
-#pragma unroll
-    for (int e = 0; e < (SPAN ? VW : 1); ++e) {
-      const float d = bs[e] - s[e];
-      s[e] += d * share;
-      m2[e] += bm2[e] + d * (d * cross);  // (with nothing before, 0 however large d is)
-    }
+    join_batch<VW, SPAN>(i, min(kRun, mine - i), bs, bm2, s, m2);
   }
   join_stats<VW, SPAN>(a, q, lds, s, m2, [&](int g, float mean, float sq) {
     a.gpart[((size_t)q.img * a.chunks + q.chunk) * a.groups + q.c0 / a.d + g] =

@@ -1,11 +1,13 @@
 """Group norm by each of its forms: what a form has to keep that no other shows.  The
 forms are named, so that a case does not move to another one unnoticed.
+
+Tolerances as in test_gpu_norm, from whose formulas these are.
 """
 import pytest
 import torch
 
 from paper_1907_11210_amd import train as tr
-from test_gpu_norm import DEV, _inputs, _lay, _unlay
+from test_gpu_norm import DEPTH, DEV, U, _inputs, _lay, _reference, _unlay
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +97,41 @@ def test_squares_that_overflow(form):
         assert float(stats[n - 1, 0, 1]) == 0 and torch.isfinite(stats).all()
         want = torch.relu(beta).to(dtype).expand(n, c)[bad][:, None, None]
         assert torch.equal(y[bad], want.expand_as(y[bad]))
+
+
+# the longest runs: 4096 values of fp32 and 8192 of bf16 in NCHW, whole maps in NHWC
+LONG = [
+    ("NCHW", F32, (64, 128, 64, 64, 4), "norm_sums_nchw", "norm_sums_nchw"),
+    ("NCHW", BF16, (64, 128, 64, 128, 2), "norm_sums_nchw", "norm_sums_nchw"),
+    ("NHWC", F32, (32, 16400, 12, 12, 1), "norm_sums_nhwc", "norm_sums_nhwc"),
+    ("NHWC", F32, (64, 128, 64, 64, 4), "norm_run_nhwc", "norm_run_grad_nhwc"),
+]
+
+
+def _statistics(form, x):
+    """The kernels' and the definition's, on the GPU."""
+    layout, dtype, shape = form[:3]
+    gn = _norm(form)
+    stats = gn.new_stats()
+    gn(_lay(x, layout), stats=stats)
+    ones, zeros = torch.ones(shape[1], device=DEV), torch.zeros(shape[1], device=DEV)
+    _, mean, rstd = _reference(x, ones, zeros, shape[4], None, 1e-5)
+    st = stats.double()
+    return (st[..., 0] - mean).abs(), (st[..., 1] / rstd - 1).abs()
+
+
+def _normal(shape, dtype, seed):
+    g = torch.Generator(DEV).manual_seed(seed)
+    return torch.randn(shape[:4], generator=g, device=DEV).to(dtype)
+
+
+@pytest.mark.parametrize("form", LONG + FORMS, ids=_ids)
+def test_an_outlier_where_runs_begin(form):
+    """The first pixel 1e4 standard deviations out: what comes first is no measure of the rest,
+    so the squares must not be taken around it.  They are off by DEPTH u of themselves."""
+    shape = form[2]
+    x = _normal(shape, form[1], 4)
+    x[:, :, 0, 0] += 1e4
+    mean, rstd = _statistics(form, x)
+    assert (rstd <= DEPTH * U).all(), float(rstd.max()) / U
+    assert (mean <= DEPTH * U * 1e4).all()
