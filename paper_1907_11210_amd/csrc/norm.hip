@@ -291,8 +291,9 @@ __global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
 }
 
 // A workgroup to some runs of a group's planes (a row of lanes each).  Where the
-// group has few runs (JOIN) it joins them itself: no launch between the two passes,
+// group has few runs (JOIN, up to kJoined) it joins them itself: no launch between the two passes,
 // and dgamma and dbeta come from workgroups behind the others.
+constexpr int kJoined = 1024;  // four a thread
 template <typename T, int VW, bool GRAD, bool JOIN>
 __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a, int parts) {
   __shared__ float lds[4];
@@ -330,29 +331,32 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a, int pa
   if constexpr (JOIN) {
     const float2* part = a.part + (size_t)img * a.chunks * a.c + c0;
     const int entries = a.chunks * a.d;
-    const float total = (float)a.d * (float)a.hw, pivot = GRAD ? 0.f : part[0].x;
-    float s1 = 0.f, s2 = 0.f;
-    for (int e = threadIdx.x; e < entries; e += 256) {
-      const int chunk = e / a.d, j = e - chunk * a.d;
-      const float2 v = part[(size_t)chunk * a.c + j];
-      if constexpr (GRAD) {
-        const float gamma = a.gamma ? a.gamma[c0 + j] : 1.f;
-        s1 += gamma * v.x;
-        s2 += gamma * v.y;
-      } else {
-        const float count = (float)min(a.chunk_len, a.hw - chunk * a.chunk_len);
-        s1 += count * (v.x - pivot);
-        s2 += v.y + count * (v.x - pivot) * (v.x - pivot);
-      }
+    const float total = (float)a.d * (float)a.hw;
+    float2 v[kJoined / 256];
+    float weight[kJoined / 256], s1 = 0.f, s2 = 0.f;  // gamma, or the run's pixels
+#pragma unroll
+    for (int i = 0; i < kJoined / 256; ++i) {
+      const int e = threadIdx.x + i * 256, chunk = e / a.d, j = e - chunk * a.d;
+      const bool mine = e < entries;
+      v[i] = mine ? part[(size_t)chunk * a.c + j] : make_float2(0.f, 0.f);
+      if constexpr (GRAD)
+        weight[i] = mine && a.gamma ? a.gamma[c0 + j] : 1.f;
+      else
+        weight[i] = mine ? (float)min(a.chunk_len, a.hw - chunk * a.chunk_len) : 0.f;
     }
-    s1 = block_sum(s1, lds);
-    s2 = block_sum(s2, lds);
+#pragma unroll
+    for (int i = 0; i < kJoined / 256; ++i) s1 += weight[i] * v[i].x;
+    s1 = block_sum(s1, lds) / total;
     if constexpr (GRAD) {
-      coef = make_float2(s1 / total, s2 / total);
+#pragma unroll
+      for (int i = 0; i < kJoined / 256; ++i) s2 += weight[i] * v[i].y;
+      coef = make_float2(s1, block_sum(s2, lds) / total);
       stats = ((const float2*)a.stats)[ig];
-    } else {
-      const float var = squares_around_mean(s1, s2, total) / total;
-      stats = make_float2(pivot + s1 / total, 1.f / sqrtf(var + a.eps));
+    } else {  // the squares around the mean of all
+#pragma unroll
+      for (int i = 0; i < kJoined / 256; ++i)
+        s2 += v[i].y + weight[i] * ((v[i].x - s1) * (v[i].x - s1));
+      stats = make_float2(s1, 1.f / sqrtf(block_sum(s2, lds) / total + a.eps));
       if (threadIdx.x == 0 && blockIdx.x % parts == 0) ((float2*)a.stats_out)[ig] = stats;
     }
   } else {
@@ -399,7 +403,7 @@ hipError_t launch_t(const NormArgs& a, int nhwc, hipStream_t stream) {
   const int rows = 256 >> a.lanes_log2, parts = (a.d * a.chunks + rows - 1) / rows;
   const unsigned apply = (unsigned)a.n * a.groups * parts;
   hipLaunchKernelGGL((norm_sums_nchw_kernel<T, VW, GRAD>), dim3(grid), wg, 0, stream, a);
-  if (a.d * a.chunks <= 1024) {  // four entries a thread
+  if (a.d * a.chunks <= kJoined) {
     hipLaunchKernelGGL((norm_apply_nchw_kernel<T, VW, GRAD, true>),
                        dim3(apply + merge - a.n * a.groups), wg, 0, stream, a, parts);
   } else {

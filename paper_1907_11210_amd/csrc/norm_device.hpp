@@ -144,15 +144,6 @@ __device__ __forceinline__ void join_batch(int before, int now, const float (&ba
   }
 }
 
-// Squares of `count` values around their mean, from the sum of the values less another one
-// and the squares of that.  Rounding may leave less than nothing; what is no number stays
-// none (a maximum with 0 would drop it), and squares that 32 bits do not hold stay infinite.
-__device__ __forceinline__ float squares_around_mean(float sum, float squares, float count) {
-  const float v = squares - sum * (sum / count);
-  if (std::isinf(squares) && std::isfinite(sum)) return squares;
-  return v < 0.f ? 0.f : v;
-}
-
 // A channel's constants: z = ((x - mean) * rstd) * gamma + beta.
 struct Channel {
   float mean, rstd, gamma, beta;

@@ -453,25 +453,38 @@ __global__ __launch_bounds__(1024) void norm_run_apply_nhwc_kernel(NormArgs a) {
   const int gl = 1 << a.join_log2, l = threadIdx.x & (gl - 1);
   for (int g = threadIdx.x >> a.join_log2; g < q.groups; g += blockDim.x >> a.join_log2) {
     const float2* part = a.gpart + (size_t)q.img * a.chunks * a.groups + q.c0 / a.d + g;
-    const float total = (float)a.d * (float)a.hw;
-    // around the first run's mean, in one go: the loads' latency is what this takes
-    const float pivot = part[0].x;
-    float sum = 0.f, sq = 0.f;
-#pragma unroll 8
-    for (int c = l; c < a.chunks; c += gl) {
-      const float2 v = part[(size_t)c * a.groups];
-      const float count = (float)min(a.chunk_len, a.hw - c * a.chunk_len) * (float)a.d;
-      sum += count * (v.x - pivot);
-      sq += v.y + count * (v.x - pivot) * (v.x - pivot);
+    const float per = (float)a.d, total = per * (float)a.hw;
+    // The mean and the squares around it, of the runs of a lane eight by eight (all loads of
+    // eight in flight: their latency is what this takes), then of the lanes; not around one
+    // run's mean, which may lie far from the others.  n: pixels.
+    constexpr int kHeld = 8;
+    float n = 0.f, mean = 0.f, sq = 0.f;
+    for (int c0 = l; c0 < a.chunks; c0 += gl * kHeld) {
+      float2 v[kHeld];
+      float w[kHeld], now = 0.f, s = 0.f, m2 = 0.f;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const int c = c0 + i * gl;
+        v[i] = c < a.chunks ? part[(size_t)c * a.groups] : make_float2(0.f, 0.f);
+        w[i] = c < a.chunks ? (float)min(a.chunk_len, a.hw - c * a.chunk_len) : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) now += w[i], s += w[i] * v[i].x;
+      s *= __builtin_amdgcn_rcpf(now);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) m2 += v[i].y + w[i] * per * ((v[i].x - s) * (v[i].x - s));
+      const float share = now * __builtin_amdgcn_rcpf(n + now), d = s - mean;
+      sq += m2 + d * (d * (n * share * per));
+      mean += d * share;
+      n += now;
     }
-    for (int m = gl >> 1; m; m >>= 1) {
-      sum += __shfl_xor(sum, m);
-      sq += __shfl_xor(sq, m);
-    }
-    const float mean = pivot + sum / total;
-    const float var = squares_around_mean(sum, sq, total) / total;
+    float all = n * mean;
+    for (int m = gl >> 1; m; m >>= 1) all += __shfl_xor(all, m);
+    all /= (float)a.hw;
+    sq += n * per * ((mean - all) * (mean - all));
+    for (int m = gl >> 1; m; m >>= 1) sq += __shfl_xor(sq, m);
     if (l == 0) {
-      const float2 st = make_float2(mean, 1.f / sqrtf(var + a.eps));
+      const float2 st = make_float2(all, 1.f / sqrtf(sq / total + a.eps));
       lds[g] = st;
       if (q.chunk == 0) ((float2*)a.stats_out)[(size_t)q.img * a.groups + q.c0 / a.d + g] = st;
     }

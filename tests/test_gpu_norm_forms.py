@@ -105,6 +105,9 @@ LONG = [
     ("NCHW", BF16, (64, 128, 64, 128, 2), "norm_sums_nchw", "norm_sums_nchw"),
     ("NHWC", F32, (32, 16400, 12, 12, 1), "norm_sums_nhwc", "norm_sums_nhwc"),
     ("NHWC", F32, (64, 128, 64, 64, 4), "norm_run_nhwc", "norm_run_grad_nhwc"),
+    ("NCHW", F32, (16, 1000, 64, 64, 1), "norm_sums_nchw", "norm_sums_nchw"),  # 1000 entries
+    ("NHWC", BF16, (1, 128, 512, 512, 32), "norm_run_nhwc", "norm_run_grad_nhwc"),  # 128 runs
+    ("NHWC", F32, (1, 2, 2048, 2048, 1), "norm_run_nhwc", "norm_run_grad_nhwc"),  # 512 runs
 ]
 
 
@@ -135,3 +138,18 @@ def test_an_outlier_where_runs_begin(form):
     mean, rstd = _statistics(form, x)
     assert (rstd <= DEPTH * U).all(), float(rstd.max()) / U
     assert (mean <= DEPTH * U * 1e4).all()
+
+
+@pytest.mark.parametrize("form", LONG + FORMS, ids=_ids)
+def test_a_first_run_far_from_the_others(form):
+    """The same where a whole channel, or the first rows of each map, are 1e4 out."""
+    shape = form[2]
+    for where in ("channel", "rows"):
+        x = _normal(shape, form[1], 5)
+        if where == "channel":
+            x[:, ::shape[1] // shape[4]] += 1e4
+        else:
+            x[:, :, :max(1, shape[2] // 64)] += 1e4
+        mean, rstd = _statistics(form, x)
+        assert (rstd <= DEPTH * U).all(), (where, float(rstd.max()) / U)
+        assert (mean <= DEPTH * U * 1e4).all(), where
