@@ -14,8 +14,8 @@ namespace {
 // Where a workgroup of 256 works in NHWC: image, run of pixels, and its threads
 // as rows of 2^lanes_log2 lanes side by side on a pixel's channels.
 struct PlaceNhwc {
-  int img, chunk, p0, p1, row, rows, ch;
-  size_t at;  // element of (img, pixel 0, ch)
+  int img, chunk, len, row, rows, ch;  // len: pixels of the run
+  size_t at;                           // element of (img, the run's first pixel, ch)
 };
 template <int VW>
 __device__ __forceinline__ PlaceNhwc place_nhwc(const NormArgs& a) {
@@ -23,19 +23,19 @@ __device__ __forceinline__ PlaceNhwc place_nhwc(const NormArgs& a) {
   const int b = blockIdx.x, cb = b % a.cblocks, t = b / a.cblocks;
   q.chunk = t % a.chunks;
   q.img = t / a.chunks;
-  q.p0 = q.chunk * a.chunk_len;
-  q.p1 = min(a.hw, q.p0 + a.chunk_len);
+  const int p0 = q.chunk * a.chunk_len;
+  q.len = min(a.chunk_len, a.hw - p0);
   q.rows = 256 >> a.lanes_log2;
   q.row = threadIdx.x >> a.lanes_log2;
   q.ch = ((cb << a.lanes_log2) + (threadIdx.x & ((1 << a.lanes_log2) - 1))) * VW;
-  q.at = (size_t)q.img * a.hw * a.c + q.ch;
+  q.at = ((size_t)q.img * a.hw + p0) * a.c + q.ch;
   return q;
 }
 
 // The same in NCHW: rows of lanes side by side on the pixels of one plane's run.
 struct PlaceNchw {
-  long long plane;  // img * c + ch
-  int img, ch, chunk, p0, p1, lane, lanes;
+  size_t at;  // element of (img, ch, the run's first pixel)
+  int img, ch, chunk, len, lane, lanes;
   bool in;
 };
 __device__ __forceinline__ PlaceNchw place_nchw(const NormArgs& a) {
@@ -43,12 +43,13 @@ __device__ __forceinline__ PlaceNchw place_nchw(const NormArgs& a) {
   const long long unit =
       (long long)blockIdx.x * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
   q.in = unit < (long long)a.n * a.c * a.chunks;
-  q.plane = q.in ? unit / a.chunks : 0;
+  const long long plane = q.in ? unit / a.chunks : 0;  // img * c + ch
   q.chunk = q.in ? (int)(unit % a.chunks) : 0;
-  q.img = (int)(q.plane / a.c);
-  q.ch = (int)(q.plane % a.c);
-  q.p0 = q.chunk * a.chunk_len;
-  q.p1 = q.in ? min(a.hw, q.p0 + a.chunk_len) : q.p0;
+  q.img = (int)(plane / a.c);
+  q.ch = (int)(plane % a.c);
+  const int p0 = q.chunk * a.chunk_len;
+  q.len = q.in ? min(a.chunk_len, a.hw - p0) : 0;
+  q.at = (size_t)plane * a.hw + p0;
   q.lanes = 1 << a.lanes_log2;
   q.lane = threadIdx.x & (q.lanes - 1);
   return q;
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
       for (int e = 0; e < VW; ++e) k[e] = channel(a, a.stats, q.img, q.ch + e);
       by_act(a.act, [&](auto act) {
 #pragma unroll 4
-        for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
+        for (int p = q.row; p < q.len; p += q.rows) {
           float f[VW], g[VW];
           unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
           unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
@@ -112,13 +113,13 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
       s2[e] = lanes_sum(s2[e], lanes);
     }
   } else {
-    const int mine = (q.p1 - q.p0 - q.row + q.rows - 1) >> (8 - a.lanes_log2);
+    const int mine = (q.len - q.row + q.rows - 1) >> (8 - a.lanes_log2);
     for (int i = 0; in && i < mine; i += kBatch<VW>) {
       Pack<T, VW> f[kBatch<VW>];
 #pragma unroll
       for (int k = 0; k < kBatch<VW>; ++k)
         if (i + k < mine)
-          f[k] = load_pack<T, VW>(x + (size_t)(q.p0 + q.row + (i + k) * q.rows) * a.c);
+          f[k] = load_pack<T, VW>(x + (size_t)(q.row + (i + k) * q.rows) * a.c);
       float mean[VW], m2[VW];
       own_stats<T, VW, kBatch<VW>, true>(f, min(kBatch<VW>, mine - i), mean, m2);
       join_batch<VW, true>(i, min(kBatch<VW>, mine - i), mean, m2, s1, s2);
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
       } else {
 #pragma unroll
         for (int w = 0; w < 4; ++w) s.x += pixels[w] * lds[w][lane * VW + e].x;
-        s.x /= (float)(q.p1 - q.p0);
+        s.x /= (float)q.len;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const float2 v = lds[w][lane * VW + e];
@@ -164,46 +165,55 @@ template <typename T, int VW, bool GRAD>
 __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
   const PlaceNchw q = place_nchw(a);
   if (!q.in) return;  // whole rows of lanes: the sums below stay in one
-  const T* x = (const T*)a.x + (size_t)q.plane * a.hw;
-  const T* dy = (const T*)a.dy + (size_t)q.plane * a.hw;
+  const T* x = (const T*)a.x + q.at;
+  const T* dy = (const T*)a.dy + q.at;
   const auto row_sum = [&](float v) {
     for (int m = q.lanes >> 1; m; m >>= 1) v += __shfl_xor(v, m);
     return v;
   };
+  const int vecs = q.len / VW, mine = (vecs - q.lane + q.lanes - 1) >> a.lanes_log2;
+  const auto load = [&](const T* from, int i, Pack<T, VW>(&f)[kBatch<VW>]) {
+#pragma unroll
+    for (int k = 0; k < kBatch<VW>; ++k)
+      if (i + k < mine) f[k] = load_pack<T, VW>(from + (q.lane + (i + k) * q.lanes) * VW);
+  };
   float2 part;
   if constexpr (GRAD) {
-    const Channel k = channel(a, a.stats, q.img, q.ch);
+    const Channel c = channel(a, a.stats, q.img, q.ch);
     float s1 = 0.f, s2 = 0.f;
     by_act(a.act, [&](auto act) {
-#pragma unroll 4
-      for (int p = q.p0 + q.lane * VW; p < q.p1; p += q.lanes * VW) {
-        float f[VW], g[VW];
-        unpack<T, VW>(load_pack<T, VW>(x + p), f);
-        unpack<T, VW>(load_pack<T, VW>(dy + p), g);
+      for (int i = 0; i < mine; i += kBatch<VW>) {
+        Pack<T, VW> f[kBatch<VW>], g[kBatch<VW>];
+        load(x, i, f);
+        load(dy, i, g);
 #pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const float xh = (f[e] - k.mean) * k.rstd;
-          const float dz = norm_act_grad<act.value>(g[e], norm_z(xh, k.gamma, k.beta));
-          s1 += dz;
-          s2 += dz * xh;
+        for (int k = 0; k < kBatch<VW>; ++k) {
+          if (i + k >= mine) break;
+          float v[VW], w[VW];
+          unpack<T, VW>(f[k], v);
+          unpack<T, VW>(g[k], w);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            const float xh = (v[e] - c.mean) * c.rstd;
+            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, c.gamma, c.beta));
+            s1 += dz;
+            s2 += dz * xh;
+          }
         }
       }
     });
     part = make_float2(row_sum(s1), row_sum(s2));
   } else {
-    const int vecs = (q.p1 - q.p0) / VW, mine = (vecs - q.lane + q.lanes - 1) >> a.lanes_log2;
     float s[VW], m2[VW];  // (the first of each)
     s[0] = m2[0] = 0.f;
     for (int i = 0; i < mine; i += kBatch<VW>) {
       Pack<T, VW> f[kBatch<VW>];
-#pragma unroll
-      for (int k = 0; k < kBatch<VW>; ++k)
-        if (i + k < mine) f[k] = load_pack<T, VW>(x + q.p0 + (q.lane + (i + k) * q.lanes) * VW);
+      load(x, i, f);
       float mean[VW], batch_m2[VW];
       own_stats<T, VW, kBatch<VW>, false>(f, min(kBatch<VW>, mine - i), mean, batch_m2);
       join_batch<VW, false>(i, min(kBatch<VW>, mine - i), mean, batch_m2, s, m2);
     }
-    join_lanes((float)(mine * VW), (float)(q.p1 - q.p0), s[0], m2[0], row_sum);
+    join_lanes((float)(mine * VW), (float)q.len, s[0], m2[0], row_sum);
     part = make_float2(s[0], m2[0]);
   }
   if (q.lane == 0) a.part[((size_t)q.img * a.chunks + q.chunk) * a.c + q.ch] = part;
@@ -279,7 +289,7 @@ __global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
     if (GRAD) coef[e] = a.coef[(size_t)q.img * a.groups + (q.ch + e) / a.d];
   }
   by_act(a.act, [&](auto act) {
-    for (int p = q.p0 + q.row; p < q.p1; p += q.rows) {
+    for (int p = q.row; p < q.len; p += q.rows) {
       float f[VW], g[VW];
       unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
       if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
@@ -310,8 +320,8 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a, int pa
   const int unit = blockIdx.x % parts * (256 >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
   const bool in = unit < a.d * a.chunks;
   const int ch = c0 + (in ? unit / a.chunks : 0), first = in ? unit % a.chunks * a.chunk_len : 0;
-  const int end = in ? min(a.hw, first + a.chunk_len) : 0, step = lanes * VW;
-  const size_t at = ((size_t)img * a.c + ch) * a.hw;
+  const int end = in ? min(a.chunk_len, a.hw - first) : 0, step = lanes * VW;
+  const size_t at = ((size_t)img * a.c + ch) * a.hw + first;
   const T* x = (const T*)a.x + at;
   const T* dy = (const T*)a.dy + at;
   T* out = (T*)a.out + at;
@@ -325,7 +335,7 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a, int pa
       }
     }
   };
-  int p = first + lane * VW;
+  int p = lane * VW;
   load(p);  // in flight meanwhile
   float2 stats, coef = make_float2(0.f, 0.f);
   if constexpr (JOIN) {

@@ -156,7 +156,7 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const int most = slab_most(vec, grad, a->span != 0);
   const auto slots = [&](int lanes, int threads) {
     const int rows = threads / lanes;
-    return (a->hw + rows - 1) / rows;
+    return ((long long)a->hw + rows - 1) / rows;  // (hw may be 2^31 - 1)
   };
   const auto lanes_of = [&](int c) { return 1 << log2_ceil(c / vec); };
   const auto fits = [&](long long c) {
@@ -178,7 +178,7 @@ bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   slab_set(a, vec, grad, c, threads);
   if (!launchable(slabs, threads)) return false;
   a->slabs = (int)slabs;
-  a->slots = slots(lanes, threads);
+  a->slots = (int)slots(lanes, threads);
   a->chunks = 1;
   a->chunk_len = a->hw;
   return true;
@@ -204,7 +204,7 @@ bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const auto units_of = [&](int c) { return (long long)a->n * ((a->c + c - 1) / c); };
   const auto most_chunks = [&](int c) {
     const long long rows = threads_of(c) / lanes_of(c), units = units_of(c);
-    const long long most = grad ? std::max((a->hw + 31) / 32ll, 256 / units) : 1 << 20;
+    const long long most = grad ? std::max((a->hw + 31ll) / 32, 256 / units) : 1 << 20;
     return std::min({std::max(64ll, (512 + units - 1) / units), most,
                      (a->hw + 4 * rows - 1) / (4 * rows)});
   };
@@ -217,7 +217,7 @@ bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const long long units = units_of(c), waves = units * (a->threads / 64);
   const long long chunks = std::min(((grad ? 4096 : 8192) + waves - 1) / waves, most_chunks(c));
   a->chunk_len = (int)((a->hw + chunks - 1) / chunks);
-  a->chunks = (a->hw + a->chunk_len - 1) / a->chunk_len;
+  a->chunks = (int)(((long long)a->hw + a->chunk_len - 1) / a->chunk_len);
   if (!launchable(units * a->chunks + a->c, a->threads)) return false;
   a->slabs = (int)(units * a->chunks);
   a->slots = 0;
@@ -229,7 +229,7 @@ bool run_nhwc(NormArgs* a, int esz, int vec, bool grad) {
 // them: 57x2 pixels, 50 channels a group, 640 groups, gradient: 21.5 -> 19 us).
 bool slab_nchw(NormArgs* a, int vec, bool grad) {
   const int vecs = a->hw / vec, lanes = 1 << std::min(6, log2_ceil(vecs));
-  const int along = (vecs + lanes - 1) / lanes, most = slab_most(vec, grad, false);
+  const int along = (int)(((long long)vecs + lanes - 1) / lanes), most = slab_most(vec, grad, false);
   if (along > most) return false;
   int threads = 64;
   const auto slots = [&] {

@@ -153,3 +153,46 @@ def test_a_first_run_far_from_the_others(form):
         mean, rstd = _statistics(form, x)
         assert (rstd <= DEPTH * U).all(), (where, float(rstd.max()) / U)
         assert (mean <= DEPTH * U * 1e4).all(), where
+
+
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+def test_a_map_of_almost_2_to_the_31(layout):
+    """Every pixel of the largest map is read and written: one channel, bf16.  Sums have chains
+    of up to 2^16 additions (the runs of a channel, 16 side by side)."""
+    hw, part, chain = 2 ** 31 - 2, 1 << 26, 1 << 16
+    shape = (1, hw, 1, 1) if layout == "NHWC" else (1, 1, hw, 1)
+    gn = tr.GroupNorm(shape, 1, BF16, layout)
+    print("norm", shape, layout, gn.kernels, flush=True)
+    g = torch.Generator(DEV).manual_seed(7)
+    x, dy, y = (torch.empty(hw, dtype=BF16, device=DEV) for _ in range(3))
+    for first in range(0, hw, part):
+        for t in (x, dy):
+            t[first:first + part].normal_(0.5, 1.0, generator=g)
+    stats = gn.new_stats()
+    y.fill_(float("nan"))
+    gn(x.view(shape), out=y.view(shape), stats=stats)
+    parts = [slice(first, min(hw, first + part)) for first in range(0, hw, part)]
+    mean = sum(float(x[p].double().sum()) for p in parts) / hw
+    var = sum(float((x[p].double() - mean).square().sum()) for p in parts) / hw
+    st = stats.double().flatten().tolist()
+    assert abs(st[0] - mean) <= chain * U * 2 and abs(st[1] * (var + 1e-5) ** 0.5 - 1) <= chain * U
+    # from the kernels' statistics: three roundings and bf16's, whose unit is 2^-8
+    sums = torch.zeros(4, dtype=torch.float64, device=DEV)
+    for p in parts:
+        xh = (x[p].double() - st[0]) * st[1]
+        assert ((y[p].double() - xh).abs() <= xh.abs() * (2.0 ** -8 + 4 * U) + 1e-6).all(), p
+        d = dy[p].double()
+        sums += torch.stack((d.sum(), (d * xh).sum(), d.abs().sum(), (d * xh).abs().sum()))
+    y.fill_(float("nan"))
+    _, dgamma, dbeta = gn.grad(x.view(shape), dy.view(shape), stats, out=y.view(shape))
+    db, dg, db_mag, dg_mag = sums.tolist()
+    assert abs(float(dbeta) - db) <= chain * U * db_mag
+    assert abs(float(dgamma) - dg) <= chain * U * dg_mag
+    # the two means are off by chain u of their magnitudes' means
+    off = chain * U * (db_mag / hw)
+    off_xh = chain * U * (dg_mag / hw)
+    for p in parts:
+        xh = (x[p].double() - st[0]) * st[1]
+        dx = st[1] * (dy[p].double() - db / hw - xh * (dg / hw))
+        tol = st[1] * (off + xh.abs() * off_xh) + dx.abs() * 2.0 ** -8 + 8 * U * (1 + xh.abs())
+        assert ((y[p].double() - dx).abs() <= tol * (1 + 2.0 ** -7)).all(), p

@@ -1,0 +1,86 @@
+"""What the group norm's plans choose, on the CPU: the library in a process of its own whose
+allocations are replaced (allocations.c)."""
+import json
+import os
+import re
+import subprocess
+import sys
+
+import pytest
+
+h2 = pytest.importorskip("paper_1907_11210_amd.huge2")
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+PLAN = """
+import ctypes, json, sys
+ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
+from paper_1907_11210_amd import huge2 as h2, train as tr
+names = []
+for n, c, h, w, groups, layout, dtype in json.load(sys.stdin):
+    desc = tr.NormDesc(n, c, h, w, groups, layout, dtype, 0, 1e-5)
+    plan = tr.huge2_norm_plan_create(desc)
+    names.append([tr.huge2_norm_plan_kernel(plan, grad) for grad in (False, True)])
+    tr.huge2_norm_plan_destroy(plan)
+json.dump(names, sys.stdout)
+"""
+
+
+@pytest.fixture(scope="module")
+def kernels(tmp_path_factory):
+    """Names of the kernels, forward and gradient, for shapes (n, c, h, w, groups, layout, type)."""
+    if not os.path.exists(h2.LIB_PATH):
+        from paper_1907_11210_amd import _build
+        _build.build()
+    lib = str(tmp_path_factory.mktemp("plan") / "allocations.so")
+    subprocess.run(["gcc", "-shared", "-fPIC", "-o", lib, os.path.join(HERE, "allocations.c")],
+                   check=True)
+
+    def plans(shapes):
+        run = subprocess.run([sys.executable, "-c", PLAN, lib], input=json.dumps(shapes), text=True,
+                             capture_output=True, cwd=os.path.dirname(HERE), timeout=120)
+        assert run.returncode == 0, run.stderr
+        return json.loads(run.stdout)
+    return plans
+
+
+def _parse(name):
+    """Kernel, and its numbers by their letters."""
+    kernel, *fields = name.split()
+    return kernel, {f[0]: int(f[1:]) for f in fields}
+
+
+@pytest.mark.parametrize("layout", [h2.HUGE2_NHWC, h2.HUGE2_NCHW], ids=["nhwc", "nchw"])
+@pytest.mark.parametrize("dtype", [h2.HUGE2_F32, h2.HUGE2_BF16], ids=["f32", "bf16"])
+def test_maps_of_almost_2_to_the_31(kernels, layout, dtype):
+    """No rounding up of a map's pixels passes 32 bits: such a map is cut into runs."""
+    sides = [(1, 1, 2 ** 31 - k) for k in (1, 2, 4, 8, 64, 512, 1022, 1024, 1025)]
+    sides += [(1, 2 ** 31 - 1, 1), (2, 1, 2 ** 30 - 1), (8, 16384, 16383)]
+    shapes = [(1, c, h, w, 1, layout, dtype) for c, h, w in sides]
+    for shape, names in zip(shapes, kernels(shapes)):
+        for name in names:
+            kernel, number = _parse(name)
+            assert kernel.startswith(("norm_run", "norm_sums")), (shape, name)
+            assert 64 <= number["k"] < 2 ** 31, (shape, name)
+
+
+def test_slabs_hold_their_maps(kernels):
+    """A slab's threads and their vectors cover a group's pixels, at most 16 vectors each."""
+    shapes = [(n, c, h, w, g, layout, dtype)
+              for n, c, h, w, g in ((1, 1, 1, 1, 1), (3, 24, 6, 6, 6), (64, 256, 16, 16, 32),
+                                    (64, 64, 64, 64, 16), (2, 32, 16, 16, 4), (1, 512, 8, 8, 32),
+                                    (300, 200, 11, 9, 8), (1, 1, 1, 16384, 1), (9, 8, 1, 1025, 4))
+              for layout in (h2.HUGE2_NHWC, h2.HUGE2_NCHW)
+              for dtype in (h2.HUGE2_F32, h2.HUGE2_BF16)]
+    slabs = 0
+    for shape, names in zip(shapes, kernels(shapes)):
+        for name in names:
+            kernel, number = _parse(name)
+            if not re.match("norm_slab", kernel):
+                continue
+            slabs += 1
+            _, c, h, w, g, layout, _ = shape
+            assert 1 <= number["r"] <= 16 and 64 <= number["t"] <= 1024, (shape, name)
+            held = number["v"] * number["t"] * number["r"]
+            assert held >= h * w * (c // g), (shape, name)
+    assert slabs >= 40
