@@ -28,12 +28,23 @@ EXPORTED = (
 )
 
 
-class NormDesc(ctypes.Structure):
+class _Desc(ctypes.Structure):
+    """A descriptor whose whole numbers fit their fields (ctypes itself keeps the low bits)."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        given = dict(zip((f for f, _ in self._fields_), args), **kw)
+        for name, kind in self._fields_:
+            if kind is ctypes.c_int32 and getattr(self, name) != given.get(name, 0):
+                raise ValueError("%s is %s, which 32 bits do not hold" % (name, given[name]))
+
+
+class NormDesc(_Desc):
     _fields_ = [(f, ctypes.c_int32) for f in ("n", "c", "h", "w", "groups", "layout", "dtype",
                                               "activation")] + [("eps", ctypes.c_float)]
 
 
-class EmbeddingDesc(ctypes.Structure):
+class EmbeddingDesc(_Desc):
     _fields_ = [(f, ctypes.c_int32) for f in ("rows", "dim", "dtype", "id_bits")] + \
         [("scale", ctypes.c_float)]
 

@@ -1,5 +1,5 @@
-"""What the group norm's plans choose, on the CPU: the library in a process of its own whose
-allocations are replaced (allocations.c)."""
+"""Descriptors of the training operators, and what the group norm's plans choose, on the CPU:
+the library in a process of its own whose allocations are replaced (allocations.c)."""
 import json
 import os
 import re
@@ -84,3 +84,20 @@ def test_slabs_hold_their_maps(kernels):
             held = number["v"] * number["t"] * number["r"]
             assert held >= h * w * (c // g), (shape, name)
     assert slabs >= 40
+
+
+def test_sizes_that_32_bits_do_not_hold():
+    """They are refused, not cut to their low bits: a table of 2^32 + 8 rows is none of 8."""
+    from paper_1907_11210_amd import train as tr
+    norm = dict(n=2, c=12, h=5, w=7, groups=4, layout=h2.HUGE2_NHWC, dtype=h2.HUGE2_F32,
+                activation=0, eps=1e-5)
+    assert tr.NormDesc(**norm).w == 7 and tr.NormDesc(2, 12, -1).h == -1
+    for field in ("n", "c", "h", "w", "groups"):
+        for value in (2 ** 32 + norm[field], 2 ** 31, -2 ** 31 - 1):
+            with pytest.raises(ValueError, match=field):
+                tr.NormDesc(**{**norm, field: value})
+    with pytest.raises(ValueError, match="n is"):
+        tr.NormDesc(2 ** 32 + 2, 12, 5, 7, 4, h2.HUGE2_NHWC, h2.HUGE2_F32, 0, 1e-5)
+    for rows, dim in ((2 ** 32 + 8, 16), (8, 2 ** 32 + 16)):
+        with pytest.raises(ValueError):
+            tr.EmbeddingDesc(rows, dim, h2.HUGE2_BF16, 64, 1.0)
