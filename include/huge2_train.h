@@ -67,8 +67,8 @@ huge2_status huge2_norm_plan_create(huge2_norm_plan** out, const huge2_norm_desc
 
 /* Enqueues y from x.  gamma and beta are [c] float; NULL gamma is all ones,
  * NULL beta all zeros.  stats is NULL or [n][groups][2] float and then receives
- * (mean, rstd), which huge2_norm_grad_execute reads.  y must not alias x.
- * Errors: INVALID_ARG, HIP. */
+ * (mean, rstd), which huge2_norm_grad_execute reads.  y and stats must not overlap
+ * each other or an input.  Errors: INVALID_ARG, HIP. */
 huge2_status huge2_norm_execute(const huge2_norm_plan* plan, const void* x, const float* gamma,
                                 const float* beta, void* y, float* stats, void* hip_stream);
 
@@ -79,7 +79,8 @@ huge2_status huge2_norm_execute(const huge2_norm_plan* plan, const void* x, cons
  *   dx = rstd * (t - mean over the group of t - xh * mean over the group of t*xh).
  * A ReLU's z is formed with the forward's own roundings, so that it masks the same
  * values both ways (its slope at 0 is 0).  dgamma and dbeta are [c] float and
- * may be NULL.  dx must not alias x or dy.  Errors: INVALID_ARG, HIP. */
+ * may be NULL.  dx, dgamma and dbeta must not overlap each other or an input.
+ * Errors: INVALID_ARG, HIP. */
 huge2_status huge2_norm_grad_execute(const huge2_norm_plan* plan, const void* x, const void* dy,
                                      const float* stats, const float* gamma, const float* beta,
                                      void* dx, float* dgamma, float* dbeta, void* hip_stream);
@@ -164,7 +165,8 @@ typedef struct {
 
 typedef struct huge2_adamw_plan huge2_adamw_plan;
 
-/* A plan for `count` tensors (>= 0), which must outlive it.  Allocates their
+/* A plan for `count` tensors (>= 0), which must outlive it.  No two of their arrays
+ * may overlap: a parameter that two layers share is listed once.  Allocates their
  * table and the list of work, copies both on hip_stream and waits for it.
  * Errors: INVALID_ARG, UNSUPPORTED (2^40 elements in all, or more), ALLOC, HIP. */
 huge2_status huge2_adamw_plan_create(huge2_adamw_plan** out, const huge2_adamw_tensor* tensors,
@@ -181,8 +183,8 @@ typedef struct {
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^step)
  *           * m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
  * in fp32, from the new m and v before they are rounded to 8 bits.  grads is a
- * host array of `count` device pointers in the plan's order; a tensor whose
- * gradient is NULL is left as it is.  Errors: INVALID_ARG, HIP. */
+ * host array of `count` device pointers in the plan's order, none into an array that the
+ * step writes; a tensor whose gradient is NULL is left as it is.  Errors: INVALID_ARG, HIP. */
 huge2_status huge2_adamw_step(const huge2_adamw_plan* plan, const void* const* grads,
                               const huge2_adamw_options* options, const float* grad_scale,
                               void* hip_stream);

@@ -1,5 +1,6 @@
-/* The device's allocation calls without a device: a plan can then be made on the CPU, to see
- * what it chose.  Nothing may be enqueued on it. */
+/* The calls that make a plan (allocations, and the copy of a list into one) without a device:
+ * a plan can then be made on the CPU, to see what it chose and refuses.  Nothing may be
+ * enqueued on it. */
 #include <stddef.h>
 #include <stdint.h>
 
@@ -10,5 +11,13 @@ int hipMalloc(void** p, size_t bytes) {
 }
 int hipFree(void* p) {
   (void)p;
+  return 0;
+}
+int hipMemcpyAsync(void* to, const void* from, size_t bytes, int kind, void* stream) {
+  (void)to, (void)from, (void)bytes, (void)kind, (void)stream;
+  return 0;
+}
+int hipStreamSynchronize(void* stream) {
+  (void)stream;
   return 0;
 }
