@@ -62,7 +62,8 @@ constexpr int kBatch = VW >= 4 ? 4 : 8;
 // Joins what the lanes hold (a mean of `own` values and the squares around it), `count`
 // values in all, in each of them; sum: over those lanes.
 template <typename F>
-__device__ __forceinline__ void join_lanes(float own, float count, float& mean, float& m2, F&& sum) {
+__device__ __forceinline__ void join_lanes(float own, float count, float& mean, float& m2,
+                                           F&& sum) {
   const float all = sum(own * mean) / fmaxf(count, 1.f);
   m2 = sum(m2 + own * ((mean - all) * (mean - all)));
   mean = all;
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(256) void norm_sums_nhwc_kernel(NormArgs a) {
 #pragma unroll
           for (int e = 0; e < VW; ++e) {
             const float xh = (f[e] - k[e].mean) * k[e].rstd;
-            const float dz = norm_act_grad<act.value>(g[e], norm_z(xh, k[e].gamma, k[e].beta));
+            const float dz = norm_act_grad<act.value, T>(g[e], norm_z(xh, k[e].gamma, k[e].beta));
             s1[e] += dz;
             s2[e] += dz * xh;
           }
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(256) void norm_sums_nchw_kernel(NormArgs a) {
 #pragma unroll
           for (int e = 0; e < VW; ++e) {
             const float xh = (v[e] - c.mean) * c.rstd;
-            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, c.gamma, c.beta));
+            const float dz = norm_act_grad<act.value, T>(w[e], norm_z(xh, c.gamma, c.beta));
             s1 += dz;
             s2 += dz * xh;
           }
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(256) void norm_apply_nhwc_kernel(NormArgs a) {
       unpack<T, VW>(load_pack<T, VW>(x + (size_t)p * a.c), f);
       if constexpr (GRAD) unpack<T, VW>(load_pack<T, VW>(dy + (size_t)p * a.c), g);
 #pragma unroll
-      for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD, act.value>(f[e], g[e], k[e], coef[e]);
+      for (int e = 0; e < VW; ++e) f[e] = norm_value<GRAD, act.value, T>(f[e], g[e], k[e], coef[e]);
       store_pack<T, VW>(out + (size_t)p * a.c, pack<T, VW>(f), a.stream);
     }
   });
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(256) void norm_apply_nchw_kernel(NormArgs a, int pa
           unpack<T, VW>(f[j], v);
           if constexpr (GRAD) unpack<T, VW>(g[j], w);
 #pragma unroll
-          for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD, act.value>(v[e], w[e], k, coef);
+          for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD, act.value, T>(v[e], w[e], k, coef);
           store_pack<T, VW>(out + p + j * step, pack<T, VW>(v), a.stream);
         }
       }

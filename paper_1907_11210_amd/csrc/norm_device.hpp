@@ -30,20 +30,27 @@ __device__ __forceinline__ void by_act(int act, F&& f) {
   }
 }
 
-// On the hardware's exponential and reciprocal, each within 1 unit in the last
-// place: with them the activations stay below the memory's time (with the library's
+// For bf16 tensors on the hardware's exponential and reciprocal, each within 1 unit in the
+// last place: with them the activations stay below the memory's time (with the library's
 // expf and a division the gradient of SiLU took 1.8 times as long).  The exponent's
 // rounding makes exp(z) off by |z| 2^-24 of itself, which 1 / (1 + exp(-z)) keeps
-// only where it is itself small.
-__device__ __forceinline__ float fast_exp(float z) {
-  return __builtin_amdgcn_exp2f(z * 1.44269504088896341f);
-}
+// only where it is itself small.  fp32 results would show these errors (tanh 10 units of 2^-24
+// of the value, SiLU 16): there the library's functions and a division (64 images of 128x32x32
+// in NCHW: tanh 15.4 -> 17.6 us, its gradient 28.1 -> 30.6, SiLU 14.2 -> 17.7 and 26.0 -> 31.3).
+template <typename T>
+constexpr bool kFastAct = sizeof(T) == 2;
+template <typename T>
 __device__ __forceinline__ float sigmoid(float z) {
-  return __builtin_amdgcn_rcpf(1.f + fast_exp(-z));
+  if constexpr (kFastAct<T>)
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
+  else
+    return 1.f / (1.f + expf(-z));
 }
 // 1 - 2 / (exp(2z) + 1), and its series near 0, where that cancels: the term left out
 // is 62/2835 z^8 of the value, 6e-8 at 0.2.
-__device__ __forceinline__ float fast_tanh(float z) {
+template <typename T>
+__device__ __forceinline__ float tanh_of(float z) {
+  if constexpr (!kFastAct<T>) return tanhf(z);
   const float far =
       1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * 2.88539008177792681f) + 1.f);
   const float q = z * z;
@@ -51,23 +58,24 @@ __device__ __forceinline__ float fast_tanh(float z) {
   return fabsf(z) < 0.2f ? near : far;
 }
 
-template <int ACT>
+template <int ACT, typename T>
 __device__ __forceinline__ float norm_act(float z) {
   if constexpr (ACT == HUGE2_NORM_RELU) return z < 0.f ? 0.f : z;
-  if constexpr (ACT == HUGE2_NORM_TANH) return fast_tanh(z);
-  if constexpr (ACT == HUGE2_NORM_SILU) return z * sigmoid(z);
+  if constexpr (ACT == HUGE2_NORM_TANH) return tanh_of<T>(z);
+  if constexpr (ACT == HUGE2_NORM_SILU)
+    return kFastAct<T> ? z * sigmoid<T>(z) : z / (1.f + expf(-z));
   return z;
 }
 // dy * activation'(z)
-template <int ACT>
+template <int ACT, typename T>
 __device__ __forceinline__ float norm_act_grad(float dy, float z) {
   if constexpr (ACT == HUGE2_NORM_RELU) return z > 0.f ? dy : 0.f;
   if constexpr (ACT == HUGE2_NORM_TANH) {
-    const float th = fast_tanh(z);
+    const float th = tanh_of<T>(z);
     return dy * (1.f - th * th);
   }
   if constexpr (ACT == HUGE2_NORM_SILU) {
-    const float s = sigmoid(z);
+    const float s = sigmoid<T>(z);
     return dy * (s * (1.f + z * (1.f - s)));
   }
   return dy;
@@ -181,17 +189,17 @@ __device__ __forceinline__ void channel_params(const NormArgs& a, int ch, Channe
 }
 
 // y, or dx, of one value.
-template <bool GRAD, int ACT>
+template <bool GRAD, int ACT, typename T>
 __device__ __forceinline__ float norm_value(float x, float dy, const Channel& k, float2 coef) {
   // (A smooth activation is bound by its operations and has no mask to keep: fewer of them.
   // 4002x5 pixels of 1280 bf16: tanh 31.8 -> 28.6 us, SiLU 23.0 -> 21.5.)
   constexpr bool kSmooth = ACT == HUGE2_NORM_TANH || ACT == HUGE2_NORM_SILU;
   if constexpr (!GRAD && kSmooth)
-    return norm_act<ACT>(fmaf(x - k.mean, k.rstd * k.gamma, k.beta));
+    return norm_act<ACT, T>(fmaf(x - k.mean, k.rstd * k.gamma, k.beta));
   const float xh = (x - k.mean) * k.rstd;
   const float z = kSmooth ? fmaf(xh, k.gamma, k.beta) : norm_z(xh, k.gamma, k.beta);
-  if constexpr (!GRAD) return norm_act<ACT>(z);
-  const float t = norm_act_grad<ACT>(dy, z) * k.gamma;
+  if constexpr (!GRAD) return norm_act<ACT, T>(z);
+  const float t = norm_act_grad<ACT, T>(dy, z) * k.gamma;
   return k.rstd * (t - coef.x - xh * coef.y);
 }
 

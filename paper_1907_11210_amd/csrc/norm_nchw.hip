@@ -43,7 +43,7 @@ __device__ __forceinline__ void direct_params(const NormArgs& a, int block) {
 #pragma unroll
           for (int e = 0; e < VW; ++e) {
             const float xh = (v[e] - st[j].x) * st[j].y;
-            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, gamma, beta));
+            const float dz = norm_act_grad<act.value, T>(w[e], norm_z(xh, gamma, beta));
             s1 += dz;
             s2 += dz * xh;
           }
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(1024) void norm_slab_nchw_kernel(NormArgs a) {
 #pragma unroll
           for (int e = 0; e < VW; ++e) {
             const float xh = (v[e] - stats.x) * stats.y;
-            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, gamma, beta));
+            const float dz = norm_act_grad<act.value, T>(w[e], norm_z(xh, gamma, beta));
             s1 += dz;
             s2 += dz * xh;
           }
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(1024) void norm_slab_nchw_kernel(NormArgs a) {
         unpack<T, VW>(f[k], v);
         if constexpr (GRAD) unpack<T, VW>(g[k], w);
 #pragma unroll
-        for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD, act.value>(v[e], w[e], c, coef);
+        for (int e = 0; e < VW; ++e) v[e] = norm_value<GRAD, act.value, T>(v[e], w[e], c, coef);
         store_pack<T, VW>(out + place[k], pack<T, VW>(v), a.stream);
       }
       if (GRAD) __builtin_amdgcn_sched_barrier(0);

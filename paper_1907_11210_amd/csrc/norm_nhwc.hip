@@ -113,7 +113,7 @@ __device__ __forceinline__ void write_rows(const NormArgs& a, const Slab& q, T* 
       unpack<T, VW>(f[i], v);
 #pragma unroll
       for (int e = 0; e < VW; ++e)
-        v[e] = norm_value<false, ACT>(v[e], 0.f, k[e], make_float2(0.f, 0.f));
+        v[e] = norm_value<false, ACT, T>(v[e], 0.f, k[e], make_float2(0.f, 0.f));
       store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v),
                         a.stream);
     }
@@ -136,7 +136,7 @@ __device__ __forceinline__ void add_grad_sums(const NormArgs& a, int first, int 
 #pragma unroll
       for (int e = 0; e < VW; ++e) {
         const float xh = (v[e] - k[e].mean) * k[e].rstd;
-        const float dz = norm_act_grad<ACT>(w[e], norm_z(xh, k[e].gamma, k[e].beta));
+        const float dz = norm_act_grad<ACT, T>(w[e], norm_z(xh, k[e].gamma, k[e].beta));
         s1[e] += dz;
         s2[e] += dz * xh;
       }
@@ -270,7 +270,7 @@ __device__ __forceinline__ void write_grad_rows(const NormArgs& a, const Slab& q
       unpack<T, VW>(f[i], v);
       unpack<T, VW>(g[i], w);
 #pragma unroll
-      for (int e = 0; e < VW; ++e) v[e] = norm_value<true, ACT>(v[e], w[e], k[e], coef[e]);
+      for (int e = 0; e < VW; ++e) v[e] = norm_value<true, ACT, T>(v[e], w[e], k[e], coef[e]);
       store_pack<T, VW>(out + (size_t)(q.row + (first + i) * q.rows) * a.c, pack<T, VW>(v),
                         a.stream);
     }
@@ -323,7 +323,7 @@ __device__ __forceinline__ void direct_params(const NormArgs& a, int block, floa
           for (int e = 0; e < VW; ++e) {
             const float2 s = st[j][SPAN ? e : 0];
             const float xh = (v[e] - s.x) * s.y;
-            const float dz = norm_act_grad<act.value>(w[e], norm_z(xh, k[e].gamma, k[e].beta));
+            const float dz = norm_act_grad<act.value, T>(w[e], norm_z(xh, k[e].gamma, k[e].beta));
             s1[e] += dz;
             s2[e] += dz * xh;
           }

@@ -196,3 +196,37 @@ def test_a_map_of_almost_2_to_the_31(layout):
         dx = st[1] * (dy[p].double() - db / hw - xh * (dg / hw))
         tol = st[1] * (off + xh.abs() * off_xh) + dx.abs() * 2.0 ** -8 + 8 * U * (1 + xh.abs())
         assert ((y[p].double() - dx).abs() <= tol * (1 + 2.0 ** -7)).all(), p
+
+
+@pytest.mark.parametrize("layout", ["NHWC", "NCHW"])
+@pytest.mark.parametrize("act", ["tanh", "silu"])
+def test_fp32_activations(act, layout):
+    """All x are zeros, so that z is beta, and one pixel, so that dbeta is dy's product with the
+    slope: fp32 results are off by the activation's own roundings.  The device's tanh and
+    exponential are within 2 and 1 units in the last place, 4u and 2u at most of the value; SiLU
+    and its slope add a sum and a quotient, u each, and products of them."""
+    z = torch.cat((torch.linspace(-20, 20, 16001), torch.logspace(-6, 1, 8000),
+                   -torch.logspace(-6, 1, 8000))).to(DEV)
+    z = z[:z.numel() // 4 * 4]
+    c = z.numel()
+    shape = (1, 1, 1, c) if layout == "NHWC" else (1, c, 1, 1)
+    x = torch.zeros(shape, device=DEV)
+    gn = tr.GroupNorm(shape, 1, F32, layout, act)
+    stats = gn.new_stats()
+    y = gn(x, None, z, stats=stats).flatten().double()
+    dbeta = gn.grad(x, torch.ones_like(x), stats, None, z)[2].double()
+    z = z.double()
+    if act == "tanh":
+        want, slope = torch.tanh(z), 1 - torch.tanh(z) ** 2
+        tol, tol_slope = 4 * U * want.abs(), 10 * U * want ** 2 + 2 * U * slope
+    else:
+        s = torch.sigmoid(z)
+        want, slope = z * s, s * (1 + z * (1 - s))
+        tol = (2 * (1 - s) + 3) * U * want.abs()
+        # s is off by 2u (1 - s) + 2u of itself, 1 - s by that of s and u of itself
+        of_s = (2 * (1 - s) + 2) * U
+        tol_slope = slope.abs() * (of_s + 3 * U) + s * z.abs() * (s * of_s + (1 - s) * 3 * U)
+    print("norm", act, layout, "off by", float(((y - want).abs() / tol).nan_to_num().max()),
+          float(((dbeta - slope).abs() / tol_slope).nan_to_num().max()), "of the tolerance", flush=True)
+    assert ((y - want).abs() <= tol).all()
+    assert ((dbeta - slope).abs() <= tol_slope).all()
