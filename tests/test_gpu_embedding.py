@@ -208,3 +208,16 @@ def test_lookup_of_more_than_a_launch_takes():
     for first in range(0, tokens, 1 << 22):
         part = slice(first, min(tokens, first + (1 << 22)))
         assert torch.equal(y[part], padded[ids[part]]), first
+
+
+def test_embedding_kernels_and_raw_entry():
+    """Which kernels a gradient takes, and the lookup through its raw entry point."""
+    emb = tr.Embedding(100, 24, torch.float32, max_tokens=5000)
+    assert [emb.kernel(n) for n in (1024, 1025)] == ["embedding_few_kernel v4",
+                                                     "embedding_sum_kernel v4"]
+    ids = torch.arange(300, device=DEV) % 101
+    table = torch.randn(100, 24, device=DEV)
+    y = torch.empty(300, 24, device=DEV)
+    tr.huge2_embedding(emb.desc, ids.data_ptr(), 300, table.data_ptr(), y.data_ptr(),
+                       torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(y, emb(ids, table))

@@ -230,3 +230,45 @@ def test_fp32_activations(act, layout):
           float(((dbeta - slope).abs() / tol_slope).nan_to_num().max()), "of the tolerance", flush=True)
     assert ((y - want).abs() <= tol).all()
     assert ((dbeta - slope).abs() <= tol_slope).all()
+
+
+@pytest.mark.parametrize("form", FORMS, ids=_ids)
+def test_graph_replays_and_streams(form):
+    """The same bits in a graph's replays, on a side stream and through the raw entry points."""
+    layout, dtype, shape = form[:3]
+    gn = _norm(form, "relu")
+    x, dy, gamma, beta = _inputs(shape, dtype, 8)
+    xs, dys, ga, be = _lay(x, layout).to(DEV), _lay(dy, layout).to(DEV), gamma.to(DEV), beta.to(DEV)
+    out, st = torch.empty_like(xs), gn.new_stats()
+    gn(xs, ga, be, out=out, stats=st)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gn(xs, ga, be, out=out, stats=st)
+        grads = gn.grad(xs, dys, st, ga, be)
+    side = torch.cuda.Stream()
+    for seed in (9, 10, 11):
+        x2, dy2, _, _ = _inputs(shape, dtype, seed)
+        xs.copy_(_lay(x2, layout))
+        dys.copy_(_lay(dy2, layout))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, st, *grads)]
+        st2 = gn.new_stats()
+        want = [gn(xs, ga, be, stats=st2), st2, *gn.grad(xs, dys, st2, ga, be)]
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        st3 = gn.new_stats()
+        again = [gn(xs, ga, be, stats=st3), st3, *gn.grad(xs, dys, st3, ga, be)]
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(again, want))
+    raw = [torch.empty_like(t) for t in want]
+    y, st4, dx, dgamma, dbeta = (t.data_ptr() for t in raw)
+    plan = tr.huge2_norm_plan_create(gn.desc)
+    stream = torch.cuda.current_stream().cuda_stream
+    tr.huge2_norm_execute(plan, xs.data_ptr(), ga.data_ptr(), be.data_ptr(), y, st4, stream)
+    tr.huge2_norm_grad_execute(plan, xs.data_ptr(), dys.data_ptr(), st4, ga.data_ptr(),
+                               be.data_ptr(), dx, dgamma, dbeta, stream)
+    tr.huge2_norm_plan_destroy(plan)
+    assert all(torch.equal(a, b) for a, b in zip(raw, want))
