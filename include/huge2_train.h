@@ -18,7 +18,8 @@
  * results are deterministic (a fixed order of summation, no floating-point
  * atomics).  A plan's workspace is shared by the calls on it: enqueue them on
  * one stream, or order them.  The calls that run a plan allocate nothing and
- * can be recorded into a HIP graph.
+ * can be recorded into a HIP graph, whose replays repeat them as they were recorded:
+ * on the same pointers, and an AdamW step with its step number, rates and decays.
  */
 #ifndef HUGE2_TRAIN_H
 #define HUGE2_TRAIN_H
@@ -184,7 +185,10 @@ typedef struct {
  *           * m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
  * in fp32, from the new m and v before they are rounded to 8 bits.  grads is a
  * host array of `count` device pointers in the plan's order, none into an array that the
- * step writes; a tensor whose gradient is NULL is left as it is.  Errors: INVALID_ARG, HIP. */
+ * step writes; a tensor whose gradient is NULL is left as it is.  The options are taken on
+ * the host: a recorded step keeps the bias corrections of its `step` and its lr in every
+ * replay, so a training loop that replays a graph enqueues its step outside of it.
+ * Errors: INVALID_ARG, HIP. */
 huge2_status huge2_adamw_step(const huge2_adamw_plan* plan, const void* const* grads,
                               const huge2_adamw_options* options, const float* grad_scale,
                               void* hip_stream);

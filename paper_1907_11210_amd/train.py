@@ -449,7 +449,9 @@ class AdamW(_Owner):
     def step(self, grads, lr, step, betas=(0.9, 0.999), eps=1e-8, grad_scale=None):
         """One step (``step`` counts from 1).  grads: for each parameter its gradient, of its
         size and gradient type, or None (the parameter stays as it is).  grad_scale: None, or
-        a float32 device tensor of one element that multiplies every gradient."""
+        a float32 device tensor of one element that multiplies every gradient.  A step that is
+        recorded into a graph keeps its step number, lr, betas and gradients in every replay:
+        enqueue the steps of a training loop outside of it."""
         k = len(self._sizes)
         if len(grads) != k:
             raise ValueError("%d gradients for %d parameters" % (len(grads), k))
