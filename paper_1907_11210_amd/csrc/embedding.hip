@@ -24,8 +24,8 @@ __device__ __forceinline__ int digit_of(int key, int pass) {
 // A row of 2^lanes_log2 lanes to a token, kLookups tokens each, whose ids and then
 // whose rows are all in flight together (1, 2 and 8 were no faster).
 //
-// Bound by the result's bytes: 65536 tokens of 256 bf16 out of 8192: 9.8 us for 34 MB,
-// and 22 MB of the table's 4 read by the XCDs together; 64 tokens of 100: 2.8 us.
+// Bound by the result's bytes: 65536 tokens of 256 bf16 out of 8192, out of the caches: 9.8 us
+// for 34 MB, and 22 MB of the table's 4 read by the XCDs together; 64 tokens of 100: 2.8 us.
 constexpr int kLookups = 4;
 template <typename T, int VW>
 __global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a, int cblocks) {

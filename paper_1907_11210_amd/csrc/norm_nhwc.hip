@@ -8,7 +8,7 @@
 //
 // Bound by those bytes.  32x32x128, 64 images, bf16, gradient in one pass: 15.8 us for
 // 50 MB and 3.8 for the launch that adds up dgamma and dbeta.  64x64x2048, 8 images,
-// bf16, forward in two: 26.5 us for the first read of 134 MB and 41.7 for the second
+// bf16, forward in two: 26.8 us for the first read of 134 MB and 42.2 for the second
 // and the result.
 #include "norm_device.hpp"
 

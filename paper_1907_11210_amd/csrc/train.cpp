@@ -165,8 +165,9 @@ void slab_set(NormArgs* a, int vec, bool grad, int c, int threads) {
   a->lds_bytes = entries * (int)sizeof(float2);
 }
 
-// Slabs of all pixels, held in registers: 64 bytes of a pixel, twice that while there
-// are two workgroups for each compute unit all the same.
+// Slabs of all pixels, held in registers: 64 bytes of a pixel where that fits, and twice
+// as many again while there are two workgroups for each compute unit all the same (64 images
+// of 8x8x2048 bf16: 512 bytes).
 bool slab_nhwc(NormArgs* a, int esz, int vec, bool grad) {
   const int base = std::lcm(a->d, vec);
   a->span = a->d % vec != 0;
@@ -309,6 +310,8 @@ void direct_nchw(NormArgs* a, int vec) {
 // of 64x40x40 12.9 -> 9.2, 4 of 816x26x14 fp32 15.4 -> 10.5).  With a slab for each compute
 // unit the slabs win: 64 of 32x32x128 17.3 and 24; but not with half a memory line of each
 // pixel: 54 of 29x79x64 fp32 by 32 bytes 37.7 and 32.4, 64 of 64x64x64 bf16 56.3 and 38.3.
+// (The forward, which holds half as much, wins with 32 bytes all the same: 64 of 64x64x64 in
+// 16 groups bf16 25.5 and 29.9, 64 of 64x64x128 in 32 38.4 and 45.0.)
 bool weak_slabs(const NormArgs& a, bool nhwc, int esz, int vec, bool grad) {
   if (grad && nhwc && a.slab_c * esz < 64 && a.slab_c < a.c) return !a.direct;
   if (a.slabs >= 256) return false;
@@ -515,9 +518,10 @@ huge2_status embed_run(const huge2_embedding_desc* desc, const void* ids, int64_
   a.rows = d.rows, a.dim = d.dim, a.id64 = d.id_bits == 64, a.scale = d.scale;
   a.lanes_log2 = embed_lanes_log2(d, vec);
   // Results of 16 MiB and more are stored past the caches, by 4 bytes and more a lane (26813
-  // rows of 1217 fp32 70 -> 48 us).  65536 rows of bf16: of 128
-  // (16 MiB) 6.2 -> 5.0 us, of 256 10.5 -> 8.3, of 512 19.3 -> 16.6, and together with a
-  // kernel that reads them 18.9 -> 18.6, 25.5 -> 25.5, 40.6 -> 40.0; of 64 no difference.
+  // rows of 1217 fp32 70 -> 48 us).  65536 rows of bf16, the table and the last result in the
+  // caches, and out of them: of 128 (16 MiB) 6.2 -> 5.0 and 7.4 -> 6.0 us, of 256 10.4 -> 8.1
+  // and 10.6 -> 9.9, of 512 19.3 -> 16.7 and 19.7 -> 17.9; together with a kernel that reads
+  // them 18.9 -> 18.6, 25.5 -> 25.5, 40.6 -> 40.0; of 64 no difference.
   a.stream = row_b * tokens >= (size_t)16 << 20;
   return launched(launch_embedding(a, d.dtype, vec, stream));
 }
