@@ -4,6 +4,7 @@
  *
  *   group norm with an activation, and its gradients: what follows a
  *     convolution (huge2.h) in a generator or a decoder;
+ *   layer norm over the channels of each pixel or token, likewise;
  *   embedding lookup with a scale, and the table's gradient: class labels of a
  *     conditional generator, maps of code indices, text tokens;
  *   an AdamW step over many tensors in one call, with the moments in 32 bits
@@ -92,6 +93,58 @@ const char* huge2_norm_plan_kernel(const huge2_norm_plan* plan, int32_t grad);
 
 /* Waits for the device and releases the plan.  NULL is accepted.  Errors: HIP. */
 huge2_status huge2_norm_plan_destroy(huge2_norm_plan* plan);
+
+/* ---- layer norm over channels ---------------------------------------------- */
+
+/* For each of the n*h*w pixels, over its c channels (which lie side by side in NHWC and
+ * h*w elements apart in NCHW),
+ *   mean = sum x / c,  var = sum (x - mean)^2 / c,  rstd = 1 / sqrt(var + eps),
+ *   xh = (x - mean) * rstd,  z = xh * gamma[channel] + beta[channel],
+ *   y = activation(z).
+ * A list of tokens is n rows with h = w = 1. */
+typedef struct {
+  int32_t n, c, h, w; /* >= 1; c*h*w below 2^31 */
+  int32_t layout;     /* huge2_layout of x, y, dy, dx */
+  int32_t dtype;      /* huge2_dtype of x, y, dy, dx; the rest is float */
+  int32_t activation; /* huge2_norm_activation */
+  float eps;          /* > 0 and finite */
+} huge2_layer_norm_desc;
+
+typedef struct huge2_layer_norm_plan huge2_layer_norm_plan;
+
+/* Chooses the kernels for desc and allocates the gradient's workspace: 8 bytes a channel for
+ * each of its workgroups, at most 4096 of them.  No work is enqueued.  Errors: INVALID_ARG,
+ * UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all), ALLOC. */
+huge2_status huge2_layer_norm_plan_create(huge2_layer_norm_plan** out,
+                                          const huge2_layer_norm_desc* desc);
+
+/* Enqueues y from x.  gamma and beta are [c] float; NULL gamma is all ones, NULL beta all
+ * zeros.  stats is NULL or [n*h*w][2] float and then receives (mean, rstd) of each pixel,
+ * which huge2_layer_norm_grad_execute reads.  y and stats must not overlap each other or an
+ * input.  Errors: INVALID_ARG, HIP. */
+huge2_status huge2_layer_norm_execute(const huge2_layer_norm_plan* plan, const void* x,
+                                      const float* gamma, const float* beta, void* y, float* stats,
+                                      void* hip_stream);
+
+/* Enqueues the gradients of a forward call for the output error dy, from the same x, gamma and
+ * beta and the stats that the call wrote:
+ *   dz = dy * activation'(z),  dbeta = sum over pixels of dz,
+ *   dgamma = sum over pixels of dz * xh,  t = dz * gamma,
+ *   dx = rstd * (t - mean over the channels of t - xh * mean over the channels of t*xh).
+ * A ReLU masks the same values both ways, as in huge2_norm_grad_execute.  dgamma and dbeta are
+ * [c] float and may be NULL.  dx, dgamma and dbeta must not overlap each other or an input.
+ * Errors: INVALID_ARG, HIP. */
+huge2_status huge2_layer_norm_grad_execute(const huge2_layer_norm_plan* plan, const void* x,
+                                           const void* dy, const float* stats, const float* gamma,
+                                           const float* beta, void* dx, float* dgamma,
+                                           float* dbeta, void* hip_stream);
+
+/* Names of the kernels that the plan launches: grad 0 for the forward, 1 for
+ * the gradients.  Storage of the plan's; "" for a NULL plan. */
+const char* huge2_layer_norm_plan_kernel(const huge2_layer_norm_plan* plan, int32_t grad);
+
+/* Waits for the device and releases the plan.  NULL is accepted.  Errors: HIP. */
+huge2_status huge2_layer_norm_plan_destroy(huge2_layer_norm_plan* plan);
 
 /* ---- embedding lookup ----------------------------------------------------- */
 

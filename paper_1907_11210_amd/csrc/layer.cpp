@@ -1,0 +1,205 @@
+// layer.cpp -- the C ABI of layer norm (declared in include/huge2_train.h): checks, plans,
+// workspaces.
+#include "huge2_train.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdio>
+#include <new>
+
+#include "kernels.hpp"
+#include "train.hpp"
+#include "train_host.hpp"
+
+using namespace huge2;
+
+struct huge2_layer_norm_plan {
+  huge2_layer_norm_desc desc;
+  bool rows;
+  int vec;
+  LayerArgs args[2];  // forward, gradient
+  void* ws;
+  char kernel_name[2][64];
+};
+
+namespace {
+
+bool valid(const huge2_layer_norm_desc& d) {
+  return d.n >= 1 && d.c >= 1 && d.h >= 1 && d.w >= 1 &&
+         (d.layout == HUGE2_NCHW || d.layout == HUGE2_NHWC) && is_dtype(d.dtype) &&
+         d.activation >= HUGE2_NORM_NONE && d.activation <= HUGE2_NORM_SILU &&
+         std::isfinite(d.eps) && d.eps > 0.f;
+}
+size_t bytes_of(const huge2_layer_norm_desc& d) {
+  return (size_t)d.n * d.c * d.h * d.w * elem_size(d.dtype);
+}
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// Rows: as many lanes as a row has vectors, up to a wave; more vectors a lane, up to what its
+// registers hold; then more waves, up to a workgroup.
+void choose_rows(LayerArgs* a, int vec, bool grad) {
+  const long long vecs = ceil_div(a->c, vec);
+  const int most = std::max(1, (grad ? kLayerGradChannels : kLayerChannels) / vec);
+  a->lanes_log2 = std::min(6, log2_ceil(vecs));
+  while (a->lanes_log2 < 10 && vecs > (long long)most << a->lanes_log2) ++a->lanes_log2;
+  const long long slots = 1ll << log2_ceil(ceil_div(vecs, 1ll << a->lanes_log2));
+  a->slots = slots > most ? 0 : (int)slots;
+  // (lanes of more than a wave are a whole workgroup)
+  a->threads = !a->slots ? 1024 : a->lanes_log2 > 6 ? 1 << a->lanes_log2 : 256;
+  const int teams = a->slots ? a->threads >> a->lanes_log2 : 1;
+  const long long all = ceil_div(a->rows, teams), most_groups = (grad ? 1024 : 2048) * 256 / a->threads;
+  const long long want = grad ? std::max(256ll, ceil_div(all, 4)) : all;
+  a->groups = (int)std::min({all, want, most_groups});
+  a->parts = a->groups;
+  if (!a->slots) {
+    const long long blocks = ceil_div(a->c, 256ll * vec);
+    a->parts = (int)std::min(a->rows, std::max(1ll, 1024 / blocks));
+  }
+}
+
+// Planes: tiles of 128 bytes of each plane, or less where the channels then fit the registers.
+// False where there are too many of them.
+bool choose_planes(LayerArgs* a, int vec, int esz, bool grad) {
+  const long long vecs = ceil_div(a->hw, vec);
+  a->lanes_log2 = std::min(3, log2_ceil(vecs));
+  const int most_held = 1024 * (grad ? kLayerGradPlanes / 2 : kLayerPlanes);  // of a tile
+  while (a->lanes_log2 > 1 && a->c > most_held >> a->lanes_log2) --a->lanes_log2;
+  const auto tiles = [&] { return ceil_div(vecs, 1ll << a->lanes_log2) * a->n; };
+  if (a->lanes_log2 == 3 && tiles() < 512) a->lanes_log2 = 2;
+  const auto slots = [&] { return ceil_div(a->c, a->threads >> a->lanes_log2); };
+  // (eight vectors of x and of dy leave 512 threads)
+  const auto most = [&] { return !grad ? kLayerPlanes : a->threads > 512 ? kLayerGradPlanes / 2 : kLayerGradPlanes; };
+  a->threads = 64;
+  while (a->threads < 1024 &&
+         (slots() > most() || (slots() > 4 && tiles() * (a->threads / 32) <= 8192)))
+    a->threads *= 2;
+  // (offsets of held channels are 32 bits of bytes)
+  const bool held = slots() <= most() && (long long)a->c * a->hw * esz < (1ll << 32);
+  a->slots = held ? 1 << log2_ceil(slots()) : 0;
+  if (tiles() >= (1ll << 31)) return false;
+  a->tiles = (uint32_t)tiles();
+  a->tiles_per_image = (int)(a->tiles / a->n);
+  division_magic((uint32_t)a->tiles_per_image, &a->tile_mul, &a->tile_shift);
+  a->groups = (int)std::min<long long>(a->tiles, (grad ? 1024 : 2048) * 256 / a->threads);
+  a->parts = a->slots ? a->groups : (int)std::min<long long>(a->n, std::max(1, 2048 / a->c));
+  return true;
+}
+
+huge2_status layer_create(huge2_layer_norm_plan** out, const huge2_layer_norm_desc* desc) {
+  if (!out) return HUGE2_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!desc || !valid(*desc)) return HUGE2_ERR_INVALID_ARG;
+  const huge2_layer_norm_desc& d = *desc;
+  const long long hw = (long long)d.h * d.w;
+  if (hw >= (1ll << 31) || hw * d.c >= (1ll << 31) || hw * d.c * d.n >= (1ll << 40))
+    return HUGE2_ERR_UNSUPPORTED;
+  huge2_layer_norm_plan* p = new (std::nothrow) huge2_layer_norm_plan();
+  if (!p) return HUGE2_ERR_ALLOC;
+  p->desc = d;
+  p->rows = d.layout == HUGE2_NHWC || hw == 1;
+  const int full = 16 / elem_size(d.dtype);
+  p->vec = (p->rows ? d.c : hw) >= full ? full : 1;
+  size_t part_b = 0;
+  for (int g = 0; g < 2; ++g) {
+    LayerArgs& a = p->args[g];
+    a = {};
+    a.n = d.n, a.c = d.c, a.hw = (int)hw, a.rows = hw * d.n;
+    a.act = d.activation;
+    a.eps = d.eps;
+    a.stream = streams(bytes_of(d));
+    if (p->rows) {
+      choose_rows(&a, p->vec, g != 0);
+    } else if (!choose_planes(&a, p->vec, elem_size(d.dtype), g != 0)) {
+      delete p;
+      return HUGE2_ERR_UNSUPPORTED;
+    }
+    if (g) part_b = (size_t)a.parts * a.c * sizeof(float2);
+    std::snprintf(p->kernel_name[g], sizeof(p->kernel_name[g]), "layer_%s%s_kernel v%d t%d r%d",
+                  p->rows && !a.slots ? "" : g ? "grad_" : "",
+                  !p->rows ? "planes" : a.slots ? "rows" : "long", p->vec, a.threads, a.slots);
+  }
+  const huge2_status st = device_alloc(&p->ws, part_b);
+  if (st != HUGE2_OK) {
+    delete p;
+    return st;
+  }
+  *out = p;
+  return HUGE2_OK;
+}
+
+huge2_status layer_run(const huge2_layer_norm_plan* p, const void* x, const float* gamma,
+                       const float* beta, void* y, float* stats, hipStream_t stream) {
+  if (!p || bad(x) || bad(y) || !aligned(gamma) || !aligned(beta) || !aligned(stats))
+    return HUGE2_ERR_INVALID_ARG;
+  const size_t bytes = bytes_of(p->desc), params = (size_t)p->desc.c * sizeof(float);
+  const size_t pixels = (size_t)p->args[0].rows * sizeof(float2);
+  if (overlaps({{y, bytes}, {stats, pixels}}, {{x, bytes}, {gamma, params}, {beta, params}}))
+    return HUGE2_ERR_INVALID_ARG;
+  if (fault("launch")) return HUGE2_ERR_HIP;
+  LayerArgs a = p->args[0];
+  a.x = x, a.gamma = gamma, a.beta = beta, a.out = y, a.stats_out = stats;
+  return launched((p->rows ? launch_layer_rows : launch_layer_planes)(a, p->desc.dtype, p->vec,
+                                                                      false, stream));
+}
+
+huge2_status layer_grad_run(const huge2_layer_norm_plan* p, const void* x, const void* dy,
+                            const float* stats, const float* gamma, const float* beta, void* dx,
+                            float* dgamma, float* dbeta, hipStream_t stream) {
+  if (!p || bad(x) || bad(dy) || bad(dx) || bad(stats) || !aligned(gamma) || !aligned(beta) ||
+      !aligned(dgamma, 4) || !aligned(dbeta, 4))
+    return HUGE2_ERR_INVALID_ARG;
+  const size_t bytes = bytes_of(p->desc), params = (size_t)p->desc.c * sizeof(float);
+  const size_t pixels = (size_t)p->args[1].rows * sizeof(float2);
+  if (overlaps({{dx, bytes}, {dgamma, params}, {dbeta, params}},
+               {{x, bytes}, {dy, bytes}, {stats, pixels}, {gamma, params}, {beta, params}}))
+    return HUGE2_ERR_INVALID_ARG;
+  if (fault("launch")) return HUGE2_ERR_HIP;
+  LayerArgs a = p->args[1];
+  a.x = x, a.dy = dy, a.stats = stats, a.gamma = gamma, a.beta = beta, a.out = dx;
+  a.dgamma = dgamma, a.dbeta = dbeta;
+  a.part = dgamma || dbeta ? (float2*)p->ws : nullptr;
+  return launched((p->rows ? launch_layer_rows : launch_layer_planes)(a, p->desc.dtype, p->vec,
+                                                                      true, stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+huge2_status huge2_layer_norm_plan_create(huge2_layer_norm_plan** out,
+                                          const huge2_layer_norm_desc* desc) {
+  try {
+    return layer_create(out, desc);
+  } catch (...) {
+    return HUGE2_ERR_ALLOC;
+  }
+}
+
+huge2_status huge2_layer_norm_execute(const huge2_layer_norm_plan* plan, const void* x,
+                                      const float* gamma, const float* beta, void* y, float* stats,
+                                      void* hip_stream) {
+  return layer_run(plan, x, gamma, beta, y, stats, (hipStream_t)hip_stream);
+}
+
+huge2_status huge2_layer_norm_grad_execute(const huge2_layer_norm_plan* plan, const void* x,
+                                           const void* dy, const float* stats, const float* gamma,
+                                           const float* beta, void* dx, float* dgamma,
+                                           float* dbeta, void* hip_stream) {
+  return layer_grad_run(plan, x, dy, stats, gamma, beta, dx, dgamma, dbeta,
+                        (hipStream_t)hip_stream);
+}
+
+const char* huge2_layer_norm_plan_kernel(const huge2_layer_norm_plan* plan, int32_t grad) {
+  return plan ? plan->kernel_name[grad != 0] : "";
+}
+
+huge2_status huge2_layer_norm_plan_destroy(huge2_layer_norm_plan* plan) {
+  if (!plan) return HUGE2_OK;
+  const huge2_status st = device_free(plan->ws);
+  delete plan;
+  return st;
+}
+
+}  // extern "C"

@@ -1,5 +1,5 @@
 // train.hpp -- kernel arguments and launchers of the operators around the
-// convolutions (huge2_train.h): group norm, embedding, AdamW.
+// convolutions (huge2_train.h): group norm, layer norm, embedding, AdamW.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -72,6 +72,44 @@ hipError_t launch_norm_grad_nhwc(const NormArgs& a, int dtype, int vec, hipStrea
 hipError_t launch_norm_nchw(const NormArgs& a, int dtype, int vec, hipStream_t stream);
 hipError_t launch_norm_grad_nchw(const NormArgs& a, int dtype, int vec, hipStream_t stream);
 hipError_t launch_norm_params(const NormArgs& a, hipStream_t stream);
+
+// ---- layer norm (layer_rows.hip, layer_planes.hip) ------------------------------
+
+struct LayerArgs {
+  const void* x;
+  const void* dy;
+  const float* stats;  // [n][hw][2]: mean, rstd (the gradient's input)
+  const float* gamma;  // null: ones
+  const float* beta;   // null: zeros
+  void* out;           // y or dx
+  float* stats_out;    // null: not wanted
+  float2* part;        // gradient: [parts][c], sums of dbeta and dgamma; null: not wanted
+  float* dgamma;
+  float* dbeta;
+  long long rows;   // pixels of all images
+  uint32_t tiles;   // planes: tiles of all images, below 2^31
+  uint32_t first_tile;  // of a launch of the forward
+  int n, c, hw;
+  int tiles_per_image;
+  uint32_t tile_mul, tile_shift;  // division by it
+  int threads, groups;  // of a workgroup, and how many of them
+  int slots;            // vectors a thread holds; 0: read again
+  int lanes_log2;       // lanes side by side on a row, or (planes) on a tile's pixels
+  int parts;
+  int act;
+  float eps;
+  int stream;  // the result is stored past the caches
+};
+// The most values of a row that a thread of the gradient holds (it has two sums and two
+// parameters for each besides, and a thread of 1024 has 128 registers), and vectors of planes.
+constexpr int kLayerChannels = 32, kLayerGradChannels = 16;
+constexpr int kLayerPlanes = 16, kLayerGradPlanes = 8;
+
+hipError_t launch_layer_rows(const LayerArgs& a, int dtype, int vec, bool grad,
+                             hipStream_t stream);
+hipError_t launch_layer_planes(const LayerArgs& a, int dtype, int vec, bool grad,
+                               hipStream_t stream);
+hipError_t launch_layer_params(const LayerArgs& a, hipStream_t stream);
 
 // ---- embedding (embedding.hip) -------------------------------------------------
 

@@ -1,11 +1,11 @@
 """Python binding of the operators around the convolutions (the C ABI in
-include/huge2_train.h): group norm with an activation, embedding lookup and the
-AdamW step, with their gradients.
+include/huge2_train.h): group norm and layer norm with an activation, embedding
+lookup and the AdamW step, with their gradients.
 
 Argument marshalling only, as in :mod:`paper_1907_11210_amd.huge2`: the ``huge2_*``
 functions mirror the C entry points and take raw device pointers (ints);
-:class:`GroupNorm`, :class:`Embedding` and :class:`AdamW` take torch tensors and
-enqueue on the current stream.  Objects belong to the device that was current when
+:class:`GroupNorm`, :class:`LayerNorm`, :class:`Embedding` and :class:`AdamW` take torch
+tensors and enqueue on the current stream.  Objects belong to the device that was current when
 they were made; one object's calls share its workspace, so make them on one stream
 or order them.
 """
@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import math
 
 from . import huge2 as h2
 
@@ -22,6 +23,8 @@ STATE_BLOCK = 256  # elements that share a scale in 8-bit states
 EXPORTED = (
     "huge2_norm_plan_create", "huge2_norm_execute", "huge2_norm_grad_execute",
     "huge2_norm_plan_kernel", "huge2_norm_plan_destroy",
+    "huge2_layer_norm_plan_create", "huge2_layer_norm_execute", "huge2_layer_norm_grad_execute",
+    "huge2_layer_norm_plan_kernel", "huge2_layer_norm_plan_destroy",
     "huge2_embedding", "huge2_embedding_grad_plan_create", "huge2_embedding_grad_execute",
     "huge2_embedding_grad_plan_kernel", "huge2_embedding_grad_plan_destroy",
     "huge2_adamw_plan_create", "huge2_adamw_step", "huge2_adamw_plan_destroy",
@@ -41,6 +44,11 @@ class _Desc(ctypes.Structure):
 
 class NormDesc(_Desc):
     _fields_ = [(f, ctypes.c_int32) for f in ("n", "c", "h", "w", "groups", "layout", "dtype",
+                                              "activation")] + [("eps", ctypes.c_float)]
+
+
+class LayerNormDesc(_Desc):
+    _fields_ = [(f, ctypes.c_int32) for f in ("n", "c", "h", "w", "layout", "dtype",
                                               "activation")] + [("eps", ctypes.c_float)]
 
 
@@ -76,6 +84,11 @@ def lib():
             "huge2_norm_grad_execute": [vp] * 10,
             "huge2_norm_plan_kernel": [vp, i32],
             "huge2_norm_plan_destroy": [vp],
+            "huge2_layer_norm_plan_create": [out, ctypes.POINTER(LayerNormDesc)],
+            "huge2_layer_norm_execute": [vp] * 7,
+            "huge2_layer_norm_grad_execute": [vp] * 10,
+            "huge2_layer_norm_plan_kernel": [vp, i32],
+            "huge2_layer_norm_plan_destroy": [vp],
             "huge2_embedding": [ctypes.POINTER(EmbeddingDesc), vp, i64, vp, vp, vp],
             "huge2_embedding_grad_plan_create": [out, ctypes.POINTER(EmbeddingDesc), i64],
             "huge2_embedding_grad_execute": [vp, vp, i64, vp, vp, vp],
@@ -120,6 +133,33 @@ def huge2_norm_plan_kernel(plan, grad=False):
 
 def huge2_norm_plan_destroy(plan):
     h2._check(lib().huge2_norm_plan_destroy(plan), "huge2_norm_plan_destroy")
+
+
+def huge2_layer_norm_plan_create(desc):
+    plan = ctypes.c_void_p()
+    h2._check(lib().huge2_layer_norm_plan_create(ctypes.byref(plan), ctypes.byref(desc)),
+              "huge2_layer_norm_plan_create")
+    return plan
+
+
+def huge2_layer_norm_execute(plan, x_ptr, gamma_ptr, beta_ptr, y_ptr, stats_ptr=0, stream=0):
+    h2._check(lib().huge2_layer_norm_execute(plan, x_ptr, gamma_ptr, beta_ptr, y_ptr, stats_ptr,
+                                             stream), "huge2_layer_norm_execute")
+
+
+def huge2_layer_norm_grad_execute(plan, x_ptr, dy_ptr, stats_ptr, gamma_ptr, beta_ptr, dx_ptr,
+                                  dgamma_ptr=0, dbeta_ptr=0, stream=0):
+    h2._check(lib().huge2_layer_norm_grad_execute(plan, x_ptr, dy_ptr, stats_ptr, gamma_ptr,
+                                                  beta_ptr, dx_ptr, dgamma_ptr, dbeta_ptr, stream),
+              "huge2_layer_norm_grad_execute")
+
+
+def huge2_layer_norm_plan_kernel(plan, grad=False):
+    return lib().huge2_layer_norm_plan_kernel(plan, int(grad)).decode()
+
+
+def huge2_layer_norm_plan_destroy(plan):
+    h2._check(lib().huge2_layer_norm_plan_destroy(plan), "huge2_layer_norm_plan_destroy")
 
 
 def huge2_embedding(desc, ids_ptr, tokens, table_ptr, y_ptr, stream=0):
@@ -231,30 +271,18 @@ class _Owner:
             pass
 
 
-class GroupNorm(_Owner):
-    """y = activation(group_norm(x) * gamma + beta) for inputs of one shape
-    (``layout`` "NHWC" or "NCHW"), and its gradients.  activation: None, "relu",
-    "tanh" or "silu"."""
-    _destroy = staticmethod(huge2_norm_plan_destroy)
+class _Norm(_Owner):
+    """The calls of a norm with a scale, a shift and an activation for each channel."""
 
-    def __init__(self, x_shape, groups, dtype, layout="NCHW", activation=None, eps=1e-5):
+    def _init(self, x_shape, c, stats_shape, dtype, activation):
         torch = _torch()
-        lay = h2._layout_code(layout)
-        if len(x_shape) != 4:
-            raise ValueError("x must be 4-D")
         if activation not in NORM_ACTIVATIONS:
             raise ValueError("unknown activation %r (none, relu, tanh, silu)" % (activation,))
-        n, c, h, w = x_shape if lay == h2.HUGE2_NCHW else [x_shape[i] for i in (0, 3, 1, 2)]
         self.x_shape, self.dtype = torch.Size(x_shape), dtype
-        self.param_shape = torch.Size((c,))
-        self.stats_shape = torch.Size((n, groups, 2))
+        self.param_shape, self.stats_shape = torch.Size((c,)), torch.Size(stats_shape)
         self.device = _current_device()
         self._index, self._f32, self._stream = self.device.index, torch.float32, _raw_stream()
-        self._execute, self._grad_execute = (lib().huge2_norm_execute,
-                                             lib().huge2_norm_grad_execute)
-        self.desc = NormDesc(n, c, h, w, groups, lay, _type_code(dtype),
-                             NORM_ACTIVATIONS[activation], eps)
-        self._plan = huge2_norm_plan_create(self.desc)
+        self._execute, self._grad_execute = (getattr(lib(), name) for name in self._names[:2])
         # (the quickest way to a new tensor)
         self._param_like = torch.empty(c, dtype=torch.float32, device=self.device)
         self._like = torch.empty_like
@@ -272,7 +300,7 @@ class GroupNorm(_Owner):
         return out, self._x(out, "out")
 
     def __call__(self, x, gamma=None, beta=None, out=None, stats=None):
-        """y; ``stats`` ([n, groups, 2] float32, :meth:`new_stats`) receives the mean and
+        """y; ``stats`` (float32 of ``stats_shape``, :meth:`new_stats`) receives the mean and
         reciprocal standard deviation that :meth:`grad` reads."""
         xp = self._x(x, "x")
         y, yp = self._out(out)
@@ -281,7 +309,7 @@ class GroupNorm(_Owner):
         status = self._execute(self._open(), xp, self._param(gamma, "gamma"),
                                self._param(beta, "beta"), yp, sp, self._stream(self._index))
         if status:
-            h2._check(status, "huge2_norm_execute")
+            h2._check(status, self._names[0])
         return y
 
     def new_stats(self):
@@ -298,13 +326,57 @@ class GroupNorm(_Owner):
                                     self._param(beta, "beta"), dxp, dgamma.data_ptr(),
                                     dbeta.data_ptr(), self._stream(self._index))
         if status:
-            h2._check(status, "huge2_norm_grad_execute")
+            h2._check(status, self._names[1])
         return dx, dgamma, dbeta
 
     @property
     def kernels(self):
         """Names of the kernels that a call and a gradient launch."""
-        return tuple(huge2_norm_plan_kernel(self._open(), g) for g in (0, 1))
+        return tuple(self._kernel(self._open(), g) for g in (0, 1))
+
+
+class GroupNorm(_Norm):
+    """y = activation(group_norm(x) * gamma + beta) for inputs of one shape
+    (``layout`` "NHWC" or "NCHW"), and its gradients.  activation: None, "relu",
+    "tanh" or "silu".  Statistics are [n, groups, 2]."""
+    _destroy = staticmethod(huge2_norm_plan_destroy)
+    _kernel = staticmethod(huge2_norm_plan_kernel)
+    _names = ("huge2_norm_execute", "huge2_norm_grad_execute")
+
+    def __init__(self, x_shape, groups, dtype, layout="NCHW", activation=None, eps=1e-5):
+        lay = h2._layout_code(layout)
+        if len(x_shape) != 4:
+            raise ValueError("x must be 4-D")
+        n, c, h, w = x_shape if lay == h2.HUGE2_NCHW else [x_shape[i] for i in (0, 3, 1, 2)]
+        self._init(x_shape, c, (n, groups, 2), dtype, activation)
+        self.desc = NormDesc(n, c, h, w, groups, lay, _type_code(dtype),
+                             NORM_ACTIVATIONS[activation], eps)
+        self._plan = huge2_norm_plan_create(self.desc)
+
+
+class LayerNorm(_Norm):
+    """y = activation(layer_norm(x) * gamma + beta) over the channels of each pixel, for inputs
+    of one shape, and its gradients.  ``layout`` "NHWC": any shape whose last axis are the
+    channels ([tokens, c], [n, h, w, c], ...); "NCHW": [n, c, h, w].  activation: None, "relu",
+    "tanh" or "silu".  Statistics are [pixels, 2]."""
+    _destroy = staticmethod(huge2_layer_norm_plan_destroy)
+    _kernel = staticmethod(huge2_layer_norm_plan_kernel)
+    _names = ("huge2_layer_norm_execute", "huge2_layer_norm_grad_execute")
+
+    def __init__(self, x_shape, dtype, layout="NHWC", activation=None, eps=1e-5):
+        lay = h2._layout_code(layout)
+        if lay == h2.HUGE2_NCHW:
+            if len(x_shape) != 4:
+                raise ValueError("x must be 4-D in NCHW")
+            n, c, h, w = x_shape
+        else:
+            if len(x_shape) == 0:
+                raise ValueError("x must have an axis of channels")
+            n, c, h, w = math.prod(x_shape[:-1]), x_shape[-1], 1, 1
+        self._init(x_shape, c, (n * h * w, 2), dtype, activation)
+        self.desc = LayerNormDesc(n, c, h, w, lay, _type_code(dtype),
+                                  NORM_ACTIVATIONS[activation], eps)
+        self._plan = huge2_layer_norm_plan_create(self.desc)
 
 
 class Embedding(_Owner):
