@@ -250,6 +250,99 @@ huge2_status huge2_adamw_step(const huge2_adamw_plan* plan, const void* const* g
  * accepted.  Errors: HIP. */
 huge2_status huge2_adamw_plan_destroy(huge2_adamw_plan* plan);
 
+/* ---- orthogonalised matrices ------------------------------------------------ */
+
+/* What a product's operands hold: two fp16 parts of a value (22 bits; results as of products in
+ * fp32), or one (11 bits; results within 2^-10 of their norm, a third of the time).  Sums are
+ * fp32 either way. */
+typedef enum { HUGE2_PRODUCTS_F32 = 0, HUGE2_PRODUCTS_F16 = 1 } huge2_products;
+
+/* Newton-Schulz steps that bring all singular values of a matrix near 1:
+ *   X = U / (|U| + eps), |U| the root of the sum of squares, then `steps` times
+ *   A = X X^T,  X = a X + (b A + c A A) X
+ * with (a, b, c) of each step, [steps][3].  (3.4445, -4.7750, 2.0315) five times brings
+ * singular values of |U| / 500 and more to between 0.7 and 1.2.  A matrix with more rows than
+ * columns is taken transposed, which gives the same.  A value that is not finite makes the
+ * whole result NaN, as the products do. */
+typedef struct {
+  int32_t steps;              /* 1 to 32 */
+  int32_t products;           /* huge2_products */
+  const double* coefficients; /* read by the call that makes a plan.  The polynomials must keep
+                                 singular values, which begin in [0, 1], below 2^10, and
+                                 |b| s^2 + |c| s^4 of their bound s below 2^22 */
+  double eps;                 /* >= 2^-126 and finite */
+} huge2_newton_schulz;
+
+typedef struct {
+  int32_t batch, rows, cols; /* >= 1; rows*cols below 2^31 */
+  int32_t dtype;             /* huge2_dtype of x and y */
+} huge2_orthogonalize_desc;
+
+typedef struct huge2_orthogonalize_plan huge2_orthogonalize_plan;
+
+/* A plan for `batch` matrices of one shape, one behind the other.  Allocates the operands of as
+ * many of them as are worked on together (up to 256 and some 4 GiB): for m the smaller and n the
+ * larger of rows and cols, each rounded up to 64, 12 m n + 8 m^2 bytes with two parts and 10 m n +
+ * 6 m^2 with one, and sums of parts of products, 64 KB each, up to some 1000.  Copies its lists
+ * of work on hip_stream and waits for it.  Errors: INVALID_ARG, UNSUPPORTED (matrices of
+ * 2^31 elements, more than 2^20 of them, 2^40 elements in all), ALLOC, HIP. */
+huge2_status huge2_orthogonalize_plan_create(huge2_orthogonalize_plan** out,
+                                             const huge2_orthogonalize_desc* desc,
+                                             const huge2_newton_schulz* ns, void* hip_stream);
+
+/* Enqueues y, the steps' result for each matrix of x, both [batch][rows][cols].  They must not
+ * overlap.  Errors: INVALID_ARG, HIP. */
+huge2_status huge2_orthogonalize_execute(const huge2_orthogonalize_plan* plan, const void* x,
+                                         void* y, void* hip_stream);
+
+/* Waits for the device and releases the plan.  NULL is accepted.  Errors: HIP. */
+huge2_status huge2_orthogonalize_plan_destroy(huge2_orthogonalize_plan* plan);
+
+/* ---- the Muon step ----------------------------------------------------------- */
+
+/* A parameter matrix [rows][cols] and its state, updated in place.  A convolution's weights
+ * [c0][c1][kh][kw] are c0 rows of c1*kh*kw. */
+typedef struct {
+  void* param;
+  float* m;   /* the momentum, which starts as zeros */
+  void* copy; /* NULL, or bfloat16: receives the updated parameter rounded */
+  int32_t rows, cols; /* >= 1; rows*cols below 2^31 */
+  int32_t dtype;      /* huge2_dtype of param */
+  int32_t grad_dtype; /* huge2_dtype of its gradient */
+  float weight_decay; /* >= 0 and finite */
+  float scale;        /* of the update, finite: such as sqrt(max(1, rows / cols)) */
+} huge2_muon_tensor;
+
+typedef struct huge2_muon_plan huge2_muon_plan;
+
+/* A plan for `count` matrices (>= 0), which must outlive it.  No two of their arrays may
+ * overlap.  Allocates and copies as huge2_orthogonalize_plan_create does.  Errors: INVALID_ARG,
+ * UNSUPPORTED (a matrix of 2^31 elements, more than 2^20 of them, 2^40 elements in all), ALLOC,
+ * HIP. */
+huge2_status huge2_muon_plan_create(huge2_muon_plan** out, const huge2_muon_tensor* tensors,
+                                    int32_t count, const huge2_newton_schulz* ns,
+                                    void* hip_stream);
+
+typedef struct {
+  double lr, momentum; /* lr >= 0 and finite, 0 <= momentum < 1 */
+  int32_t nesterov;    /* 0 or 1 */
+} huge2_muon_options;
+
+/* Enqueues one step: with g = grad (* *grad_scale, a device float, where that is not NULL),
+ *   m = momentum m + (1 - momentum) g,
+ *   U = nesterov ? momentum m + (1 - momentum) g : m,
+ *   param = param (1 - lr weight_decay) - lr scale X,  X the Newton-Schulz steps' result for U,
+ * in fp32.  grads is a host array of `count` device pointers in the plan's order, none into an
+ * array that the step writes; a matrix whose gradient is NULL is left as it is.  A recorded step
+ * keeps its options in every replay.  Errors: INVALID_ARG, HIP. */
+huge2_status huge2_muon_step(const huge2_muon_plan* plan, const void* const* grads,
+                             const huge2_muon_options* options, const float* grad_scale,
+                             void* hip_stream);
+
+/* Waits for the device and releases the plan (not the matrices).  NULL is accepted.
+ * Errors: HIP. */
+huge2_status huge2_muon_plan_destroy(huge2_muon_plan* plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,7 +19,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["plan.cpp", "capi.cpp", "kernels.hip", "grouped.hip", "wavek.hip",
            "gemm_f32.hip", "train.cpp", "norm.hip", "norm_nhwc.hip",
            "norm_nchw.hip", "embedding.hip", "adamw.hip", "layer.cpp", "layer_rows.hip",
-           "layer_planes.hip"]
+           "layer_planes.hip", "muon.cpp", "newton.hip"]
 
 # Packed-FP32 VALU ops are disabled for all device code; the host pass only
 # warns that it does not know the feature.  MFMA accumulators live in

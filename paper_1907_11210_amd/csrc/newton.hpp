@@ -1,0 +1,89 @@
+// newton.hpp -- kernel arguments and launchers of the Newton-Schulz products (newton.hip):
+// orthogonalised matrices and the Muon step.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstddef>
+#include <cstdint>
+
+namespace huge2 {
+
+// Operands of the products are fp16 in fragments of 32 rows by 16 columns, 1 KB each, as a
+// matrix instruction takes them: lane l has row l % 32, columns 8 (l / 32) to + 8.  A matrix of
+// R rows and K columns is [R / 32][K / 16] fragments, both sizes rounded up to kNsPad, zeros
+// behind the end.  Two such planes, of the value and of what it leaves over, are 22 bits.
+constexpr int kNsPad = 64, kNsFrag = 512;  // elements
+constexpr int kNsMatrices = 256;  // of a group: their gradients are kernel arguments
+constexpr int kNsBlock = 64;      // rows and columns of a packing workgroup
+
+typedef uint16_t half_bits;
+
+// X is m x n, m <= n: a matrix with more rows than columns is taken transposed.
+struct NsMatrix {
+  half_bits* x;       // X [m][n]: hi, and with two parts lo
+  half_bits* t0;      // its transpose [n][m], hi and lo: of even steps
+  half_bits* t1;      // ... and of odd ones
+  half_bits* a;       // X X^T - mu I [m][m], hi and lo
+  half_bits* b;       // [m][m]: hi, and with two parts lo
+  float* squares;     // [tiles of X]: of their elements
+  double* norm;       // [norm_count]: sums of squares of the input
+  float* mu;          // trace(X X^T) / m
+  int m, n, mp, np;   // mp, np: rounded up to kNsPad
+  int tall;           // the input is n x m
+  int x_tiles;        // tiles of X
+  int norm_count;
+  int norm_chunk;     // elements of a sum
+  long long count;    // m * n
+  // what the last step writes: y behind the call's pointer, or a parameter
+  long long out_at;   // elements
+  void* param;
+  void* copy;
+  float* momentum;
+  int bf16, grad_bf16;
+  float decay, scale;
+};
+
+struct NsWork {
+  int matrix, ti, tj;
+  int k0, k1;  // stages of the product
+  int slot;    // of the partial tiles, -1: the whole sum; a join: the first
+  int slots;   // a join: how many
+  int size;    // of the tile: 0 kNsSmall, 1 kNsLarge
+};
+constexpr int kNsSmall = 64, kNsLarge = 128;
+constexpr int ns_stage(int parts) { return parts == 2 ? 32 : 64; }  // columns
+constexpr int kNsSlot = kNsLarge * kNsLarge;  // elements of a partial tile
+
+enum NsKind { kNsGram = 0, kNsSquare = 1, kNsApply = 2 };
+
+struct NsArgs {
+  const NsMatrix* mats;
+  const NsWork* works;
+  float* part;
+  int kind, step, last;
+  int from;              // the step reads t0 or t1 and writes the other
+  float a, b, c;         // of the step's polynomial
+  float in_scale;        // of a product's sum
+  float own_scale;       // of the values that are added to it
+  float out_scale;       // of what is stored
+  float lr;
+  void* out;             // null: parameters
+  uint64_t skip[kNsMatrices / 64];  // matrices without a gradient
+};
+struct NsInput {
+  const NsMatrix* mats;
+  const uint2* works;    // (matrix, chunk of a sum), or (matrix, packed block)
+  int muon, nesterov;
+  float momentum, rest;  // rest: 1 - momentum
+  double eps;
+  float out_scale;
+  const float* grad_scale;
+  const void* src[kNsMatrices];
+};
+
+hipError_t launch_ns_norm(const NsInput& a, unsigned works, hipStream_t stream);
+hipError_t launch_ns_pack(const NsInput& a, unsigned works, int parts, hipStream_t stream);
+hipError_t launch_ns_product(const NsArgs& a, unsigned works, int parts, hipStream_t stream);
+hipError_t launch_ns_join(const NsArgs& a, unsigned works, int parts, hipStream_t stream);
+
+}  // namespace huge2

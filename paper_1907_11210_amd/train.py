@@ -1,11 +1,11 @@
 """Python binding of the operators around the convolutions (the C ABI in
 include/huge2_train.h): group norm and layer norm with an activation, embedding
-lookup and the AdamW step, with their gradients.
+lookup and the AdamW step, with their gradients; orthogonalised matrices and the Muon step.
 
 Argument marshalling only, as in :mod:`paper_1907_11210_amd.huge2`: the ``huge2_*``
 functions mirror the C entry points and take raw device pointers (ints);
-:class:`GroupNorm`, :class:`LayerNorm`, :class:`Embedding` and :class:`AdamW` take torch
-tensors and enqueue on the current stream.  Objects belong to the device that was current when
+:class:`GroupNorm`, :class:`LayerNorm`, :class:`Embedding`, :class:`AdamW`,
+:class:`Orthogonalize` and :class:`Muon` take torch tensors and enqueue on the current stream.  Objects belong to the device that was current when
 they were made; one object's calls share its workspace, so make them on one stream
 or order them.
 """
@@ -17,6 +17,8 @@ import math
 
 from . import huge2 as h2
 
+PRODUCTS = {"f32": 0, "f16": 1}
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # of a Newton-Schulz step
 NORM_ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "tanh": 2, "silu": 3}
 STATE_BLOCK = 256  # elements that share a scale in 8-bit states
 
@@ -28,6 +30,9 @@ EXPORTED = (
     "huge2_embedding", "huge2_embedding_grad_plan_create", "huge2_embedding_grad_execute",
     "huge2_embedding_grad_plan_kernel", "huge2_embedding_grad_plan_destroy",
     "huge2_adamw_plan_create", "huge2_adamw_step", "huge2_adamw_plan_destroy",
+    "huge2_orthogonalize_plan_create", "huge2_orthogonalize_execute",
+    "huge2_orthogonalize_plan_destroy",
+    "huge2_muon_plan_create", "huge2_muon_step", "huge2_muon_plan_destroy",
 )
 
 
@@ -68,6 +73,26 @@ class AdamWOptions(ctypes.Structure):
         [("step", ctypes.c_int64)]
 
 
+class NewtonSchulz(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("products", ctypes.c_int32),
+                ("coefficients", ctypes.POINTER(ctypes.c_double)), ("eps", ctypes.c_double)]
+
+
+class OrthogonalizeDesc(_Desc):
+    _fields_ = [(f, ctypes.c_int32) for f in ("batch", "rows", "cols", "dtype")]
+
+
+class MuonTensor(_Desc):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("param", "m", "copy")] + \
+        [(f, ctypes.c_int32) for f in ("rows", "cols", "dtype", "grad_dtype")] + \
+        [("weight_decay", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class MuonOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double),
+                ("nesterov", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -97,6 +122,14 @@ def lib():
             "huge2_adamw_plan_create": [out, ctypes.POINTER(AdamWTensor), i32, i32, vp],
             "huge2_adamw_step": [vp, vp, ctypes.POINTER(AdamWOptions), vp, vp],
             "huge2_adamw_plan_destroy": [vp],
+            "huge2_orthogonalize_plan_create": [out, ctypes.POINTER(OrthogonalizeDesc),
+                                                ctypes.POINTER(NewtonSchulz), vp],
+            "huge2_orthogonalize_execute": [vp] * 4,
+            "huge2_orthogonalize_plan_destroy": [vp],
+            "huge2_muon_plan_create": [out, ctypes.POINTER(MuonTensor), i32,
+                                       ctypes.POINTER(NewtonSchulz), vp],
+            "huge2_muon_step": [vp, vp, ctypes.POINTER(MuonOptions), vp, vp],
+            "huge2_muon_plan_destroy": [vp],
         }
         for name in EXPORTED:
             fn = getattr(L, name)
@@ -205,6 +238,56 @@ def huge2_adamw_step(plan, grad_ptrs, options, grad_scale_ptr=0, stream=0):
 
 def huge2_adamw_plan_destroy(plan):
     h2._check(lib().huge2_adamw_plan_destroy(plan), "huge2_adamw_plan_destroy")
+
+
+def huge2_orthogonalize_plan_create(desc, ns, stream=0):
+    plan = ctypes.c_void_p()
+    h2._check(lib().huge2_orthogonalize_plan_create(ctypes.byref(plan), ctypes.byref(desc),
+                                                    ctypes.byref(ns), stream),
+              "huge2_orthogonalize_plan_create")
+    return plan
+
+
+def huge2_orthogonalize_execute(plan, x_ptr, y_ptr, stream=0):
+    h2._check(lib().huge2_orthogonalize_execute(plan, x_ptr, y_ptr, stream),
+              "huge2_orthogonalize_execute")
+
+
+def huge2_orthogonalize_plan_destroy(plan):
+    h2._check(lib().huge2_orthogonalize_plan_destroy(plan), "huge2_orthogonalize_plan_destroy")
+
+
+def huge2_muon_plan_create(tensors, ns, stream=0):
+    """tensors: a sequence of :class:`MuonTensor`."""
+    plan = ctypes.c_void_p()
+    arr = (MuonTensor * len(tensors))(*tensors)
+    h2._check(lib().huge2_muon_plan_create(ctypes.byref(plan), arr, len(tensors),
+                                           ctypes.byref(ns), stream), "huge2_muon_plan_create")
+    return plan
+
+
+def huge2_muon_step(plan, grad_ptrs, options, grad_scale_ptr=0, stream=0):
+    """grad_ptrs: the address of an array of device pointers, one a tensor."""
+    h2._check(lib().huge2_muon_step(plan, grad_ptrs, ctypes.byref(options), grad_scale_ptr,
+                                    stream), "huge2_muon_step")
+
+
+def huge2_muon_plan_destroy(plan):
+    h2._check(lib().huge2_muon_plan_destroy(plan), "huge2_muon_plan_destroy")
+
+
+def newton_schulz(steps=5, coefficients=COEFFICIENTS, products="f32", eps=1e-7):
+    """:class:`NewtonSchulz` of `steps` steps, with one triple of coefficients or one for each."""
+    if products not in PRODUCTS:
+        raise ValueError("unknown products %r (f32, f16)" % (products,))
+    if steps != int(steps) or not 1 <= steps <= 32:
+        raise ValueError("steps must be 1 to 32")
+    triples = [tuple(t) for t in coefficients] if hasattr(coefficients[0], "__len__") else \
+        [tuple(coefficients)] * steps
+    if len(triples) != steps or any(len(t) != 3 for t in triples):
+        raise ValueError("coefficients must be one triple, or one for each of %d steps" % steps)
+    values = (ctypes.c_double * (3 * steps))(*(v for t in triples for v in t))
+    return NewtonSchulz(steps, PRODUCTS[products], values, eps)
 
 
 # ---- torch conveniences -----------------------------------------------------
@@ -438,7 +521,42 @@ class Embedding(_Owner):
         return huge2_embedding_grad_plan_kernel(self._open(), tokens)
 
 
-class AdamW(_Owner):
+class _Optimizer(_Owner):
+    """The gradients of a step over a list of parameters."""
+
+    def _gradients(self, grads, grad_scale):
+        """An array of the gradients' pointers (0: None) and the scale's pointer."""
+        k = len(self._sizes)
+        if len(grads) != k:
+            raise ValueError("%d gradients for %d parameters" % (len(grads), k))
+        try:
+            ptrs = self._pointers(grads, self._sizes, self.grad_dtypes)
+        except TypeError:  # some are None
+            kept = [i for i, g in enumerate(grads) if g is not None]
+            ptrs = [0] * k
+            for i, p in zip(kept, self._pointers(*([x[i] for i in kept] for x in (
+                    grads, self._sizes, self.grad_dtypes)))):
+                ptrs[i] = p
+        sp = 0
+        if grad_scale is not None:
+            if grad_scale.get_device() != self._index or \
+                    grad_scale.dtype != _torch().float32 or grad_scale.numel() != 1:
+                raise ValueError("grad_scale must be one float32 on %s" % self.device)
+            sp = grad_scale.data_ptr()
+        return array.array("Q", ptrs), sp
+
+    def _pointers(self, grads, sizes, dtypes):
+        # whole lists at a time: a loop over each gradient's properties takes twice as long
+        T = _torch().Tensor
+        if list(map(T.numel, grads)) != sizes or [g.dtype for g in grads] != dtypes or \
+                not all(map(T.is_contiguous, grads)) or \
+                list(map(T.get_device, grads)) != [self._index] * len(sizes):
+            raise ValueError("gradients must be contiguous tensors on %s of their parameters' "
+                             "sizes and of the types %s" % (self.device, dtypes))
+        return list(map(T.data_ptr, grads))
+
+
+class AdamW(_Optimizer):
     """AdamW over a list of parameters, all in one call, in place.
 
     params        contiguous float32 or bfloat16 tensors.
@@ -524,34 +642,113 @@ class AdamW(_Owner):
         a float32 device tensor of one element that multiplies every gradient.  A step that is
         recorded into a graph keeps its step number, lr, betas and gradients in every replay:
         enqueue the steps of a training loop outside of it."""
-        k = len(self._sizes)
-        if len(grads) != k:
-            raise ValueError("%d gradients for %d parameters" % (len(grads), k))
-        try:
-            ptrs = self._pointers(grads, self._sizes, self.grad_dtypes)
-        except TypeError:  # some are None
-            kept = [i for i, g in enumerate(grads) if g is not None]
-            ptrs = [0] * k
-            for i, p in zip(kept, self._pointers(*([x[i] for i in kept] for x in (
-                    grads, self._sizes, self.grad_dtypes)))):
-                ptrs[i] = p
-        sp = 0
-        if grad_scale is not None:
-            if grad_scale.get_device() != self._index or \
-                    grad_scale.dtype != _torch().float32 or grad_scale.numel() != 1:
-                raise ValueError("grad_scale must be one float32 on %s" % self.device)
-            sp = grad_scale.data_ptr()
-        ptrs = array.array("Q", ptrs)
+        ptrs, sp = self._gradients(grads, grad_scale)
         huge2_adamw_step(self._open(), ptrs.buffer_info()[0],
                          AdamWOptions(lr, betas[0], betas[1], eps, step), sp,
                          self._stream(self._index))
 
-    def _pointers(self, grads, sizes, dtypes):
-        # whole lists at a time: a loop over each gradient's properties takes twice as long
-        T = _torch().Tensor
-        if list(map(T.numel, grads)) != sizes or [g.dtype for g in grads] != dtypes or \
-                not all(map(T.is_contiguous, grads)) or \
-                list(map(T.get_device, grads)) != [self._index] * len(sizes):
-            raise ValueError("gradients must be contiguous tensors on %s of their parameters' "
-                             "sizes and of the types %s" % (self.device, dtypes))
-        return list(map(T.data_ptr, grads))
+
+class Orthogonalize(_Owner):
+    """Newton-Schulz steps of matrices of one shape [..., rows, cols], which bring their singular
+    values near 1.  products: "f32" (results as of products in fp32, the default for float32) or
+    "f16" (within 2^-10 of a result's norm, the default for bfloat16).  coefficients: one triple
+    (a, b, c), or one for each step."""
+    _destroy = staticmethod(huge2_orthogonalize_plan_destroy)
+
+    def __init__(self, shape, dtype, products=None, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
+        torch = _torch()
+        if len(shape) < 2:
+            raise ValueError("x must have rows and columns")
+        self.device = _current_device()
+        self._index, self._stream = self.device.index, _raw_stream()
+        self.shape, self.dtype = torch.Size(shape), dtype
+        code = _type_code(dtype)
+        self.products = products or ("f32" if dtype == torch.float32 else "f16")
+        self.desc = OrthogonalizeDesc(math.prod(shape[:-2]), *shape[-2:], code)
+        self._plan = huge2_orthogonalize_plan_create(
+            self.desc, newton_schulz(steps, coefficients, self.products, eps),
+            self._stream(self._index))
+
+    def __call__(self, x, out=None):
+        xp = _take(x, "x", self._index, self.shape, self.dtype)
+        if out is None:
+            out = _torch().empty(self.shape, dtype=self.dtype, device=self.device)
+        huge2_orthogonalize_execute(self._open(), xp,
+                                    _take(out, "out", self._index, self.shape, self.dtype),
+                                    self._stream(self._index))
+        return out
+
+
+class Muon(_Optimizer):
+    """The Muon step over a list of matrices, all in one call, in place: momentum, whose
+    Newton-Schulz steps are the update.  Other parameters (norms, biases, tables) go to
+    :class:`AdamW`.
+
+    params        contiguous float32 or bfloat16 tensors of two axes or more; the first are the
+                  rows (a convolution's weights: its first channels).
+    weight_decay  one number, or one for each parameter.
+    scales        None (sqrt(max(1, rows / cols))), or for each parameter what its update is
+                  multiplied by.
+    copies        None, or for each parameter None or a bfloat16 tensor that receives the
+                  updated parameter (the working weights of float32 parameters).
+    grad_dtypes   None (the copies', else the parameters' own types), or one for each parameter.
+    m             a list of float32 momenta to go on from; made as zeros where not given.
+    products, steps, coefficients, eps
+                  of the Newton-Schulz steps, as in :class:`Orthogonalize` (products: "f32" if
+                  any parameter is float32).
+    """
+    _destroy = staticmethod(huge2_muon_plan_destroy)
+
+    def __init__(self, params, weight_decay=0.0, scales=None, copies=None, grad_dtypes=None,
+                 m=None, products=None, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
+        torch = _torch()
+        self.device = _current_device()
+        self._index, self._stream = self.device.index, _raw_stream()
+        self.params = list(params)
+        k = len(self.params)
+        if any(p.dim() < 2 or p.numel() == 0 for p in self.params):
+            raise ValueError("parameters must be matrices (two axes or more, no empty one)")
+        shapes = [(p.shape[0], p.numel() // p.shape[0]) for p in self.params]
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else \
+            [weight_decay] * k
+        self.scales = [math.sqrt(max(1.0, r / c)) for r, c in shapes] if scales is None else \
+            list(scales)
+        self.copies = list(copies) if copies is not None else [None] * k
+        self.m = [torch.zeros(p.shape, dtype=torch.float32, device=self.device)
+                  for p in self.params] if m is None else list(m)
+        if grad_dtypes is None:
+            grad_dtypes = [(p if c is None else c).dtype for p, c in zip(self.params, self.copies)]
+        self.grad_dtypes = list(grad_dtypes)
+        if any(len(x) != k for x in (decay, self.scales, self.copies, self.m, self.grad_dtypes)):
+            raise ValueError("every list needs one entry for each of %d parameters" % k)
+        self.products = products or \
+            ("f32" if any(p.dtype == torch.float32 for p in self.params) else "f16")
+        tensors = []
+        for p, mt, c, shape, gd, wd, scale in zip(self.params, self.m, self.copies, shapes,
+                                                  self.grad_dtypes, decay, self.scales):
+
+            def same(t, name, dtype):
+                if t.numel() != p.numel():
+                    raise ValueError("%s has %d elements, expected %d"
+                                     % (name, t.numel(), p.numel()))
+                return _take(t, name, self._index, t.shape, dtype)
+
+            tensors.append(MuonTensor(
+                param=same(p, "param", p.dtype), m=same(mt, "m", torch.float32),
+                copy=None if c is None else same(c, "copy", torch.bfloat16), rows=shape[0],
+                cols=shape[1], dtype=_type_code(p.dtype), grad_dtype=_type_code(gd),
+                weight_decay=wd, scale=scale))
+        self._sizes = [p.numel() for p in self.params]
+        self._plan = huge2_muon_plan_create(
+            tensors, newton_schulz(steps, coefficients, self.products, eps),
+            self._stream(self._index))
+
+    def step(self, grads, lr, momentum=0.95, nesterov=True, grad_scale=None):
+        """One step.  grads: for each parameter its gradient, of its size and gradient type, or
+        None (the parameter and its momentum stay as they are).  grad_scale: None, or a float32
+        device tensor of one element that multiplies every gradient.  A step that is recorded
+        into a graph keeps its lr, momentum and gradients in every replay."""
+        ptrs, sp = self._gradients(grads, grad_scale)
+        huge2_muon_step(self._open(), ptrs.buffer_info()[0],
+                        MuonOptions(lr, momentum, int(bool(nesterov))), sp,
+                        self._stream(self._index))
