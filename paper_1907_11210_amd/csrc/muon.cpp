@@ -112,7 +112,7 @@ size_t workspace(const NsMatrix& t, int parts) {
   const size_t whole = (size_t)t.mp * t.np * sizeof(half_bits);
   const size_t square = (size_t)t.mp * t.mp * sizeof(half_bits);
   return round256(parts * whole) + 2 * round256(2 * whole) + round256(2 * square) +
-         round256(parts * square) + round256(t.x_tiles * sizeof(float)) +
+         round256(parts * square) + round256(t.squares_count * sizeof(float)) +
          round256(t.norm_count * sizeof(double)) + 256;
 }
 void place(NsMatrix* t, int parts, char* at) {
@@ -128,7 +128,7 @@ void place(NsMatrix* t, int parts, char* at) {
   t->t1 = (half_bits*)take(2 * whole);
   t->a = (half_bits*)take(2 * square);
   t->b = (half_bits*)take(parts * square);
-  t->squares = (float*)take(t->x_tiles * sizeof(float));
+  t->squares = (float*)take(t->squares_count * sizeof(float));
   t->norm = (double*)take(t->norm_count * sizeof(double));
   t->mu = (float*)take(sizeof(float));
 }
@@ -145,21 +145,21 @@ void shape(NsMatrix* t, long long rows, long long cols) {
   t->norm_chunk = (int)(ceil_div(std::max(4096ll, ceil_div(t->count, 512)), 256) * 256);
   t->norm_count = (int)ceil_div(t->count, t->norm_chunk);
   const int size = tile_size(tile_of(*t));
-  t->x_tiles = (int)(ceil_div(t->mp, size) * ceil_div(t->np, size));
+  const int blocks = size == kNsLarge ? 4 : 1;  // of a tile whose squares are kept apart
+  t->squares_count = (int)(ceil_div(t->mp, size) * ceil_div(t->np, size)) * blocks;
 }
 
 // The products' tiles, cut along their sum where there are too few of them to fill the compute
 // units: `slots` counts partial tiles.
 void product_works(const NsEngine& e, const Group& g, int kind, std::vector<NsWork>* works,
                    std::vector<NsWork>* joins, int* slots) {
-  const int stage = ns_stage(e.parts);
   const auto each = [&](auto&& f) {
     for (int i = 0; i < g.count; ++i) {
       const NsMatrix& t = e.mats[g.first + i];
       const int size = tile_of(t), edge = tile_size(size);
       const int rows = (int)ceil_div(t.mp, edge);
       const int cols = (int)ceil_div(kind == kNsApply ? t.np : t.mp, edge);
-      const int stages = (kind == kNsGram ? t.np : t.mp) / stage;
+      const int stages = (kind == kNsGram ? t.np : t.mp) / ns_stage(e.parts, size);
       for (int r = 0; r < rows; ++r)
         for (int c = kind == kNsApply ? 0 : r; c < cols; ++c) f(i, size, r, c, stages);
     }
@@ -167,10 +167,10 @@ void product_works(const NsEngine& e, const Group& g, int kind, std::vector<NsWo
   const auto weight = [](int size) { return size ? 2 : 1; };  // of a stage
   long long all = 0;
   each([&](int, int size, int, int, int stages) { all += (long long)stages * weight(size); });
-  const long long share = std::max(16ll, all / 512);
+  const long long share = std::max(32ll, all / 512);
   *slots = 0;
   each([&](int i, int size, int r, int c, int stages) {
-    const int cuts = (int)std::max(1ll, std::min<long long>(stages / 8, stages * weight(size) / share));
+    const int cuts = (int)std::max(1ll, std::min<long long>(stages / 16, stages * weight(size) / share));
     NsWork w = {i, r, c, 0, stages, -1, 0, size};
     if (cuts > 1) {
       NsWork join = w;
@@ -274,21 +274,21 @@ huge2_status engine_run(const NsEngine& e, const Group& g, NsInput in, NsArgs ca
     const Step& s = e.steps[k];
     call.step = (int)k;
     call.from = (int)k & 1;
-    call.last = k + 1 == e.steps.size();
+    const bool last = k + 1 == e.steps.size();
     call.a = s.a, call.b = s.b, call.c = s.c;
     for (int kind = 0; kind < 3; ++kind) {
-      call.kind = kind;
+      call.kind = kind == kNsApply && last ? kNsLast : kind;
       call.in_scale = power(kind == kNsGram ? -2 * s.x : kind == kNsSquare ? -2 * s.gram : -s.poly - s.x);
       call.own_scale = power(kind == kNsSquare ? -s.gram : -s.x);
       call.out_scale = power(kind == kNsGram ? s.gram : kind == kNsSquare ? s.poly
-                             : call.last     ? 0
+                             : last          ? 0
                                              : e.steps[k + 1].x);
       call.works = (const NsWork*)(table + g.product[kind].at);
       if (st == HUGE2_OK)
-        st = launched(launch_ns_product(call, g.product[kind].count, e.parts, stream));
+        st = launched(launch_ns_product(call, g.product[kind].count, false, e.parts, stream));
       call.works = (const NsWork*)(table + g.join[kind].at);
       if (st == HUGE2_OK && g.join[kind].count)
-        st = launched(launch_ns_join(call, g.join[kind].count, e.parts, stream));
+        st = launched(launch_ns_product(call, g.join[kind].count, true, e.parts, stream));
     }
   }
   return st;

@@ -30,11 +30,20 @@ __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
   __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)from,
                                    (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
-// All of this wave's loads into LDS have arrived and its reads have been taken, in all waves.
+// All but the last LEFT of this wave's loads into LDS have arrived and its reads have been
+// taken, and so in all waves.
+template <int LEFT>
 __device__ __forceinline__ void stage_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+}
+
+// (By value: of two members of a structure the compiler else selects the addresses, and the
+// structure goes to scratch memory.)
+template <typename T>
+__device__ __forceinline__ T pick(bool first, T a, T b) {
+  return first ? a : b;
 }
 
 struct Parts4 {
@@ -85,6 +94,29 @@ __device__ __forceinline__ float input(const void* p, int bf16, long long i) {
   return bf16 ? to_f32<uint16_t>(((const uint16_t*)p)[i]) : ((const float*)p)[i];
 }
 
+// Four from element i, zeros from `end` on.  (A batch's matrices begin at any element.)
+__device__ __forceinline__ void input4(const void* p, int bf16, long long i, long long end,
+                                       float (&v)[4]) {
+  typedef u32x4 u32x4_any __attribute__((aligned(4)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef u32x2 u32x2_any __attribute__((aligned(2)));
+  if (i + 4 <= end) {
+    if (bf16) {
+      const u32x2 w = *(const u32x2_any*)((const uint16_t*)p + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    } else {
+      const u32x4 w = *(const u32x4_any*)((const float*)p + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = i + e < end ? input(p, bf16, i + e) : 0.f;
+  }
+}
+
 }  // namespace
 
 // The momentum's update, and sums of squares of what is orthogonalised.  In 64 bits: squares
@@ -99,15 +131,33 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
   const long long first = (long long)work.y * t.norm_chunk;
   const long long end = min(first + t.norm_chunk, t.count);
   double s = 0;
-  for (long long i = first + threadIdx.x; i < end; i += 256) {
-    const float g = input(src, t.grad_bf16, i) * gs;
-    float m = 0.f;
-    if (a.muon) {
-      m = a.momentum * t.momentum[i] + a.rest * g;
-      t.momentum[i] = m;
+  constexpr int kAhead = 4;  // vectors of four in flight
+  for (long long i = first + threadIdx.x * 4; i < end; i += kAhead * 1024) {
+    float g[kAhead][4], m[kAhead][4];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      input4(src, t.grad_bf16, i + k * 1024, end, g[k]);
+      if (a.muon) input4(t.momentum, 0, i + k * 1024, end, m[k]);
     }
-    const double u = update(a, g, m);
-    s += u * u;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const long long at = i + k * 1024;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        g[k][e] *= gs;
+        if (a.muon) m[k][e] = a.momentum * m[k][e] + a.rest * g[k][e];
+        const double u = update(a, g[k][e], m[k][e]);
+        s += u * u;
+      }
+      if (!a.muon) continue;
+      if (at + 4 <= end) {
+        *(float4*)(t.momentum + at) = make_float4(m[k][0], m[k][1], m[k][2], m[k][3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at + e < end) t.momentum[at + e] = m[k][e];
+      }
+    }
   }
   for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
@@ -148,7 +198,7 @@ __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
   }
   __syncthreads();
   // pieces of 8 elements of a fragment's row: two orientations, 64 rows, 8 pieces a row
-  half_bits* const to[2] = {t.tall ? t.t0 : t.x, t.tall ? t.x : t.t0};
+  half_bits* const to[2] = {pick(t.tall != 0, t.t0, t.x), pick(t.tall != 0, t.x, t.t0)};
 #pragma unroll
   for (int o = 0; o < 2; ++o) {
     const int depth = (o == 0) == (t.tall == 0) ? t.np : t.mp;  // columns of the fragments' matrix
@@ -178,85 +228,130 @@ __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
 
 namespace {
 
-// A tile of SIZE x SIZE of a product P Q^T by four waves, each a quarter.
-template <int PARTS, int SIZE>
+// A tile of SIZE x SIZE of a product P Q^T by four waves, each a quarter: KIND's operands, and
+// what becomes of the sums.
+template <int PARTS, int KIND, int SIZE>
 struct Product {
-  static constexpr int kStage = ns_stage(PARTS), kWave = SIZE / 2, kBlocks = kWave / 32;
-  static constexpr int kFrags = kStage / 16;                 // of a stage and row of fragments
-  static constexpr int kRows = SIZE / 32;                    // rows of fragments of P, of Q
+  static constexpr bool kGram = KIND == kNsGram, kSquare = KIND == kNsSquare;
+  static constexpr bool kApply = KIND == kNsApply || KIND == kNsLast;
+  static constexpr int kStage = ns_stage(PARTS, SIZE == kNsLarge);
+  static constexpr int kBlocks = SIZE / 64;     // of 32 x 32, along a side of a wave's quarter
+  static constexpr int kOfWave = kBlocks * kBlocks;
+  static constexpr int kFrags = kStage / 16;    // of a stage and row of fragments
+  static constexpr int kRows = SIZE / 32;       // rows of fragments of P, of Q
   static constexpr int kStageFrags = 2 * kRows * kFrags * PARTS;
+  static constexpr int kLoads = kStageFrags / 4;  // of a wave and stage
   static constexpr int kBytes = kStageFrags * 1024;
-  typedef f32x16 Acc[kBlocks][kBlocks];
+  typedef f32x16 Acc[kOfWave];
 
-  // Stage s: fragments [P, Q][row][column][part] in LDS.
-  static __device__ __forceinline__ void issue(const half_bits* const (&op)[2],
-                                               const size_t (&plane)[2], const int (&row0)[2],
-                                               const int (&rows)[2], int depth, int s, char* lds) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-#pragma unroll
-    for (int i = 0; i < kStageFrags / 4; ++i) {
-      const int f = i * 4 + wave, part = f % PARTS, col = f / PARTS % kFrags;
-      const int row = f / PARTS / kFrags % kRows, side = f / PARTS / kFrags / kRows;
-      // (rows behind the end: the last once more, for results that are not stored)
-      const int r = min(row0[side] + row, rows[side] - 1);
-      const half_bits* from = op[side] + part * plane[side] +
-                              ((size_t)r * (depth / 16) + s * kFrags + col) * kNsFrag + lane * 8;
-      load_to_lds(from, lds + f * 1024);
-    }
+  static __device__ __forceinline__ int wave() {
+    return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   }
 
-  static __device__ __forceinline__ void multiply(const char* lds, Acc& acc) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wi = wave >> 1, wj = wave & 1;
+  struct Frags {
+    half8 p[kFrags][kBlocks][PARTS], q[kFrags][kBlocks][PARTS];
+  };
+  // Fragments lie in a stage's buffer as [P, Q][row][column][part].
+  static __device__ __forceinline__ void read(const char* lds, Frags& f) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int k = 0; k < kFrags; ++k) {
-      half8 p[kBlocks][PARTS], q[kBlocks][PARTS];
+    for (int k = 0; k < kFrags; ++k)
 #pragma unroll
       for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
         for (int h = 0; h < PARTS; ++h) {
           const auto at = [&](int row) { return ((row * kFrags + k) * PARTS + h) * 1024 + lane * 16; };
-          p[i][h] = *(const half8*)(lds + at(wi * kBlocks + i));
-          q[i][h] = *(const half8*)(lds + at(kRows + wj * kBlocks + i));
+          f.p[k][i][h] = *(const half8*)(lds + at((wave() >> 1) * kBlocks + i));
+          f.q[k][i][h] = *(const half8*)(lds + at(kRows + (wave() & 1) * kBlocks + i));
         }
+  }
+  static __device__ __forceinline__ void multiply(const Frags& f, Acc& acc) {
 #pragma unroll
-      for (int i = 0; i < kBlocks; ++i)
+    for (int k = 0; k < kFrags; ++k) {
+      // (the products of one sum apart from each other)
 #pragma unroll
-        for (int j = 0; j < kBlocks; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[i][0], q[j][0], acc[i][j], 0, 0, 0);
-          if constexpr (PARTS == 2) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[i][0], q[j][1], acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[i][1], q[j][0], acc[i][j], 0, 0, 0);
-          }
-        }
+      for (int h = 0; h < (PARTS == 2 ? 3 : 1); ++h)
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+          for (int j = 0; j < kBlocks; ++j)
+            acc[i * kBlocks + j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                f.p[k][i][h == 2], f.q[k][j][h == 1], acc[i * kBlocks + j], 0, 0, 0);
     }
   }
 
   static __device__ __forceinline__ void run(const NsArgs& a, const NsMatrix& t, const NsWork& w,
                                              char* lds, Acc& acc) {
-    const half_bits* const op[2] = {a.kind == kNsGram ? t.x : a.kind == kNsSquare ? t.a : t.b,
-                                    a.kind == kNsGram ? t.x : a.kind == kNsSquare ? t.a
-                                    : a.from               ? t.t1
-                                                           : t.t0};
-    const int depth = a.kind == kNsGram ? t.np : t.mp;
+    const int lane = threadIdx.x & 63;
+    const half_bits* const t_now = pick(a.from != 0, t.t1, t.t0);
+    const half_bits* const op[2] = {kGram ? t.x : kSquare ? t.a : t.b,
+                                    kGram ? t.x : kSquare ? t.a : t_now};
+    const int depth = (kGram ? t.np : t.mp) / 16;  // columns of fragments
     const size_t square = (size_t)t.mp * t.mp, whole = (size_t)t.mp * t.np;
-    const size_t plane[2] = {a.kind == kNsGram ? whole : square,
-                             a.kind == kNsSquare ? square : whole};
-    const int row0[2] = {w.ti * kRows, w.tj * kRows};
-    const int rows[2] = {t.mp / 32, (a.kind == kNsApply ? t.np : t.mp) / 32};
+    const size_t plane[2] = {kGram ? whole : square, kSquare ? square : whole};
+    const int rows[2] = {t.mp / 32, (kApply ? t.np : t.mp) / 32};
+    // a wave's fragments of stage k0
+    const half_bits* from[kLoads];
 #pragma unroll
-    for (int i = 0; i < kBlocks; ++i)
+    for (int i = 0; i < kLoads; ++i) {
+      const int f = i * 4 + wave(), part = f % PARTS, col = f / PARTS % kFrags;
+      const int row = f / PARTS / kFrags % kRows;
+      const bool second = f / PARTS / kFrags / kRows;
+      // (rows behind the end: the last once more, for results that are not stored)
+      const int r = min(pick(second, w.tj, w.ti) * kRows + row, pick(second, rows[1], rows[0]) - 1);
+      from[i] = pick(second, op[1], op[0]) + part * pick(second, plane[1], plane[0]) +
+                ((size_t)r * depth + (size_t)w.k0 * kFrags + col) * kNsFrag;
+    }
 #pragma unroll
-      for (int j = 0; j < kBlocks; ++j)
+    for (int k = 0; k < kOfWave; ++k)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    issue(op, plane, row0, rows, depth, w.k0, lds);
-    for (int s = w.k0; s < w.k1; ++s) {
-      stage_barrier();
-      char* const now = lds + (s - w.k0 & 1) * kBytes;
-      char* const next = lds + (s - w.k0 + 1 & 1) * kBytes;
-      if (s + 1 < w.k1) issue(op, plane, row0, rows, depth, s + 1, next);
+      for (int e = 0; e < 16; ++e) acc[k][e] = 0.f;
+    // While a stage is multiplied from registers, the next is read from LDS and the three behind
+    // it arrive.
+    const int stages = w.k1 - w.k0;
+    const auto buffer = [&](int s) { return lds + s % kNsBuffers * kBytes; };
+    const auto load = [&](int s) {
+      if (s >= stages) return;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        load_to_lds(from[i] + lane * 8, buffer(s) + (i * 4 + wave()) * 1024);
+        from[i] += kFrags * kNsFrag;
+      }
+    };
+    Frags f[2];
+#pragma unroll
+    for (int k = 0; k < kNsBuffers; ++k) load(k);
+    if (stages < kNsBuffers)
+      stage_barrier<0>();
+    else
+      stage_barrier<(kNsBuffers - 1) * kLoads>();
+    read(buffer(0), f[0]);
+    int s = 0;
+    // (stage s + 1 has arrived, of the later ones two are on their way)
+    const auto step = [&](Frags& now, Frags& next) {
+      stage_barrier<(kNsBuffers - 2) * kLoads>();
+      load(s + kNsBuffers);
+      read(buffer(s + 1), next);
       multiply(now, acc);
+      ++s;
+    };
+    while (s + kNsBuffers + 1 <= stages) {
+      step(f[0], f[1]);
+      step(f[1], f[0]);
+    }
+    // the last stages, all on their way or here
+    const auto last = [&](Frags& now, Frags& next) {
+      if (s + 1 < stages) {
+        stage_barrier<0>();
+        read(buffer(s + 1), next);
+      }
+      multiply(now, acc);
+      ++s;
+    };
+#pragma unroll 1
+    while (s < stages) {
+      last(f[0], f[1]);
+      if (s < stages) last(f[1], f[0]);
     }
   }
 
@@ -264,210 +359,275 @@ struct Product {
   static __device__ __forceinline__ void store_part(float* part, int slot, const Acc& acc) {
     float* to = part + (size_t)slot * kNsSlot + threadIdx.x * 4;
 #pragma unroll
-    for (int i = 0; i < kBlocks; ++i)
+    for (int k = 0; k < kOfWave; ++k)
 #pragma unroll
-      for (int j = 0; j < kBlocks; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *(float4*)(to + ((i * kBlocks + j) * 4 + g) * 1024) =
-              make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                          acc[i][j][4 * g + 3]);
+      for (int g = 0; g < 4; ++g)
+        *(float4*)(to + (k * 4 + g) * 1024) = make_float4(acc[k][4 * g], acc[k][4 * g + 1],
+                                                          acc[k][4 * g + 2], acc[k][4 * g + 3]);
   }
+  // A block's sums over the parts, in their order.
   static __device__ __forceinline__ void load_parts(const float* part, int slot, int slots,
-                                                    Acc& acc) {
-    const float* from = part + (size_t)slot * kNsSlot + threadIdx.x * 4;
+                                                    int block, f32x16& acc) {
+    const float* from = part + (size_t)slot * kNsSlot + block * 4096 + threadIdx.x * 4;
 #pragma unroll
-    for (int i = 0; i < kBlocks; ++i)
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < slots; ++k) {
 #pragma unroll
-      for (int j = 0; j < kBlocks; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int k = 0; k < slots; ++k) {
-            const float4 v =
-                *(const float4*)(from + (size_t)k * kNsSlot + ((i * kBlocks + j) * 4 + g) * 1024);
-            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-          }
-          acc[i][j][4 * g] = s.x, acc[i][j][4 * g + 1] = s.y;
-          acc[i][j][4 * g + 2] = s.z, acc[i][j][4 * g + 3] = s.w;
-        }
-  }
-
-  // Four elements of a lane, at rows i to i + 3 and column j of the tile's matrix: where they lie
-  // in its transpose's fragments (`depth` columns), and after transpose4 in its own.
-  static __device__ __forceinline__ size_t across(int i, int j, int depth) {
-    return ((size_t)(j / 32) * (depth / 16) + i / 16) * kNsFrag + (i / 8 & 1) * 256 + (j & 31) * 8 +
-           (i & 4);
-  }
-  static __device__ __forceinline__ size_t along(int i, int j, int depth) {
-    const int r = i + (j & 3), k = j & ~3;
-    return ((size_t)(r / 32) * (depth / 16) + k / 16) * kNsFrag + (k / 8 & 1) * 256 + (r & 31) * 8 +
-           (k & 4);
-  }
-  static __device__ __forceinline__ void put(half_bits* to, size_t at, half4 v) {
-    *(half4*)(to + at) = v;
-  }
-
-  static __device__ __forceinline__ void finish(const NsArgs& a, const NsMatrix& t,
-                                                const NsWork& w, float* lds, Acc& acc) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int i0 = w.ti * SIZE + (wave >> 1) * kWave + (lane >> 5) * 4;
-    const int j0 = w.tj * SIZE + (wave & 1) * kWave + (lane & 31);
-    const size_t square = (size_t)t.mp * t.mp, whole = (size_t)t.mp * t.np;
-    float mu;
-    if (a.kind == kNsGram) {
-      mu = 1.f / (float)t.m;  // (any value would do: in the first step X has norm 1)
-      if (a.step > 0) {
-        float s = 0.f;
-        for (int i = threadIdx.x; i < t.x_tiles; i += 256) s += t.squares[i];
-        mu = block_total(s, lds) / (float)t.m;
-      }
-      if (w.ti == 0 && w.tj == 0 && threadIdx.x == 0) *t.mu = mu;
-    } else {
-      mu = *t.mu;
-    }
-    const float linear = a.b + 2.f * a.c * mu, constant = a.a + mu * (a.b + mu * a.c);
-    float squares = 0.f;
-#pragma unroll
-    for (int bi = 0; bi < kBlocks; ++bi) {
-#pragma unroll
-      for (int bj = 0; bj < kBlocks; ++bj) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int i = i0 + bi * 32 + g * 8, j = j0 + bj * 32;
-          if (i >= t.mp || j >= (a.kind == kNsApply ? t.np : t.mp)) continue;  // whole blocks
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = acc[bi][bj][4 * g + e] * a.in_scale;
-          if (a.kind == kNsGram) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (i + e == j && j < t.m) v[e] -= mu;
-              v[e] *= a.out_scale;
-            }
-            const Parts4 p = split4(v);
-            const size_t to = along(i, j, t.mp);
-            put(t.a, to, transpose4(p.hi));
-            put(t.a + square, to, transpose4(p.lo));
-            if (w.ti != w.tj) {
-              put(t.a, across(i, j, t.mp), p.hi);
-              put(t.a + square, across(i, j, t.mp), p.lo);
-            }
-          } else if (a.kind == kNsSquare) {
-            const size_t at = across(i, j, t.mp);  // (A is symmetric)
-            const half4 hi = *(const half4*)(t.a + at), lo = *(const half4*)(t.a + square + at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              v[e] = (a.c * v[e] + linear * (((float)hi[e] + (float)lo[e]) * a.own_scale)) *
-                     a.out_scale;
-            const Parts4 p = split4(v);
-            const size_t to = along(i, j, t.mp);
-            put(t.b, to, transpose4(p.hi));
-            if (PARTS == 2) put(t.b + square, to, transpose4(p.lo));
-            if (w.ti != w.tj) {
-              put(t.b, at, p.hi);
-              if (PARTS == 2) put(t.b + square, at, p.lo);
-            }
-          } else {
-            const size_t at = across(i, j, t.mp);
-            const half_bits* own = a.from ? t.t1 : t.t0;
-            const half4 hi = *(const half4*)(own + at), lo = *(const half4*)(own + whole + at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              v[e] += constant * (((float)hi[e] + (float)lo[e]) * a.own_scale);
-            if (!a.last) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                squares += v[e] * v[e];
-                v[e] *= a.out_scale;
-              }
-              const Parts4 p = split4(v);
-              const size_t to = along(i, j, t.np);
-              put(t.x, to, transpose4(p.hi));
-              if (PARTS == 2) put(t.x + whole, to, transpose4(p.lo));
-              put((a.from ? t.t0 : t.t1), at, p.hi);
-              put((a.from ? t.t0 : t.t1) + whole, at, p.lo);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (i + e < t.m && j < t.n) result(a, t, i + e, j, v[e]);
-            }
-          }
-        }
-      }
-    }
-    if (a.kind == kNsApply && !a.last) {
-      squares = block_total(squares, lds);
-      if (threadIdx.x == 0) {
-        const int across_tiles = (t.np + SIZE - 1) / SIZE;
-        t.squares[w.ti * across_tiles + w.tj] = squares;
+      for (int g = 0; g < 4; ++g) {
+        const float4 v = *(const float4*)(from + (size_t)k * kNsSlot + g * 1024);
+        acc[4 * g] += v.x, acc[4 * g + 1] += v.y, acc[4 * g + 2] += v.z, acc[4 * g + 3] += v.w;
       }
     }
   }
 
-  static __device__ __forceinline__ void result(const NsArgs& a, const NsMatrix& t, int i, int j,
-                                                float v) {
-    const long long at = t.tall ? (long long)j * t.m + i : (long long)i * t.n + j;
-    if (a.out) {
-      if (t.bf16)
-        ((uint16_t*)a.out)[t.out_at + at] = f32_to_bf16_rne(v);
-      else
-        ((float*)a.out)[t.out_at + at] = v;
+  static __device__ __forceinline__ float mean_square(const NsArgs& a, const NsMatrix& t,
+                                                      const NsWork& w, float* lds) {
+    if (!kGram) return *t.mu;
+    float mu = 1.f / (float)t.m;  // (any value would do: in the first step X has norm 1)
+    if (a.step > 0) {
+      float s = 0.f;
+      for (int i = threadIdx.x; i < t.squares_count; i += 256) s += t.squares[i];
+      mu = block_total(s, lds) / (float)t.m;
+    }
+    if (w.ti == 0 && w.tj == 0 && threadIdx.x == 0) *t.mu = mu;
+    return mu;
+  }
+
+  // Blocks of 32 x 32: of a tile, by the wave and its number.
+  static __device__ __forceinline__ int block_row(const NsWork& w, int k) {
+    return w.ti * kRows + (wave() >> 1) * kBlocks + k / kBlocks;
+  }
+  static __device__ __forceinline__ int block_column(const NsWork& w, int k) {
+    return w.tj * kRows + (wave() & 1) * kBlocks + k % kBlocks;
+  }
+  static __device__ __forceinline__ bool inside(const NsMatrix& t, int bi, int bj) {
+    return bi * 32 < t.mp && bj * 32 < (kApply ? t.np : t.mp);
+  }
+  // A lane has four elements of each of four groups of rows, at one column.  In the fragments of
+  // the block's transpose (`depth` columns of them) they lie at across + 256 g, in its own after
+  // transpose4 at along + 64 g.
+  static __device__ __forceinline__ half_bits* across(half_bits* p, int bi, int bj, int depth) {
+    const int lane = threadIdx.x & 63;
+    return p + ((size_t)bj * depth + 2 * bi) * kNsFrag + ((lane & 31) * 8 + (lane >> 5) * 4);
+  }
+  static __device__ __forceinline__ half_bits* along(half_bits* p, int bi, int bj, int depth) {
+    const int lane = threadIdx.x & 63, r = (lane >> 5) * 4 + (lane & 3), k = lane & 28;
+    return p + ((size_t)bi * depth + 2 * bj) * kNsFrag +
+           ((k >> 4) * kNsFrag + (k >> 3 & 1) * 256 + r * 8 + (k & 4));
+  }
+
+  // What is added to a block's sums: A', which is symmetric, or X.
+  struct Own {
+    half4 hi[4], lo[4];
+  };
+  static __device__ __forceinline__ void load_own(const NsArgs& a, const NsMatrix& t, int bi,
+                                                  int bj, Own& own) {
+    if (kGram || !inside(t, bi, bj)) return;
+    const size_t plane = (size_t)t.mp * (kSquare ? t.mp : t.np);
+    const half_bits* hi =
+        across(kSquare ? t.a : pick(a.from != 0, t.t1, t.t0), bi, bj, t.mp / 16);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      own.hi[g] = *(const half4*)(hi + g * 256);
+      own.lo[g] = *(const half4*)(hi + plane + g * 256);
+    }
+  }
+
+  // What becomes of a block's sums.
+  static __device__ __forceinline__ void finish(const NsArgs& a, const NsMatrix& t, bool mirror,
+                                                float mu, int bi, int bj, const Own& own,
+                                                const f32x16& acc, float& squares) {
+    if (!inside(t, bi, bj)) return;
+    const int lane = threadIdx.x & 63;
+    const size_t plane = (size_t)t.mp * (kApply ? t.np : t.mp);
+    const float linear =
+        (kApply ? a.a + mu * (a.b + mu * a.c) : a.b + 2.f * a.c * mu) * a.own_scale;
+    const float factor = kSquare ? a.c * a.in_scale : a.in_scale;
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      v[e] = factor * acc[e];
+      if (!kGram) v[e] += linear * ((float)own.hi[e / 4][e % 4] + (float)own.lo[e / 4][e % 4]);
+    }
+    if constexpr (KIND == kNsLast) {
+      result(a, t, bi, bj, v);
       return;
     }
-    const float p = input(t.param, t.bf16, at);
-    const float r = p * (1.f - a.lr * t.decay) - a.lr * t.scale * v;
+    if (kGram && bi == bj) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if ((lane >> 5) * 4 + e / 4 * 8 + e % 4 == (lane & 31) && bj * 32 + (lane & 31) < t.m)
+          v[e] -= mu;
+    }
+    half_bits* const to = along(kGram ? t.a : kSquare ? t.b : t.x, bi, bj,
+                                (kApply ? t.np : t.mp) / 16);
+    half_bits* const at =
+        across(kGram ? t.a : kSquare ? t.b : pick(a.from != 0, t.t0, t.t1), bi, bj, t.mp / 16);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (kApply) squares += v[4 * g + e] * v[4 * g + e];
+        f[e] = v[4 * g + e] * a.out_scale;
+      }
+      const Parts4 p = split4(f);
+      *(half4*)(to + g * 64) = transpose4(p.hi);
+      if (PARTS == 2 || kGram) *(half4*)(to + plane + g * 64) = transpose4(p.lo);
+      if (kApply || mirror) {
+        *(half4*)(at + g * 256) = p.hi;
+        if (PARTS == 2 || !kSquare) *(half4*)(at + plane + g * 256) = p.lo;
+      }
+    }
+  }
+
+  // The last step's values: the caller's result, or the parameters' update.
+  static __device__ __forceinline__ void result(const NsArgs& a, const NsMatrix& t, int bi, int bj,
+                                                const float (&v)[16]) {
+    const int lane = threadIdx.x & 63;
+    const int i = bi * 32 + (lane >> 5) * 4, j = bj * 32 + (lane & 31);
+    const long long down = t.tall ? 1 : t.n;
+    const long long at = t.tall ? (long long)j * t.m + i : (long long)i * t.n + j;
     if (t.bf16)
-      ((uint16_t*)t.param)[at] = f32_to_bf16_rne(r);
+      put_result<uint16_t>(a, t, i, j, at, down, v);
     else
-      ((float*)t.param)[at] = r;
-    if (t.copy) ((uint16_t*)t.copy)[at] = f32_to_bf16_rne(r);
+      put_result<uint32_t>(a, t, i, j, at, down, v);
+  }
+  template <typename T>
+  static __device__ __forceinline__ void put_result(const NsArgs& a, const NsMatrix& t, int i,
+                                                    int j, long long at, long long down,
+                                                    const float (&v)[16]) {
+    T* to = a.out ? (T*)a.out + t.out_at + at : (T*)t.param + at;
+    uint16_t* copy = a.out ? nullptr : (uint16_t*)t.copy;
+    if (copy) copy += at;
+    const bool in = j < t.n;
+    float p[16];
+    if (!a.out) {
+      const T* from = to;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = in && i + e / 4 * 8 + e % 4 < t.m ? to_f32<T>(*from) : 0.f;
+        from += e % 4 == 3 ? 5 * down : down;
+      }
+    }
+    const float keep = 1.f - a.lr * t.decay, rate = a.lr * t.scale;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      if (in && i + e / 4 * 8 + e % 4 < t.m) {
+        const float r = a.out ? v[e] : p[e] * keep - rate * v[e];
+        store_pack<T, 1>(to, pack<T, 1>({r}));
+        if (copy) *copy = f32_to_bf16_rne(r);
+      }
+      to += e % 4 == 3 ? 5 * down : down;
+      copy += e % 4 == 3 ? 5 * down : down;
+    }
+  }
+
+  // A tile's sums of squares, of each of kOfWave blocks of its waves where they are joined
+  // one by one, else of all and zeros.
+  static __device__ __forceinline__ void put_squares(const NsMatrix& t, const NsWork& w, int block,
+                                                     float squares, float* lds) {
+    if (KIND != kNsApply) return;
+    squares = block_total(squares, lds);
+    const int tile = w.ti * ((t.np + SIZE - 1) / SIZE) + w.tj;
+    if (block >= 0) {
+      if (threadIdx.x == 0) t.squares[tile * kOfWave + block] = squares;
+    } else if (threadIdx.x < kOfWave) {
+      t.squares[tile * kOfWave + threadIdx.x] = threadIdx.x ? 0.f : squares;
+    }
+  }
+
+  static __device__ __forceinline__ void tile(const NsArgs& a, const NsMatrix& t, const NsWork& w,
+                                              char* lds) {
+    Own own[kOfWave];
+    if (w.slot < 0) {
+#pragma unroll
+      for (int k = 0; k < kOfWave; ++k) load_own(a, t, block_row(w, k), block_column(w, k), own[k]);
+    }
+    Acc acc;
+    run(a, t, w, lds, acc);
+    if (w.slot >= 0) return store_part(a.part, w.slot, acc);
+    __syncthreads();
+    const float mu = mean_square(a, t, w, (float*)lds);
+    float squares = 0.f;
+    // (One block's code, which is run once: four times as long it waits for its own loads.)
+#pragma unroll 1
+    for (int k = 0; k < kOfWave; ++k) {
+      finish(a, t, w.ti != w.tj, mu, block_row(w, k), block_column(w, k), own[0], acc[0], squares);
+#pragma unroll
+      for (int i = 1; i < kOfWave; ++i) {
+        own[i - 1] = own[i];
+        acc[i - 1] = acc[i];
+      }
+    }
+    put_squares(t, w, -1, squares, (float*)lds);
+  }
+  static __device__ __forceinline__ void join(const NsArgs& a, const NsMatrix& t, const NsWork& w,
+                                              int block, float* lds) {
+    if (block >= kOfWave) return;
+    const int bi = block_row(w, block), bj = block_column(w, block);
+    Own own;
+    load_own(a, t, bi, bj, own);
+    f32x16 acc;
+    load_parts(a.part, w.slot, w.slots, block, acc);
+    const float mu = mean_square(a, t, w, lds);
+    float squares = 0.f;
+    finish(a, t, w.ti != w.tj, mu, bi, bj, own, acc, squares);
+    put_squares(t, w, block, squares, lds);
   }
 };
 
 }  // namespace
 
-template <int PARTS>
+template <int PARTS, int KIND>
 __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const NsWork w = a.works[blockIdx.x];
   if (a.skip[w.matrix >> 6] >> (w.matrix & 63) & 1) return;
   const NsMatrix t = a.mats[w.matrix];
-  const auto tile = [&](auto product) {
-    typedef decltype(product) Of;
-    typename Of::Acc acc;
-    Of::run(a, t, w, lds, acc);
-    if (w.slot >= 0) {
-      Of::store_part(a.part, w.slot, acc);
-    } else {
-      __syncthreads();
-      Of::finish(a, t, w, (float*)lds, acc);
-    }
-  };
   if (w.size)
-    tile(Product<PARTS, kNsLarge>());
+    Product<PARTS, KIND, kNsLarge>::tile(a, t, w, lds);
   else
-    tile(Product<PARTS, kNsSmall>());
+    Product<PARTS, KIND, kNsSmall>::tile(a, t, w, lds);
 }
 
-// Adds up the partial tiles, in their order.
-template <int PARTS>
+// Adds up the partial tiles, in their order, a block of each wave's to a workgroup.
+template <int PARTS, int KIND>
 __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a) {
   __shared__ float lds[4];
   const NsWork w = a.works[blockIdx.x];
   if (a.skip[w.matrix >> 6] >> (w.matrix & 63) & 1) return;
   const NsMatrix t = a.mats[w.matrix];
-  const auto tile = [&](auto product) {
-    typedef decltype(product) Of;
-    typename Of::Acc acc;
-    Of::load_parts(a.part, w.slot, w.slots, acc);
-    Of::finish(a, t, w, lds, acc);
-  };
   if (w.size)
-    tile(Product<PARTS, kNsLarge>());
+    Product<PARTS, KIND, kNsLarge>::join(a, t, w, blockIdx.y, lds);
   else
-    tile(Product<PARTS, kNsSmall>());
+    Product<PARTS, KIND, kNsSmall>::join(a, t, w, blockIdx.y, lds);
 }
+
+namespace {
+
+template <int PARTS, int KIND>
+void launch_kind(const NsArgs& a, unsigned works, bool join, hipStream_t stream) {
+  constexpr int kLds = kNsBuffers * Product<PARTS, KIND, kNsLarge>::kBytes;
+  static_assert(kLds <= 65536 && kNsBuffers * Product<PARTS, KIND, kNsSmall>::kBytes <= kLds, "");
+  if (join)
+    hipLaunchKernelGGL((ns_join_kernel<PARTS, KIND>), dim3(works, 4), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((ns_product_kernel<PARTS, KIND>), dim3(works), dim3(256), kLds, stream, a);
+}
+template <int PARTS>
+hipError_t launch_parts(const NsArgs& a, unsigned works, bool join, hipStream_t stream) {
+  switch (a.kind) {
+    case kNsGram: launch_kind<PARTS, kNsGram>(a, works, join, stream); break;
+    case kNsSquare: launch_kind<PARTS, kNsSquare>(a, works, join, stream); break;
+    case kNsApply: launch_kind<PARTS, kNsApply>(a, works, join, stream); break;
+    default: launch_kind<PARTS, kNsLast>(a, works, join, stream);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
 
 hipError_t launch_ns_norm(const NsInput& a, unsigned works, hipStream_t stream) {
   hipLaunchKernelGGL(ns_norm_kernel, dim3(works), dim3(256), 0, stream, a);
@@ -478,16 +638,10 @@ hipError_t launch_ns_pack(const NsInput& a, unsigned works, int parts, hipStream
                      stream, a);
   return hipGetLastError();
 }
-hipError_t launch_ns_product(const NsArgs& a, unsigned works, int parts, hipStream_t stream) {
-  const int lds = 2 * (parts == 2 ? Product<2, kNsLarge>::kBytes : Product<1, kNsLarge>::kBytes);
-  hipLaunchKernelGGL(parts == 2 ? ns_product_kernel<2> : ns_product_kernel<1>, dim3(works),
-                     dim3(256), lds, stream, a);
-  return hipGetLastError();
-}
-hipError_t launch_ns_join(const NsArgs& a, unsigned works, int parts, hipStream_t stream) {
-  hipLaunchKernelGGL(parts == 2 ? ns_join_kernel<2> : ns_join_kernel<1>, dim3(works), dim3(256), 0,
-                     stream, a);
-  return hipGetLastError();
+hipError_t launch_ns_product(const NsArgs& a, unsigned works, bool join, int parts,
+                             hipStream_t stream) {
+  return parts == 2 ? launch_parts<2>(a, works, join, stream)
+                    : launch_parts<1>(a, works, join, stream);
 }
 
 }  // namespace huge2

@@ -25,12 +25,12 @@ struct NsMatrix {
   half_bits* t1;      // ... and of odd ones
   half_bits* a;       // X X^T - mu I [m][m], hi and lo
   half_bits* b;       // [m][m]: hi, and with two parts lo
-  float* squares;     // [tiles of X]: of their elements
+  float* squares;     // [squares_count]: of X's elements, by tiles and their blocks
   double* norm;       // [norm_count]: sums of squares of the input
   float* mu;          // trace(X X^T) / m
   int m, n, mp, np;   // mp, np: rounded up to kNsPad
   int tall;           // the input is n x m
-  int x_tiles;        // tiles of X
+  int squares_count;
   int norm_count;
   int norm_chunk;     // elements of a sum
   long long count;    // m * n
@@ -51,16 +51,19 @@ struct NsWork {
   int size;    // of the tile: 0 kNsSmall, 1 kNsLarge
 };
 constexpr int kNsSmall = 64, kNsLarge = 128;
-constexpr int ns_stage(int parts) { return parts == 2 ? 32 : 64; }  // columns
+// Columns of a stage.
+constexpr int ns_stage(int parts, int size) { return (parts == 2 ? 16 : 32) * (size ? 1 : 2); }
+constexpr int kNsBuffers = 4;
 constexpr int kNsSlot = kNsLarge * kNsLarge;  // elements of a partial tile
 
-enum NsKind { kNsGram = 0, kNsSquare = 1, kNsApply = 2 };
+// Products: A = X X^T, A A, B X, and B X of the last step.
+enum NsKind { kNsGram = 0, kNsSquare = 1, kNsApply = 2, kNsLast = 3 };
 
 struct NsArgs {
   const NsMatrix* mats;
   const NsWork* works;
   float* part;
-  int kind, step, last;
+  int kind, step;
   int from;              // the step reads t0 or t1 and writes the other
   float a, b, c;         // of the step's polynomial
   float in_scale;        // of a product's sum
@@ -83,7 +86,7 @@ struct NsInput {
 
 hipError_t launch_ns_norm(const NsInput& a, unsigned works, hipStream_t stream);
 hipError_t launch_ns_pack(const NsInput& a, unsigned works, int parts, hipStream_t stream);
-hipError_t launch_ns_product(const NsArgs& a, unsigned works, int parts, hipStream_t stream);
-hipError_t launch_ns_join(const NsArgs& a, unsigned works, int parts, hipStream_t stream);
+hipError_t launch_ns_product(const NsArgs& a, unsigned works, bool join, int parts,
+                             hipStream_t stream);
 
 }  // namespace huge2
