@@ -26,6 +26,7 @@ struct Works {
 // Matrices whose products share launches.
 struct Group {
   int first, count;
+  int size[3];  // the largest tile of each product
   Works norm, pack, product[3], join[3];
 };
 
@@ -108,11 +109,18 @@ bool valid(const huge2_newton_schulz* ns) {
 int pad(int v) { return (v + kNsPad - 1) / kNsPad * kNsPad; }
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
+// Sums of squares by blocks of tiles of any size.
+size_t squares_room(const NsMatrix& t) {
+  size_t most = 0;
+  for (const NsTile& tile : kNsTiles)
+    most = std::max<size_t>(most, ceil_div(t.mp, tile.rows) * ceil_div(t.np, tile.cols) * tile.blocks());
+  return most;
+}
 size_t workspace(const NsMatrix& t, int parts) {
   const size_t whole = (size_t)t.mp * t.np * sizeof(half_bits);
   const size_t square = (size_t)t.mp * t.mp * sizeof(half_bits);
   return round256(parts * whole) + 2 * round256(2 * whole) + round256(2 * square) +
-         round256(parts * square) + round256(t.squares_count * sizeof(float)) +
+         round256(parts * square) + round256(squares_room(t) * sizeof(float)) +
          round256(t.norm_count * sizeof(double)) + 256;
 }
 void place(NsMatrix* t, int parts, char* at) {
@@ -128,13 +136,10 @@ void place(NsMatrix* t, int parts, char* at) {
   t->t1 = (half_bits*)take(2 * whole);
   t->a = (half_bits*)take(2 * square);
   t->b = (half_bits*)take(parts * square);
-  t->squares = (float*)take(t->squares_count * sizeof(float));
+  t->squares = (float*)take(squares_room(*t) * sizeof(float));
   t->norm = (double*)take(t->norm_count * sizeof(double));
   t->mu = (float*)take(sizeof(float));
 }
-
-int tile_of(const NsMatrix& t) { return t.mp >= 256; }
-int tile_size(int size) { return size ? kNsLarge : kNsSmall; }
 
 void shape(NsMatrix* t, long long rows, long long cols) {
   t->tall = rows > cols;
@@ -144,47 +149,76 @@ void shape(NsMatrix* t, long long rows, long long cols) {
   t->count = rows * cols;
   t->norm_chunk = (int)(ceil_div(std::max(4096ll, ceil_div(t->count, 512)), 256) * 256);
   t->norm_count = (int)ceil_div(t->count, t->norm_chunk);
-  const int size = tile_size(tile_of(*t));
-  const int blocks = size == kNsLarge ? 4 : 1;  // of a tile whose squares are kept apart
-  t->squares_count = (int)(ceil_div(t->mp, size) * ceil_div(t->np, size)) * blocks;
 }
 
-// The products' tiles, cut along their sum where there are too few of them to fill the compute
-// units: `slots` counts partial tiles.
-void product_works(const NsEngine& e, const Group& g, int kind, std::vector<NsWork>* works,
+// Tiles of a product, of the given size; f(row, column) of each if wanted.
+template <typename F>
+void each_tile(const NsMatrix& t, int kind, int size, F&& f) {
+  const NsTile& tile = kNsTiles[size];
+  const long long rows = ceil_div(t.mp, tile.rows);
+  const long long cols = ceil_div(kind == kNsApply ? t.np : t.mp, tile.cols);
+  for (long long r = 0; r < rows; ++r)
+    for (long long c = kind == kNsApply ? 0 : r * tile.rows / tile.cols; c < cols; ++c)
+      f((int)r, (int)c);
+}
+
+constexpr int kUnits = 256;  // compute units
+
+int tile_size(const NsMatrix& t, int kind, const long long (&tiles)[kNsSizes]) {
+  if (t.mp >= 256 && tiles[2] >= kUnits * 3 / 4) return 2;
+  return t.mp >= 128 && tiles[1] >= 32 ? 1 : 0;
+}
+
+// A product's tiles.  Where they do not fill the compute units, or leave some over that would
+// run alone, those are cut along their sum: `slots` counts partial tiles.
+void product_works(NsEngine& e, const Group& g, int kind, std::vector<NsWork>* works,
                    std::vector<NsWork>* joins, int* slots) {
-  const auto each = [&](auto&& f) {
-    for (int i = 0; i < g.count; ++i) {
-      const NsMatrix& t = e.mats[g.first + i];
-      const int size = tile_of(t), edge = tile_size(size);
-      const int rows = (int)ceil_div(t.mp, edge);
-      const int cols = (int)ceil_div(kind == kNsApply ? t.np : t.mp, edge);
-      const int stages = (kind == kNsGram ? t.np : t.mp) / ns_stage(e.parts, size);
-      for (int r = 0; r < rows; ++r)
-        for (int c = kind == kNsApply ? 0 : r; c < cols; ++c) f(i, size, r, c, stages);
-    }
-  };
-  const auto weight = [](int size) { return size ? 2 : 1; };  // of a stage
-  long long all = 0;
-  each([&](int, int size, int, int, int stages) { all += (long long)stages * weight(size); });
-  const long long share = std::max(32ll, all / 512);
+  long long tiles[kNsSizes] = {};
+  for (int i = 0; i < g.count; ++i)
+    for (int size = 0; size < kNsSizes; ++size)
+      each_tile(e.mats[g.first + i], kind, size, [&](int, int) { ++tiles[size]; });
+  std::vector<NsWork> all;
+  double cost = 0;  // of all, in stages of a 128 x 128 tile
+  const auto weight = [](const NsWork& w) { return w.size == 2 ? 2.0 : w.size == 1 ? 1.0 : 0.8; };
+  for (int i = 0; i < g.count; ++i) {
+    NsMatrix& t = e.mats[g.first + i];
+    const int size = tile_size(t, kind, tiles);
+    if (kind == kNsApply) t.squares_count = 0;
+    const int stages = (kind == kNsGram ? t.np : t.mp) / (kNsTiles[size].stage / e.parts);
+    each_tile(t, kind, size, [&](int r, int c) {
+      all.push_back({i, r, c, 0, stages, -1, 0, size});
+      cost += stages * weight(all.back());
+      if (kind == kNsApply) t.squares_count += kNsTiles[size].blocks();
+    });
+  }
+  std::stable_sort(all.begin(), all.end(), [&](const NsWork& a, const NsWork& b) {
+    return a.k1 * weight(a) > b.k1 * weight(b);
+  });
+  const double share = std::max(16.0, cost / kUnits);  // of a compute unit
+  // whole tiles, as many as all units take alike
+  const size_t whole = all.size() / kUnits * kUnits;
+  double left = 0;
+  for (size_t k = whole; k < all.size(); ++k) left += all[k].k1 * weight(all[k]);
   *slots = 0;
-  each([&](int i, int size, int r, int c, int stages) {
-    const int cuts = (int)std::max(1ll, std::min<long long>(stages / 16, stages * weight(size) / share));
-    NsWork w = {i, r, c, 0, stages, -1, 0, size};
+  for (size_t k = 0; k < all.size(); ++k) {
+    NsWork w = all[k];
+    const int stages = w.k1;
+    // the rest in pieces of what a unit has of it, or of what is over a unit's share
+    const double piece = k < whole ? share : std::max(16.0, left / kUnits);
+    const int cuts = (int)std::max(1.0, std::min(stages / 8.0, std::floor(stages * weight(w) / piece)));
     if (cuts > 1) {
       NsWork join = w;
       join.slot = *slots, join.slots = cuts;
       joins->push_back(join);
-      for (int k = 0; k < cuts; ++k) {
-        w.k0 = (int)((long long)stages * k / cuts), w.k1 = (int)((long long)stages * (k + 1) / cuts);
+      for (int c = 0; c < cuts; ++c) {
+        w.k0 = (int)((long long)stages * c / cuts), w.k1 = (int)((long long)stages * (c + 1) / cuts);
         w.slot = (*slots)++;
         works->push_back(w);
       }
     } else {
       works->push_back(w);
     }
-  });
+  }
 }
 
 constexpr size_t kGroupBytes = (size_t)4 << 30;  // matrices beyond start another group
@@ -197,7 +231,7 @@ huge2_status engine_create(NsEngine* e, const huge2_newton_schulz& ns, hipStream
   for (int i = 0; i < (int)e->mats.size(); ++i) {
     const size_t own = workspace(e->mats[i], e->parts);
     if (i == 0 || e->groups.back().count == kNsMatrices || bytes + own > kGroupBytes) {
-      e->groups.push_back({i, 0, {}, {}, {}, {}});
+      e->groups.push_back({i, 0, {}, {}, {}, {}, {}});
       bytes = 0;
     }
     ++e->groups.back().count;
@@ -228,6 +262,7 @@ huge2_status engine_create(NsEngine* e, const huge2_newton_schulz& ns, hipStream
       int slots;
       product_works(*e, g, kind, &works, &joins, &slots);
       most_slots = std::max(most_slots, slots);
+      for (const NsWork& w : works) g.size[kind] = std::max(g.size[kind], w.size);
       append(&g.product[kind], works);
       append(&g.join[kind], joins);
     }
@@ -285,10 +320,12 @@ huge2_status engine_run(const NsEngine& e, const Group& g, NsInput in, NsArgs ca
                                              : e.steps[k + 1].x);
       call.works = (const NsWork*)(table + g.product[kind].at);
       if (st == HUGE2_OK)
-        st = launched(launch_ns_product(call, g.product[kind].count, false, e.parts, stream));
+        st = launched(launch_ns_product(call, g.product[kind].count, g.size[kind], false,
+                                        e.parts, stream));
       call.works = (const NsWork*)(table + g.join[kind].at);
       if (st == HUGE2_OK && g.join[kind].count)
-        st = launched(launch_ns_product(call, g.join[kind].count, true, e.parts, stream));
+        st = launched(launch_ns_product(call, g.join[kind].count, g.size[kind], true, e.parts,
+                                        stream));
     }
   }
   return st;

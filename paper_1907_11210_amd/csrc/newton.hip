@@ -117,6 +117,39 @@ __device__ __forceinline__ void input4(const void* p, int bf16, long long i, lon
   }
 }
 
+// `of` elements of up to VW, at any element's alignment.
+template <typename T, int VW>
+__device__ __forceinline__ void load_some(const T* p, int of, float* f) {
+  typedef uint32_t words __attribute__((ext_vector_type(VW * sizeof(T) / 4 > 1 ? VW * sizeof(T) / 4 : 2)));
+  typedef words words_any __attribute__((aligned(sizeof(T))));
+  if (VW > 1 && of == VW) {
+    const words w = *(const words_any*)p;
+#pragma unroll
+    for (int e = 0; e < VW; ++e)
+      f[e] = sizeof(T) == 4 ? __uint_as_float(w[e])
+                            : __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VW; ++e) f[e] = e < of ? to_f32<T>(p[e]) : 0.f;
+  }
+}
+template <typename T, int VW>
+__device__ __forceinline__ void store_some(T* p, int of, const float (&f)[VW]) {
+  typedef uint32_t words __attribute__((ext_vector_type(VW * sizeof(T) / 4 > 1 ? VW * sizeof(T) / 4 : 2)));
+  typedef words words_any __attribute__((aligned(sizeof(T))));
+  if (VW > 1 && of == VW) {
+    const Pack<T, VW> r = pack<T, VW>(f);
+    words w;
+#pragma unroll
+    for (int e = 0; e < VW * (int)sizeof(T) / 4; ++e) w[e] = r.w[e];
+    *(words_any*)p = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < VW; ++e)
+      if (e < of) store_pack<T, 1>(p + e, pack<T, 1>({f[e]}));
+  }
+}
+
 }  // namespace
 
 // The momentum's update, and sums of squares of what is orthogonalised.  In 64 bits: squares
@@ -228,18 +261,20 @@ __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
 
 namespace {
 
-// A tile of SIZE x SIZE of a product P Q^T by four waves, each a quarter: KIND's operands, and
-// what becomes of the sums.
+// A tile of a product P Q^T by four waves, each a quarter: KIND's operands, and what becomes of
+// the sums.
 template <int PARTS, int KIND, int SIZE>
 struct Product {
+  static constexpr NsTile kTile = kNsTiles[SIZE];
   static constexpr bool kGram = KIND == kNsGram, kSquare = KIND == kNsSquare;
   static constexpr bool kApply = KIND == kNsApply || KIND == kNsLast;
-  static constexpr int kStage = ns_stage(PARTS, SIZE == kNsLarge);
-  static constexpr int kBlocks = SIZE / 64;     // of 32 x 32, along a side of a wave's quarter
-  static constexpr int kOfWave = kBlocks * kBlocks;
-  static constexpr int kFrags = kStage / 16;    // of a stage and row of fragments
-  static constexpr int kRows = SIZE / 32;       // rows of fragments of P, of Q
-  static constexpr int kStageFrags = 2 * kRows * kFrags * PARTS;
+  // blocks of 32 x 32 along the sides of a wave's quarter
+  static constexpr int kDown = kTile.rows / 64, kRight = kTile.cols / 64;
+  static constexpr int kOfWave = kDown * kRight;
+  static constexpr int kFrags = kTile.stage / 16 / PARTS;  // of a stage and row of fragments
+  static constexpr int kBuffers = kTile.buffers;
+  static constexpr int kP = kTile.rows / 32, kQ = kTile.cols / 32;  // rows of fragments
+  static constexpr int kStageFrags = (kP + kQ) * kFrags * PARTS;
   static constexpr int kLoads = kStageFrags / 4;  // of a wave and stage
   static constexpr int kBytes = kStageFrags * 1024;
   typedef f32x16 Acc[kOfWave];
@@ -249,21 +284,23 @@ struct Product {
   }
 
   struct Frags {
-    half8 p[kFrags][kBlocks][PARTS], q[kFrags][kBlocks][PARTS];
+    half8 p[kFrags][kDown][PARTS], q[kFrags][kRight][PARTS];
   };
   // Fragments lie in a stage's buffer as [P, Q][row][column][part].
   static __device__ __forceinline__ void read(const char* lds, Frags& f) {
     const int lane = threadIdx.x & 63;
+    const auto at = [&](int row, int k, int h) {
+      return *(const half8*)(lds + ((row * kFrags + k) * PARTS + h) * 1024 + lane * 16);
+    };
 #pragma unroll
     for (int k = 0; k < kFrags; ++k)
 #pragma unroll
-      for (int i = 0; i < kBlocks; ++i)
+      for (int h = 0; h < PARTS; ++h) {
 #pragma unroll
-        for (int h = 0; h < PARTS; ++h) {
-          const auto at = [&](int row) { return ((row * kFrags + k) * PARTS + h) * 1024 + lane * 16; };
-          f.p[k][i][h] = *(const half8*)(lds + at((wave() >> 1) * kBlocks + i));
-          f.q[k][i][h] = *(const half8*)(lds + at(kRows + (wave() & 1) * kBlocks + i));
-        }
+        for (int i = 0; i < kDown; ++i) f.p[k][i][h] = at((wave() >> 1) * kDown + i, k, h);
+#pragma unroll
+        for (int i = 0; i < kRight; ++i) f.q[k][i][h] = at(kP + (wave() & 1) * kRight + i, k, h);
+      }
   }
   static __device__ __forceinline__ void multiply(const Frags& f, Acc& acc) {
 #pragma unroll
@@ -272,11 +309,11 @@ struct Product {
 #pragma unroll
       for (int h = 0; h < (PARTS == 2 ? 3 : 1); ++h)
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i)
+        for (int i = 0; i < kDown; ++i)
 #pragma unroll
-          for (int j = 0; j < kBlocks; ++j)
-            acc[i * kBlocks + j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                f.p[k][i][h == 2], f.q[k][j][h == 1], acc[i * kBlocks + j], 0, 0, 0);
+          for (int j = 0; j < kRight; ++j)
+            acc[i * kRight + j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                f.p[k][i][h == 2], f.q[k][j][h == 1], acc[i * kRight + j], 0, 0, 0);
     }
   }
 
@@ -295,10 +332,11 @@ struct Product {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int f = i * 4 + wave(), part = f % PARTS, col = f / PARTS % kFrags;
-      const int row = f / PARTS / kFrags % kRows;
-      const bool second = f / PARTS / kFrags / kRows;
+      const int row = f / PARTS / kFrags;
+      const bool second = row >= kP;
       // (rows behind the end: the last once more, for results that are not stored)
-      const int r = min(pick(second, w.tj, w.ti) * kRows + row, pick(second, rows[1], rows[0]) - 1);
+      const int r = min(pick(second, w.tj * kQ + row - kP, w.ti * kP + row),
+                        pick(second, rows[1], rows[0]) - 1);
       from[i] = pick(second, op[1], op[0]) + part * pick(second, plane[1], plane[0]) +
                 ((size_t)r * depth + (size_t)w.k0 * kFrags + col) * kNsFrag;
     }
@@ -306,53 +344,61 @@ struct Product {
     for (int k = 0; k < kOfWave; ++k)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[k][e] = 0.f;
-    // While a stage is multiplied from registers, the next is read from LDS and the three behind
-    // it arrive.
+    // While a stage is multiplied from registers, the next is read from LDS and the ones behind
+    // it arrive.  (Behind the last stage it arrives again, so that every wait counts the same
+    // loads.)
     const int stages = w.k1 - w.k0;
-    const auto buffer = [&](int s) { return lds + s % kNsBuffers * kBytes; };
-    const auto load = [&](int s) {
-      if (s >= stages) return;
+    int ahead = 0;  // stages whose loads have been issued
+    int into = 0;   // the buffer that the next of them goes to
+    const auto load = [&] {
+      const int step = ahead + 1 < stages ? kFrags * kNsFrag : 0;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        load_to_lds(from[i] + lane * 8, buffer(s) + (i * 4 + wave()) * 1024);
-        from[i] += kFrags * kNsFrag;
+        load_to_lds(from[i] + lane * 8, lds + into * kBytes + (i * 4 + wave()) * 1024);
+        from[i] += step;
       }
+      ++ahead;
+      into = into + 1 == kBuffers ? 0 : into + 1;
     };
     Frags f[2];
 #pragma unroll
-    for (int k = 0; k < kNsBuffers; ++k) load(k);
-    if (stages < kNsBuffers)
-      stage_barrier<0>();
-    else
-      stage_barrier<(kNsBuffers - 1) * kLoads>();
-    read(buffer(0), f[0]);
-    int s = 0;
-    // (stage s + 1 has arrived, of the later ones two are on their way)
+    for (int k = 0; k < kBuffers; ++k) load();
+    stage_barrier<(kBuffers - 1) * kLoads>();
+    read(lds, f[0]);
+    int next_buffer = 1;
     const auto step = [&](Frags& now, Frags& next) {
-      stage_barrier<(kNsBuffers - 2) * kLoads>();
-      load(s + kNsBuffers);
-      read(buffer(s + 1), next);
+      stage_barrier<(kBuffers - 2) * kLoads>();
+      __builtin_amdgcn_sched_barrier(0);
+      read(lds + next_buffer * kBytes, next);
+      load();
       multiply(now, acc);
-      ++s;
+      order();
+      __builtin_amdgcn_sched_barrier(0);
+      next_buffer = next_buffer + 1 == kBuffers ? 0 : next_buffer + 1;
     };
-    while (s + kNsBuffers + 1 <= stages) {
+    int s = 0;
+#pragma unroll 1
+    for (; s + 2 <= stages; s += 2) {
       step(f[0], f[1]);
       step(f[1], f[0]);
     }
-    // the last stages, all on their way or here
-    const auto last = [&](Frags& now, Frags& next) {
-      if (s + 1 < stages) {
-        stage_barrier<0>();
-        read(buffer(s + 1), next);
-      }
-      multiply(now, acc);
-      ++s;
-    };
-#pragma unroll 1
-    while (s < stages) {
-      last(f[0], f[1]);
-      if (s < stages) last(f[1], f[0]);
-    }
+    if (s < stages) step(f[0], f[1]);
+    stage_barrier<0>();
+  }
+  // The order of a stage's instructions: reads and loads between products, which they else delay.
+  static __device__ __forceinline__ void order() {
+    constexpr int kReads = kFrags * PARTS * (kDown + kRight);
+    constexpr int kProducts = kFrags * (PARTS == 2 ? 3 : 1) * kOfWave;
+    constexpr int kEach = (kReads + kLoads + kProducts - 1) / kProducts + 1;
+    constexpr int kWith = (kReads + kEach - 1) / kEach;  // products followed by reads
+    unroll_stages<kProducts>([](auto i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      constexpr int kAt = decltype(i)::value;
+      if constexpr (kAt < kWith)
+        __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+      else if constexpr (kAt - kWith < kLoads)
+        __builtin_amdgcn_sched_group_barrier(0x010, kLoads > kProducts - kWith ? kLoads : 1, 0);
+    });
   }
 
   // Partial sums lie as the threads hold them.
@@ -396,13 +442,14 @@ struct Product {
 
   // Blocks of 32 x 32: of a tile, by the wave and its number.
   static __device__ __forceinline__ int block_row(const NsWork& w, int k) {
-    return w.ti * kRows + (wave() >> 1) * kBlocks + k / kBlocks;
+    return w.ti * kP + (wave() >> 1) * kDown + k / kRight;
   }
   static __device__ __forceinline__ int block_column(const NsWork& w, int k) {
-    return w.tj * kRows + (wave() & 1) * kBlocks + k % kBlocks;
+    return w.tj * kQ + (wave() & 1) * kRight + k % kRight;
   }
+  // (Of a symmetric product a block on or over the diagonal, which is stored twice.)
   static __device__ __forceinline__ bool inside(const NsMatrix& t, int bi, int bj) {
-    return bi * 32 < t.mp && bj * 32 < (kApply ? t.np : t.mp);
+    return bi * 32 < t.mp && (kApply ? bj * 32 < t.np : bj * 32 < t.mp && bj >= bi);
   }
   // A lane has four elements of each of four groups of rows, at one column.  In the fragments of
   // the block's transpose (`depth` columns of them) they lie at across + 256 g, in its own after
@@ -435,8 +482,8 @@ struct Product {
   }
 
   // What becomes of a block's sums.
-  static __device__ __forceinline__ void finish(const NsArgs& a, const NsMatrix& t, bool mirror,
-                                                float mu, int bi, int bj, const Own& own,
+  static __device__ __forceinline__ void finish(const NsArgs& a, const NsMatrix& t, float mu,
+                                                int bi, int bj, const Own& own,
                                                 const f32x16& acc, float& squares) {
     if (!inside(t, bi, bj)) return;
     const int lane = threadIdx.x & 63;
@@ -475,7 +522,7 @@ struct Product {
       const Parts4 p = split4(f);
       *(half4*)(to + g * 64) = transpose4(p.hi);
       if (PARTS == 2 || kGram) *(half4*)(to + plane + g * 64) = transpose4(p.lo);
-      if (kApply || mirror) {
+      if (kApply || bi != bj) {
         *(half4*)(at + g * 256) = p.hi;
         if (PARTS == 2 || !kSquare) *(half4*)(at + plane + g * 256) = p.lo;
       }
@@ -485,43 +532,40 @@ struct Product {
   // The last step's values: the caller's result, or the parameters' update.
   static __device__ __forceinline__ void result(const NsArgs& a, const NsMatrix& t, int bi, int bj,
                                                 const float (&v)[16]) {
+    if (t.bf16)
+      t.tall ? put_result<uint16_t, 4>(a, t, bi, bj, v) : put_result<uint16_t, 1>(a, t, bi, bj, v);
+    else
+      t.tall ? put_result<uint32_t, 4>(a, t, bi, bj, v) : put_result<uint32_t, 1>(a, t, bi, bj, v);
+  }
+  // VW: elements of a lane side by side, which begin at any.
+  template <typename T, int VW>
+  static __device__ __forceinline__ void put_result(const NsArgs& a, const NsMatrix& t, int bi,
+                                                    int bj, const float (&v)[16]) {
     const int lane = threadIdx.x & 63;
     const int i = bi * 32 + (lane >> 5) * 4, j = bj * 32 + (lane & 31);
-    const long long down = t.tall ? 1 : t.n;
-    const long long at = t.tall ? (long long)j * t.m + i : (long long)i * t.n + j;
-    if (t.bf16)
-      put_result<uint16_t>(a, t, i, j, at, down, v);
-    else
-      put_result<uint32_t>(a, t, i, j, at, down, v);
-  }
-  template <typename T>
-  static __device__ __forceinline__ void put_result(const NsArgs& a, const NsMatrix& t, int i,
-                                                    int j, long long at, long long down,
-                                                    const float (&v)[16]) {
-    T* to = a.out ? (T*)a.out + t.out_at + at : (T*)t.param + at;
-    uint16_t* copy = a.out ? nullptr : (uint16_t*)t.copy;
-    if (copy) copy += at;
-    const bool in = j < t.n;
+    const long long at = VW == 4 ? (long long)j * t.m + i : (long long)i * t.n + j;
+    const long long row = VW == 4 ? 1 : t.n;
+    T* const to = a.out ? (T*)a.out + t.out_at + at : (T*)t.param + at;
+    uint16_t* const copy = a.out || !t.copy ? nullptr : (uint16_t*)t.copy + at;
+    const auto each = [&](auto&& f) {  // f(element, elements of it)
+      if (j >= t.n) return;
+#pragma unroll
+      for (int e = 0; e < 16; e += VW) {
+        const int r = e / 4 * 8 + e % 4;
+        if (i + r < t.m) f(e, r, min(VW, t.m - i - r));
+      }
+    };
     float p[16];
-    if (!a.out) {
-      const T* from = to;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[e] = in && i + e / 4 * 8 + e % 4 < t.m ? to_f32<T>(*from) : 0.f;
-        from += e % 4 == 3 ? 5 * down : down;
-      }
-    }
+    if (!a.out)
+      each([&](int e, int r, int of) { load_some<T, VW>(to + r * row, of, p + e); });
     const float keep = 1.f - a.lr * t.decay, rate = a.lr * t.scale;
+    each([&](int e, int r, int of) {
+      float f[VW];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      if (in && i + e / 4 * 8 + e % 4 < t.m) {
-        const float r = a.out ? v[e] : p[e] * keep - rate * v[e];
-        store_pack<T, 1>(to, pack<T, 1>({r}));
-        if (copy) *copy = f32_to_bf16_rne(r);
-      }
-      to += e % 4 == 3 ? 5 * down : down;
-      copy += e % 4 == 3 ? 5 * down : down;
-    }
+      for (int k = 0; k < VW; ++k) f[k] = a.out ? v[e + k] : p[e + k] * keep - rate * v[e + k];
+      store_some<T, VW>(to + r * row, of, f);
+      if (copy) store_some<uint16_t, VW>(copy + r * row, of, f);
+    });
   }
 
   // A tile's sums of squares, of each of kOfWave blocks of its waves where they are joined
@@ -530,7 +574,7 @@ struct Product {
                                                      float squares, float* lds) {
     if (KIND != kNsApply) return;
     squares = block_total(squares, lds);
-    const int tile = w.ti * ((t.np + SIZE - 1) / SIZE) + w.tj;
+    const int tile = w.ti * ((t.np + kTile.cols - 1) / kTile.cols) + w.tj;
     if (block >= 0) {
       if (threadIdx.x == 0) t.squares[tile * kOfWave + block] = squares;
     } else if (threadIdx.x < kOfWave) {
@@ -540,26 +584,38 @@ struct Product {
 
   static __device__ __forceinline__ void tile(const NsArgs& a, const NsMatrix& t, const NsWork& w,
                                               char* lds) {
-    Own own[kOfWave];
-    if (w.slot < 0) {
+    // (before the product where the registers hold them, else a block ahead)
+    constexpr int kOwn = kOfWave <= 4 ? kOfWave : 2;
+    Own own[kOwn];
+    const auto load_owns = [&] {
 #pragma unroll
-      for (int k = 0; k < kOfWave; ++k) load_own(a, t, block_row(w, k), block_column(w, k), own[k]);
-    }
+      for (int k = 0; k < kOwn; ++k) load_own(a, t, block_row(w, k), block_column(w, k), own[k]);
+    };
+    if (kOwn == kOfWave && w.slot < 0) load_owns();
     Acc acc;
     run(a, t, w, lds, acc);
     if (w.slot >= 0) return store_part(a.part, w.slot, acc);
-    __syncthreads();
+    if (kOwn < kOfWave) load_owns();
     const float mu = mean_square(a, t, w, (float*)lds);
     float squares = 0.f;
     // (One block's code, which is run once: four times as long it waits for its own loads.)
 #pragma unroll 1
     for (int k = 0; k < kOfWave; ++k) {
-      finish(a, t, w.ti != w.tj, mu, block_row(w, k), block_column(w, k), own[0], acc[0], squares);
+      Own now;
+      f32x16 sums;
 #pragma unroll
-      for (int i = 1; i < kOfWave; ++i) {
-        own[i - 1] = own[i];
-        acc[i - 1] = acc[i];
+      for (int i = 0; i < kOfWave; ++i) {
+        if (k != i) continue;  // (a branch of the whole wave)
+        sums = acc[i];
+        now = own[i % kOwn];
+        asm volatile("");  // (not a chain of selections)
       }
+      if (kOwn < kOfWave && k + kOwn < kOfWave) {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+          if (k % kOwn == i) load_own(a, t, block_row(w, k + kOwn), block_column(w, k + kOwn), own[i]);
+      }
+      finish(a, t, mu, block_row(w, k), block_column(w, k), now, sums, squares);
     }
     put_squares(t, w, -1, squares, (float*)lds);
   }
@@ -573,7 +629,7 @@ struct Product {
     load_parts(a.part, w.slot, w.slots, block, acc);
     const float mu = mean_square(a, t, w, lds);
     float squares = 0.f;
-    finish(a, t, w.ti != w.tj, mu, bi, bj, own, acc, squares);
+    finish(a, t, mu, bi, bj, own, acc, squares);
     put_squares(t, w, block, squares, lds);
   }
 };
@@ -582,14 +638,16 @@ struct Product {
 
 template <int PARTS, int KIND>
 __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ __attribute__((aligned(16))) char lds[kNsLds];
   const NsWork w = a.works[blockIdx.x];
   if (a.skip[w.matrix >> 6] >> (w.matrix & 63) & 1) return;
   const NsMatrix t = a.mats[w.matrix];
-  if (w.size)
-    Product<PARTS, KIND, kNsLarge>::tile(a, t, w, lds);
+  if (w.size == 2)
+    Product<PARTS, KIND, 2>::tile(a, t, w, lds);
+  else if (w.size == 1)
+    Product<PARTS, KIND, 1>::tile(a, t, w, lds);
   else
-    Product<PARTS, KIND, kNsSmall>::tile(a, t, w, lds);
+    Product<PARTS, KIND, 0>::tile(a, t, w, lds);
 }
 
 // Adds up the partial tiles, in their order, a block of each wave's to a workgroup.
@@ -599,30 +657,32 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a) {
   const NsWork w = a.works[blockIdx.x];
   if (a.skip[w.matrix >> 6] >> (w.matrix & 63) & 1) return;
   const NsMatrix t = a.mats[w.matrix];
-  if (w.size)
-    Product<PARTS, KIND, kNsLarge>::join(a, t, w, blockIdx.y, lds);
+  if (w.size == 2)
+    Product<PARTS, KIND, 2>::join(a, t, w, blockIdx.y, lds);
+  else if (w.size == 1)
+    Product<PARTS, KIND, 1>::join(a, t, w, blockIdx.y, lds);
   else
-    Product<PARTS, KIND, kNsSmall>::join(a, t, w, blockIdx.y, lds);
+    Product<PARTS, KIND, 0>::join(a, t, w, blockIdx.y, lds);
 }
 
 namespace {
 
 template <int PARTS, int KIND>
-void launch_kind(const NsArgs& a, unsigned works, bool join, hipStream_t stream) {
-  constexpr int kLds = kNsBuffers * Product<PARTS, KIND, kNsLarge>::kBytes;
-  static_assert(kLds <= 65536 && kNsBuffers * Product<PARTS, KIND, kNsSmall>::kBytes <= kLds, "");
+void launch_kind(const NsArgs& a, unsigned works, int size, bool join, hipStream_t stream) {
+  // (partial sums of a tile: a workgroup for each block of a wave)
   if (join)
-    hipLaunchKernelGGL((ns_join_kernel<PARTS, KIND>), dim3(works, 4), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((ns_join_kernel<PARTS, KIND>), dim3(works, kNsTiles[size].blocks()), dim3(256),
+                       0, stream, a);
   else
-    hipLaunchKernelGGL((ns_product_kernel<PARTS, KIND>), dim3(works), dim3(256), kLds, stream, a);
+    hipLaunchKernelGGL((ns_product_kernel<PARTS, KIND>), dim3(works), dim3(256), 0, stream, a);
 }
 template <int PARTS>
-hipError_t launch_parts(const NsArgs& a, unsigned works, bool join, hipStream_t stream) {
+hipError_t launch_parts(const NsArgs& a, unsigned works, int size, bool join, hipStream_t stream) {
   switch (a.kind) {
-    case kNsGram: launch_kind<PARTS, kNsGram>(a, works, join, stream); break;
-    case kNsSquare: launch_kind<PARTS, kNsSquare>(a, works, join, stream); break;
-    case kNsApply: launch_kind<PARTS, kNsApply>(a, works, join, stream); break;
-    default: launch_kind<PARTS, kNsLast>(a, works, join, stream);
+    case kNsGram: launch_kind<PARTS, kNsGram>(a, works, size, join, stream); break;
+    case kNsSquare: launch_kind<PARTS, kNsSquare>(a, works, size, join, stream); break;
+    case kNsApply: launch_kind<PARTS, kNsApply>(a, works, size, join, stream); break;
+    default: launch_kind<PARTS, kNsLast>(a, works, size, join, stream);
   }
   return hipGetLastError();
 }
@@ -638,10 +698,10 @@ hipError_t launch_ns_pack(const NsInput& a, unsigned works, int parts, hipStream
                      stream, a);
   return hipGetLastError();
 }
-hipError_t launch_ns_product(const NsArgs& a, unsigned works, bool join, int parts,
+hipError_t launch_ns_product(const NsArgs& a, unsigned works, int size, bool join, int parts,
                              hipStream_t stream) {
-  return parts == 2 ? launch_parts<2>(a, works, join, stream)
-                    : launch_parts<1>(a, works, join, stream);
+  return parts == 2 ? launch_parts<2>(a, works, size, join, stream)
+                    : launch_parts<1>(a, works, size, join, stream);
 }
 
 }  // namespace huge2

@@ -48,13 +48,20 @@ struct NsWork {
   int k0, k1;  // stages of the product
   int slot;    // of the partial tiles, -1: the whole sum; a join: the first
   int slots;   // a join: how many
-  int size;    // of the tile: 0 kNsSmall, 1 kNsLarge
+  int size;    // of the tile: its place in kNsTiles
 };
-constexpr int kNsSmall = 64, kNsLarge = 128;
-// Columns of a stage.
-constexpr int ns_stage(int parts, int size) { return (parts == 2 ? 16 : 32) * (size ? 1 : 2); }
-constexpr int kNsBuffers = 4;
-constexpr int kNsSlot = kNsLarge * kNsLarge;  // elements of a partial tile
+// A workgroup's part of a product: rows of P by rows of Q, `stage` columns of them at a time
+// (half as many with two parts), of which `buffers` fit its LDS.
+struct NsTile {
+  int rows, cols, stage, buffers;
+  constexpr int lds() const { return (rows + cols) * stage * 2 * buffers; }
+  constexpr int blocks() const { return rows / 64 * (cols / 64); }  // of 32 x 32 to a wave
+};
+constexpr int kNsSizes = 3;
+constexpr NsTile kNsTiles[kNsSizes] = {{64, 64, 64, 4}, {128, 128, 32, 4}, {256, 128, 32, 3}};
+constexpr int kNsLds = kNsTiles[2].lds();
+static_assert(kNsLds >= kNsTiles[1].lds() && kNsLds >= kNsTiles[0].lds(), "");
+constexpr int kNsSlot = 256 * 128;  // elements of a partial tile
 
 // Products: A = X X^T, A A, B X, and B X of the last step.
 enum NsKind { kNsGram = 0, kNsSquare = 1, kNsApply = 2, kNsLast = 3 };
@@ -86,7 +93,8 @@ struct NsInput {
 
 hipError_t launch_ns_norm(const NsInput& a, unsigned works, hipStream_t stream);
 hipError_t launch_ns_pack(const NsInput& a, unsigned works, int parts, hipStream_t stream);
-hipError_t launch_ns_product(const NsArgs& a, unsigned works, bool join, int parts,
+// size: the largest of the works'.
+hipError_t launch_ns_product(const NsArgs& a, unsigned works, int size, bool join, int parts,
                              hipStream_t stream);
 
 }  // namespace huge2
