@@ -282,7 +282,7 @@ typedef struct huge2_orthogonalize_plan huge2_orthogonalize_plan;
 
 /* A plan for `batch` matrices of one shape, one behind the other.  Allocates the operands of as
  * many of them as are worked on together (up to 256 and some 4 GiB): for m the smaller and n the
- * larger of rows and cols, each rounded up to 64, 12 m n + 8 m^2 bytes with two parts and 10 m n +
+ * larger of rows and cols, each rounded up to 64, 12 m n + 8 m^2 bytes with two parts and 12 m n +
  * 6 m^2 with one, and sums of parts of products, 64 KB each, up to some 1000.  Copies its lists
  * of work on hip_stream and waits for it.  Errors: INVALID_ARG, UNSUPPORTED (matrices of
  * 2^31 elements, more than 2^20 of them, 2^40 elements in all), ALLOC, HIP. */

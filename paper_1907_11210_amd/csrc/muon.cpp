@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <memory>
 #include <vector>
@@ -26,8 +27,8 @@ struct Works {
 // Matrices whose products share launches.
 struct Group {
   int first, count;
-  int size[3];  // the largest tile of each product
-  Works norm, pack, product[3], join[3];
+  int size[4];  // of each product's tiles
+  Works norm, pack, product[4], join[4];
 };
 
 // The polynomial and the powers of two that a step's operands are stored times: their
@@ -119,7 +120,7 @@ size_t squares_room(const NsMatrix& t) {
 size_t workspace(const NsMatrix& t, int parts) {
   const size_t whole = (size_t)t.mp * t.np * sizeof(half_bits);
   const size_t square = (size_t)t.mp * t.mp * sizeof(half_bits);
-  return round256(parts * whole) + 2 * round256(2 * whole) + round256(2 * square) +
+  return 3 * round256(2 * whole) + round256(2 * square) +
          round256(parts * square) + round256(squares_room(t) * sizeof(float)) +
          round256(t.norm_count * sizeof(double)) + 256;
 }
@@ -131,7 +132,7 @@ void place(NsMatrix* t, int parts, char* at) {
     at += round256(bytes);
     return p;
   };
-  t->x = (half_bits*)take(parts * whole);
+  t->x = (half_bits*)take(2 * whole);
   t->t0 = (half_bits*)take(2 * whole);
   t->t1 = (half_bits*)take(2 * whole);
   t->a = (half_bits*)take(2 * square);
@@ -155,57 +156,61 @@ void shape(NsMatrix* t, long long rows, long long cols) {
 template <typename F>
 void each_tile(const NsMatrix& t, int kind, int size, F&& f) {
   const NsTile& tile = kNsTiles[size];
-  const long long rows = ceil_div(t.mp, tile.rows);
-  const long long cols = ceil_div(kind == kNsApply ? t.np : t.mp, tile.cols);
+  const bool symmetric = kind == kNsGram || kind == kNsSquare, turned = kind == kNsLast && t.tall;
+  const long long rows = ceil_div(turned ? t.np : t.mp, tile.rows);
+  const long long cols = ceil_div(symmetric || turned ? t.mp : t.np, tile.cols);
   for (long long r = 0; r < rows; ++r)
-    for (long long c = kind == kNsApply ? 0 : r * tile.rows / tile.cols; c < cols; ++c)
+    for (long long c = symmetric ? r * tile.rows / tile.cols : 0; c < cols; ++c)
       f((int)r, (int)c);
 }
 
 constexpr int kUnits = 256;  // compute units
 
-int tile_size(const NsMatrix& t, int kind, const long long (&tiles)[kNsSizes]) {
-  if (t.mp >= 256 && tiles[2] >= kUnits * 3 / 4) return 2;
-  return t.mp >= 128 && tiles[1] >= 32 ? 1 : 0;
+// The size of a product's tiles.  Large ones need the least of LDS and the caches, and enough
+// columns to be worth their long prologue and epilogue; small ones start and end sooner.
+int tile_size(const NsEngine& e, const Group& g, int kind) {
+  if (const char* f = std::getenv("HUGE2_NS_TILE")) return std::abs(std::atoi(f)) % kNsSizes;
+  long long tiles[kNsSizes] = {}, columns[kNsSizes] = {};
+  for (int i = 0; i < g.count; ++i)
+    for (int size = 0; size < kNsSizes; ++size)
+      each_tile(e.mats[g.first + i], kind, size, [&](int, int) {
+        ++tiles[size];
+        columns[size] += (kind == kNsGram ? e.mats[g.first + i].np : e.mats[g.first + i].mp) * e.parts;
+      });
+  if (tiles[2] >= kUnits * 3 / 4 && columns[2] >= tiles[2] * 2048) return 2;
+  return columns[1] >= kUnits * (kind == kNsLast ? 1024ll : 512ll) ? 1 : 0;
 }
 
 // A product's tiles.  Where they do not fill the compute units, or leave some over that would
 // run alone, those are cut along their sum: `slots` counts partial tiles.
-void product_works(NsEngine& e, const Group& g, int kind, std::vector<NsWork>* works,
+void product_works(NsEngine& e, Group& g, int kind, std::vector<NsWork>* works,
                    std::vector<NsWork>* joins, int* slots) {
-  long long tiles[kNsSizes] = {};
-  for (int i = 0; i < g.count; ++i)
-    for (int size = 0; size < kNsSizes; ++size)
-      each_tile(e.mats[g.first + i], kind, size, [&](int, int) { ++tiles[size]; });
+  const int size = g.size[kind] = tile_size(e, g, kind);
   std::vector<NsWork> all;
-  double cost = 0;  // of all, in stages of a 128 x 128 tile
-  const auto weight = [](const NsWork& w) { return w.size == 2 ? 2.0 : w.size == 1 ? 1.0 : 0.8; };
+  double cost = 0;  // stages of all
   for (int i = 0; i < g.count; ++i) {
     NsMatrix& t = e.mats[g.first + i];
-    const int size = tile_size(t, kind, tiles);
     if (kind == kNsApply) t.squares_count = 0;
     const int stages = (kind == kNsGram ? t.np : t.mp) / (kNsTiles[size].stage / e.parts);
     each_tile(t, kind, size, [&](int r, int c) {
-      all.push_back({i, r, c, 0, stages, -1, 0, size});
-      cost += stages * weight(all.back());
+      all.push_back({i, r, c, 0, stages, -1, 0});
+      cost += stages;
       if (kind == kNsApply) t.squares_count += kNsTiles[size].blocks();
     });
   }
-  std::stable_sort(all.begin(), all.end(), [&](const NsWork& a, const NsWork& b) {
-    return a.k1 * weight(a) > b.k1 * weight(b);
-  });
-  const double share = std::max(16.0, cost / kUnits);  // of a compute unit
-  // whole tiles, as many as all units take alike
+  std::stable_sort(all.begin(), all.end(),
+                   [](const NsWork& a, const NsWork& b) { return a.k1 > b.k1; });
+  // whole tiles, as many as all units take alike, and the rest in pieces of a unit's share
   const size_t whole = all.size() / kUnits * kUnits;
   double left = 0;
-  for (size_t k = whole; k < all.size(); ++k) left += all[k].k1 * weight(all[k]);
+  for (size_t k = whole; k < all.size(); ++k) left += all[k].k1;
   *slots = 0;
   for (size_t k = 0; k < all.size(); ++k) {
     NsWork w = all[k];
     const int stages = w.k1;
-    // the rest in pieces of what a unit has of it, or of what is over a unit's share
-    const double piece = k < whole ? share : std::max(16.0, left / kUnits);
-    const int cuts = (int)std::max(1.0, std::min(stages / 8.0, std::floor(stages * weight(w) / piece)));
+    const double piece = std::max(16.0, (k < whole ? cost : left) / kUnits);
+    // (rounded down behind whole tiles, which hide an uneven end)
+    const int cuts = std::max(1, std::min(stages / 8, (int)(stages / piece + (whole ? 0.0 : 0.6))));
     if (cuts > 1) {
       NsWork join = w;
       join.slot = *slots, join.slots = cuts;
@@ -257,12 +262,11 @@ huge2_status engine_create(NsEngine* e, const huge2_newton_schulz& ns, hipStream
     }
     append(&g.norm, norm);
     append(&g.pack, pack);
-    for (int kind = 0; kind < 3; ++kind) {
+    for (int kind = 0; kind < 4; ++kind) {
       std::vector<NsWork> works, joins;
       int slots;
       product_works(*e, g, kind, &works, &joins, &slots);
       most_slots = std::max(most_slots, slots);
-      for (const NsWork& w : works) g.size[kind] = std::max(g.size[kind], w.size);
       append(&g.product[kind], works);
       append(&g.join[kind], joins);
     }
@@ -297,6 +301,7 @@ huge2_status engine_run(const NsEngine& e, const Group& g, NsInput in, NsArgs ca
   in.mats = call.mats = (const NsMatrix*)table + g.first;
   in.eps = e.eps;
   in.out_scale = (float)std::ldexp(1.0, e.steps[0].x);
+  in.keep_lo = e.steps.size() == 1;
   for (int i = 0; i < g.count; ++i)
     if (!in.src[i]) call.skip[i >> 6] |= 1ull << (i & 63);
   in.works = (const uint2*)(table + g.norm.at);
@@ -311,21 +316,22 @@ huge2_status engine_run(const NsEngine& e, const Group& g, NsInput in, NsArgs ca
     call.from = (int)k & 1;
     const bool last = k + 1 == e.steps.size();
     call.a = s.a, call.b = s.b, call.c = s.c;
-    for (int kind = 0; kind < 3; ++kind) {
-      call.kind = kind == kNsApply && last ? kNsLast : kind;
-      call.in_scale = power(kind == kNsGram ? -2 * s.x : kind == kNsSquare ? -2 * s.gram : -s.poly - s.x);
+    call.keep_lo = k + 2 == e.steps.size();
+    for (const int kind : {(int)kNsGram, (int)kNsSquare, last ? (int)kNsLast : (int)kNsApply}) {
+      const bool apply = kind == kNsApply || kind == kNsLast;
+      call.kind = kind;
+      call.in_scale = power(apply ? -s.poly - s.x : kind == kNsGram ? -2 * s.x : -2 * s.gram);
       call.own_scale = power(kind == kNsSquare ? -s.gram : -s.x);
-      call.out_scale = power(kind == kNsGram ? s.gram : kind == kNsSquare ? s.poly
-                             : last          ? 0
-                                             : e.steps[k + 1].x);
-      call.works = (const NsWork*)(table + g.product[kind].at);
-      if (st == HUGE2_OK)
-        st = launched(launch_ns_product(call, g.product[kind].count, g.size[kind], false,
-                                        e.parts, stream));
-      call.works = (const NsWork*)(table + g.join[kind].at);
-      if (st == HUGE2_OK && g.join[kind].count)
-        st = launched(launch_ns_product(call, g.join[kind].count, g.size[kind], true, e.parts,
-                                        stream));
+      call.out_scale = power(kind == kNsGram     ? s.gram
+                             : kind == kNsSquare ? s.poly
+                             : last              ? 0
+                                                 : e.steps[k + 1].x);
+      for (const bool join : {false, true}) {
+        const Works& works = join ? g.join[kind] : g.product[kind];
+        call.works = (const NsWork*)(table + works.at);
+        if (st == HUGE2_OK && works.count)
+          st = launched(launch_ns_product(call, works.count, g.size[kind], join, e.parts, stream));
+      }
     }
   }
   return st;

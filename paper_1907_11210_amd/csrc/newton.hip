@@ -117,39 +117,6 @@ __device__ __forceinline__ void input4(const void* p, int bf16, long long i, lon
   }
 }
 
-// `of` elements of up to VW, at any element's alignment.
-template <typename T, int VW>
-__device__ __forceinline__ void load_some(const T* p, int of, float* f) {
-  typedef uint32_t words __attribute__((ext_vector_type(VW * sizeof(T) / 4 > 1 ? VW * sizeof(T) / 4 : 2)));
-  typedef words words_any __attribute__((aligned(sizeof(T))));
-  if (VW > 1 && of == VW) {
-    const words w = *(const words_any*)p;
-#pragma unroll
-    for (int e = 0; e < VW; ++e)
-      f[e] = sizeof(T) == 4 ? __uint_as_float(w[e])
-                            : __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-  } else {
-#pragma unroll
-    for (int e = 0; e < VW; ++e) f[e] = e < of ? to_f32<T>(p[e]) : 0.f;
-  }
-}
-template <typename T, int VW>
-__device__ __forceinline__ void store_some(T* p, int of, const float (&f)[VW]) {
-  typedef uint32_t words __attribute__((ext_vector_type(VW * sizeof(T) / 4 > 1 ? VW * sizeof(T) / 4 : 2)));
-  typedef words words_any __attribute__((aligned(sizeof(T))));
-  if (VW > 1 && of == VW) {
-    const Pack<T, VW> r = pack<T, VW>(f);
-    words w;
-#pragma unroll
-    for (int e = 0; e < VW * (int)sizeof(T) / 4; ++e) w[e] = r.w[e];
-    *(words_any*)p = w;
-  } else {
-#pragma unroll
-    for (int e = 0; e < VW; ++e)
-      if (e < of) store_pack<T, 1>(p + e, pack<T, 1>({f[e]}));
-  }
-}
-
 }  // namespace
 
 // The momentum's update, and sums of squares of what is orthogonalised.  In 64 bits: squares
@@ -236,7 +203,7 @@ __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
   for (int o = 0; o < 2; ++o) {
     const int depth = (o == 0) == (t.tall == 0) ? t.np : t.mp;  // columns of the fragments' matrix
     const int fr = o == 0 ? r0 : c0, fk = o == 0 ? c0 : r0;
-    const bool second = PARTS == 2 || to[o] == t.t0;
+    const bool second = PARTS == 2 || a.keep_lo || to[o] == t.t0;
 #pragma unroll
     for (int p = threadIdx.x; p < 64 * 8; p += 256) {
       // (a fragment's rows side by side: 32 pieces of 16 bytes)
@@ -321,12 +288,14 @@ struct Product {
                                              char* lds, Acc& acc) {
     const int lane = threadIdx.x & 63;
     const half_bits* const t_now = pick(a.from != 0, t.t1, t.t0);
-    const half_bits* const op[2] = {kGram ? t.x : kSquare ? t.a : t.b,
-                                    kGram ? t.x : kSquare ? t.a : t_now};
+    const half_bits* const b = t.b;
+    const bool turn = turned(t);
+    const half_bits* const op[2] = {kGram ? t.x : kSquare ? t.a : pick(turn, t_now, b),
+                                    kGram ? t.x : kSquare ? t.a : pick(turn, b, t_now)};
     const int depth = (kGram ? t.np : t.mp) / 16;  // columns of fragments
     const size_t square = (size_t)t.mp * t.mp, whole = (size_t)t.mp * t.np;
-    const size_t plane[2] = {kGram ? whole : square, kSquare ? square : whole};
-    const int rows[2] = {t.mp / 32, (kApply ? t.np : t.mp) / 32};
+    const size_t plane[2] = {kGram || turn ? whole : square, kSquare || turn ? square : whole};
+    const int rows[2] = {(turn ? t.np : t.mp) / 32, (kApply && !turn ? t.np : t.mp) / 32};
     // a wave's fragments of stage k0
     const half_bits* from[kLoads];
 #pragma unroll
@@ -440,6 +409,12 @@ struct Product {
     return mu;
   }
 
+  // The last step's product is X^T = T B where the input was taken transposed, so that lanes
+  // have neighbours of the result's rows.
+  static __device__ __forceinline__ bool turned(const NsMatrix& t) {
+    return KIND == kNsLast && t.tall;
+  }
+
   // Blocks of 32 x 32: of a tile, by the wave and its number.
   static __device__ __forceinline__ int block_row(const NsWork& w, int k) {
     return w.ti * kP + (wave() >> 1) * kDown + k / kRight;
@@ -449,6 +424,7 @@ struct Product {
   }
   // (Of a symmetric product a block on or over the diagonal, which is stored twice.)
   static __device__ __forceinline__ bool inside(const NsMatrix& t, int bi, int bj) {
+    if (turned(t)) return bi * 32 < t.np && bj * 32 < t.mp;
     return bi * 32 < t.mp && (kApply ? bj * 32 < t.np : bj * 32 < t.mp && bj >= bi);
   }
   // A lane has four elements of each of four groups of rows, at one column.  In the fragments of
@@ -472,8 +448,9 @@ struct Product {
                                                   int bj, Own& own) {
     if (kGram || !inside(t, bi, bj)) return;
     const size_t plane = (size_t)t.mp * (kSquare ? t.mp : t.np);
-    const half_bits* hi =
-        across(kSquare ? t.a : pick(a.from != 0, t.t1, t.t0), bi, bj, t.mp / 16);
+    const half_bits* hi = turned(t) ? across(t.x, bi, bj, t.np / 16)
+                                    : across(kSquare ? t.a : pick(a.from != 0, t.t1, t.t0), bi, bj,
+                                             t.mp / 16);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       own.hi[g] = *(const half4*)(hi + g * 256);
@@ -484,7 +461,8 @@ struct Product {
   // What becomes of a block's sums.
   static __device__ __forceinline__ void finish(const NsArgs& a, const NsMatrix& t, float mu,
                                                 int bi, int bj, const Own& own,
-                                                const f32x16& acc, float& squares) {
+                                                const float (&params)[16], const f32x16& acc,
+                                                float& squares) {
     if (!inside(t, bi, bj)) return;
     const int lane = threadIdx.x & 63;
     const size_t plane = (size_t)t.mp * (kApply ? t.np : t.mp);
@@ -498,7 +476,7 @@ struct Product {
       if (!kGram) v[e] += linear * ((float)own.hi[e / 4][e % 4] + (float)own.lo[e / 4][e % 4]);
     }
     if constexpr (KIND == kNsLast) {
-      result(a, t, bi, bj, v);
+      result(a, t, bi, bj, params, v);
       return;
     }
     if (kGram && bi == bj) {
@@ -521,7 +499,8 @@ struct Product {
       }
       const Parts4 p = split4(f);
       *(half4*)(to + g * 64) = transpose4(p.hi);
-      if (PARTS == 2 || kGram) *(half4*)(to + plane + g * 64) = transpose4(p.lo);
+      if (PARTS == 2 || kGram || (kApply && a.keep_lo))
+        *(half4*)(to + plane + g * 64) = transpose4(p.lo);
       if (kApply || bi != bj) {
         *(half4*)(at + g * 256) = p.hi;
         if (PARTS == 2 || !kSquare) *(half4*)(at + plane + g * 256) = p.lo;
@@ -529,42 +508,36 @@ struct Product {
     }
   }
 
-  // The last step's values: the caller's result, or the parameters' update.
-  static __device__ __forceinline__ void result(const NsArgs& a, const NsMatrix& t, int bi, int bj,
-                                                const float (&v)[16]) {
-    if (t.bf16)
-      t.tall ? put_result<uint16_t, 4>(a, t, bi, bj, v) : put_result<uint16_t, 1>(a, t, bi, bj, v);
-    else
-      t.tall ? put_result<uint32_t, 4>(a, t, bi, bj, v) : put_result<uint32_t, 1>(a, t, bi, bj, v);
+  // The last step's values: the caller's result, or the parameters' update.  f(element of the
+  // lane's 16, element of the matrix) of those inside.
+  template <typename F>
+  static __device__ __forceinline__ void each_result(const NsMatrix& t, int bi, int bj, F&& f) {
+    const int rows = pick(t.tall != 0, t.n, t.m), cols = pick(t.tall != 0, t.m, t.n);
+    const int lane = threadIdx.x & 63, i = bi * 32 + (lane >> 5) * 4, j = bj * 32 + (lane & 31);
+    if (j >= cols) return;
+    const long long at = (long long)i * cols + j;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int r = e / 4 * 8 + e % 4;
+      if (i + r < rows) f(e, at + (long long)r * cols);
+    }
   }
-  // VW: elements of a lane side by side, which begin at any.
-  template <typename T, int VW>
-  static __device__ __forceinline__ void put_result(const NsArgs& a, const NsMatrix& t, int bi,
-                                                    int bj, const float (&v)[16]) {
-    const int lane = threadIdx.x & 63;
-    const int i = bi * 32 + (lane >> 5) * 4, j = bj * 32 + (lane & 31);
-    const long long at = VW == 4 ? (long long)j * t.m + i : (long long)i * t.n + j;
-    const long long row = VW == 4 ? 1 : t.n;
-    T* const to = a.out ? (T*)a.out + t.out_at + at : (T*)t.param + at;
-    uint16_t* const copy = a.out || !t.copy ? nullptr : (uint16_t*)t.copy + at;
-    const auto each = [&](auto&& f) {  // f(element, elements of it)
-      if (j >= t.n) return;
-#pragma unroll
-      for (int e = 0; e < 16; e += VW) {
-        const int r = e / 4 * 8 + e % 4;
-        if (i + r < t.m) f(e, r, min(VW, t.m - i - r));
-      }
-    };
-    float p[16];
-    if (!a.out)
-      each([&](int e, int r, int of) { load_some<T, VW>(to + r * row, of, p + e); });
+  static __device__ __forceinline__ void load_params(const NsArgs& a, const NsMatrix& t, int bi,
+                                                     int bj, float (&p)[16]) {
+    if (KIND != kNsLast || a.out || !inside(t, bi, bj)) return;
+    each_result(t, bi, bj, [&](int e, long long at) { p[e] = input(t.param, t.bf16, at); });
+  }
+  static __device__ __forceinline__ void result(const NsArgs& a, const NsMatrix& t, int bi, int bj,
+                                                const float (&p)[16], const float (&v)[16]) {
     const float keep = 1.f - a.lr * t.decay, rate = a.lr * t.scale;
-    each([&](int e, int r, int of) {
-      float f[VW];
-#pragma unroll
-      for (int k = 0; k < VW; ++k) f[k] = a.out ? v[e + k] : p[e + k] * keep - rate * v[e + k];
-      store_some<T, VW>(to + r * row, of, f);
-      if (copy) store_some<uint16_t, VW>(copy + r * row, of, f);
+    void* const to = pick(a.out != nullptr, a.out, t.param);
+    each_result(t, bi, bj, [&](int e, long long at) {
+      const float r = a.out ? v[e] : p[e] * keep - rate * v[e];
+      if (t.bf16)
+        ((uint16_t*)to)[t.out_at + at] = f32_to_bf16_rne(r);
+      else
+        ((float*)to)[t.out_at + at] = r;
+      if (!a.out && t.copy) ((uint16_t*)t.copy)[at] = f32_to_bf16_rne(r);
     });
   }
 
@@ -584,18 +557,25 @@ struct Product {
 
   static __device__ __forceinline__ void tile(const NsArgs& a, const NsMatrix& t, const NsWork& w,
                                               char* lds) {
-    // (before the product where the registers hold them, else a block ahead)
-    constexpr int kOwn = kOfWave <= 4 ? kOfWave : 2;
+    // (before the product where the registers hold them, else two blocks ahead)
+    constexpr bool kBefore = kOfWave <= 4;
+    constexpr int kOwn = kBefore ? kOfWave : 2;
     Own own[kOwn];
+    float next_params[16];
     const auto load_owns = [&] {
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) load_own(a, t, block_row(w, k), block_column(w, k), own[k]);
     };
-    if (kOwn == kOfWave && w.slot < 0) load_owns();
+    const auto params_of = [&](int k) {
+      load_params(a, t, block_row(w, k), block_column(w, k), next_params);
+    };
+    if (kOfWave == 1 && w.slot < 0) params_of(0);
+    if (kBefore && w.slot < 0) load_owns();
     Acc acc;
     run(a, t, w, lds, acc);
     if (w.slot >= 0) return store_part(a.part, w.slot, acc);
-    if (kOwn < kOfWave) load_owns();
+    if (!kBefore) load_owns();
+    if (kOfWave > 1) params_of(0);
     const float mu = mean_square(a, t, w, (float*)lds);
     float squares = 0.f;
     // (One block's code, which is run once: four times as long it waits for its own loads.)
@@ -615,66 +595,70 @@ struct Product {
         for (int i = 0; i < kOwn; ++i)
           if (k % kOwn == i) load_own(a, t, block_row(w, k + kOwn), block_column(w, k + kOwn), own[i]);
       }
-      finish(a, t, mu, block_row(w, k), block_column(w, k), now, sums, squares);
+      float params[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) params[e] = next_params[e];
+      if (k + 1 < kOfWave) params_of(k + 1);
+      finish(a, t, mu, block_row(w, k), block_column(w, k), now, params, sums, squares);
     }
     put_squares(t, w, -1, squares, (float*)lds);
   }
   static __device__ __forceinline__ void join(const NsArgs& a, const NsMatrix& t, const NsWork& w,
                                               int block, float* lds) {
-    if (block >= kOfWave) return;
     const int bi = block_row(w, block), bj = block_column(w, block);
     Own own;
     load_own(a, t, bi, bj, own);
+    float params[16];
+    load_params(a, t, bi, bj, params);
     f32x16 acc;
     load_parts(a.part, w.slot, w.slots, block, acc);
     const float mu = mean_square(a, t, w, lds);
     float squares = 0.f;
-    finish(a, t, mu, bi, bj, own, acc, squares);
+    finish(a, t, mu, bi, bj, own, params, acc, squares);
     put_squares(t, w, block, squares, lds);
   }
 };
 
 }  // namespace
 
-template <int PARTS, int KIND>
-__global__ __launch_bounds__(256, 2) void ns_product_kernel(NsArgs a) {
-  __shared__ __attribute__((aligned(16))) char lds[kNsLds];
+template <int PARTS, int KIND, int SIZE>
+__global__ __launch_bounds__(256, kNsTiles[SIZE].waves) void ns_product_kernel(NsArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[kNsTiles[SIZE].lds()];
   const NsWork w = a.works[blockIdx.x];
   if (a.skip[w.matrix >> 6] >> (w.matrix & 63) & 1) return;
   const NsMatrix t = a.mats[w.matrix];
-  if (w.size == 2)
-    Product<PARTS, KIND, 2>::tile(a, t, w, lds);
-  else if (w.size == 1)
-    Product<PARTS, KIND, 1>::tile(a, t, w, lds);
-  else
-    Product<PARTS, KIND, 0>::tile(a, t, w, lds);
+  Product<PARTS, KIND, SIZE>::tile(a, t, w, lds);
 }
 
 // Adds up the partial tiles, in their order, a block of each wave's to a workgroup.
-template <int PARTS, int KIND>
+template <int PARTS, int KIND, int SIZE>
 __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a) {
   __shared__ float lds[4];
   const NsWork w = a.works[blockIdx.x];
   if (a.skip[w.matrix >> 6] >> (w.matrix & 63) & 1) return;
   const NsMatrix t = a.mats[w.matrix];
-  if (w.size == 2)
-    Product<PARTS, KIND, 2>::join(a, t, w, blockIdx.y, lds);
-  else if (w.size == 1)
-    Product<PARTS, KIND, 1>::join(a, t, w, blockIdx.y, lds);
-  else
-    Product<PARTS, KIND, 0>::join(a, t, w, blockIdx.y, lds);
+  Product<PARTS, KIND, SIZE>::join(a, t, w, blockIdx.y, lds);
 }
 
 namespace {
 
-template <int PARTS, int KIND>
-void launch_kind(const NsArgs& a, unsigned works, int size, bool join, hipStream_t stream) {
+template <int PARTS, int KIND, int SIZE>
+void launch_size(const NsArgs& a, unsigned works, bool join, hipStream_t stream) {
   // (partial sums of a tile: a workgroup for each block of a wave)
   if (join)
-    hipLaunchKernelGGL((ns_join_kernel<PARTS, KIND>), dim3(works, kNsTiles[size].blocks()), dim3(256),
-                       0, stream, a);
+    hipLaunchKernelGGL((ns_join_kernel<PARTS, KIND, SIZE>), dim3(works, kNsTiles[SIZE].blocks()),
+                       dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((ns_product_kernel<PARTS, KIND>), dim3(works), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((ns_product_kernel<PARTS, KIND, SIZE>), dim3(works), dim3(256), 0, stream,
+                       a);
+}
+template <int PARTS, int KIND>
+void launch_kind(const NsArgs& a, unsigned works, int size, bool join, hipStream_t stream) {
+  switch (size) {
+    case 0: return launch_size<PARTS, KIND, 0>(a, works, join, stream);
+    case 1: return launch_size<PARTS, KIND, 1>(a, works, join, stream);
+    default: return launch_size<PARTS, KIND, 2>(a, works, join, stream);
+  }
 }
 template <int PARTS>
 hipError_t launch_parts(const NsArgs& a, unsigned works, int size, bool join, hipStream_t stream) {

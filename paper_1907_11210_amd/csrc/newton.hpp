@@ -20,7 +20,7 @@ typedef uint16_t half_bits;
 
 // X is m x n, m <= n: a matrix with more rows than columns is taken transposed.
 struct NsMatrix {
-  half_bits* x;       // X [m][n]: hi, and with two parts lo
+  half_bits* x;       // X [m][n], hi and lo (of one part lo for the last step alone)
   half_bits* t0;      // its transpose [n][m], hi and lo: of even steps
   half_bits* t1;      // ... and of odd ones
   half_bits* a;       // X X^T - mu I [m][m], hi and lo
@@ -48,19 +48,18 @@ struct NsWork {
   int k0, k1;  // stages of the product
   int slot;    // of the partial tiles, -1: the whole sum; a join: the first
   int slots;   // a join: how many
-  int size;    // of the tile: its place in kNsTiles
 };
 // A workgroup's part of a product: rows of P by rows of Q, `stage` columns of them at a time
 // (half as many with two parts), of which `buffers` fit its LDS.
 struct NsTile {
   int rows, cols, stage, buffers;
+  int waves;  // of a SIMD, which its registers leave room for
   constexpr int lds() const { return (rows + cols) * stage * 2 * buffers; }
   constexpr int blocks() const { return rows / 64 * (cols / 64); }  // of 32 x 32 to a wave
 };
 constexpr int kNsSizes = 3;
-constexpr NsTile kNsTiles[kNsSizes] = {{64, 64, 64, 4}, {128, 128, 32, 4}, {256, 128, 32, 3}};
-constexpr int kNsLds = kNsTiles[2].lds();
-static_assert(kNsLds >= kNsTiles[1].lds() && kNsLds >= kNsTiles[0].lds(), "");
+constexpr NsTile kNsTiles[kNsSizes] = {
+    {64, 64, 64, 3, 3}, {128, 128, 32, 4, 2}, {256, 128, 32, 3, 2}};
 constexpr int kNsSlot = 256 * 128;  // elements of a partial tile
 
 // Products: A = X X^T, A A, B X, and B X of the last step.
@@ -76,6 +75,7 @@ struct NsArgs {
   float in_scale;        // of a product's sum
   float own_scale;       // of the values that are added to it
   float out_scale;       // of what is stored
+  int keep_lo;           // the next step is the last
   float lr;
   void* out;             // null: parameters
   uint64_t skip[kNsMatrices / 64];  // matrices without a gradient
@@ -84,6 +84,7 @@ struct NsInput {
   const NsMatrix* mats;
   const uint2* works;    // (matrix, chunk of a sum), or (matrix, packed block)
   int muon, nesterov;
+  int keep_lo;           // there is one step
   float momentum, rest;  // rest: 1 - momentum
   double eps;
   float out_scale;
@@ -93,7 +94,7 @@ struct NsInput {
 
 hipError_t launch_ns_norm(const NsInput& a, unsigned works, hipStream_t stream);
 hipError_t launch_ns_pack(const NsInput& a, unsigned works, int parts, hipStream_t stream);
-// size: the largest of the works'.
+// size: of the tiles, their place in kNsTiles.
 hipError_t launch_ns_product(const NsArgs& a, unsigned works, int size, bool join, int parts,
                              hipStream_t stream);
 
