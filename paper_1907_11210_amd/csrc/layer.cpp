@@ -41,15 +41,20 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 // registers hold; then more waves, up to a workgroup.
 void choose_rows(LayerArgs* a, int vec, bool grad) {
   const long long vecs = ceil_div(a->c, vec);
-  const int most = std::max(1, (grad ? kLayerGradChannels : kLayerChannels) / vec);
+  const auto most = [&] {
+    const int channels = a->lanes_log2 > 6 ? kLayerWideChannels : grad ? kLayerGradChannels : kLayerChannels;
+    return std::max(1, channels / vec);
+  };
   a->lanes_log2 = std::min(6, log2_ceil(vecs));
-  while (a->lanes_log2 < 10 && vecs > (long long)most << a->lanes_log2) ++a->lanes_log2;
-  const long long slots = 1ll << log2_ceil(ceil_div(vecs, 1ll << a->lanes_log2));
-  a->slots = slots > most ? 0 : (int)slots;
+  while (a->lanes_log2 < 10 && vecs > (long long)most() << a->lanes_log2) ++a->lanes_log2;
+  const long long slots = a->lanes_log2 > 6 ? most()
+                                            : 1ll << log2_ceil(ceil_div(vecs, 1ll << a->lanes_log2));
+  a->slots = vecs > (long long)most() << a->lanes_log2 ? 0 : (int)slots;
   // (lanes of more than a wave are a whole workgroup)
   a->threads = !a->slots ? 1024 : a->lanes_log2 > 6 ? 1 << a->lanes_log2 : 256;
   const int teams = a->slots ? a->threads >> a->lanes_log2 : 1;
-  const long long all = ceil_div(a->rows, teams), most_groups = (grad ? 1024 : 2048) * 256 / a->threads;
+  const long long all = ceil_div(a->rows, teams);
+  const long long most_groups = (grad ? 1024 : 2048) * 256 / a->threads;
   const long long want = grad ? std::max(256ll, ceil_div(all, 4)) : all;
   a->groups = (int)std::min({all, want, most_groups});
   a->parts = a->groups;

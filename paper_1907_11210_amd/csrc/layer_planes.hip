@@ -42,21 +42,17 @@ template <int N>
 __device__ __forceinline__ void rows_sum(float (&v)[N], int threads, int lanes_log2,
                                          float* lds) {
   const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1);
-  for (int m = 32; m >= lanes; m >>= 1) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] += __shfl_xor(v[e], m);
-  }
-  const int waves = threads >> 6;
-  if (waves == 1) return;
+  scatter_sum<N>(v, lanes_log2);
   __syncthreads();
-  if ((int)(threadIdx.x & 63) < lanes) {
+  if ((int)(threadIdx.x & 7) < lanes) {
+    float* const to = lds + ((threadIdx.x >> 6) * lanes + lane) * N + scatter_at<N>();
 #pragma unroll
-    for (int e = 0; e < N; ++e) lds[((threadIdx.x >> 6) * lanes + lane) * N + e] = v[e];
+    for (int e = 0; e < (N > 7 ? N / 8 : 1); ++e) to[e] = v[e];
   }
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < N; ++e) v[e] = lds[lane * N + e];
-  for (int w = 1; w < waves; ++w) {
+  for (int w = 1; w < threads >> 6; ++w) {
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] += lds[(w * lanes + lane) * N + e];
   }
@@ -79,7 +75,7 @@ __device__ __forceinline__ Channel slot_params(const LayerArgs& a, int ch) {
 // compiler holds what does not change, and 40 of 128 registers spill.)
 template <typename T, int VW, int R, bool RAGGED>
 __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
-  extern __shared__ float lds[];
+  extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const int row = threadIdx.x >> a.lanes_log2, rows = a.threads >> a.lanes_log2;
   const size_t rows_b = (size_t)rows * a.hw * sizeof(T);
@@ -155,7 +151,7 @@ __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
 // workgroup's tiles (R = 0: layer_plane_sums_kernel does).
 template <typename T, int VW, int R, bool RAGGED>
 __global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(LayerArgs a) {
-  extern __shared__ float lds[];
+  extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const int row = threadIdx.x >> a.lanes_log2, rows = a.threads >> a.lanes_log2;
   const size_t rows_b = (size_t)rows * a.hw * sizeof(T);
@@ -246,10 +242,8 @@ __global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(
   if (!R || !a.part) return;
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) {
-    for (int m = lanes >> 1; m; m >>= 1) {
-      db[k] += __shfl_xor(db[k], m);
-      dg[k] += __shfl_xor(dg[k], m);
-    }
+    db[k] = side_sum(db[k], a.lanes_log2);
+    dg[k] = side_sum(dg[k], a.lanes_log2);
     const int ch = row + k * rows;
     if (lane == 0 && ch < a.c) a.part[(size_t)blockIdx.x * a.c + ch] = make_float2(db[k], dg[k]);
   }

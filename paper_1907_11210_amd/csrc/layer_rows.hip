@@ -1,103 +1,187 @@
 // layer_rows.hip -- layer norm of rows of channels: NHWC, lists of tokens, 1x1 maps.
+#include <algorithm>
+
 #include "layer_device.hpp"
 
 namespace huge2 {
 
 namespace {
 
-// Sum over the 2^lanes_log2 lanes side by side on a row, in each of them; lds: a float
+// Sum over the 2^lanes_log2 lanes side by side on a row, in each of them; lds: a value
 // for each wave (rows of more than a wave, which are a workgroup's only one).
 __device__ __forceinline__ float row_sum(float v, int lanes_log2, float* lds) {
-  if (lanes_log2 > 6) return block_sum(v, lds);
-  for (int m = (1 << lanes_log2) >> 1; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
-}
-__device__ __forceinline__ float2 row_sums(float2 v, int lanes_log2, float2* lds) {
-  for (int m = (1 << min(lanes_log2, 6)) >> 1; m; m >>= 1) {
-    v.x += __shfl_xor(v.x, m);
-    v.y += __shfl_xor(v.y, m);
-  }
+  v = side_sum(v, lanes_log2);
   if (lanes_log2 <= 6) return v;
   __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
   v = lds[0];
-  for (int w = 1; w < (int)blockDim.x >> 6; ++w) {
+  for (int w = 1; w < 1 << (lanes_log2 - 6); ++w) v += lds[w];
+  return v;
+}
+__device__ __forceinline__ float2 row_sums(float2 v, int lanes_log2, float2* lds) {
+  v.x = side_sum(v.x, lanes_log2);
+  v.y = side_sum(v.y, lanes_log2);
+  if (lanes_log2 <= 6) return v;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = lds[0];
+  for (int w = 1; w < 1 << (lanes_log2 - 6); ++w) {
     v.x += lds[w].x;
     v.y += lds[w].y;
   }
   return v;
 }
 
-// gamma and beta of a vector's channels.
+// gamma and beta of a vector's channels, by 16 bytes.  (By 4 a wave's loads of a row's
+// parameters take longer than the row: 64x64x2048, 8 images, 50 us without parameters and 79.)
+template <int VW>
+__device__ __forceinline__ void load_params(const float* p, int ch, float none, float (&f)[VW]) {
+  typedef u32x4 floats __attribute__((aligned(4)));
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < VW; ++e) f[e] = none;
+  } else if constexpr (VW == 1) {
+    f[0] = p[ch];
+  } else {
+#pragma unroll
+    for (int e = 0; e < VW; e += 4) {
+      const u32x4 v = *(const floats*)(p + ch + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[e + i] = __uint_as_float(v[i]);
+    }
+  }
+}
 template <int VW>
 __device__ __forceinline__ void vector_params(const LayerArgs& a, int ch, float (&g)[VW],
                                               float (&b)[VW]) {
-#pragma unroll
-  for (int e = 0; e < VW; ++e) {
-    g[e] = a.gamma ? a.gamma[ch + e] : 1.f;
-    b[e] = a.beta ? a.beta[ch + e] : 0.f;
-  }
+  load_params<VW>(a.gamma, ch, 1.f, g);
+  load_params<VW>(a.beta, ch, 0.f, b);
 }
+
+// A lane's gamma and beta for the rows that follow each other in its team: where rows are a
+// wave's in LDS ([c] each, rounded up to 4; 2048 channels take 16 KB), else read for each row.
+template <int VW, bool WAVE>
+struct Params {
+  float* lds;
+  __device__ __forceinline__ Params(const LayerArgs& a, float* room) : lds(room) {
+    if constexpr (WAVE) {
+      for (int i = threadIdx.x * 4; i < a.c; i += 1024) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const float* from = p ? a.beta : a.gamma;
+          float v[4];
+          if (i + 4 <= a.c) {
+            load_params<4>(from, i, p ? 0.f : 1.f, v);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = from && i + e < a.c ? from[i + e] : p ? 0.f : 1.f;
+          }
+          *(float4*)(lds + p * rounded(a.c) + i) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+      }
+      __syncthreads();
+    }
+  }
+  static __device__ __forceinline__ int rounded(int c) { return (c + 3) & ~3; }
+  __device__ __forceinline__ void read(const LayerArgs& a, int ch, float (&g)[VW],
+                                       float (&b)[VW]) const {
+    if constexpr (WAVE) {
+#pragma unroll
+      for (int e = 0; e < VW; ++e) {
+        g[e] = lds[ch + e];
+        b[e] = lds[rounded(a.c) + ch + e];
+      }
+    } else {
+      vector_params<VW>(a, ch, g, b);
+    }
+  }
+};
+
+}  // namespace
+
+// How a row's channels fill its lanes' vectors: all of them, some, or with a last vector that
+// repeats elements of the one before.
+enum RowFill { kFull = 0, kPart = 1, kRagged = 2 };
+
+namespace {
+
+template <int VW, int R, int FILL>
+struct Lanes {
+  Piece q[R];
+  __device__ __forceinline__ Lanes(const LayerArgs& a, int l) {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      q[k] = piece<VW, FILL == kRagged>(((long long)(k << a.lanes_log2) + l) * VW, a.c);
+  }
+  __device__ __forceinline__ bool in(int k) const { return FILL == kFull || q[k].in; }
+  // Whether element e of vector k counts.
+  __device__ __forceinline__ bool counts(int k, int e) const {
+    return in(k) && (FILL != kRagged || e >= q[k].skip);
+  }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* row, Pack<T, VW> (&f)[R]) const {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      if (in(k)) f[k] = load_run<T, VW>(row + q[k].at);
+  }
+};
 
 }  // namespace
 
 // A row is held by 2^lanes_log2 lanes, R vectors each: read once, its mean, the squares
-// around it, and the result from registers.  Rows follow each other in a team of lanes,
-// which keeps its channels' gamma and beta.
-template <typename T, int VW, int R, bool RAGGED>
-__global__ __launch_bounds__(1024) void layer_rows_kernel(LayerArgs a) {
+// around it, and the result from registers.  Rows follow each other in a team of lanes, the
+// next on its way while one is worked on.  WAVE: teams are waves or parts of them, else a
+// workgroup.
+//
+// Bound by the bytes: 64x64x2048, 8 images, bf16.
+template <typename T, int VW, int R, int FILL, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void layer_rows_kernel(LayerArgs a) {
   __shared__ float lds[16];
+  extern __shared__ __attribute__((aligned(16))) float kept[];  // WAVE: gamma and beta
   const int lanes = 1 << a.lanes_log2, l = threadIdx.x & (lanes - 1);
-  const int teams = blockDim.x >> a.lanes_log2, team = threadIdx.x >> a.lanes_log2;
+  const int teams = a.threads >> a.lanes_log2, team = threadIdx.x >> a.lanes_log2;
   const float inv = 1.f / (float)a.c;
+  const Lanes<VW, R, FILL> of(a, l);
+  const Params<VW, WAVE> params(a, kept);
   by_act(a.act, [&](auto act) {
-    Piece q[R];
-    float g[R][VW], b[R][VW];
+    constexpr int ACT = decltype(act)::value;
+    const long long step = (long long)gridDim.x * teams;
+    long long r = (long long)blockIdx.x * teams + team;
+    Pack<T, VW> f[R] = {};
+    if (r < a.rows) of.load((const T*)a.x + r * a.c, f);
+    for (; r < a.rows; r += step) {
+      float v[R][VW], s[4] = {};
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      q[k] = piece<VW, RAGGED>((k * lanes + l) * VW, a.c);
-      vector_params<VW>(a, q[k].at, g[k], b[k]);
-    }
-    for (long long r = (long long)blockIdx.x * teams + team; r < a.rows;
-         r += (long long)gridDim.x * teams) {
-      const T* x = (const T*)a.x + r * a.c;
-      Pack<T, VW> f[R] = {};
-      float s = 0.f;
+      for (int k = 0; k < R; ++k) unpack<T, VW>(f[k], v[k]);
+      if (r + step < a.rows) of.load((const T*)a.x + (r + step) * a.c, f);
 #pragma unroll
       for (int k = 0; k < R; ++k)
-        if (q[k].in) f[k] = load_run<T, VW>(x + q[k].at);
 #pragma unroll
-      for (int k = 0; k < R; ++k) {
-        float v[VW];
-        unpack<T, VW>(f[k], v);
+        for (int e = 0; e < VW; ++e) s[e & 3] += of.counts(k, e) ? v[k][e] : 0.f;
+      const float mean = row_sum((s[0] + s[1]) + (s[2] + s[3]), a.lanes_log2, lds) * inv;
 #pragma unroll
-        for (int e = 0; e < VW; ++e)
-          if (q[k].in && (!RAGGED || e >= q[k].skip)) s += v[e];
-        forget(f[k]);
-      }
-      const float mean = row_sum(s, a.lanes_log2, lds) * inv;
-      s = 0.f;
+      for (int e = 0; e < 4; ++e) s[e] = 0.f;
 #pragma unroll
-      for (int k = 0; k < R; ++k) {
-        float v[VW];
-        unpack<T, VW>(f[k], v);
+      for (int k = 0; k < R; ++k)
 #pragma unroll
-        for (int e = 0; e < VW; ++e)
-          if (q[k].in && (!RAGGED || e >= q[k].skip)) s += (v[e] - mean) * (v[e] - mean);
-        forget(f[k]);
-      }
-      const float rstd = 1.f / sqrtf(row_sum(s, a.lanes_log2, lds) * inv + a.eps);
+        for (int e = 0; e < VW; ++e) {
+          v[k][e] -= mean;
+          const float d = of.counts(k, e) ? v[k][e] : 0.f;
+          s[e & 3] += d * d;
+        }
+      const float rstd =
+          1.f / sqrtf(row_sum((s[0] + s[1]) + (s[2] + s[3]), a.lanes_log2, lds) * inv + a.eps);
       T* y = (T*)a.out + r * a.c;
+      asm volatile("" ::: "memory");  // (gamma and beta stay where they are)
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        float v[VW];
-        unpack<T, VW>(f[k], v);
+        float g[VW], b[VW];
+        params.read(a, of.q[k].at, g, b);
 #pragma unroll
-        for (int e = 0; e < VW; ++e)
-          v[e] = norm_value<false, decltype(act)::value, T>(v[e], 0.f, {mean, rstd, g[k][e], b[k][e]},
-                                                            make_float2(0.f, 0.f));
-        if (q[k].in) store_run<T, VW>(y + q[k].at, pack<T, VW>(v), a.stream);
+        for (int e = 0; e < VW; ++e) v[k][e] = layer_value<ACT, T>(v[k][e], rstd, g[e], b[e]);
+        if (of.in(k)) store_run<T, VW>(y + of.q[k].at, pack<T, VW>(v[k]), a.stream);
       }
       if (a.stats_out && l == 0) ((float2*)a.stats_out)[r] = make_float2(mean, rstd);
     }
@@ -107,77 +191,69 @@ __global__ __launch_bounds__(1024) void layer_rows_kernel(LayerArgs a) {
 // The gradient by the same rows: x and dy held, the two means, dx from registers.  A thread
 // adds up dgamma and dbeta of its channels over the team's rows; the teams' sums are joined
 // in LDS, the workgroups' by layer_params_kernel.
-template <typename T, int VW, int R, bool RAGGED>
-__global__ __launch_bounds__(1024) void layer_grad_rows_kernel(LayerArgs a) {
+template <typename T, int VW, int R, int FILL, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void layer_grad_rows_kernel(LayerArgs a) {
   __shared__ float2 lds[16];
-  extern __shared__ float2 sums[];  // [teams - 1][lanes * R * VW], rows of up to a wave
+  // WAVE: gamma and beta, then [teams - 1][lanes * R * VW] sums
+  extern __shared__ __attribute__((aligned(16))) float kept[];
   const int lanes = 1 << a.lanes_log2, l = threadIdx.x & (lanes - 1);
-  const int teams = blockDim.x >> a.lanes_log2, team = threadIdx.x >> a.lanes_log2;
+  const int teams = a.threads >> a.lanes_log2, team = threadIdx.x >> a.lanes_log2;
+  float2* const sums = (float2*)kept;
   const float inv = 1.f / (float)a.c;
-  Piece q[R];
-  float dg[R][VW], db[R][VW];
-#pragma unroll
-  for (int k = 0; k < R; ++k) {
-    q[k] = piece<VW, RAGGED>((k * lanes + l) * VW, a.c);
-#pragma unroll
-    for (int e = 0; e < VW; ++e) dg[k][e] = db[k][e] = 0.f;
-  }
+  const Lanes<VW, R, FILL> of(a, l);
+  float dg[R][VW] = {}, db[R][VW] = {};
+  const Params<VW, WAVE> params(a, kept);
   by_act(a.act, [&](auto act) {
     constexpr int ACT = decltype(act)::value;
-    float g[R][VW], b[R][VW];
-#pragma unroll
-    for (int k = 0; k < R; ++k) vector_params<VW>(a, q[k].at, g[k], b[k]);
-    for (long long r = (long long)blockIdx.x * teams + team; r < a.rows;
-         r += (long long)gridDim.x * teams) {
-      const T* x = (const T*)a.x + r * a.c;
-      const T* dy = (const T*)a.dy + r * a.c;
-      Pack<T, VW> f[R] = {}, d[R] = {};
-#pragma unroll
-      for (int k = 0; k < R; ++k)
-        if (q[k].in) {
-          f[k] = load_run<T, VW>(x + q[k].at);
-          d[k] = load_run<T, VW>(dy + q[k].at);
-        }
-      const float2 st = ((const float2*)a.stats)[r];
+    const long long step = (long long)gridDim.x * teams;
+    long long r = (long long)blockIdx.x * teams + team;
+    Pack<T, VW> f[R] = {}, d[R] = {};
+    float2 st = make_float2(0.f, 0.f);
+    const auto load = [&](long long row) {
+      of.load((const T*)a.x + row * a.c, f);
+      of.load((const T*)a.dy + row * a.c, d);
+      st = ((const float2*)a.stats)[row];
+    };
+    if (r < a.rows) load(r);
+    for (; r < a.rows; r += step) {
+      float xh[R][VW], t[R][VW];
       float2 s = make_float2(0.f, 0.f);
+      const float rstd = st.y;
+      asm volatile("" ::: "memory");  // (gamma and beta stay where they are)
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        float v[VW], w[VW];
+        float v[VW], w[VW], g[VW], b[VW];
+        params.read(a, of.q[k].at, g, b);
         unpack<T, VW>(f[k], v);
         unpack<T, VW>(d[k], w);
 #pragma unroll
         for (int e = 0; e < VW; ++e) {
-          if (!q[k].in || (RAGGED && e < q[k].skip)) continue;
-          float xh, dz;
-          layer_dz<ACT, T>(v[e], w[e], {st.x, st.y, g[k][e], b[k][e]}, xh, dz);
-          const float t = dz * g[k][e];
-          s.x += t;
-          s.y += t * xh;
+          float dz;
+          layer_dz<ACT, T>(v[e], w[e], {st.x, st.y, g[e], b[e]}, xh[k][e], dz);
+          t[k][e] = dz * g[e];
+          if (!of.counts(k, e)) continue;
+          s.x += t[k][e];
+          s.y += t[k][e] * xh[k][e];
           db[k][e] += dz;
-          dg[k][e] += dz * xh;
+          dg[k][e] += dz * xh[k][e];
         }
-        forget(f[k]);
-        forget(d[k]);
       }
+      if (r + step < a.rows) load(r + step);
       s = row_sums(s, a.lanes_log2, lds);
-      s.x *= inv, s.y *= inv;
+      // dx = rstd (t - s.x / c - xh s.y / c)
+      const float c0 = -rstd * (s.x * inv), c1 = -rstd * (s.y * inv);
       T* out = (T*)a.out + r * a.c;
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        float v[VW], w[VW];
-        unpack<T, VW>(f[k], v);
-        unpack<T, VW>(d[k], w);
+        float v[VW];
 #pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          float xh, dz;
-          layer_dz<ACT, T>(v[e], w[e], {st.x, st.y, g[k][e], b[k][e]}, xh, dz);
-          v[e] = st.y * (dz * g[k][e] - s.x - xh * s.y);
-        }
-        if (q[k].in) store_run<T, VW>(out + q[k].at, pack<T, VW>(v), a.stream);
+        for (int e = 0; e < VW; ++e) v[e] = fmaf(xh[k][e], c1, fmaf(t[k][e], rstd, c0));
+        if (of.in(k)) store_run<T, VW>(out + of.q[k].at, pack<T, VW>(v), a.stream);
       }
     }
   });
   if (!a.part) return;
+  if (teams > 1) __syncthreads();  // (gamma and beta have been read)
   float2* mine = sums + (team - 1) * lanes * R * VW;
   if (team > 0) {
 #pragma unroll
@@ -199,7 +275,7 @@ __global__ __launch_bounds__(1024) void layer_grad_rows_kernel(LayerArgs a) {
         s.x += v.x;
         s.y += v.y;
       }
-      if (q[k].in && (!RAGGED || e >= q[k].skip)) part[q[k].at + e] = s;
+      if (of.counts(k, e)) part[of.q[k].at + e] = s;
     }
 }
 
@@ -231,14 +307,14 @@ __global__ __launch_bounds__(1024) void layer_long_kernel(LayerArgs a) {
           for (int e = 0; e < VW; ++e)
             if (!RAGGED || e >= q.skip) s.x += v[e];
         });
-        const float mean = row_sums(s, 7, lds).x * inv;
+        const float mean = row_sums(s, 10, lds).x * inv;
         s = make_float2(0.f, 0.f);
         each([&](const Piece& q, float (&v)[VW], float (&)[VW]) {
 #pragma unroll
           for (int e = 0; e < VW; ++e)
             if (!RAGGED || e >= q.skip) s.x += (v[e] - mean) * (v[e] - mean);
         });
-        const float rstd = 1.f / sqrtf(row_sums(s, 7, lds).x * inv + a.eps);
+        const float rstd = 1.f / sqrtf(row_sums(s, 10, lds).x * inv + a.eps);
         each([&](const Piece& q, float (&v)[VW], float (&)[VW]) {
           float g[VW], b[VW];
           vector_params<VW>(a, q.at, g, b);
@@ -264,7 +340,7 @@ __global__ __launch_bounds__(1024) void layer_long_kernel(LayerArgs a) {
             s.y += dz * g[e] * xh;
           }
         });
-        s = row_sums(s, 7, lds);
+        s = row_sums(s, 10, lds);
         s.x *= inv, s.y *= inv;
         each([&](const Piece& q, float (&v)[VW], float (&w)[VW]) {
           float g[VW], b[VW];
@@ -318,7 +394,7 @@ __global__ __launch_bounds__(1024) void layer_params_kernel(LayerArgs a) {
   const int ch = blockIdx.x * 16 + col;
   float2 s = make_float2(0.f, 0.f);
   if (ch < a.c) {
-#pragma unroll 4
+#pragma unroll 16
     for (int r = row; r < a.parts; r += 64) {
       const float2 v = a.part[(size_t)r * a.c + ch];
       s.x += v.x;
@@ -364,39 +440,53 @@ void launch_long(const LayerArgs& a, bool grad, hipStream_t stream) {
                        dim3((a.c + 256 * VW - 1) / (256 * VW), a.parts), dim3(256), 0, stream, a);
 }
 
-template <typename T, int VW, int R, bool RAGGED>
+template <typename T, int VW, int R, int FILL>
 void launch_held(const LayerArgs& a, bool grad, hipStream_t stream) {
   const int teams = a.threads >> a.lanes_log2;
-  const int lds = (teams - 1) * R * VW * (int)sizeof(float2) << a.lanes_log2;
-  if (!grad)
-    hipLaunchKernelGGL((layer_rows_kernel<T, VW, R, RAGGED>), dim3(a.groups), dim3(a.threads), 0,
-                       stream, a);
-  else if constexpr (R * VW <= kLayerGradChannels)
-    hipLaunchKernelGGL((layer_grad_rows_kernel<T, VW, R, RAGGED>), dim3(a.groups),
-                       dim3(a.threads), lds, stream, a);
+  // gamma and beta; then sums of all teams but one
+  const int params = (a.c + 3) / 4 * 4 * (int)sizeof(float2);
+  const int lds = std::max(params, (teams - 1) * R * VW * (int)sizeof(float2) << a.lanes_log2);
+  constexpr bool kWide = R * VW == kLayerWideChannels;  // teams of waves have no others
+  if (a.lanes_log2 <= 6) {
+    if (!grad)
+      hipLaunchKernelGGL((layer_rows_kernel<T, VW, R, FILL, true>), dim3(a.groups),
+                         dim3(a.threads), params, stream, a);
+    else if constexpr (R * VW <= kLayerGradChannels)
+      hipLaunchKernelGGL((layer_grad_rows_kernel<T, VW, R, FILL, true>), dim3(a.groups),
+                         dim3(a.threads), lds, stream, a);
+  } else if constexpr (kWide) {
+    if (!grad)
+      hipLaunchKernelGGL((layer_rows_kernel<T, VW, R, FILL, false>), dim3(a.groups),
+                         dim3(a.threads), 0, stream, a);
+    else
+      hipLaunchKernelGGL((layer_grad_rows_kernel<T, VW, R, FILL, false>), dim3(a.groups),
+                         dim3(a.threads), 0, stream, a);
+  }
 }
 
-template <typename T, int VW, bool RAGGED>
+template <typename T, int VW, int FILL>
 void launch_rows(const LayerArgs& a, bool grad, hipStream_t stream) {
   switch (a.slots) {
-    case 0: return launch_long<T, VW, RAGGED>(a, grad, stream);
-    case 1: return launch_held<T, VW, 1, RAGGED>(a, grad, stream);
-    case 2: return launch_held<T, VW, 2, RAGGED>(a, grad, stream);
-    case 4: return launch_held<T, VW, 4, RAGGED>(a, grad, stream);
+    case 0: return launch_long<T, VW, FILL == kRagged>(a, grad, stream);
+    case 1: return launch_held<T, VW, 1, FILL>(a, grad, stream);
+    case 2: return launch_held<T, VW, 2, FILL>(a, grad, stream);
+    case 4: return launch_held<T, VW, 4, FILL>(a, grad, stream);
     default:
-      if constexpr (VW == 4) launch_held<T, VW, 8, RAGGED>(a, grad, stream);
+      if constexpr (VW == 4) launch_held<T, VW, 8, FILL>(a, grad, stream);
   }
 }
 
 template <typename T>
 void launch_type(const LayerArgs& a, int vec, bool grad, hipStream_t stream) {
-  constexpr int kFull = 16 / (int)sizeof(T);
+  constexpr int kVec = 16 / (int)sizeof(T);
   if (vec == 1)
-    launch_held<T, 1, 1, false>(a, grad, stream);
-  else if (a.c % kFull)
-    launch_rows<T, kFull, true>(a, grad, stream);
+    launch_held<T, 1, 1, kPart>(a, grad, stream);
+  else if (a.c % kVec)
+    launch_rows<T, kVec, kRagged>(a, grad, stream);
+  else if (a.slots == 0 || a.c != kVec * a.slots << a.lanes_log2)
+    launch_rows<T, kVec, kPart>(a, grad, stream);
   else
-    launch_rows<T, kFull, false>(a, grad, stream);
+    launch_rows<T, kVec, kFull>(a, grad, stream);
 }
 
 }  // namespace

@@ -100,10 +100,10 @@ struct LayerArgs {
   float eps;
   int stream;  // the result is stored past the caches
 };
-// The most values of a row that a thread of the gradient holds (it has two sums and two
-// parameters for each besides, and a thread of 1024 has 128 registers), and vectors of planes.
-constexpr int kLayerChannels = 32, kLayerGradChannels = 16;
-constexpr int kLayerPlanes = 16, kLayerGradPlanes = 8;
+// The most values of a row that a thread holds (the gradient's has two more for each, and two
+// sums): of rows that are a wave's or less, and of those that are a workgroup's.
+constexpr int kLayerChannels = 32, kLayerGradChannels = 16, kLayerWideChannels = 16;
+constexpr int kLayerPlanes = 16, kLayerGradPlanes = 8;  // vectors of planes
 
 hipError_t launch_layer_rows(const LayerArgs& a, int dtype, int vec, bool grad,
                              hipStream_t stream);

@@ -112,7 +112,7 @@ def test_held_values_cover_a_pixel(script):  # noqa: F811
             assert 64 <= t <= 1024 and t & (t - 1) == 0, (shape, name)
             if "rows" in kernel:
                 held += 1
-                assert v * t * r >= c and v * r <= (16 if grad else 32), (shape, name)
+                assert v * t * r >= c and v * r <= (16 if grad or c > 2048 else 32), (shape, name)
                 assert v == 1 or c >= v, (shape, name)
             elif "planes" in kernel:
                 assert v == 1 or h * w >= v, (shape, name)
