@@ -69,19 +69,23 @@ void choose_rows(LayerArgs* a, int vec, bool grad) {
 bool choose_planes(LayerArgs* a, int vec, int esz, bool grad) {
   const long long vecs = ceil_div(a->hw, vec);
   a->lanes_log2 = std::min(3, log2_ceil(vecs));
-  const int most_held = 1024 * (grad ? kLayerGradPlanes / 2 : kLayerPlanes);  // of a tile
+  // (a thread of 1024 holds 128 registers, of 512 twice as many)
+  const auto most = [&](int threads) {
+    return !grad           ? kLayerPlanes
+           : threads <= 512 ? kLayerGradPlanes
+                            : std::min(kLayerGradPlanes, kLayerWideChannels / vec);
+  };
+  const long long most_held = std::max(1024 * most(1024), 512 * most(512));  // of a tile
   while (a->lanes_log2 > 1 && a->c > most_held >> a->lanes_log2) --a->lanes_log2;
   const auto tiles = [&] { return ceil_div(vecs, 1ll << a->lanes_log2) * a->n; };
   if (a->lanes_log2 == 3 && tiles() < 512) a->lanes_log2 = 2;
   const auto slots = [&] { return ceil_div(a->c, a->threads >> a->lanes_log2); };
-  // (eight vectors of x and of dy leave 512 threads)
-  const auto most = [&] { return !grad ? kLayerPlanes : a->threads > 512 ? kLayerGradPlanes / 2 : kLayerGradPlanes; };
   a->threads = 64;
-  while (a->threads < 1024 &&
-         (slots() > most() || (slots() > 4 && tiles() * (a->threads / 32) <= 8192)))
+  while (a->threads < (grad && slots() <= most(512) ? 512 : 1024) &&
+         (slots() > most(a->threads) || (slots() > 4 && tiles() * (a->threads / 32) <= 8192)))
     a->threads *= 2;
   // (offsets of held channels are 32 bits of bytes)
-  const bool held = slots() <= most() && (long long)a->c * a->hw * esz < (1ll << 32);
+  const bool held = slots() <= most(a->threads) && (long long)a->c * a->hw * esz < (1ll << 32);
   a->slots = held ? 1 << log2_ceil(slots()) : 0;
   if (tiles() >= (1ll << 31)) return false;
   a->tiles = (uint32_t)tiles();

@@ -105,11 +105,17 @@ __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
         }
       }
     };
+    // (their parameters with them, where the registers hold both)
+    constexpr bool kParams = R > 0 && R <= 8;
+    Channel params[kParams ? R : 1];
     if constexpr (R) {
 #pragma unroll
       for (int k = 0; k < R; ++k) {
         const int ch = row + k * rows;
-        if (i.q.in && ch < a.c) f[k] = load_run<T, VW>(slot_at(x, rows_b, k, offset));
+        if (i.q.in && ch < a.c) {
+          f[k] = load_run<T, VW>(slot_at(x, rows_b, k, offset));
+          if constexpr (kParams) params[k] = slot_params(a, ch);
+        }
       }
     }
     float s[VW] = {}, mean[VW], rstd[VW];
@@ -131,7 +137,7 @@ __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
 #pragma unroll
     for (int e = 0; e < VW; ++e) rstd[e] = 1.f / sqrtf(s[e] * inv + a.eps);
     each([&](int k, int ch, float (&v)[VW]) {
-      const Channel p = R ? slot_params(a, ch) : plane_params(a, ch);
+      const Channel p = kParams ? params[k] : R ? slot_params(a, ch) : plane_params(a, ch);
 #pragma unroll
       for (int e = 0; e < VW; ++e)
         v[e] = norm_value<false, decltype(act)::value, T>(
@@ -150,7 +156,8 @@ __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
 // The gradient by the same tiles.  A thread adds up dgamma and dbeta of its channels over the
 // workgroup's tiles (R = 0: layer_plane_sums_kernel does).
 template <typename T, int VW, int R, bool RAGGED>
-__global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(LayerArgs a) {
+__global__ __launch_bounds__(R * VW > kLayerWideChannels ? 512 : 1024) void
+layer_grad_planes_kernel(LayerArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const int row = threadIdx.x >> a.lanes_log2, rows = a.threads >> a.lanes_log2;
@@ -158,6 +165,9 @@ __global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(
   const float inv = 1.f / (float)a.c;
   constexpr int kHeld = R ? R : 1;
   float dg[kHeld] = {}, db[kHeld] = {};
+  // x and dy become what dx is made of (a smooth activation takes longer than the rest), or are
+  // kept, where that would be too many registers.
+  constexpr bool kMade = R > 0 && R * VW <= 2 * kLayerWideChannels;
   by_act(a.act, [&](auto act) {
     constexpr int ACT = decltype(act)::value;
     for (uint32_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
@@ -167,6 +177,7 @@ __global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(
       T* out = (T*)a.out + i.first;
       const uint32_t offset = ((uint32_t)row * (uint32_t)a.hw + i.q.at) * sizeof(T);
       Pack<T, VW> f[kHeld] = {}, d[kHeld] = {};
+      Channel params[kMade ? R : 1];
       const auto each = [&](auto&& g) {  // g(slot, channel, x, dy)
         if constexpr (R) {
 #pragma unroll
@@ -195,6 +206,7 @@ __global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(
           if (i.q.in && ch < a.c) {
             f[k] = load_run<T, VW>(slot_at(x, rows_b, k, offset));
             d[k] = load_run<T, VW>(slot_at(dy, rows_b, k, offset));
+            if constexpr (kMade) params[k] = slot_params(a, ch);
           }
         }
       }
@@ -207,15 +219,17 @@ __global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(
 #pragma unroll
         for (int e = 0; e < VW; ++e) st[e] = make_float2(0.f, 0.f);
       }
-      float s[2 * VW] = {};
+      float s[2 * VW] = {}, made[kMade ? R : 1][2 * VW];
       each([&](int k, int ch, float (&v)[VW], float (&w)[VW]) {
-        const Channel p = R ? slot_params(a, ch) : plane_params(a, ch);
+        const Channel p = kMade ? params[k] : R ? slot_params(a, ch) : plane_params(a, ch);
 #pragma unroll
         for (int e = 0; e < VW; ++e) {
           float xh, dz;
           layer_dz<ACT, T>(v[e], w[e], {st[e].x, st[e].y, p.gamma, p.beta}, xh, dz);
-          s[e] += dz * p.gamma;
-          s[VW + e] += dz * p.gamma * xh;
+          const float t = dz * p.gamma;
+          s[e] += t;
+          s[VW + e] += t * xh;
+          if constexpr (kMade) made[k][e] = xh, made[k][VW + e] = t;
           if (R && (!RAGGED || e >= i.q.skip)) {
             db[k] += dz;
             dg[k] += dz * xh;
@@ -225,18 +239,34 @@ __global__ __launch_bounds__(R == 8 ? 512 : 1024) void layer_grad_planes_kernel(
       rows_sum<2 * VW>(s, a.threads, a.lanes_log2, lds);
 #pragma unroll
       for (int e = 0; e < 2 * VW; ++e) s[e] *= inv;
-      asm volatile("" ::: "memory");  // (gamma and beta are read again, not held)
-      each([&](int k, int ch, float (&v)[VW], float (&w)[VW]) {
-        const Channel p = R ? slot_params(a, ch) : plane_params(a, ch);
+      // dx = rstd (t - the mean of t - xh times the mean of t xh)
+      if constexpr (kMade) {
+        float c0[VW], c1[VW];
 #pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          float xh, dz;
-          layer_dz<ACT, T>(v[e], w[e], {st[e].x, st[e].y, p.gamma, p.beta}, xh, dz);
-          v[e] = st[e].y * (dz * p.gamma - s[e] - xh * s[VW + e]);
+        for (int e = 0; e < VW; ++e) c0[e] = -st[e].y * s[e], c1[e] = -st[e].y * s[VW + e];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          float v[VW];
+#pragma unroll
+          for (int e = 0; e < VW; ++e)
+            v[e] = fmaf(made[k][e], c1[e], fmaf(made[k][VW + e], st[e].y, c0[e]));
+          if (i.q.in && row + k * rows < a.c)
+            store_run<T, VW>(slot_at(out, rows_b, k, offset), pack<T, VW>(v), a.stream);
         }
-        T* to = R ? slot_at(out, rows_b, k, offset) : out + (size_t)ch * a.hw + i.q.at;
-        store_run<T, VW>(to, pack<T, VW>(v), a.stream);
-      });
+      } else {
+        asm volatile("" ::: "memory");  // (gamma and beta are read again, not held)
+        each([&](int k, int ch, float (&v)[VW], float (&w)[VW]) {
+          const Channel p = R ? slot_params(a, ch) : plane_params(a, ch);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            float xh, dz;
+            layer_dz<ACT, T>(v[e], w[e], {st[e].x, st[e].y, p.gamma, p.beta}, xh, dz);
+            v[e] = st[e].y * (dz * p.gamma - s[e] - xh * s[VW + e]);
+          }
+          T* to = R ? slot_at(out, rows_b, k, offset) : out + (size_t)ch * a.hw + i.q.at;
+          store_run<T, VW>(to, pack<T, VW>(v), a.stream);
+        });
+      }
     }
   });
   if (!R || !a.part) return;

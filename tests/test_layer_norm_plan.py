@@ -118,7 +118,8 @@ def test_held_values_cover_a_pixel(script):  # noqa: F811
                 assert v == 1 or h * w >= v, (shape, name)
                 if r:
                     held += 1
-                    assert t * r >= c and r <= (16 if not grad else 8 if t <= 512 else 4), (shape, name)
+                    assert t * r >= c, (shape, name)
+                    assert r <= (16 if not grad else 8 if t <= 512 else min(8, 16 // v)), (shape, name)
             else:
                 assert c > 16384, (shape, name)
     assert held > len(shapes)
