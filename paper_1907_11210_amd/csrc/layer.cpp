@@ -39,7 +39,7 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 // Rows: as many lanes as a row has vectors, up to a wave; more vectors a lane, up to what its
 // registers hold; then more waves, up to a workgroup.
-void choose_rows(LayerArgs* a, int vec, bool grad) {
+void choose_rows(LayerArgs* a, int vec, int esz, bool grad) {
   const long long vecs = ceil_div(a->c, vec);
   const auto most = [&] {
     const int channels = a->lanes_log2 > 6 ? kLayerWideChannels : grad ? kLayerGradChannels : kLayerChannels;
@@ -55,7 +55,10 @@ void choose_rows(LayerArgs* a, int vec, bool grad) {
   const int teams = a->slots ? a->threads >> a->lanes_log2 : 1;
   const long long all = ceil_div(a->rows, teams);
   const long long most_groups = (grad ? 1024 : 2048) * 256 / a->threads;
-  const long long want = grad ? std::max(256ll, ceil_div(all, 4)) : all;
+  // The gradient's sums of a workgroup's rows, 8 bytes a channel written and read, stay under
+  // 4% of its bytes: 32768 rows of 1024 bf16 with 512 workgroups 47.7 us, with 1024 52.5;
+  // 65536 of 128 with 512 and 1024 22.5 and 20.7; 1024 of 512 with 256 and 1024 10.6 and 12.9.
+  const long long want = grad ? std::max(256ll, a->rows * esz * 3 / 400) : all;
   a->groups = (int)std::min({all, want, most_groups});
   a->parts = a->groups;
   if (!a->slots) {
@@ -64,8 +67,12 @@ void choose_rows(LayerArgs* a, int vec, bool grad) {
   }
 }
 
-// Planes: tiles of 128 bytes of each plane, or less where the channels then fit the registers.
-// False where there are too many of them.
+// Planes: tiles of 128 bytes of each plane, or less where the channels then fit the registers
+// (or where there would be a few workgroups alone), and four vectors a thread.  64 images of
+// 256x16x16 bf16, 8, 4 and 2 lanes on a tile: 9.8, 10.5 and 13.3 us, the gradient 14.7, 17.0 and
+// 20.2; 64 of 128x64x64 35, 43 and 67, 55, 69 and 114.  With 8, 4, 2 and 1 vectors a thread 36.9,
+// 36.0, 38.7 and 88, the gradient 70, 55, 56 and 93.
+// False where there are too many tiles.
 bool choose_planes(LayerArgs* a, int vec, int esz, bool grad) {
   const long long vecs = ceil_div(a->hw, vec);
   a->lanes_log2 = std::min(3, log2_ceil(vecs));
@@ -78,12 +85,11 @@ bool choose_planes(LayerArgs* a, int vec, int esz, bool grad) {
   const long long most_held = std::max(1024 * most(1024), 512 * most(512));  // of a tile
   while (a->lanes_log2 > 1 && a->c > most_held >> a->lanes_log2) --a->lanes_log2;
   const auto tiles = [&] { return ceil_div(vecs, 1ll << a->lanes_log2) * a->n; };
-  if (a->lanes_log2 == 3 && tiles() < 512) a->lanes_log2 = 2;
+  while (a->lanes_log2 > 1 && tiles() < 64) --a->lanes_log2;
   const auto slots = [&] { return ceil_div(a->c, a->threads >> a->lanes_log2); };
   a->threads = 64;
-  while (a->threads < (grad && slots() <= most(512) ? 512 : 1024) &&
-         (slots() > most(a->threads) || (slots() > 4 && tiles() * (a->threads / 32) <= 8192)))
-    a->threads *= 2;
+  while (a->threads < 512 && slots() > 4) a->threads *= 2;
+  if (slots() > 8) a->threads = 1024;  // (1000 channels: 8 vectors 17.3 us, 16 21.2)
   // (offsets of held channels are 32 bits of bytes)
   const bool held = slots() <= most(a->threads) && (long long)a->c * a->hw * esz < (1ll << 32);
   a->slots = held ? 1 << log2_ceil(slots()) : 0;
@@ -119,7 +125,7 @@ huge2_status layer_create(huge2_layer_norm_plan** out, const huge2_layer_norm_de
     a.eps = d.eps;
     a.stream = streams(bytes_of(d));
     if (p->rows) {
-      choose_rows(&a, p->vec, g != 0);
+      choose_rows(&a, p->vec, elem_size(d.dtype), g != 0);
     } else if (!choose_planes(&a, p->vec, elem_size(d.dtype), g != 0)) {
       delete p;
       return HUGE2_ERR_UNSUPPORTED;
