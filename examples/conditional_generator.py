@@ -1,15 +1,17 @@
 """Training a class-conditional generator on the library, one step as it is used:
 
   labels -> embedding, added to the noise -> transposed convolutions, each but the last
-  followed by group norm with ReLU -> tanh -> images; then the gradients back through
-  all of them (data and weight gradients of the convolutions, the norms', the table's)
-  and one AdamW step, which also writes the bf16 working weights.
+  followed by group norm (or layer norm over channels) with ReLU -> tanh -> images; then
+  the gradients back through all of them (data and weight gradients of the convolutions,
+  the norms', the table's) and one AdamW step, which also writes the bf16 working weights.
+  With --optimizer muon the convolutions' weights take a Muon step, the rest AdamW's.
 
 Activations and gradients are bf16 NCHW (the layout of the weight gradients), parameters
 and their moments fp32, or the moments in 8 bits with --states 8.  The task is synthetic:
 each class has an image of its own to reproduce whatever the noise.
 
     python examples/conditional_generator.py --steps 200
+    python examples/conditional_generator.py --steps 200 --norm layer --optimizer muon
 """
 from __future__ import annotations
 
@@ -31,7 +33,7 @@ class Generator:
     side: noise and label of `dim` values -> channels[0] x 4 x 4 -> ... -> 3 channels."""
 
     def __init__(self, batch, classes=10, dim=64, channels=(256, 128, 64), groups=16, states=32,
-                 seed=0, device="cuda"):
+                 seed=0, device="cuda", norm="group", optimizer="adamw"):
         g = torch.Generator().manual_seed(seed)
         self.batch, self.dim, self.channels = batch, dim, tuple(channels)
         widths = (dim,) + self.channels + (3,)
@@ -40,8 +42,9 @@ class Generator:
         shapes = [(a, b, 4, 4) for a, b in zip(widths, widths[1:])]
         self.embedding = train.Embedding(classes, dim, torch.bfloat16, scale=math.sqrt(dim),
                                          max_tokens=batch)
-        self.norms = [train.GroupNorm((batch, c, 4 << i, 4 << i), groups, torch.bfloat16, "NCHW",
-                                      "relu") for i, c in enumerate(self.channels)]
+        maps = [(batch, c, 4 << i, 4 << i) for i, c in enumerate(self.channels)]
+        self.norms = [train.LayerNorm(m, torch.bfloat16, "NCHW", "relu") if norm == "layer" else
+                      train.GroupNorm(m, groups, torch.bfloat16, "NCHW", "relu") for m in maps]
         self.stats = [n.new_stats() for n in self.norms]
         # parameters: the table, the convolutions' weights, the norms' gammas and betas
         table = torch.randn(classes, dim, generator=g) / math.sqrt(dim)
@@ -55,9 +58,16 @@ class Generator:
         norms = len(gammas)
         self.table, self.weights = self.work[0], self.work[1:]
         self.gammas, self.betas = self.params[k:k + norms], self.params[k + norms:]
-        self.optimizer = train.AdamW(
-            self.params, states, weight_decay=[0.01] * k + [0.0] * (2 * norms),
-            copies=self.work + [None] * (2 * norms))
+        decay = [0.01] * k + [0.0] * (2 * norms)
+        copies = self.work + [None] * (2 * norms)
+        # Muon takes the convolutions' weights, [inputs, outputs and taps] as matrices
+        self.matrices = list(range(1, k)) if optimizer == "muon" else []
+        self.others = [i for i in range(len(self.params)) if i not in self.matrices]
+        pick = lambda values, of: [values[i] for i in of]  # noqa: E731
+        self.muon = train.Muon(pick(self.params, self.matrices), pick(decay, self.matrices),
+                               copies=pick(copies, self.matrices), products="f16")
+        self.optimizer = train.AdamW(pick(self.params, self.others), states,
+                                     pick(decay, self.others), pick(copies, self.others))
         self.steps = 0
 
     def forward(self, noise, labels):
@@ -89,13 +99,16 @@ class Generator:
         dtable = self.embedding.grad(labels, dx.reshape(self.batch, self.dim))
         return [dtable] + dws[::-1] + dgammas[::-1] + dbetas[::-1]
 
-    def step(self, noise, labels, target, lr=2e-3):
-        """One training step on the mean square error; its loss (a device tensor)."""
+    def step(self, noise, labels, target, lr=2e-3, matrix_lr=2e-2):
+        """One training step on the mean square error; its loss (a device tensor).  matrix_lr:
+        Muon's, whose updates have singular values near 1."""
         images, kept = self.forward(noise, labels)
         diff = images.float() - target
         grads = self.backward(diff * (2 / diff.numel()), images, kept, labels)
         self.steps += 1
-        self.optimizer.step(grads, lr=lr, step=self.steps, betas=(0.5, 0.99))
+        self.muon.step([grads[i] for i in self.matrices], lr=matrix_lr, momentum=0.9)
+        self.optimizer.step([grads[i] for i in self.others], lr=lr, step=self.steps,
+                            betas=(0.5, 0.99))
         return (diff * diff).mean()
 
 
@@ -109,8 +122,8 @@ def class_images(classes, size, device="cuda"):
     return 0.8 * torch.cat([image, -image, image.roll(size // 4, 3)], 1)
 
 
-def train_generator(steps, batch=64, classes=10, states=32, seed=0, report=None):
-    gen = Generator(batch, classes, states=states, seed=seed)
+def train_generator(steps, batch=64, classes=10, states=32, seed=0, report=None, **kw):
+    gen = Generator(batch, classes, states=states, seed=seed, **kw)
     patterns = class_images(classes, 4 << len(gen.channels))
     rng = torch.Generator("cuda").manual_seed(seed)
     losses = []
@@ -129,8 +142,11 @@ def main():
     ap.add_argument("--batch", type=int, default=64)
     ap.add_argument("--classes", type=int, default=10)
     ap.add_argument("--states", type=int, default=32, choices=(32, 8))
+    ap.add_argument("--norm", default="group", choices=("group", "layer"))
+    ap.add_argument("--optimizer", default="adamw", choices=("adamw", "muon"))
     a = ap.parse_args()
-    train_generator(a.steps, a.batch, a.classes, a.states, report=20)
+    train_generator(a.steps, a.batch, a.classes, a.states, report=20, norm=a.norm,
+                    optimizer=a.optimizer)
 
 
 if __name__ == "__main__":

@@ -113,8 +113,9 @@ typedef struct {
 typedef struct huge2_layer_norm_plan huge2_layer_norm_plan;
 
 /* Chooses the kernels for desc and allocates the gradient's workspace: 8 bytes a channel for
- * each of its workgroups, at most 4096 of them.  No work is enqueued.  Errors: INVALID_ARG,
- * UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all), ALLOC. */
+ * each of its workgroups, at most 4096 of them or 2% of x, dy and dx beyond 256.  No work is enqueued.  Errors: INVALID_ARG,
+ * UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or more channels or tiles of pixels
+ * than launches can take: 2^24 channels and 2^37 pixels always fit), ALLOC. */
 huge2_status huge2_layer_norm_plan_create(huge2_layer_norm_plan** out,
                                           const huge2_layer_norm_desc* desc);
 
@@ -253,8 +254,8 @@ huge2_status huge2_adamw_plan_destroy(huge2_adamw_plan* plan);
 /* ---- orthogonalised matrices ------------------------------------------------ */
 
 /* What a product's operands hold: two fp16 parts of a value (22 bits; results as of products in
- * fp32), or one (11 bits; results within 2^-10 of their norm, a third of the time).  Sums are
- * fp32 either way. */
+ * fp32), or one (11 bits; results within 2^-10 of their norm, 2^-6 for matrices of low rank, in
+ * less than half of the time).  Sums are fp32 either way. */
 typedef enum { HUGE2_PRODUCTS_F32 = 0, HUGE2_PRODUCTS_F16 = 1 } huge2_products;
 
 /* Newton-Schulz steps that bring all singular values of a matrix near 1:
@@ -269,12 +270,12 @@ typedef struct {
   int32_t products;           /* huge2_products */
   const double* coefficients; /* read by the call that makes a plan.  The polynomials must keep
                                  singular values, which begin in [0, 1], below 2^10, and
-                                 |b| s^2 + |c| s^4 of their bound s below 2^22 */
+                                 |b| s^2 + 3 |c| s^4 of their bound s below 2^24 */
   double eps;                 /* >= 2^-126 and finite */
 } huge2_newton_schulz;
 
 typedef struct {
-  int32_t batch, rows, cols; /* >= 1; rows*cols below 2^31 */
+  int32_t batch, rows, cols; /* >= 1; rows and cols up to 2^28, rows*cols below 2^31 */
   int32_t dtype;             /* huge2_dtype of x and y */
 } huge2_orthogonalize_desc;
 
@@ -283,9 +284,9 @@ typedef struct huge2_orthogonalize_plan huge2_orthogonalize_plan;
 /* A plan for `batch` matrices of one shape, one behind the other.  Allocates the operands of as
  * many of them as are worked on together (up to 256 and some 4 GiB): for m the smaller and n the
  * larger of rows and cols, each rounded up to 64, 12 m n + 8 m^2 bytes with two parts and 12 m n +
- * 6 m^2 with one, and sums of parts of products, 64 KB each, up to some 1000.  Copies its lists
- * of work on hip_stream and waits for it.  Errors: INVALID_ARG, UNSUPPORTED (matrices of
- * 2^31 elements, more than 2^20 of them, 2^40 elements in all), ALLOC, HIP. */
+ * 6 m^2 with one, and partial sums of products, up to some 100 MB.  Copies its lists of work on
+ * hip_stream and waits for it.  Errors: INVALID_ARG, UNSUPPORTED (larger matrices, more than
+ * 2^20 of them, 2^40 elements in all), ALLOC, HIP. */
 huge2_status huge2_orthogonalize_plan_create(huge2_orthogonalize_plan** out,
                                              const huge2_orthogonalize_desc* desc,
                                              const huge2_newton_schulz* ns, void* hip_stream);
@@ -306,7 +307,7 @@ typedef struct {
   void* param;
   float* m;   /* the momentum, which starts as zeros */
   void* copy; /* NULL, or bfloat16: receives the updated parameter rounded */
-  int32_t rows, cols; /* >= 1; rows*cols below 2^31 */
+  int32_t rows, cols; /* >= 1 and up to 2^28; rows*cols below 2^31 */
   int32_t dtype;      /* huge2_dtype of param */
   int32_t grad_dtype; /* huge2_dtype of its gradient */
   float weight_decay; /* >= 0 and finite */
@@ -317,8 +318,7 @@ typedef struct huge2_muon_plan huge2_muon_plan;
 
 /* A plan for `count` matrices (>= 0), which must outlive it.  No two of their arrays may
  * overlap.  Allocates and copies as huge2_orthogonalize_plan_create does.  Errors: INVALID_ARG,
- * UNSUPPORTED (a matrix of 2^31 elements, more than 2^20 of them, 2^40 elements in all), ALLOC,
- * HIP. */
+ * UNSUPPORTED (a larger matrix, more than 2^20 of them, 2^40 elements in all), ALLOC, HIP. */
 huge2_status huge2_muon_plan_create(huge2_muon_plan** out, const huge2_muon_tensor* tensors,
                                     int32_t count, const huge2_newton_schulz* ns,
                                     void* hip_stream);

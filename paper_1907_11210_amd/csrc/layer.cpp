@@ -110,10 +110,13 @@ huge2_status layer_create(huge2_layer_norm_plan** out, const huge2_layer_norm_de
   const long long hw = (long long)d.h * d.w;
   if (hw >= (1ll << 31) || hw * d.c >= (1ll << 31) || hw * d.c * d.n >= (1ll << 40))
     return HUGE2_ERR_UNSUPPORTED;
+  const bool rows = d.layout == HUGE2_NHWC || hw == 1;
+  // (a workgroup of 256 for a channel of planes, of 1024 for 16 channels' sums)
+  if (!launchable(rows ? d.c / 16 + 1 : d.c, rows ? 1024 : 256)) return HUGE2_ERR_UNSUPPORTED;
   huge2_layer_norm_plan* p = new (std::nothrow) huge2_layer_norm_plan();
   if (!p) return HUGE2_ERR_ALLOC;
   p->desc = d;
-  p->rows = d.layout == HUGE2_NHWC || hw == 1;
+  p->rows = rows;
   const int full = 16 / elem_size(d.dtype);
   p->vec = (p->rows ? d.c : hw) >= full ? full : 1;
   size_t part_b = 0;

@@ -251,7 +251,7 @@ huge2_status engine_create(NsEngine* e, const huge2_newton_schulz& ns, hipStream
     image.resize(list->at + round256(bytes));
     if (bytes) std::memcpy(image.data() + list->at, works.data(), bytes);
   };
-  int most_slots = 0;
+  size_t parts_b = 0;
   for (Group& g : e->groups) {
     std::vector<uint2> norm, pack;
     for (int i = 0; i < g.count; ++i) {
@@ -266,12 +266,11 @@ huge2_status engine_create(NsEngine* e, const huge2_newton_schulz& ns, hipStream
       std::vector<NsWork> works, joins;
       int slots;
       product_works(*e, g, kind, &works, &joins, &slots);
-      most_slots = std::max(most_slots, slots);
+      parts_b = std::max(parts_b, slots * kNsTiles[g.size[kind]].slot() * sizeof(float));
       append(&g.product[kind], works);
       append(&g.join[kind], joins);
     }
   }
-  const size_t parts_b = (size_t)most_slots * kNsSlot * sizeof(float);
   huge2_status st = device_alloc(&e->ws, parts_b + ws_b);
   if (st == HUGE2_OK && !e->mats.empty()) st = device_alloc(&e->table, image.size());
   if (st != HUGE2_OK) return st;
@@ -343,6 +342,7 @@ bool valid(const huge2_orthogonalize_desc& d) {
   return d.batch >= 1 && d.rows >= 1 && d.cols >= 1 && is_dtype(d.dtype);
 }
 constexpr long long kMostElements = 1ll << 31;  // of a matrix, below
+constexpr int kMostSide = 1 << 28;
 constexpr int kMostMatrices = 1 << 20;
 
 size_t bytes_of(const huge2_orthogonalize_desc& d) {
@@ -356,7 +356,8 @@ huge2_status orthogonalize_create(huge2_orthogonalize_plan** out,
   *out = nullptr;
   if (!desc || !valid(*desc) || !valid(ns)) return HUGE2_ERR_INVALID_ARG;
   const long long count = (long long)desc->rows * desc->cols;
-  if (count >= kMostElements || desc->batch > kMostMatrices ||
+  if (count >= kMostElements || std::max(desc->rows, desc->cols) > kMostSide ||
+      desc->batch > kMostMatrices ||
       count * desc->batch >= (1ll << 40))
     return HUGE2_ERR_UNSUPPORTED;
   std::unique_ptr<huge2_orthogonalize_plan> p(new huge2_orthogonalize_plan());
@@ -409,7 +410,8 @@ huge2_status muon_create(huge2_muon_plan** out, const huge2_muon_tensor* tensors
     const huge2_muon_tensor& t = tensors[i];
     if (!valid(t)) return HUGE2_ERR_INVALID_ARG;
     const long long n = (long long)t.rows * t.cols;
-    if (n >= kMostElements || (total += n) >= (1ll << 40)) return HUGE2_ERR_UNSUPPORTED;
+    if (n >= kMostElements || std::max(t.rows, t.cols) > kMostSide || (total += n) >= (1ll << 40))
+      return HUGE2_ERR_UNSUPPORTED;
     for (const Span& s : {Span{t.param, (size_t)n * elem_size(t.dtype)},
                           Span{t.m, (size_t)n * sizeof(float)}, Span{t.copy, (size_t)n * 2}})
       spans.push_back(s);

@@ -5,14 +5,15 @@
 // are computed.  The products take fp16 operands times powers of two, sums are fp32.
 //
 // Two parts a value, hi + lo, are 22 bits, and hi hi + hi lo + lo hi gives fp32's accuracy: after
-// five steps 4e-7 of the result's norm against 2e-7 for products in fp32, and 4e-6 against 2e-6
-// where singular values fall with the square of their rank.
+// five steps 4e-7 of the result's norm (products in fp32 2e-7), 4e-6 (2e-6) where singular values
+// fall with the square of their rank, up to 1e-4 where all but a few are nothing and what
+// roundings leave in their place grows 480 times.
 //
-// One part is 11 bits.  Two things keep its error below 7e-4 of the result's norm, whatever the
-// singular values (2e-3 and, for steep ones, 2e-2 without them; bf16 1e-2 and 0.15).  The term
-// a X, which carries what small singular values grow from, is formed from both parts.  And A is
-// stored less mu I, mu the mean of its diagonal, which in the last steps is near 1 and would
-// round off what the other elements hold: with A = A' + mu I,
+// One part is 11 bits: 7e-4 of the result's norm, of falling singular values 3e-4, of a matrix
+// of low rank up to 1e-2 (bf16 products 1e-2, 0.15 and more).  Two things keep it there.  The term
+// a X, which carries what small singular values grow from, is formed from both parts (else 2e-2
+// where they fall).  And A is stored less mu I, mu the mean of its diagonal, which in the last
+// steps is near 1 and would round off what the other elements hold (else 2e-3): with A = A' + mu I,
 //   a I + b A + c A A = (a + b mu + c mu^2) I + B,  B = (b + 2 c mu) A' + c A' A'.
 #include "huge2_train.h"
 #include "newton.hpp"
@@ -372,7 +373,7 @@ struct Product {
 
   // Partial sums lie as the threads hold them.
   static __device__ __forceinline__ void store_part(float* part, int slot, const Acc& acc) {
-    float* to = part + (size_t)slot * kNsSlot + threadIdx.x * 4;
+    float* to = part + slot * kTile.slot() + threadIdx.x * 4;
 #pragma unroll
     for (int k = 0; k < kOfWave; ++k)
 #pragma unroll
@@ -383,14 +384,14 @@ struct Product {
   // A block's sums over the parts, in their order.
   static __device__ __forceinline__ void load_parts(const float* part, int slot, int slots,
                                                     int block, f32x16& acc) {
-    const float* from = part + (size_t)slot * kNsSlot + block * 4096 + threadIdx.x * 4;
+    const float* from = part + slot * kTile.slot() + block * 4096 + threadIdx.x * 4;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll 4
     for (int k = 0; k < slots; ++k) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 v = *(const float4*)(from + (size_t)k * kNsSlot + g * 1024);
+        const float4 v = *(const float4*)(from + k * kTile.slot() + g * 1024);
         acc[4 * g] += v.x, acc[4 * g + 1] += v.y, acc[4 * g + 2] += v.z, acc[4 * g + 3] += v.w;
       }
     }

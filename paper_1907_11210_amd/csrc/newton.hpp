@@ -55,13 +55,12 @@ struct NsTile {
   int rows, cols, stage, buffers;
   int waves;  // of a SIMD, which its registers leave room for
   constexpr int lds() const { return (rows + cols) * stage * 2 * buffers; }
+  constexpr size_t slot() const { return (size_t)rows * cols; }  // elements of a partial tile
   constexpr int blocks() const { return rows / 64 * (cols / 64); }  // of 32 x 32 to a wave
 };
 constexpr int kNsSizes = 3;
 constexpr NsTile kNsTiles[kNsSizes] = {
     {64, 64, 64, 3, 3}, {128, 128, 32, 4, 2}, {256, 128, 32, 3, 2}};
-constexpr int kNsSlot = 256 * 128;  // elements of a partial tile
-
 // Products: A = X X^T, A A, B X, and B X of the last step.
 enum NsKind { kNsGram = 0, kNsSquare = 1, kNsApply = 2, kNsLast = 3 };
 
@@ -82,7 +81,7 @@ struct NsArgs {
 };
 struct NsInput {
   const NsMatrix* mats;
-  const uint2* works;    // (matrix, chunk of a sum), or (matrix, packed block)
+  const uint2* works;    // (matrix, chunk of a sum or packed block)
   int muon, nesterov;
   int keep_lo;           // there is one step
   float momentum, rest;  // rest: 1 - momentum

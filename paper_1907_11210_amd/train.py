@@ -651,7 +651,8 @@ class AdamW(_Optimizer):
 class Orthogonalize(_Owner):
     """Newton-Schulz steps of matrices of one shape [..., rows, cols], which bring their singular
     values near 1.  products: "f32" (results as of products in fp32, the default for float32) or
-    "f16" (within 2^-10 of a result's norm, the default for bfloat16).  coefficients: one triple
+    "f16" (within 2^-10 of a result's norm, 2^-6 for matrices of low rank; the default for
+    bfloat16).  coefficients: one triple
     (a, b, c), or one for each step."""
     _destroy = staticmethod(huge2_orthogonalize_plan_destroy)
 

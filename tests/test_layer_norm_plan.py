@@ -36,7 +36,8 @@ def test_refuses_descriptors(kw):
 @pytest.mark.parametrize("kw", [
     dict(h=1 << 16, w=1 << 15), dict(h=1 << 14, w=1 << 14, c=12),
     dict(n=1 << 20, h=1 << 10, w=1 << 10),
-    dict(n=(1 << 31) - 1, c=1, h=1, w=65, layout=h2.HUGE2_NCHW)])
+    dict(n=(1 << 31) - 1, c=1, h=1, w=65, layout=h2.HUGE2_NCHW),
+    dict(n=1, c=1 << 26, h=1, w=1), dict(n=1, c=1 << 24, h=1, w=2, layout=h2.HUGE2_NCHW)])
 def test_refuses_what_is_too_large(kw):
     assert _create(**kw) == h2.HUGE2_ERR_UNSUPPORTED
 
