@@ -208,7 +208,8 @@ void product_works(NsEngine& e, Group& g, int kind, std::vector<NsWork>* works,
   for (size_t k = 0; k < all.size(); ++k) {
     NsWork w = all[k];
     const int stages = w.k1;
-    const double piece = std::max(16.0, (k < whole ? cost : left) / kUnits);
+    // (pieces of 1024 columns of small tiles: shorter ones lose more to the join than they gain)
+    const double piece = std::max(size == 0 ? 32.0 : 16.0, (k < whole ? cost : left) / kUnits);
     // (rounded down behind whole tiles, which hide an uneven end)
     const int cuts = std::max(1, std::min(stages / 8, (int)(stages / piece + (whole ? 0.0 : 0.6))));
     if (cuts > 1) {
