@@ -387,28 +387,30 @@ __global__ __launch_bounds__(256) void layer_long_sums_kernel(LayerArgs a) {
   });
 }
 
-// dgamma and dbeta from the workgroups' sums: 16 channels, 64 rows of threads.
-__global__ __launch_bounds__(1024) void layer_params_kernel(LayerArgs a) {
+// dgamma and dbeta from the workgroups' sums, 2^cols_log2 channels side by side.  Bound by launch
+// and latency: 4 channels wherever that is at most a workgroup to each compute unit (983 sums of
+// 128 channels 3.8 us, 6.9 by 16; 491 of 1024 4.7 against 5.1), 16 of more (491 of 2048 5.4 us,
+// 7.2 by 4; 256 of 16384 7.6 and 22.9).
+__global__ __launch_bounds__(1024) void layer_params_kernel(LayerArgs a, int cols_log2) {
   __shared__ float2 lds[16][16];
-  const int col = threadIdx.x & 15, row = threadIdx.x >> 4;
-  const int ch = blockIdx.x * 16 + col;
+  const int cols = 1 << cols_log2, col = threadIdx.x & (cols - 1), row = threadIdx.x >> cols_log2;
+  const int ch = (blockIdx.x << cols_log2) + col, rows = 1024 >> cols_log2;
   float2 s = make_float2(0.f, 0.f);
   if (ch < a.c) {
-#pragma unroll 16
-    for (int r = row; r < a.parts; r += 64) {
+#pragma unroll 8
+    for (int r = row; r < a.parts; r += rows) {
       const float2 v = a.part[(size_t)r * a.c + ch];
       s.x += v.x;
       s.y += v.y;
     }
   }
-#pragma unroll
-  for (int m = 16; m < 64; m <<= 1) {
+  for (int m = cols; m < 64; m <<= 1) {
     s.x += __shfl_xor(s.x, m);
     s.y += __shfl_xor(s.y, m);
   }
-  if ((threadIdx.x & 63) < 16) lds[threadIdx.x >> 6][col] = s;
+  if ((int)(threadIdx.x & 63) < cols) lds[threadIdx.x >> 6][col] = s;
   __syncthreads();
-  if (threadIdx.x >= 16 || ch >= a.c) return;
+  if ((int)threadIdx.x >= cols || ch >= a.c) return;
   s = lds[0][col];
   for (int w = 1; w < 16; ++w) {
     s.x += lds[w][col].x;
@@ -419,8 +421,10 @@ __global__ __launch_bounds__(1024) void layer_params_kernel(LayerArgs a) {
 }
 
 hipError_t launch_layer_params(const LayerArgs& a, hipStream_t stream) {
+  const int log2 = a.c <= 1024 ? 2 : 4;
   if (a.part)
-    hipLaunchKernelGGL(layer_params_kernel, dim3((a.c + 15) / 16), dim3(1024), 0, stream, a);
+    hipLaunchKernelGGL(layer_params_kernel, dim3((unsigned)((a.c + (1ll << log2) - 1) >> log2)),
+                       dim3(1024), 0, stream, a, log2);
   return hipGetLastError();
 }
 
