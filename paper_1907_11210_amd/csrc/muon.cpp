@@ -148,7 +148,7 @@ void shape(NsMatrix* t, long long rows, long long cols) {
   t->n = (int)std::max(rows, cols);
   t->mp = pad(t->m), t->np = pad(t->n);
   t->count = rows * cols;
-  t->norm_chunk = (int)(ceil_div(std::max(4096ll, ceil_div(t->count, 512)), 256) * 256);
+  t->norm_chunk = (int)(ceil_div(std::max(4096ll, ceil_div(t->count, 1024)), 256) * 256);
   t->norm_count = (int)ceil_div(t->count, t->norm_chunk);
 }
 

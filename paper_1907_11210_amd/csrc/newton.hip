@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
   const long long first = (long long)work.y * t.norm_chunk;
   const long long end = min(first + t.norm_chunk, t.count);
   double s = 0;
-  constexpr int kAhead = 4;  // vectors of four in flight
+  constexpr int kAhead = 8;  // vectors of four in flight
   for (long long i = first + threadIdx.x * 4; i < end; i += kAhead * 1024) {
     float g[kAhead][4], m[kAhead][4];
 #pragma unroll
