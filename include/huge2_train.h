@@ -8,7 +8,10 @@
  *   embedding lookup with a scale, and the table's gradient: class labels of a
  *     conditional generator, maps of code indices, text tokens;
  *   an AdamW step over many tensors in one call, with the moments in 32 bits
- *     or in 8: what takes the weight gradients.
+ *     or in 8: what takes the weight gradients;
+ *   orthogonalised matrices by Newton-Schulz steps, and a Muon step over many
+ *     matrices in one call, whose updates they are: what takes the gradients of
+ *     the convolutions' weights where AdamW takes the rest.
  *
  * The conventions of huge2.h hold: device pointers owned by the caller,
  * contiguous in the stated order and 16-byte aligned unless stated; every
@@ -20,7 +23,7 @@
  * atomics).  A plan's workspace is shared by the calls on it: enqueue them on
  * one stream, or order them.  The calls that run a plan allocate nothing and
  * can be recorded into a HIP graph, whose replays repeat them as they were recorded:
- * on the same pointers, and an AdamW step with its step number, rates and decays.
+ * on the same pointers, and an AdamW or Muon step with its step number, rates and decays.
  */
 #ifndef HUGE2_TRAIN_H
 #define HUGE2_TRAIN_H
@@ -113,9 +116,9 @@ typedef struct {
 typedef struct huge2_layer_norm_plan huge2_layer_norm_plan;
 
 /* Chooses the kernels for desc and allocates the gradient's workspace: 8 bytes a channel for
- * each of its workgroups, at most 4096 of them or 2% of x, dy and dx beyond 256.  No work is enqueued.  Errors: INVALID_ARG,
- * UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or more channels or tiles of pixels
- * than launches can take: 2^24 channels and 2^37 pixels always fit), ALLOC. */
+ * each of its workgroups, of which there are 4096 at most.  No work is enqueued.  Errors:
+ * INVALID_ARG, UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or more channels or
+ * tiles of pixels than launches can take: 2^24 channels and 2^37 pixels always fit), ALLOC. */
 huge2_status huge2_layer_norm_plan_create(huge2_layer_norm_plan** out,
                                           const huge2_layer_norm_desc* desc);
 

@@ -42,13 +42,15 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 void choose_rows(LayerArgs* a, int vec, int esz, bool grad) {
   const long long vecs = ceil_div(a->c, vec);
   const auto most = [&] {
-    const int channels = a->lanes_log2 > 6 ? kLayerWideChannels : grad ? kLayerGradChannels : kLayerChannels;
+    const int channels = a->lanes_log2 > 6 ? kLayerWideChannels
+                         : grad            ? kLayerGradChannels
+                                           : kLayerChannels;
     return std::max(1, channels / vec);
   };
   a->lanes_log2 = std::min(6, log2_ceil(vecs));
   while (a->lanes_log2 < 10 && vecs > (long long)most() << a->lanes_log2) ++a->lanes_log2;
-  const long long slots = a->lanes_log2 > 6 ? most()
-                                            : 1ll << log2_ceil(ceil_div(vecs, 1ll << a->lanes_log2));
+  const long long slots =
+      a->lanes_log2 > 6 ? most() : 1ll << log2_ceil(ceil_div(vecs, 1ll << a->lanes_log2));
   a->slots = vecs > (long long)most() << a->lanes_log2 ? 0 : (int)slots;
   // (lanes of more than a wave are a whole workgroup)
   a->threads = !a->slots ? 1024 : a->lanes_log2 > 6 ? 1 << a->lanes_log2 : 256;

@@ -101,7 +101,8 @@ __device__ __forceinline__ int scatter_at() {
 }
 template <int N>
 __device__ __forceinline__ void scatter_sum(float (&v)[N], int log2) {
-  constexpr int kHalf = N > 1 ? N / 2 : 1, kQuarter = N > 3 ? N / 4 : 1, kEighth = N > 7 ? N / 8 : 1;
+  constexpr int kHalf = N > 1 ? N / 2 : 1, kQuarter = N > 3 ? N / 4 : 1;
+  constexpr int kEighth = N > 7 ? N / 8 : 1;
 #pragma unroll
   for (int e = 0; e < kHalf; ++e) v[e] = swap_sum32(v[e], v[N > 1 ? e + kHalf : e]);
 #pragma unroll
@@ -123,7 +124,8 @@ __device__ __forceinline__ void scatter_sum(float (&v)[N], int log2) {
 // y of a value less its mean.  A ReLU's z is rounded as the gradient rounds it.
 template <int ACT, typename T>
 __device__ __forceinline__ float layer_value(float d, float rstd, float gamma, float beta) {
-  const float z = ACT == HUGE2_NORM_RELU ? norm_z(d * rstd, gamma, beta) : fmaf(d, rstd * gamma, beta);
+  const float z =
+      ACT == HUGE2_NORM_RELU ? norm_z(d * rstd, gamma, beta) : fmaf(d, rstd * gamma, beta);
   return norm_act<ACT, T>(z);
 }
 // xh and dz of one value.

@@ -73,6 +73,9 @@ __device__ __forceinline__ Channel slot_params(const LayerArgs& a, int ch) {
 // A tile's channels are held by the rows of a workgroup, R vectors a thread, or (R = 0) read
 // again for each of the sums and the result.  (A tile to a workgroup: in a loop over tiles the
 // compiler holds what does not change, and 40 of 128 registers spill.)
+//
+// 64 images of 256x16x16 bf16 8.0 us, 17 MB: one round of 256 tiles, bound by its latency (loads,
+// two sums through LDS, stores); 64 of 128x64x64 36 us, 134 MB at 3.7 TB/s.
 template <typename T, int VW, int R, bool RAGGED>
 __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -155,6 +158,9 @@ __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
 
 // The gradient by the same tiles.  A thread adds up dgamma and dbeta of its channels over the
 // workgroup's tiles (R = 0: layer_plane_sums_kernel does).
+//
+// 5 images of 200x33x41 fp32 with SiLU 10.9 us, 16 MB: one round of 215 tiles, in which fp32's
+// exponential and division take as long as the loads; 64 of 128x64x64 bf16 55 us, 3.7 TB/s.
 template <typename T, int VW, int R, bool RAGGED>
 __global__ __launch_bounds__(R * VW > kLayerWideChannels ? 512 : 1024) void
 layer_grad_planes_kernel(LayerArgs a) {

@@ -135,7 +135,10 @@ struct Lanes {
 // next on its way while one is worked on.  WAVE: teams are waves or parts of them, else a
 // workgroup.
 //
-// Bound by the bytes: 64x64x2048, 8 images, bf16.
+// Bound by the bytes: 8 images of 64x64x2048 bf16 49 us, 268 MB at 5.5 TB/s (a copy: 5.2, which
+// this passes since the results leave past the caches).  In small calls by latency: a load, two
+// sums over lanes, a store, 3.7 us of 64 rows of 512.  Teams are waves or less as long as a
+// wave's registers hold a row (32 channels a lane), since a wave's sums need no barrier.
 template <typename T, int VW, int R, int FILL, bool WAVE>
 __global__ __launch_bounds__(WAVE ? 256 : 1024) void layer_rows_kernel(LayerArgs a) {
   __shared__ float lds[16];
@@ -191,6 +194,10 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void layer_rows_kernel(LayerArgs
 // The gradient by the same rows: x and dy held, the two means, dx from registers.  A thread
 // adds up dgamma and dbeta of its channels over the team's rows; the teams' sums are joined
 // in LDS, the workgroups' by layer_params_kernel.
+//
+// Bound by the bytes: 32768 rows of 1024 bf16 41 us, 201 MB at 4.9 TB/s, and 5 us of
+// layer_params_kernel; 65536 rows of 128 15.9 us, 3.2 TB/s: four or five rows a
+// team one behind the other, each a load, sums over lanes and a store, and the sums' join.
 template <typename T, int VW, int R, int FILL, bool WAVE>
 __global__ __launch_bounds__(WAVE ? 256 : 1024) void layer_grad_rows_kernel(LayerArgs a) {
   __shared__ float2 lds[16];
@@ -279,7 +286,10 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void layer_grad_rows_kernel(Laye
     }
 }
 
-// Rows of any length, a workgroup each, read again for each of the sums and the result.
+// Rows of any length (over 32 or 16 channels a thread of the largest workgroup), a workgroup
+// each, read again for each of the sums and the result, from the caches as far as those hold the
+// rows in work: 1024 rows of 32768 bf16 36 us, 134 MB at 3.7 TB/s, the gradient 48 and 27 of
+// layer_long_sums_kernel.
 template <typename T, int VW, bool RAGGED, bool GRAD>
 __global__ __launch_bounds__(1024) void layer_long_kernel(LayerArgs a) {
   __shared__ float2 lds[16];
@@ -388,16 +398,16 @@ __global__ __launch_bounds__(256) void layer_long_sums_kernel(LayerArgs a) {
 }
 
 // dgamma and dbeta from the workgroups' sums, 2^cols_log2 channels side by side.  Bound by launch
-// and latency: 4 channels wherever that is at most a workgroup to each compute unit (983 sums of
-// 128 channels 3.8 us, 6.9 by 16; 491 of 1024 4.7 against 5.1), 16 of more (491 of 2048 5.4 us,
-// 7.2 by 4; 256 of 16384 7.6 and 22.9).
+// and latency: 4 channels of fewer than 1024 (983 sums of 128 channels 3.9 us, 6.9 by 16), 16 of
+// more, whose lines 4 would read four times (491 of 1024 4.7 us either way, of 2048 5.2 and 7.2,
+// 256 of 16384 7.5 and 22.9).
 __global__ __launch_bounds__(1024) void layer_params_kernel(LayerArgs a, int cols_log2) {
   __shared__ float2 lds[16][16];
   const int cols = 1 << cols_log2, col = threadIdx.x & (cols - 1), row = threadIdx.x >> cols_log2;
   const int ch = (blockIdx.x << cols_log2) + col, rows = 1024 >> cols_log2;
   float2 s = make_float2(0.f, 0.f);
   if (ch < a.c) {
-#pragma unroll 8
+#pragma unroll 16
     for (int r = row; r < a.parts; r += rows) {
       const float2 v = a.part[(size_t)r * a.c + ch];
       s.x += v.x;
@@ -421,7 +431,7 @@ __global__ __launch_bounds__(1024) void layer_params_kernel(LayerArgs a, int col
 }
 
 hipError_t launch_layer_params(const LayerArgs& a, hipStream_t stream) {
-  const int log2 = a.c <= 1024 ? 2 : 4;
+  const int log2 = a.c < 1024 ? 2 : 4;
   if (a.part)
     hipLaunchKernelGGL(layer_params_kernel, dim3((unsigned)((a.c + (1ll << log2) - 1) >> log2)),
                        dim3(1024), 0, stream, a, log2);

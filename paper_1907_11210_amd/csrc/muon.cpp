@@ -114,7 +114,8 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 size_t squares_room(const NsMatrix& t) {
   size_t most = 0;
   for (const NsTile& tile : kNsTiles)
-    most = std::max<size_t>(most, ceil_div(t.mp, tile.rows) * ceil_div(t.np, tile.cols) * tile.blocks());
+    most = std::max<size_t>(
+        most, ceil_div(t.mp, tile.rows) * ceil_div(t.np, tile.cols) * tile.blocks());
   return most;
 }
 size_t workspace(const NsMatrix& t, int parts) {
@@ -167,7 +168,13 @@ void each_tile(const NsMatrix& t, int kind, int size, F&& f) {
 constexpr int kUnits = 256;  // compute units
 
 // The size of a product's tiles.  Large ones need the least of LDS and the caches, and enough
-// columns to be worth their long prologue and epilogue; small ones start and end sooner.
+// columns to be worth their long prologue and epilogue; small ones start and end sooner.  Whole
+// passes in us with the small, middle and large tiles alone:
+//   1 of 4096x8192, one part                       4950  2950  2710
+//   6 of 4096x4096 and the like, one part         11600  7700  6600
+//   5 of 100x16384 to 128x48, two parts             903   801   889
+//   48 of 33x700 to 644x89, one part                278   270   365
+//   6 of 1000x333, two parts                        200   220   304
 int tile_size(const NsEngine& e, const Group& g, int kind) {
   if (const char* f = std::getenv("HUGE2_NS_TILE")) return std::abs(std::atoi(f)) % kNsSizes;
   long long tiles[kNsSizes] = {}, columns[kNsSizes] = {};
@@ -175,14 +182,17 @@ int tile_size(const NsEngine& e, const Group& g, int kind) {
     for (int size = 0; size < kNsSizes; ++size)
       each_tile(e.mats[g.first + i], kind, size, [&](int, int) {
         ++tiles[size];
-        columns[size] += (kind == kNsGram ? e.mats[g.first + i].np : e.mats[g.first + i].mp) * e.parts;
+        const NsMatrix& t = e.mats[g.first + i];
+        columns[size] += (kind == kNsGram ? t.np : t.mp) * e.parts;
       });
   if (tiles[2] >= kUnits * 3 / 4 && columns[2] >= tiles[2] * 2048) return 2;
   return columns[1] >= kUnits * (kind == kNsLast ? 1024ll : 512ll) ? 1 : 0;
 }
 
 // A product's tiles.  Where they do not fill the compute units, or leave some over that would
-// run alone, those are cut along their sum: `slots` counts partial tiles.
+// run alone, those are cut along their sum: `slots` counts partial tiles.  (4096x8192: 272 large
+// tiles of the first product are 256 and 16 in 16 pieces each.  Uncut, 16 units have
+// two tiles and the others wait for them.)
 void product_works(NsEngine& e, Group& g, int kind, std::vector<NsWork>* works,
                    std::vector<NsWork>* joins, int* slots) {
   const int size = g.size[kind] = tile_size(e, g, kind);
@@ -217,7 +227,8 @@ void product_works(NsEngine& e, Group& g, int kind, std::vector<NsWork>* works,
       join.slot = *slots, join.slots = cuts;
       joins->push_back(join);
       for (int c = 0; c < cuts; ++c) {
-        w.k0 = (int)((long long)stages * c / cuts), w.k1 = (int)((long long)stages * (c + 1) / cuts);
+        w.k0 = (int)((long long)stages * c / cuts);
+        w.k1 = (int)((long long)stages * (c + 1) / cuts);
         w.slot = (*slots)++;
         works->push_back(w);
       }

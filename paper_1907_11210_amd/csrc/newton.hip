@@ -121,7 +121,10 @@ __device__ __forceinline__ void input4(const void* p, int bf16, long long i, lon
 }  // namespace
 
 // The momentum's update, and sums of squares of what is orthogonalised.  In 64 bits: squares
-// of any two floats' sum neither overflow nor vanish.
+// of any two floats' sum neither overflow nor vanish.  Bound by the bytes where there are enough:
+// 88 M elements of bf16 gradients and fp32 momenta 155 us, 881 MB at 5.7 TB/s
+// (eight vectors in flight 161 us; 48 small matrices 13.5 us, 20.3 with eight).  At most 1024 sums
+// of a matrix: with 512 33.6 M bf16 elements took 57 us, now 37.
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
   __shared__ double lds[4];
   const uint2 work = a.works[blockIdx.x];
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
   const long long first = (long long)work.y * t.norm_chunk;
   const long long end = min(first + t.norm_chunk, t.count);
   double s = 0;
-  constexpr int kAhead = 8;  // vectors of four in flight
+  constexpr int kAhead = 4;  // vectors of four in flight
   for (long long i = first + threadIdx.x * 4; i < end; i += kAhead * 1024) {
     float g[kAhead][4], m[kAhead][4];
 #pragma unroll
@@ -167,7 +170,9 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
 }
 
 // X = U / (norm + eps) and its transpose as fragments, a block of 64 x 64 of the input to a
-// workgroup.
+// workgroup.  Bound by the bytes: of 33.6 M bf16 elements 76 us, 269 MB at 3.5 TB/s, of which three
+// quarters are written in pieces of 512 bytes.  (The products then need no transpose: read by
+// the other axis, a fragment would be 16 loads of 2 bytes a lane.)
 template <int PARTS>
 __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
   __shared__ float tile[kNsBlock][kNsBlock + 1];
@@ -231,6 +236,18 @@ namespace {
 
 // A tile of a product P Q^T by four waves, each a quarter: KIND's operands, and what becomes of
 // the sums.
+//
+// Bound by the matrix units and the reads of LDS that feed them: of one matrix of 4096x8192 B X
+// takes 287 us, 275 GF at 958 TFLOP/s (a large library product of fp16 1080), its matrix units
+// busy for 56% of the cycles, without conflicts of LDS banks; A, half of the tiles, 162 us and
+// 17 of the join, 770 TFLOP/s; A A 79 and 7, 800.  With two parts three products each: B X of
+// 100x16384 to 1024x8192 71 us.  Where matrices are small (6 of 1000x333, 8 to 19 us a product)
+// bound by latency: a launch, three stages' loads, one or a few rounds of tiles.  What made it
+// fast on the large matrix: operands stored as fragments, so that loads go straight into LDS and reads are
+// 16 bytes a lane side by side; three or four stages on their way and a wait that counts them
+// instead of a wait for all; fragments read a stage ahead of their products; the order of
+// instructions (below); the epilogue as a loop over blocks (its straight code was read from
+// memory once and took longer than the work).
 template <int PARTS, int KIND, int SIZE>
 struct Product {
   static constexpr NsTile kTile = kNsTiles[SIZE];
@@ -594,7 +611,8 @@ struct Product {
       if (kOwn < kOfWave && k + kOwn < kOfWave) {
 #pragma unroll
         for (int i = 0; i < kOwn; ++i)
-          if (k % kOwn == i) load_own(a, t, block_row(w, k + kOwn), block_column(w, k + kOwn), own[i]);
+          if (k % kOwn == i)
+            load_own(a, t, block_row(w, k + kOwn), block_column(w, k + kOwn), own[i]);
       }
       float params[16];
 #pragma unroll
@@ -631,7 +649,8 @@ __global__ __launch_bounds__(256, kNsTiles[SIZE].waves) void ns_product_kernel(N
   Product<PARTS, KIND, SIZE>::tile(a, t, w, lds);
 }
 
-// Adds up the partial tiles, in their order, a block of each wave's to a workgroup.
+// Adds up the partial tiles, in their order, a block of each wave's to a workgroup: 6 to 20 us,
+// bound by latency (16 tiles of 16 parts: 34 MB).
 template <int PARTS, int KIND, int SIZE>
 __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs a) {
   __shared__ float lds[4];

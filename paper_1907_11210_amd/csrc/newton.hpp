@@ -50,7 +50,11 @@ struct NsWork {
   int slots;   // a join: how many
 };
 // A workgroup's part of a product: rows of P by rows of Q, `stage` columns of them at a time
-// (half as many with two parts), of which `buffers` fit its LDS.
+// (half as many with two parts), of which `buffers` fit its LDS.  256x128 leaves 8 blocks of sums
+// a wave, 128 registers, beside two stages' fragments: with 72 KB of LDS two workgroups a unit,
+// of which one computes while the other waits at its barrier.  A wave reads 6 fragments for 8
+// products of them, with 128x128 4 for 4, with 64x64 2 for 1: what tile_size weighs against
+// the number of tiles.
 struct NsTile {
   int rows, cols, stage, buffers;
   int waves;  // of a SIMD, which its registers leave room for

@@ -5,9 +5,9 @@ lookup and the AdamW step, with their gradients; orthogonalised matrices and the
 Argument marshalling only, as in :mod:`paper_1907_11210_amd.huge2`: the ``huge2_*``
 functions mirror the C entry points and take raw device pointers (ints);
 :class:`GroupNorm`, :class:`LayerNorm`, :class:`Embedding`, :class:`AdamW`,
-:class:`Orthogonalize` and :class:`Muon` take torch tensors and enqueue on the current stream.  Objects belong to the device that was current when
-they were made; one object's calls share its workspace, so make them on one stream
-or order them.
+:class:`Orthogonalize` and :class:`Muon` take torch tensors and enqueue on the
+current stream.  Objects belong to the device that was current when they were made;
+one object's calls share its workspace, so make them on one stream or order them.
 """
 from __future__ import annotations
 
@@ -282,6 +282,7 @@ def newton_schulz(steps=5, coefficients=COEFFICIENTS, products="f32", eps=1e-7):
         raise ValueError("unknown products %r (f32, f16)" % (products,))
     if steps != int(steps) or not 1 <= steps <= 32:
         raise ValueError("steps must be 1 to 32")
+    steps = int(steps)
     triples = [tuple(t) for t in coefficients] if hasattr(coefficients[0], "__len__") else \
         [tuple(coefficients)] * steps
     if len(triples) != steps or any(len(t) != 3 for t in triples):
