@@ -170,8 +170,9 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
 }
 
 // X = U / (norm + eps) and its transpose as fragments, a block of 64 x 64 of the input to a
-// workgroup.  Bound by the bytes: of 33.6 M bf16 elements 76 us, 269 MB at 3.5 TB/s, of which three
-// quarters are written in pieces of 512 bytes.  (The products then need no transpose: read by
+// workgroup.  Bound by the bytes, most of them written, in pieces of 512: of 33.6 M bf16 elements
+// 62 us, 269 MB at 4.3 TB/s; of 88 M and their momenta 215 us, 4.9 TB/s (read by one element a
+// lane instead of four 77 and 355 us).  (The products then need no transpose: read by
 // the other axis, a fragment would be 16 loads of 2 bytes a lane.)
 template <int PARTS>
 __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
@@ -191,17 +192,23 @@ __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
   const int across = (t.tall ? t.mp : t.np) / kNsBlock;
   const int r0 = (int)(work.y / across) * kNsBlock, c0 = (int)(work.y % across) * kNsBlock;
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll 4
-  for (int r = wave; r < kNsBlock; r += 4) {
-    float v = 0.f;
-    if (r0 + r < rows && c0 + lane < cols) {
-      const long long i = (long long)(r0 + r) * cols + c0 + lane;
-      const float g = input(src, t.grad_bf16, i) * gs;
-      v = (float)(update(a, g, a.muon ? t.momentum[i] : 0.f) * inv);
-    }
-    tile[r][lane] = v * a.out_scale;
+  // four neighbours of each fourth of the rows to a thread, all on their way at once
+  const int col = (threadIdx.x & 15) * 4, row = threadIdx.x >> 4;
+  float g[4][4], m[4][4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = r0 + row + 16 * k;
+    const long long first = (long long)r * cols, end = r < rows ? first + cols : 0;
+    input4(src, t.grad_bf16, first + c0 + col, end, g[k]);
+    if (a.muon) input4(t.momentum, 0, first + c0 + col, end, m[k]);
   }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float v = (float)(update(a, g[k][e] * gs, a.muon ? m[k][e] : 0.f) * inv);
+      tile[row + 16 * k][col + e] = v * a.out_scale;
+    }
   __syncthreads();
   // pieces of 8 elements of a fragment's row: two orientations, 64 rows, 8 pieces a row
   half_bits* const to[2] = {pick(t.tall != 0, t.t0, t.x), pick(t.tall != 0, t.x, t.t0)};
