@@ -4,7 +4,8 @@ arXiv 1907.11210).
 The computation lives in ``libhuge2.so`` (HIP kernels for gfx950 behind the C
 ABI of ``include/huge2.h``); :mod:`paper_1907_11210_amd.huge2` is its Python
 binding.  :mod:`paper_1907_11210_amd.train` binds ``include/huge2_train.h``: group
-norm, embedding and AdamW for the networks around the convolutions.
+norm, layer norm, embedding, AdamW, orthogonalised matrices and Muon for the networks around
+the convolutions.
 :mod:`paper_1907_11210_amd.workloads` generates the seeded synthetic
 inputs of the benchmark and the tests.
 """
