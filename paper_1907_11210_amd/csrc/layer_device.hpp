@@ -65,11 +65,13 @@ __device__ __forceinline__ float from_xor4(float v) {
 // The upper halves of pairs of 16 (32) lanes of a, and the lower ones of b, change places: the
 // sum of the two is a's of both halves in the lower, b's in the upper.
 __device__ __forceinline__ float swap_sum16(float a, float b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  const auto r =
+      __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ float swap_sum32(float a, float b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  const auto r =
+      __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 // Sum over 2^log2 lanes side by side (of a wave), the same bits in each of them: every step

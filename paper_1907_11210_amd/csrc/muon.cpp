@@ -175,6 +175,9 @@ constexpr int kUnits = 256;  // compute units
 //   5 of 100x16384 to 128x48, two parts             903   801   889
 //   48 of 33x700 to 644x89, one part                278   270   365
 //   6 of 1000x333, two parts                        200   220   304
+// So large ones where there are three for four units, with 2048 columns each, and middle ones
+// from 512 columns a unit on; of the last product, whose results leave by single elements and
+// hide behind other tiles' products, from 1024 on.
 int tile_size(const NsEngine& e, const Group& g, int kind) {
   if (const char* f = std::getenv("HUGE2_NS_TILE")) return std::abs(std::atoi(f)) % kNsSizes;
   long long tiles[kNsSizes] = {}, columns[kNsSizes] = {};
@@ -218,7 +221,8 @@ void product_works(NsEngine& e, Group& g, int kind, std::vector<NsWork>* works,
   for (size_t k = 0; k < all.size(); ++k) {
     NsWork w = all[k];
     const int stages = w.k1;
-    // (pieces of 1024 columns of small tiles: shorter ones lose more to the join than they gain)
+    // (pieces of 32 stages of small tiles: shorter ones lose more to the join than they gain,
+    // with half as many 207 us for 203 of 6 of 1000x333, 830 for 816 of 100x16384 to 128x48)
     const double piece = std::max(size == 0 ? 32.0 : 16.0, (k < whole ? cost : left) / kUnits);
     // (rounded down behind whole tiles, which hide an uneven end)
     const int cuts = std::max(1, std::min(stages / 8, (int)(stages / piece + (whole ? 0.0 : 0.6))));

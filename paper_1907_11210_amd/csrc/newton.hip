@@ -246,15 +246,15 @@ namespace {
 //
 // Bound by the matrix units and the reads of LDS that feed them: of one matrix of 4096x8192 B X
 // takes 287 us, 275 GF at 958 TFLOP/s (a large library product of fp16 1080), its matrix units
-// busy for 55% of the cycles, without conflicts of LDS banks; A, half of the tiles, 162 us and
-// 17 of the join, 770 TFLOP/s; A A 79 and 7, 800.  With two parts three products each: B X of
+// busy for 55% of the cycles, without conflicts of LDS banks; A, half of the tiles, 162 us and 17
+// of the join, 770 TFLOP/s; A A 79 and 7, 800.  With two parts three products each: B X of
 // 100x16384 to 1024x8192 71 us.  Where matrices are small (6 of 1000x333, 8 to 19 us a product)
 // bound by latency: a launch, three stages' loads, one or a few rounds of tiles.  What made it
-// fast on the large matrix: operands stored as fragments, so that loads go straight into LDS and reads are
-// 16 bytes a lane side by side; three or four stages on their way and a wait that counts them
-// instead of a wait for all; fragments read a stage ahead of their products; the order of
-// instructions (below); the epilogue as a loop over blocks (its straight code was read from
-// memory once and took longer than the work).
+// fast on the large matrix: operands stored as fragments, so that loads go straight into LDS and
+// reads are 16 bytes a lane side by side; three or four stages on their way and a wait that counts
+// them instead of a wait for all; fragments read a stage ahead of their products; the order of
+// instructions (below); the epilogue as a loop over blocks (its straight code was read from memory
+// once and took longer than the work).
 template <int PARTS, int KIND, int SIZE>
 struct Product {
   static constexpr NsTile kTile = kNsTiles[SIZE];
