@@ -651,13 +651,12 @@ class AdamW(_Optimizer):
 
 class Orthogonalize(_Owner):
     """Newton-Schulz steps of matrices of one shape [..., rows, cols], which bring their singular
-    values near 1.  products: "f32" (results as of products in fp32, the default for float32) or
-    "f16" (within 2^-10 of a result's norm, 2^-6 for matrices of low rank; the default for
-    bfloat16).  coefficients: one triple
-    (a, b, c), or one for each step."""
+    values near 1.  products: "f32" (results as of products in fp32, whatever the tensors' type)
+    or "f16" (within 2^-10 of a result's norm, 2^-6 for matrices of low rank).  coefficients: one
+    triple (a, b, c), or one for each step."""
     _destroy = staticmethod(huge2_orthogonalize_plan_destroy)
 
-    def __init__(self, shape, dtype, products=None, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
+    def __init__(self, shape, dtype, products="f32", steps=5, coefficients=COEFFICIENTS, eps=1e-7):
         torch = _torch()
         if len(shape) < 2:
             raise ValueError("x must have rows and columns")
@@ -665,7 +664,7 @@ class Orthogonalize(_Owner):
         self._index, self._stream = self.device.index, _raw_stream()
         self.shape, self.dtype = torch.Size(shape), dtype
         code = _type_code(dtype)
-        self.products = products or ("f32" if dtype == torch.float32 else "f16")
+        self.products = products or "f32"
         self.desc = OrthogonalizeDesc(math.prod(shape[:-2]), *shape[-2:], code)
         self._plan = huge2_orthogonalize_plan_create(
             self.desc, newton_schulz(steps, coefficients, self.products, eps),
@@ -696,13 +695,12 @@ class Muon(_Optimizer):
     grad_dtypes   None (the copies', else the parameters' own types), or one for each parameter.
     m             a list of float32 momenta to go on from; made as zeros where not given.
     products, steps, coefficients, eps
-                  of the Newton-Schulz steps, as in :class:`Orthogonalize` (products: "f32" if
-                  any parameter is float32).
+                  of the Newton-Schulz steps, as in :class:`Orthogonalize`.
     """
     _destroy = staticmethod(huge2_muon_plan_destroy)
 
     def __init__(self, params, weight_decay=0.0, scales=None, copies=None, grad_dtypes=None,
-                 m=None, products=None, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
+                 m=None, products="f32", steps=5, coefficients=COEFFICIENTS, eps=1e-7):
         torch = _torch()
         self.device = _current_device()
         self._index, self._stream = self.device.index, _raw_stream()
@@ -723,8 +721,7 @@ class Muon(_Optimizer):
         self.grad_dtypes = list(grad_dtypes)
         if any(len(x) != k for x in (decay, self.scales, self.copies, self.m, self.grad_dtypes)):
             raise ValueError("every list needs one entry for each of %d parameters" % k)
-        self.products = products or \
-            ("f32" if any(p.dtype == torch.float32 for p in self.params) else "f16")
+        self.products = products or "f32"
         tensors = []
         for p, mt, c, shape, gd, wd, scale in zip(self.params, self.m, self.copies, shapes,
                                                   self.grad_dtypes, decay, self.scales):
