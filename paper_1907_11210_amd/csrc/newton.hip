@@ -6,11 +6,13 @@
 //
 // Two parts a value, hi + lo, are 22 bits, and hi hi + hi lo + lo hi gives fp32's accuracy: after
 // five steps 4e-7 of the result's norm (products in fp32 2e-7), 4e-6 (2e-6) where singular values
-// fall with the square of their rank, up to 1e-4 where all but a few are nothing and what
-// roundings leave in their place grows 480 times.
+// fall with the square of their rank, 2e-5 to 5e-4 (4e-6 to 4e-3) where all but a few are nothing
+// and what roundings leave in their place grows 480 times.
 //
-// One part is 11 bits: 7e-4 of the result's norm, of falling singular values 3e-4, of a matrix
-// of low rank up to 1e-2 (bf16 products 1e-2, 0.15 and more).  Two things keep it there.  The term
+// One part is 11 bits: 7e-4 of the result's norm, of falling singular values 3e-4, of small
+// matrices more (16 x 16 2e-3).  Of a matrix of low rank what is left in place of its missing
+// singular values is some 0.25 / m: 6e-2 of 3 x 3, 3e-2 of 8 x 8, 6e-3 of 32 x 32, 2e-3 of
+// 1024 x 1024 (bf16 products 0.15 and more).  Two things keep it there.  The term
 // a X, which carries what small singular values grow from, is formed from both parts (else 2e-2
 // where they fall).  And A is stored less mu I, mu the mean of its diagonal, which in the last
 // steps is near 1 and would round off what the other elements hold (else 2e-3): with A = A' + mu I,
