@@ -117,8 +117,9 @@ typedef struct huge2_layer_norm_plan huge2_layer_norm_plan;
 
 /* Chooses the kernels for desc and allocates the gradient's workspace: 8 bytes a channel for
  * each of its workgroups, of which there are 4096 at most.  No work is enqueued.  Errors:
- * INVALID_ARG, UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or more channels or
- * tiles of pixels than launches can take: 2^24 channels and 2^37 pixels always fit), ALLOC. */
+ * INVALID_ARG, UNSUPPORTED (c*h*w of 2^31 or more, 2^40 elements in all, or more than launches
+ * can take: 2^26 - 16 channels; in NCHW with h*w > 1 2^24 channels, or 2^31 pieces of the images'
+ * planes, each of 128 bytes or a plane's rest), ALLOC. */
 huge2_status huge2_layer_norm_plan_create(huge2_layer_norm_plan** out,
                                           const huge2_layer_norm_desc* desc);
 

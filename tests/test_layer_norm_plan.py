@@ -131,3 +131,36 @@ def test_sizes_that_32_bits_do_not_hold():
         for value in (2 ** 32 + 2, 2 ** 31, -2 ** 31 - 1):
             with pytest.raises(ValueError, match=field):
                 _desc(**{field: value})
+
+
+STATUS = START + """
+done = []
+for n, c, h, w, layout, dtype in json.load(sys.stdin):
+    plan, d = ctypes.c_void_p(), tr.LayerNormDesc(n, c, h, w, layout, dtype, 0, 1e-5)
+    done.append(tr.lib().huge2_layer_norm_plan_create(ctypes.byref(plan), ctypes.byref(d)))
+    tr.huge2_layer_norm_plan_destroy(plan)
+json.dump(done, sys.stdout)
+"""
+
+
+def test_the_largest_that_fits(script):  # noqa: F811
+    """The limits that the header gives, from both sides: in NCHW below 2^24 channels and 2^31
+    pieces of 128 bytes of the images' planes, else below 2^26 - 16 channels; 2^40 elements."""
+    nchw, nhwc, f32, bf16 = h2.HUGE2_NCHW, h2.HUGE2_NHWC, h2.HUGE2_F32, h2.HUGE2_BF16
+    inside, outside = [], []
+    for dtype, piece in ((f32, 32), (bf16, 64)):  # pixels of 128 bytes
+        for hw in (1, 2, 3, 7, piece - 1, piece, piece + 1, 2 * piece, 2 * piece + 1, 10 * piece - 1,
+                   997 * piece + 1, (1 << 20) - 1):
+            pieces = -(-hw // piece)
+            most = min(((1 << 31) - 1) // pieces, ((1 << 40) - 1) // hw)
+            inside.append((most, 1, 1, hw, nchw, dtype))
+            if most < (1 << 31) - 1:
+                outside.append((most + 1, 1, 1, hw, nchw, dtype))
+        inside += [(1 << 20, 1, 1 << 9, (1 << 11) - 1, nhwc, dtype),
+                   ((1 << 31) - 1, 2, 1, 1, nhwc, dtype), (1, (1 << 24) - 1, 2, 63, nchw, dtype)]
+        outside += [(1, 1 << 24, 1, 2, nchw, dtype), (1 << 20, 1, 1 << 10, 1 << 10, nhwc, dtype)]
+        for layout in (nchw, nhwc):
+            inside.append((1, (1 << 26) - 17, 1, 1, layout, dtype))
+            outside.append((1, (1 << 26) - 16, 1, 1, layout, dtype))
+    assert script(STATUS, inside) == [h2.HUGE2_OK] * len(inside)
+    assert script(STATUS, outside) == [h2.HUGE2_ERR_UNSUPPORTED] * len(outside)
