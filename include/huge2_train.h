@@ -271,7 +271,7 @@ typedef enum { HUGE2_PRODUCTS_F32 = 0, HUGE2_PRODUCTS_F16 = 1 } huge2_products;
  *   X = U / (|U| + eps), |U| the root of the sum of squares, then `steps` times
  *   A = X X^T,  X = a X + (b A + c A A) X
  * with (a, b, c) of each step, [steps][3].  (3.4445, -4.7750, 2.0315) five times brings
- * singular values of |U| / 500 and more to between 0.7 and 1.2.  A matrix with more rows than
+ * singular values of |U| / 500 and more to between 0.68 and 1.21.  A matrix with more rows than
  * columns is taken transposed, which gives the same.  A value that is not finite makes the
  * whole result NaN, as the products do. */
 typedef struct {

@@ -57,9 +57,11 @@ void choose_rows(LayerArgs* a, int vec, int esz, bool grad) {
   const int teams = a->slots ? a->threads >> a->lanes_log2 : 1;
   const long long all = ceil_div(a->rows, teams);
   const long long most_groups = (grad ? 1024 : 2048) * 256 / a->threads;
-  // The gradient's sums of a workgroup's rows, 8 bytes a channel written and read, stay under
-  // 4% of its bytes: 32768 rows of 1024 bf16 with 512 workgroups 47.7 us, with 1024 52.5;
-  // 65536 of 128 with 512 and 1024 22.5 and 20.7; 1024 of 512 with 256 and 1024 10.6 and 12.9.
+  // The gradient's sums of a workgroup's rows, 8 bytes a channel written and read, are 4% of its
+  // bytes from 17000 rows of bf16 on (8500 of fp32): 32768 rows of 1024 bf16 with 512 workgroups
+  // 47.7 us, with 1024 52.5; 65536 of 128 with 512 and 1024 22.5 and 20.7.  Fewer rows have 256
+  // workgroups, a unit's one, whatever their sums take: 1024 of 512, where they are 67%, with 256
+  // and 1024 10.6 and 12.9.
   const long long want = grad ? std::max(256ll, a->rows * esz * 3 / 400) : all;
   a->groups = (int)std::min({all, want, most_groups});
   a->parts = a->groups;

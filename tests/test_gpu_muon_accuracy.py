@@ -6,6 +6,8 @@ roundings up to 3.4 times as high, five steps 480 times, so that what a product 
 is seen in the result.  Matrices are sums of products of whole numbers, which fp32 and bf16
 hold without a rounding, so that their rank is what it says.
 """
+import math
+
 import pytest
 import torch
 
@@ -90,6 +92,27 @@ def test_a_steps_products_are_fp32_where_nothing_else_is_asked_for(dtype):
     muon.step([x.to(DEV, dtype) for x in xs], lr=1.0, momentum=0.0, nesterov=False)
     for p, x in zip(params, xs):
         assert off(-p, x) <= bound_f32(x.shape) + ROUNDING[dtype], tuple(x.shape)
+
+
+def test_five_steps_bring_singular_values_near_one():
+    """Those of |U| / 500 and more to between 0.68 and 1.21; the polynomials' own ends, 0.6818 and
+    1.2024, are among them (products in fp32 move none by more than 2^-12 sqrt(300) / 20)."""
+    fine = torch.logspace(-math.log10(500), 0, 1 << 20, dtype=torch.float64)
+    y = fine
+    a, b, c = tr.COEFFICIENTS
+    for _ in range(5):
+        y = a * y + b * y ** 3 + c * y ** 5
+    ends = fine[torch.stack((y.argmin(), y.argmax()))]
+    s = torch.cat((ends, torch.logspace(math.log10(1 / 499), math.log10(0.04), 298,
+                                        dtype=torch.float64)))
+    s = torch.cat((s, (1 - (s * s).sum()).sqrt()[None]))  # |U| = 1
+    g = torch.Generator().manual_seed(6)
+    u, v = (torch.linalg.qr(torch.randn(n, len(s), generator=g).double())[0] for n in (320, 500))
+    x = ((u * s) @ v.T).float()
+    got = torch.linalg.svdvals(tr.Orthogonalize(x.shape, torch.float32)(x.to(DEV)).cpu().double())
+    got = got[:len(s)]
+    print("from %.4f to %.4f" % (float(got.min()), float(got.max())), flush=True)
+    assert 0.68 <= float(got.min()) <= 0.684 and 1.2 <= float(got.max()) <= 1.21
 
 
 # ---- products in f16: the bounds that are documented ---------------------------------
