@@ -179,7 +179,7 @@ constexpr int kUnits = 256;  // compute units
 // from 512 columns a unit on; of the last product, whose results leave by single elements and
 // hide behind other tiles' products, from 1024 on.
 int tile_size(const NsEngine& e, const Group& g, int kind) {
-  if (const char* f = std::getenv("HUGE2_NS_TILE")) return std::abs(std::atoi(f)) % kNsSizes;
+  if (const char* f = std::getenv("HUGE2_NS_TILE")) return (unsigned)std::atoi(f) % kNsSizes;
   long long tiles[kNsSizes] = {}, columns[kNsSizes] = {};
   for (int i = 0; i < g.count; ++i)
     for (int size = 0; size < kNsSizes; ++size)

@@ -124,3 +124,13 @@ def test_the_lists_with_whole_rounds_and_a_cut_rest(launches):
     gram = [f for f in found if f[2] == 0][:2]
     assert gram[0] == ("product", 1, 0, 2, 512, 1) and gram[1] == ("join", 1, 0, 2, 16, 8)
     assert _tiles([(4096, 8192)], 0, 2) == 256 + 16
+
+
+@pytest.mark.parametrize("tile", ["-2147483648", "-1", "0", "2", "2147483647", "x"])
+def test_sizes_of_tiles_by_the_environment(launches, monkeypatch, tile):
+    """Any number chooses one of the three."""
+    monkeypatch.setenv("HUGE2_NS_TILE", tile)
+    for found in _products(launches([([(100, 90)], "f32")])[0]):
+        assert found[3] in (0, 1, 2) and found[4] == _tiles([(100, 90)], *found[2:4])
+        if tile in ("0", "2"):
+            assert found[3] == int(tile)
