@@ -74,8 +74,10 @@ __device__ __forceinline__ Channel slot_params(const LayerArgs& a, int ch) {
 // again for each of the sums and the result.  (A tile to a workgroup: in a loop over tiles the
 // compiler holds what does not change, and 40 of 128 registers spill.)
 //
-// 64 images of 256x16x16 bf16 8.0 us, 17 MB: one round of 256 tiles, bound by its latency (loads,
-// two sums through LDS, stores); 64 of 128x64x64 36 us, 134 MB at 3.7 TB/s.
+// 64 images of 256x16x16 bf16 8.2 us, 17 MB: one round of 256 tiles, bound by its latency (loads,
+// two sums through LDS, stores).  64 of 128x64x64 34 us, 134 MB at 4.0 TB/s, fetched and written
+// once each: the same latency in every round, with nothing of the next tile on its way; fp32
+// 54 us, 4.9 TB/s.  2048 channels in tiles of 32 bytes, 64 images of 16x16, 35 us, 3.9 TB/s.
 template <typename T, int VW, int R, bool RAGGED>
 __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -160,7 +162,11 @@ __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
 // workgroup's tiles (R = 0: layer_plane_sums_kernel does).
 //
 // 5 images of 200x33x41 fp32 with SiLU 10.9 us, 16 MB: one round of 215 tiles, in which fp32's
-// exponential and division take as long as the loads; 64 of 128x64x64 bf16 55 us, 3.7 TB/s.
+// exponential and division take as long as the loads, and 22 MB are fetched for the 11 of x and
+// dy: an odd map's tiles share lines, and tiles side by side are on different dies.  64 of
+// 128x64x64 bf16 46 us, 4.4 TB/s, fetched once.  From 512 channels on tiles are narrower than a
+// line, and each die fetches its own: 64 images of 1024x16x16 41 us, twice the bytes; of
+// 2048x16x16 120 us, four times, 538 MB.
 template <typename T, int VW, int R, bool RAGGED>
 __global__ __launch_bounds__(R * VW > kLayerWideChannels ? 512 : 1024) void
 layer_grad_planes_kernel(LayerArgs a) {

@@ -170,14 +170,19 @@ constexpr int kUnits = 256;  // compute units
 // The size of a product's tiles.  Large ones need the least of LDS and the caches, and enough
 // columns to be worth their long prologue and epilogue; small ones start and end sooner.  Whole
 // passes in us with the small, middle and large tiles alone:
-//   1 of 4096x8192, one part                       4950  2950  2710
-//   6 of 4096x4096 and the like, one part         11600  7700  6600
-//   5 of 100x16384 to 128x48, two parts             903   801   889
-//   48 of 33x700 to 644x89, one part                278   270   365
+//   1 of 4096x8192, two parts                     10980  6430  6130
+//     one part                                     4960  2910  2730
+//   6 of 4096x4096 and the like, two parts        24820 14900 13670
+//     one part                                    11440  7530  6430
+//   5 of 100x16384 to 128x48, two parts             869   816   899
+//     one part                                      524   505   565
+//   48 of 33x700 to 644x89, two parts               371   412   501
+//     one part                                      260   254   340
 //   6 of 1000x333, two parts                        200   220   304
 // So large ones where there are three for four units, with 2048 columns each, and middle ones
 // from 512 columns a unit on; of the last product, whose results leave by single elements and
-// hide behind other tiles' products, from 1024 on.
+// hide behind other tiles' products, from 1024 on.  (It takes 6150, 2730, 13670, 6460, 793, 474,
+// 378, 260 and 197.)
 int tile_size(const NsEngine& e, const Group& g, int kind) {
   if (const char* f = std::getenv("HUGE2_NS_TILE")) return (unsigned)std::atoi(f) % kNsSizes;
   long long tiles[kNsSizes] = {}, columns[kNsSizes] = {};

@@ -124,9 +124,9 @@ __device__ __forceinline__ void input4(const void* p, int bf16, long long i, lon
 
 // The momentum's update, and sums of squares of what is orthogonalised.  In 64 bits: squares
 // of any two floats' sum neither overflow nor vanish.  Bound by the bytes where there are enough:
-// 88 M elements of bf16 gradients and fp32 momenta 155 us, 881 MB at 5.7 TB/s
+// 88 M elements of bf16 gradients and fp32 momenta 150 to 156 us, 881 MB at 5.7 to 5.9 TB/s
 // (eight vectors in flight 161 us; 48 small matrices 13.5 us, 20.3 with eight).  At most 1024 sums
-// of a matrix: with 512 33.6 M bf16 elements took 57 us, now 37.
+// of a matrix: with 512 33.6 M bf16 elements took 57 us, now 33 to 35.
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
   __shared__ double lds[4];
   const uint2 work = a.works[blockIdx.x];
@@ -173,9 +173,10 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsInput a) {
 
 // X = U / (norm + eps) and its transpose as fragments, a block of 64 x 64 of the input to a
 // workgroup.  Bound by the bytes, most of them written, in pieces of 512: of 33.6 M bf16 elements
-// 62 us, 269 MB at 4.3 TB/s; of 88 M and their momenta 215 us, 4.9 TB/s (read by one element a
-// lane instead of four 77 and 355 us).  (The products then need no transpose: read by
-// the other axis, a fragment would be 16 loads of 2 bytes a lane.)
+// 75 us, 337 MB at 4.5 TB/s (with one part 62 us, 269 MB at 4.3); of 88 M and their momenta 241,
+// 5.1 TB/s (215, 4.9 TB/s; read by one element a lane instead of four 77 and 355 us with one
+// part).  (The products then need no transpose: read by the other axis, a fragment would be 16
+// loads of 2 bytes a lane.)
 template <int PARTS>
 __global__ __launch_bounds__(256) void ns_pack_kernel(NsInput a) {
   __shared__ float tile[kNsBlock][kNsBlock + 1];
@@ -247,11 +248,13 @@ namespace {
 // the sums.
 //
 // Bound by the matrix units and the reads of LDS that feed them: of one matrix of 4096x8192 B X
-// takes 287 us, 275 GF at 958 TFLOP/s (a large library product of fp16 1080), its matrix units
-// busy for 55% of the cycles, without conflicts of LDS banks; A, half of the tiles, 162 us and 17
-// of the join, 770 TFLOP/s; A A 79 and 7, 800.  With two parts three products each: B X of
-// 100x16384 to 1024x8192 71 us.  Where matrices are small (6 of 1000x333, 8 to 19 us a product)
-// bound by latency: a launch, three stages' loads, one or a few rounds of tiles.  What made it
+// with two parts, three products each, takes 666 us, 825 GF at 1240 TFLOP/s (large library
+// products of fp16 1080), its matrix units busy for 77% of the cycles, without conflicts of LDS
+// banks; A, half of the tiles, 358 us and 16 of the join, 1100 TFLOP/s of what is needed; A A 185
+// and 9, 1060.  With one part 287 us, 275 GF at 958 TFLOP/s, busy for 55%; 162 and 17, 770; 79
+// and 7, 800.  Where matrices are smaller, bound by what the dies' caches fetch, X once as it is
+// and once transposed: 48 of 33x700 to 644x89 117 MB and 48 written in the 29 us of B X, 5.7 TB/s;
+// 6 of 1000x333 58 MB in 16, 3.6 TB/s, two rounds of tiles.  What made it
 // fast on the large matrix: operands stored as fragments, so that loads go straight into LDS and
 // reads are 16 bytes a lane side by side; three or four stages on their way and a wait that counts
 // them instead of a wait for all; fragments read a stage ahead of their products; the order of
