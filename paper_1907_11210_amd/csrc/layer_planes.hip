@@ -164,7 +164,7 @@ __global__ __launch_bounds__(1024) void layer_planes_kernel(LayerArgs a) {
 // 5 images of 200x33x41 fp32 with SiLU 10.9 us, 16 MB: one round of 215 tiles, in which fp32's
 // exponential and division take as long as the loads, and 22 MB are fetched for the 11 of x and
 // dy: an odd map's tiles share lines, and tiles side by side are on different dies.  64 of
-// 128x64x64 bf16 46 us, 4.4 TB/s, fetched once.  From 512 channels on tiles are narrower than a
+// 128x64x64 bf16 46 us, 4.4 TB/s, fetched once.  Over 512 channels tiles are narrower than a
 // line, and each die fetches its own: 64 images of 1024x16x16 41 us, twice the bytes; of
 // 2048x16x16 120 us, four times, 538 MB.
 template <typename T, int VW, int R, bool RAGGED>

@@ -652,7 +652,7 @@ class AdamW(_Optimizer):
 class Orthogonalize(_Owner):
     """Newton-Schulz steps of matrices of one shape [..., rows, cols], which bring their singular
     values near 1.  products: "f32" (results as of products in fp32, whatever the tensors' type)
-    or "f16" (in less than half of the time; off by up to 2^-6 of a result's norm, 2^-3 where
+    or "f16" (large matrices in 45% of the time; off by up to 2^-6 of a result's norm, 2^-3 where
     rows or columns are fewer than 32: the most for matrices of low rank).  coefficients: one
     triple (a, b, c), or one for each step."""
     _destroy = staticmethod(huge2_orthogonalize_plan_destroy)
