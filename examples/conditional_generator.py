@@ -61,7 +61,7 @@ class Generator:
         decay = [0.01] * k + [0.0] * (2 * norms)
         copies = self.work + [None] * (2 * norms)
         # Muon takes the convolutions' weights, [inputs, outputs and taps] as matrices; with sides
-        # from 32 on products in f16, which take less time, leave each update within 2^-6
+        # from 32 on products in f16, which take less time, leave an update within some 2^-6
         self.matrices = list(range(1, k)) if optimizer == "muon" else []
         self.others = [i for i in range(len(self.params)) if i not in self.matrices]
         pick = lambda values, of: [values[i] for i in of]  # noqa: E731

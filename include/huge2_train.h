@@ -258,13 +258,15 @@ huge2_status huge2_adamw_plan_destroy(huge2_adamw_plan* plan);
 /* ---- orthogonalised matrices ------------------------------------------------ */
 
 /* What a product's operands hold: two fp16 parts of a value (22 bits), or one (11 bits, in
- * 45% of the time for large matrices, 60 to 90% for small ones).  Sums are fp32 either way.  Five
- * steps with the polynomial below, for matrices whose smaller side is up to 8192, are off by these parts of a result's norm.  Two
- * parts, as products in fp32: 2^-12 at most up to 1024 and 2^-10 beyond, where fp32's longer sums
- * count; some 2^-19 where no singular value is next to nothing.  One part: 2^-3 at most where the
- * smaller side is below 32, 2^-6 from 32 on, and there 2^-8 where all singular values are
- * |U| / 100 or more.  Matrices of low rank are the worst: what roundings leave in place of their
- * missing singular values grows 480 times. */
+ * 45% of the time for large matrices, 60 to 90% for small ones).  Sums are fp32 either way.  How
+ * far off results are, of their norm, after five steps with the polynomial below, depends on the
+ * matrix: what roundings leave in place of a singular value that is missing grows 480 times.
+ * Two parts give what products in fp32 give: some 2^-19 where no singular value is next to
+ * nothing, 2^-16 to 2^-12 where the rank is low and entries are of any size, more where they are
+ * of few sizes and sums are long (rank 1, 8192 x 8192: 2^-8), and 2^-11 + (rows + cols) 2^-17 at
+ * most.  One part gives some 2^-10; where the rank is low up to 2^-6 if rows and cols are 32 or
+ * more, up to 2^-3 if one of them is less.  (That is of hundreds of matrices, and no bound of all:
+ * where it matters, take two parts.) */
 typedef enum { HUGE2_PRODUCTS_F32 = 0, HUGE2_PRODUCTS_F16 = 1 } huge2_products;
 
 /* Newton-Schulz steps that bring all singular values of a matrix near 1:
