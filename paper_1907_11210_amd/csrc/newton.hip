@@ -12,10 +12,11 @@
 // One part is 11 bits: 7e-4 of the result's norm, of falling singular values 3e-4, of small
 // matrices more (16 x 16 2e-3).  Of a matrix of low rank what is left in place of its missing
 // singular values is up to 6e-2 of 3 x 3, 3e-2 of 8 x 8, 1e-2 from 32 x 32 on where entries are of
-// few sizes and round alike, else 0.25 / m (bf16 products 0.15 and more).  Two things keep it there.  The term
-// a X, which carries what small singular values grow from, is formed from both parts (else 2e-2
-// where they fall).  And A is stored less mu I, mu the mean of its diagonal, which in the last
-// steps is near 1 and would round off what the other elements hold (else 2e-3): with A = A' + mu I,
+// few sizes and round alike, else 0.25 / m (bf16 products 0.15 and more).  Two things keep it
+// there.  The term a X, which carries what small singular values grow from, is formed from both
+// parts (else 2e-2 where they fall).  And A is stored less mu I, mu the mean of its diagonal, which
+// in the last steps is near 1 and would round off what the other elements hold (else 2e-3): with
+// A = A' + mu I,
 //   a I + b A + c A A = (a + b mu + c mu^2) I + B,  B = (b + 2 c mu) A' + c A' A'.
 #include "huge2_train.h"
 #include "newton.hpp"

@@ -652,9 +652,9 @@ class AdamW(_Optimizer):
 class Orthogonalize(_Owner):
     """Newton-Schulz steps of matrices of one shape [..., rows, cols], which bring their singular
     values near 1.  products: "f32" (results as of products in fp32, whatever the tensors' type)
-    or "f16" (large matrices in 45% of the time; off by some 2^-10 of a result's norm, of low rank by
-    up to 2^-6, or 2^-3 where rows or columns are fewer than 32).  coefficients: one
-    triple (a, b, c), or one for each step."""
+    or "f16" (large matrices in 45% of the time; off by some 2^-10 of a result's norm, of low rank
+    by up to 2^-6, or 2^-3 where rows or columns are fewer than 32).  coefficients: one triple
+    (a, b, c), or one for each step."""
     _destroy = staticmethod(huge2_orthogonalize_plan_destroy)
 
     def __init__(self, shape, dtype, products="f32", steps=5, coefficients=COEFFICIENTS, eps=1e-7):
